@@ -66,7 +66,13 @@
 extern "C" {
 #endif
 
-typedef enum { WHTMIX_F32 = 0, WHTMIX_BF16 = 1, WHTMIX_I32 = 2 } whtmix_dtype_t;
+/* WHTMIX_E4M3 (8-bit floats: 4 exponent and 3 mantissa bits, no infinity, largest 448) is a type of the layer operators
+ * only; the mixer's calls return WHTMIX_ERR_BAD_DTYPE for it. */
+typedef enum { WHTMIX_F32 = 0, WHTMIX_BF16 = 1, WHTMIX_I32 = 2, WHTMIX_E4M3 = 3 } whtmix_dtype_t;
+
+/* Activations of whtmix_linear: z; max(z, 0); z / (1 + e^(-2u)) with u = sqrt(2 / pi) (z + 0.044715 z^3), the tanh form of the
+ * Gaussian error linear unit; z / (1 + e^(-z)). */
+typedef enum { WHTMIX_ACT_NONE = 0, WHTMIX_ACT_RELU = 1, WHTMIX_ACT_GELU = 2, WHTMIX_ACT_SILU = 3 } whtmix_activation_t;
 
 typedef enum {
     WHTMIX_OK = 0,
@@ -222,6 +228,65 @@ WHTMIX_API int whtmix_block_forward(const void *x, const void *w_in, const void 
 WHTMIX_API int whtmix_block_backward(const void *x, const void *w_in, const void *gains, const void *w_out,
                                      const void *dy, void *dx, void *dw_in, void *dgains, void *dw_out, int64_t B,
                                      int64_t N, int64_t C, int dtype, void *stream);
+
+/* ---- The layer around the mixer ----
+ * A transformer layer is h = x + block(norm(x)), y = h + W2 act(W1 norm(h) + b1) + b2 (Section III-B: the block is linear and
+ * the feed-forward half supplies the nonlinearity).  The four calls below are its norm and its products.  They take rows: T
+ * tokens of D, K or N channels, channels contiguous, `*_stride` elements from one row to the next (at least a row's length;
+ * of no meaning where T <= 1).  T >= 0; channels from 1 to 2^24; T < 2^31 - 256 and every matrix at most 2^40 elements
+ * (WHTMIX_ERR_BAD_SHAPE).  Any size and any alignment of the element type runs (WHTMIX_ERR_MISALIGNED below that); 16-byte
+ * aligned rows are the fast ones.  An output may share no address range with an input or another output, except where stated.
+ * T = 0: nothing is read, gradients of parameters are set to zero.  All sums are float32, in a fixed order. */
+
+/* RMS norm with the residual's addition, one row of D channels at a time:
+ *     h = x + residual,    y = h w / sqrt(mean(h^2) + eps)
+ *   x, residual  [T, D] (dtype WHTMIX_F32 or WHTMIX_BF16); residual may be NULL
+ *   w            [D] float32 gains
+ *   h            [T, D] (dtype): the sum, rounded once; NULL if it is not wanted; unused without a residual.  It may be x or
+ *                the residual itself (same pointer and stride).
+ *   y            [T, D]: of `dtype` where out_dtype is dtype (it may then be x or the residual itself, if h is not), or
+ *                WHTMIX_E4M3: y / y_scale[t], rounded to nearest, ties to even
+ *   y_scale      [T] float32, WHTMIX_E4M3 only (else unused): max |y| / 448 of the row; a row of zeros has scale 0 and values 0
+ * y is computed from the unrounded sum.  A row with an infinity or a NaN yields NaN as the formula does (and a NaN scale). */
+WHTMIX_API int whtmix_rms_norm(const void *x, const void *residual, const float *w, void *h, void *y, float *y_scale,
+                               int64_t T, int64_t D, int64_t x_stride, int64_t residual_stride, int64_t h_stride,
+                               int64_t y_stride, float eps, int dtype, int out_dtype, void *stream);
+
+/* Backward of whtmix_rms_norm from the stored sum h: with r = 1 / sqrt(mean(h^2) + eps) and a = dy w,
+ *     dx = r a - h r^3 mean(a h) + dh,     dw = sum over the rows of dy h r
+ *   h, dy, dx  [T, D] (dtype); dh [T, D] (dtype) the gradient that reaches h directly, or NULL.  dx is the gradient of x and of
+ *              the residual alike; it may be dy or dh itself (same pointer and stride).
+ *   dw         [D] float32, overwritten.  Two launches. */
+WHTMIX_API int whtmix_rms_norm_backward(const void *h, const float *w, const void *dy, const void *dh, void *dx, float *dw,
+                                        int64_t T, int64_t D, int64_t h_stride, int64_t dy_stride, int64_t dh_stride,
+                                        int64_t dx_stride, float eps, int dtype, void *stream);
+
+/* Matrix product with bias, activation and residual in its epilogue, on the tensor cores:
+ *     p = x w^T + bias,    y = act(p) + residual
+ *   x, w       [T, K] and [N, K], both of `dtype`: WHTMIX_BF16, or WHTMIX_E4M3 with float32 scales a row, x_scale [T] and
+ *              w_scale [N] (p = x_scale[t] w_scale[n] sum_k x w + bias); scales are NULL for WHTMIX_BF16
+ *   bias       [N] float32, or NULL
+ *   residual   [T, N] of out_dtype, or NULL
+ *   preact     [T, N] bf16: p, rounded once, for whtmix_linear_backward; NULL if it is not wanted; out_dtype WHTMIX_BF16 only
+ *   y          [T, N] of out_dtype: WHTMIX_BF16 or WHTMIX_F32; it may be the residual itself (same pointer and stride)
+ *   act        a whtmix_activation_t
+ * float32 accumulation and epilogue, one rounding. */
+WHTMIX_API int whtmix_linear(const void *x, const void *w, const float *x_scale, const float *w_scale, const float *bias,
+                             const void *residual, void *preact, void *y, int64_t T, int64_t N, int64_t K,
+                             int64_t x_stride, int64_t w_stride, int64_t residual_stride, int64_t preact_stride,
+                             int64_t y_stride, int act, int dtype, int out_dtype, void *stream);
+
+/* Backward of whtmix_linear (WHTMIX_BF16) for the upstream gradient dy of y (which is the residual's gradient as it stands):
+ *     dp = dy act'(preact),   dx = dp w,   dw = dp^T x,   db = sum over the rows of dp
+ *   x [T, K], w [N, K], dy [T, N], preact [T, N] bf16 (NULL for WHTMIX_ACT_NONE)
+ *   dx         [T, K] bf16, or NULL
+ *   dw         [N, K] contiguous, of dw_dtype WHTMIX_BF16 or WHTMIX_F32, overwritten; or NULL
+ *   db         [N] float32, overwritten; or NULL
+ * dp is rounded to bf16 for the two products (an activation gradient, as the block's dM and dZ); db sums it unrounded. */
+WHTMIX_API int whtmix_linear_backward(const void *x, const void *w, const void *dy, const void *preact, void *dx, void *dw,
+                                      float *db, int64_t T, int64_t N, int64_t K, int64_t x_stride, int64_t w_stride,
+                                      int64_t dy_stride, int64_t preact_stride, int64_t dx_stride, int act, int dw_dtype,
+                                      void *stream);
 
 /* Synchronises `stream` and reports device-side failures of the calls enqueued on it since the
  * previous whtmix_sync: WHTMIX_ERR_TIMEOUT if a bounded device-wide wait gave up (the library

@@ -874,6 +874,14 @@ int forward_in_fixed_scratch(const void* x, const void* gains, void* y, int64_t 
   c.reset_arrivals = true;
   return run(c, scratch, scratch_bytes, true, stream);
 }
+// What the layer operators' entry points (whtmix_layer.cu) share with this file's.
+namespace host {
+int fail(cudaError_t e) { return cuda_fail(e); }
+int device(int* dev, int* sms) { return device_check(dev, sms); }
+int workspace(int dev, cudaStream_t stream, size_t bytes, int slot, void** out) {
+  return cached_workspace(dev, stream, bytes, out, slot);
+}
+}  // namespace host
 // Device address of the fixed scratch on device `dev`, or null if no call has set it up there.
 void* noalloc_scratch_of(int dev);
 }  // namespace whtmix

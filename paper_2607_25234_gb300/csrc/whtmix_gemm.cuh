@@ -1,0 +1,422 @@
+// whtmix_gemm.cuh -- matrix products on the 5th-generation tensor cores with the linear layer's epilogue.
+//
+//   C[m, n] = sum over k of A[m, k] B[n, k]        y = act(s_m s_n C + b_n) + r
+//
+// One persistent CTA per SM, 384 threads, tiles of 128 x BN (BN = 64, 128, 256) in turn, the K axis in blocks of 128 bytes:
+//   warp 0     TMA loads of A and B blocks into a ring of stages (192 KB in all);
+//   warp 1     four tcgen05.mma a block (fp32 accumulators in tensor memory, two tiles' worth: the next tile's products run
+//              while the last one's accumulator is read);
+//   warps 4-11 epilogue, two groups of four warps; a group takes every other panel of 128 bytes of a row: accumulator ->
+//              registers, the epilogue, a 128 x 128-byte panel in shared memory, TMA store.
+// A and B may lie with k along a row (the forward; A of dx = dp W) or with m / n along a row (B of dx; both of dw = dp^T x, the
+// contraction down the rows): the panels are multiplied as they lie.  What lies past an edge reads as zero and is not stored, so
+// that every size runs; rows that are not 16-byte aligned are stored (and the residual read) with plain accesses, through the
+// same shared-memory panel.
+// Splits: item s of a split tile takes its share of the K blocks and stores fp32 partial rows [s * split_rows + m]; the caller
+// adds them up in a fixed order.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "whtmix_kernels.cuh"
+#include "whtmix_linear.cuh"
+#include "whtmix_tc.cuh"
+#include "whtmix_tma.cuh"
+
+namespace whtmix {
+namespace linear {
+
+struct Gemm {
+  CUtensorMap ta, tb, ty, tr, tp;
+  // plain accesses where a matrix has no tensor map (y_plain and so on; elements, strides in elements)
+  void* y;
+  const void* r;
+  void* p;
+  long long ys, rs, ps;
+  const float *bias, *sm, *sn;  // sm, sn: scales of the rows of A and B, or null
+  int M, N, kblocks, tiles_m, tiles_n, splits, split_rows, act;
+  bool has_r, has_p, y_plain, r_plain, p_plain;
+  unsigned int* err;
+};
+
+constexpr int GEMM_THREADS = 384;
+constexpr int GEMM_BM = 128;
+constexpr uint32_t RING_BYTES = 192 * 1024, PANEL_BYTES = 128 * 128;
+constexpr size_t GEMM_SMEM = RING_BYTES + 2 * PANEL_BYTES + 1024;  // 1024: alignment slack
+
+template <int BN>
+struct Ring {
+  static constexpr uint32_t A = GEMM_BM * 128, B = BN * 128, STAGE = A + B;
+  static constexpr int STAGES = RING_BYTES / STAGE;  // 4, 6, 8
+};
+
+template <int BN>
+struct GemmBars {
+  uint64_t full[Ring<BN>::STAGES], empty[Ring<BN>::STAGES], dfull[2], dempty[2], rfull[2];
+};
+
+__device__ __forceinline__ void tmem_ld32(uint32_t ta, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+               "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+                 "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]),
+                 "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]),
+                 "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+               : "r"(ta) : "memory");
+}
+
+// Panels with m or n along their 128-byte rows: 64 elements of it a panel, `panel` bytes to the next 64, 1024 to the next 8 k.
+__device__ __forceinline__ uint64_t mn_major_desc(uint32_t addr, uint32_t panel) {
+  return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(panel >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ float activate(float z, int act) {
+  switch (act) {
+    case ACT_RELU: return z < 0.f ? 0.f : z;
+    case ACT_GELU: return __fdividef(z, 1.f + __expf(-GELU_2A * (z + GELU_B * z * z * z)));
+    case ACT_SILU: return __fdividef(z, 1.f + __expf(-z));
+    default: return z;
+  }
+}
+
+template <typename O> struct Panel;  // a 128-byte row of the output
+template <> struct Panel<__nv_bfloat16> {
+  static constexpr int W = 64;
+};
+template <> struct Panel<float> {
+  static constexpr int W = 32;
+};
+
+// byte of element c of row r of a swizzled panel
+template <typename O>
+__device__ __forceinline__ uint32_t panel_at(int r, int c) {
+  constexpr int E = 16 / sizeof(O);
+  return r * 128 + (((c / E) ^ (r & 7)) << 4) + (c % E) * static_cast<int>(sizeof(O));
+}
+
+// The group's 128 threads copy a panel between shared memory and rows m0 .. of an unaligned matrix.
+template <typename O, bool STORE>
+__device__ __forceinline__ void panel_plain(unsigned char* s, void* g, long long stride, int m0, int M, int col0, int N, int gt) {
+  constexpr int W = Panel<O>::W;
+  const int lane = gt & 31, warp = gt >> 5;
+  for (int r = warp; r < GEMM_BM; r += 4) {
+    if (m0 + r >= M) break;
+    O* row = static_cast<O*>(g) + (m0 + r) * stride + col0;
+#pragma unroll
+    for (int c = lane; c < W; c += 32) {
+      if (col0 + c < N) {
+        O* q = reinterpret_cast<O*>(s + panel_at<O>(r, c));
+        if (STORE) row[c] = *q; else *q = row[c];
+      }
+    }
+  }
+}
+
+template <typename O>
+__device__ __forceinline__ void panel_put(unsigned char* s, int row, const float* v);
+template <>
+__device__ __forceinline__ void panel_put<__nv_bfloat16>(unsigned char* s, int row, const float* v) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    uint32_t h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * q + 2 * j], v[8 * q + 2 * j + 1]);
+      h[j] = *reinterpret_cast<uint32_t*>(&b);
+    }
+    *reinterpret_cast<uint4*>(s + row * 128 + ((q ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+  }
+}
+template <>
+__device__ __forceinline__ void panel_put<float>(unsigned char* s, int row, const float* v) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    *reinterpret_cast<float4*>(s + row * 128 + ((q ^ (row & 7)) << 4)) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+}
+template <typename O>
+__device__ __forceinline__ void panel_add(const unsigned char* s, int row, float* v);
+template <>
+__device__ __forceinline__ void panel_add<__nv_bfloat16>(const unsigned char* s, int row, float* v) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const uint4 u = *reinterpret_cast<const uint4*>(s + row * 128 + ((q ^ (row & 7)) << 4));
+    const uint32_t a[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[8 * q + 2 * j] += __uint_as_float(a[j] << 16);
+      v[8 * q + 2 * j + 1] += __uint_as_float(a[j] & 0xffff0000u);
+    }
+  }
+}
+template <>
+__device__ __forceinline__ void panel_add<float>(const unsigned char* s, int row, float* v) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float4 u = *reinterpret_cast<const float4*>(s + row * 128 + ((q ^ (row & 7)) << 4));
+    v[4 * q] += u.x, v[4 * q + 1] += u.y, v[4 * q + 2] += u.z, v[4 * q + 3] += u.w;
+  }
+}
+
+// E4M3: A and B are e4m3 (else bf16); A_MN, B_MN: m / n along the rows of A / B (bf16 only); O: the output's type.
+template <bool E4M3, bool A_MN, bool B_MN, int BN, typename O>
+__global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant__ Gemm a) {
+  static_assert(!E4M3 || (!A_MN && !B_MN), "8-bit operands lie with k along their rows");
+  using R = Ring<BN>;
+  constexpr int S = R::STAGES, BK = E4M3 ? 128 : 64, PW = Panel<O>::W, PANELS = BN / PW;
+  constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                             (static_cast<uint32_t>(BN >> 3) << 17) | ((128u >> 4) << 24);
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ GemmBars<BN> bars;
+  __shared__ uint32_t tmem_slot;
+  __shared__ float s_bias[2][64], s_scale[2][64];
+  unsigned char* smem = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
+  const uint32_t ring = tc::smem_u32(smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (warp == 0) tc::tmem_alloc(&tmem_slot, 2 * BN);
+  if (tid == 32) {
+    for (int s = 0; s < S; ++s) tc::mbar_init(&bars.full[s], 1), tc::mbar_init(&bars.empty[s], 1);
+    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], 8), tc::mbar_init(&bars.rfull[s], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma::prefetch(&a.ta);
+    tma::prefetch(&a.tb);
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  pdl_wait();
+  const uint32_t tmem = tmem_slot;
+  const int items = a.tiles_m * a.tiles_n * a.splits;
+  // item -> tile (n fastest) and split (slowest)
+  auto place = [&](int item, int& m0, int& n0, int& split) {
+    const int tile = item % (a.tiles_m * a.tiles_n);
+    split = item / (a.tiles_m * a.tiles_n);
+    m0 = tile / a.tiles_n * GEMM_BM;
+    n0 = tile % a.tiles_n * BN;
+  };
+  auto first_block = [&](int split) { return static_cast<int>(static_cast<long long>(a.kblocks) * split / a.splits); };
+  unsigned bad = 0;
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      for (int item = blockIdx.x; item < items && !bad; item += gridDim.x) {
+        int m0, n0, split;
+        place(item, m0, n0, split);
+        const int k1 = first_block(split + 1);
+        for (int kb = first_block(split); kb < k1; ++kb, ++it) {
+          const int s = it % S;
+          if (!tc::mbar_wait(&bars.empty[s], ((it / S) & 1) ^ 1)) {
+            bad |= 1;
+            break;
+          }
+          const uint32_t sa = ring + s * R::STAGE, sb = sa + R::A;
+          tma::expect_tx(&bars.full[s], R::STAGE);
+          if constexpr (A_MN) {
+#pragma unroll
+            for (int i = 0; i < GEMM_BM / 64; ++i) tma::load_2d(sa + i * 8192, &a.ta, m0 + 64 * i, kb * BK, &bars.full[s]);
+          } else {
+            tma::load_2d(sa, &a.ta, kb * BK, m0, &bars.full[s]);
+          }
+          if constexpr (B_MN) {
+#pragma unroll
+            for (int i = 0; i < BN / 64; ++i) tma::load_2d(sb + i * 8192, &a.tb, n0 + 64 * i, kb * BK, &bars.full[s]);
+          } else {
+            tma::load_2d(sb, &a.tb, kb * BK, n0, &bars.full[s]);
+          }
+        }
+      }
+      // the copies in flight have landed before the CTA can end
+      for (uint32_t j = it > S ? it - S : 0; j < it; ++j)
+        if (!tc::mbar_wait(&bars.full[j % S], (j / S) & 1)) bad |= 1;
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t it = 0, i = 0;
+      for (int item = blockIdx.x; item < items && !bad; item += gridDim.x, ++i) {
+        int m0, n0, split;
+        place(item, m0, n0, split);
+        const int d = i & 1, k0 = first_block(split), k1 = first_block(split + 1);
+        if (!tc::mbar_wait(&bars.dempty[d], ((i >> 1) & 1) ^ 1)) {
+          bad |= 2;
+          break;
+        }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int kb = k0; kb < k1; ++kb, ++it) {
+          const int s = it % S;
+          if (!tc::mbar_wait(&bars.full[s], (it / S) & 1)) {
+            bad |= 4;
+            break;
+          }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t sa = ring + s * R::STAGE, sb = sa + R::A;
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {  // 32 bytes of k
+            const uint64_t da = A_MN ? mn_major_desc(sa + ks * 2048, 8192) : tc::sw128_desc(sa + ks * 32);
+            const uint64_t db = B_MN ? mn_major_desc(sb + ks * 2048, 8192) : tc::sw128_desc(sb + ks * 32);
+            const uint32_t acc = kb > k0 || ks > 0;
+            if constexpr (E4M3)
+              mma_e4m3(tmem + d * BN, da, db, IDESC, acc);
+            else
+              tc::mma_bf16(tmem + d * BN, da, db, IDESC, acc);
+          }
+          tc::mma_commit(&bars.empty[s]);
+        }
+        tc::mma_commit(&bars.dfull[d]);
+      }
+      // every product has completed before the tensor memory is freed
+      for (uint32_t j = i > 2 ? i - 2 : 0; j < i; ++j)
+        if (!tc::mbar_wait(&bars.dfull[j & 1], (j >> 1) & 1)) bad |= 2;
+    }
+  } else if (warp >= 4) {
+    const int g = (warp - 4) >> 2, gt = tid - 128 - 128 * g, row = 32 * (warp & 3) + lane;
+    unsigned char* st = smem + RING_BYTES + g * PANEL_BYTES;
+    const uint32_t st_u = tc::smem_u32(st), lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+    uint32_t i = 0, loads = 0;
+    auto sync_group = [&] { asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory"); };
+    auto wait = [&](uint64_t* b, uint32_t parity) {  // (after one wait has given up none is waited for)
+      if (!bad && !tc::mbar_wait(b, parity)) bad |= 8;
+    };
+    for (int item = blockIdx.x; item < items; item += gridDim.x, ++i) {
+      int m0, n0, split;
+      place(item, m0, n0, split);
+      const int d = i & 1, yrow = split * a.split_rows + m0;
+      const int panels = min(PANELS, (a.N - n0 + PW - 1) / PW);
+      const float sm = a.sm && m0 + row < a.M ? a.sm[m0 + row] : 1.f;
+      bool waited = false;
+      for (int p = g; p < panels; p += 2) {
+        const int col0 = n0 + p * PW;
+        if (gt == 0) tma::wait_read();
+        if (gt < PW) {
+          s_bias[g][gt] = a.bias && col0 + gt < a.N ? a.bias[col0 + gt] : 0.f;
+          s_scale[g][gt] = a.sn && col0 + gt < a.N ? a.sn[col0 + gt] : 1.f;
+        }
+        sync_group();  // the panel is free, its bias has arrived
+        auto load_r = [&] {
+          if (a.r_plain) {
+            panel_plain<O, false>(st, const_cast<void*>(a.r), a.rs, m0, a.M, col0, a.N, gt);
+          } else if (gt == 0) {
+            tma::expect_tx(&bars.rfull[g], PANEL_BYTES);
+            tma::load_2d(st_u, &a.tr, col0, m0, &bars.rfull[g]);
+          }
+        };
+        if (a.has_r && !a.has_p) load_r();
+        if (!waited) {
+          wait(&bars.dfull[d], (i >> 1) & 1);
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          waited = true;
+        }
+        __syncwarp();
+        float v[PW];
+#pragma unroll
+        for (int c = 0; c < PW; c += 32) tmem_ld32(tmem + lanes + d * BN + p * PW + c, v + c);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (p + 2 >= panels) {  // the accumulator has been read
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) tma::arrive(&bars.dempty[d]);
+        }
+        if (a.sm) {
+#pragma unroll
+          for (int c = 0; c < PW; ++c) v[c] *= sm * s_scale[g][c];
+        }
+        if (a.bias) {
+#pragma unroll
+          for (int c = 0; c < PW; ++c) v[c] += s_bias[g][c];
+        }
+        if constexpr (PW == 64) {
+          if (a.has_p) {
+            panel_put<__nv_bfloat16>(st, row, v);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            sync_group();
+            if (a.p_plain) {
+              panel_plain<__nv_bfloat16, true>(st, a.p, a.ps, m0, a.M, col0, a.N, gt);
+            } else if (gt == 0) {
+              tma::store_2d(&a.tp, col0, m0, st_u);
+              tma::commit();
+              tma::wait_read();
+            }
+            sync_group();
+            if (a.has_r) load_r();
+          }
+        }
+        switch (a.act) {
+#define WHTMIX_ACT(A)                                             \
+  case A:                                                         \
+    _Pragma("unroll") for (int c = 0; c < PW; ++c) v[c] = activate(v[c], A); \
+    break
+          WHTMIX_ACT(ACT_RELU);
+          WHTMIX_ACT(ACT_GELU);
+          WHTMIX_ACT(ACT_SILU);
+#undef WHTMIX_ACT
+          default: break;
+        }
+        if (a.has_r) {
+          if (a.r_plain)
+            sync_group();
+          else
+            wait(&bars.rfull[g], loads++ & 1);
+          panel_add<O>(st, row, v);
+        }
+        panel_put<O>(st, row, v);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        sync_group();
+        if (a.y_plain) {
+          panel_plain<O, true>(st, a.y, a.ys, m0, a.M, col0, a.N, gt);
+        } else if (gt == 0) {
+          tma::store_2d(&a.ty, col0, yrow, st_u);
+          tma::commit();
+        }
+      }
+      if (!waited) {  // no panel of this tile for this group
+        wait(&bars.dfull[d], (i >> 1) & 1);
+        __syncwarp();
+        if (lane == 0) tma::arrive(&bars.dempty[d]);
+      }
+    }
+    if (gt == 0) tma::wait_done();
+    if (bad && loads && !tc::mbar_wait(&bars.rfull[g], (loads - 1) & 1)) bad |= 16;  // a residual panel in flight
+  }
+  if (bad) atomicOr(a.err, bad << 16);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  pdl_trigger();
+  if (warp == 0) tc::tmem_dealloc(tmem, 2 * BN);
+}
+
+// One instance's launch: a persistent grid of at most one CTA per SM.
+template <bool E4M3, bool A_MN, bool B_MN, int BN, typename O>
+cudaError_t launch_gemm(const Gemm& g, int sms, cudaStream_t stream) {
+  const void* k = reinterpret_cast<const void*>(k_gemm<E4M3, A_MN, B_MN, BN, O>);
+  static std::atomic<uint64_t> raised{0};  // devices (of the first 64) where the shared-memory limit is raised
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!bit || !(raised.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(GEMM_SMEM));
+    if (e != cudaSuccess) return e;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  const long long items = static_cast<long long>(g.tiles_m) * g.tiles_n * g.splits;
+  Gemm c = g;
+  void* args[] = {&c};
+  return launch_pdl(k, static_cast<unsigned>(items < sms ? items : sms), GEMM_THREADS, GEMM_SMEM, stream, args);
+}
+
+// whtmix_gemm_fwd.cu: y from x and W; whtmix_gemm_bwd.cu: dx (A with k, B with n along its rows) and dw (both m / n)
+cudaError_t gemm_forward(const Gemm& g, bool e4m3, bool out_f32, int bn, int sms, cudaStream_t stream);
+cudaError_t gemm_dx(const Gemm& g, int bn, int sms, cudaStream_t stream);
+cudaError_t gemm_dw(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
+
+}  // namespace linear
+}  // namespace whtmix

@@ -1,0 +1,362 @@
+// whtmix_linear.cu -- host side of the linear layer (y = act(x W^T + b) + r and its backward) and the passes around its products:
+// rows copied to a 16-byte pitch where the tensor maps need one, dp = dy act'(p) with the bias's gradient, the sum of a split
+// weight gradient's partial products.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "whtmix_gemm.cuh"
+#include "whtmix_linear.cuh"
+#include "whtmix_norm.cuh"
+
+namespace whtmix {
+namespace linear {
+
+constexpr int THREADS_256 = 256;
+
+// ---- rows to a 16-byte pitch ----
+// dst [rows, pitch] = src [rows, cols] (stride elements a row), zeros beyond cols; a thread writes 16 bytes.  pitch * sizeof(E) is
+// a multiple of 16.
+template <typename E>
+__global__ void __launch_bounds__(THREADS_256) k_pitch(E* __restrict__ dst, const E* __restrict__ src, long long rows, int cols,
+                                                       long long stride, int pitch) {
+  constexpr int V = 16 / sizeof(E);
+  pdl_wait();
+  const int per_row = pitch / V;
+  const long long n = rows * per_row, step = static_cast<long long>(gridDim.x) * THREADS_256;
+  for (long long i = static_cast<long long>(blockIdx.x) * THREADS_256 + threadIdx.x; i < n; i += step) {
+    const long long r = i / per_row;
+    const int c = static_cast<int>(i - r * per_row) * V;
+    const E* s = src + r * stride + c;
+    __align__(16) E v[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = c + j < cols ? s[j] : E(0);
+    *reinterpret_cast<uint4*>(dst + r * pitch + c) = *reinterpret_cast<const uint4*>(v);
+  }
+  pdl_trigger();
+}
+
+static cudaError_t to_pitch(void* dst, const void* src, long long rows, int cols, long long stride, int pitch, int es, int sms,
+                            cudaStream_t stream) {
+  const long long n = rows * (pitch / (16 / es)), need = (n + THREADS_256 - 1) / THREADS_256, most = 8ll * sms;
+  void* args[] = {&dst, &src, &rows, &cols, &stride, &pitch};
+  return launch_pdl(es == 1 ? reinterpret_cast<const void*>(k_pitch<uint8_t>) : reinterpret_cast<const void*>(k_pitch<uint16_t>),
+                    static_cast<unsigned>(need < most ? need : most), THREADS_256, 0, stream, args);
+}
+
+// ---- dp and db ----
+__device__ __forceinline__ float slope(float z, int act) {
+  if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
+  const float u2 = act == ACT_GELU ? GELU_2A * (z + GELU_B * z * z * z) : z;
+  const float du2 = act == ACT_GELU ? GELU_2A * (1.f + 3.f * GELU_B * z * z) : 1.f;
+  const float e = __expf(-u2), s = __fdividef(1.f, 1.f + e);
+  // s (1 + z (1 - s) du2); far below zero 1 - s is 1 and s is 0
+  return s * (1.f + z * (1.f - s) * du2);
+}
+
+// dp[t, n] = bf16(dy act'(p)); part[chunk][n] = the chunk's rows' float32 sum of dy act'(p), before the rounding.  A CTA takes 256
+// columns (a thread 8: consecutive with AL, else every 32nd) and the rows of chunk blockIdx.y, 8 at a time.  dp, part: or null.
+template <bool AL>
+__global__ void __launch_bounds__(THREADS_256) k_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
+  __shared__ float s[8][32][9];
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c0 = blockIdx.x * 256 + (AL ? 8 * lane : lane);
+  constexpr int STEP = AL ? 1 : 32;
+  const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
+  float acc[8] = {};
+  pdl_wait();
+  const uint16_t *dy = static_cast<const uint16_t*>(a.dy), *p = static_cast<const uint16_t*>(a.p);
+  auto load = [&](const uint16_t* row, float (&f)[8]) {
+    if constexpr (AL) {
+      const uint4 u = c0 < a.N ? *reinterpret_cast<const uint4*>(row + c0) : make_uint4(0u, 0u, 0u, 0u);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = c0 + 32 * j < a.N ? __uint_as_float(static_cast<uint32_t>(row[c0 + 32 * j]) << 16) : 0.f;
+    }
+  };
+#pragma unroll 2
+  for (long long t = t0 + g; t < t1; t += 8) {
+    float d[8], z[8];
+    load(dy + t * a.dys, d);
+    if (a.act != ACT_NONE) {
+      load(p + t * a.ps, z);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[j] *= slope(z[j], a.act);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] += d[j];
+    if (dp) {
+      if constexpr (AL) {
+        uint32_t h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          __nv_bfloat162 b = __floats2bfloat162_rn(d[2 * j], d[2 * j + 1]);
+          h[j] = *reinterpret_cast<uint32_t*>(&b);
+        }
+        if (c0 < a.N) *reinterpret_cast<uint4*>(dp + t * dps + c0) = make_uint4(h[0], h[1], h[2], h[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c0 + 32 * j < a.N) dp[t * dps + c0 + 32 * j] = __float2bfloat16_rn(d[j]);
+      }
+    }
+  }
+  if (part) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[g][lane][j] = acc[j];
+    __syncthreads();
+    const int l = AL ? threadIdx.x >> 3 : threadIdx.x & 31, j = AL ? threadIdx.x & 7 : threadIdx.x >> 5;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += s[i][l][j];
+    const int c = blockIdx.x * 256 + (AL ? 8 * l + j : l + STEP * j);
+    if (c < a.N) part[static_cast<long long>(blockIdx.y) * a.N + c] = sum;
+  }
+  pdl_trigger();
+}
+
+// ---- the sum of a split product ----
+// out [rows, cols] contiguous = sum over s of part[s * split_rows + row][pitch], in ascending s
+template <typename O>
+__global__ void __launch_bounds__(THREADS_256) k_sum_splits(O* __restrict__ out, const float* part, int rows, int cols, int pitch,
+                                                            int split_rows, int splits) {
+  pdl_wait();
+  const int quads = (cols + 3) / 4;
+  const long long n = static_cast<long long>(rows) * quads, step = static_cast<long long>(gridDim.x) * THREADS_256;
+  for (long long i = static_cast<long long>(blockIdx.x) * THREADS_256 + threadIdx.x; i < n; i += step) {
+    const int r = static_cast<int>(i / quads), c = static_cast<int>(i - static_cast<long long>(r) * quads) * 4;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(part + (static_cast<long long>(s) * split_rows + r) * pitch + c));
+      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+    const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+    O* o = out + static_cast<long long>(r) * cols + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + j < cols) o[j] = static_cast<O>(f[j]);
+  }
+  pdl_trigger();
+}
+
+// ---- host ----
+
+static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
+static int pitch_of(int cols, int es) { return (cols + 16 / es - 1) / (16 / es) * (16 / es); }
+static int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+
+// Tile width and splits of a product of tiles_m rows of tiles, N columns and kblocks K blocks.  A tile's block takes the larger of
+// its products (2 BN clocks) and its operands' way out of shared memory ((128 + BN) clocks at 128 bytes a clock); a tile costs
+// about TILE_CLOCKS besides, and a split product's partial tiles their way through memory.
+struct Plan {
+  int bn, splits;
+};
+static Plan plan_product(long long tiles_m, int N, int kblocks, int sms, int max_splits) {
+  constexpr double TILE_CLOCKS = 1500.0;
+  Plan best{256, 1};
+  double best_cost = 1e300;
+  for (int bn = 256; bn >= 64; bn >>= 1) {
+    const long long tiles = tiles_m * ceil_div(N, bn);
+    const double block = 2 * bn > 128 + bn ? 2 * bn : 128 + bn;
+    // one split, or as many as fill 1 .. 4 waves
+    for (int w = 0; w <= 4; ++w) {
+      const long long fill = w == 0 ? 1 : static_cast<long long>(w) * sms / tiles;
+      const int s = static_cast<int>(fill < max_splits ? (fill < kblocks ? fill : kblocks) : (max_splits < kblocks ? max_splits : kblocks));
+      if (s < 1 || (w > 0 && s == 1)) continue;
+      const double waves = ceil_div(tiles * s, sms);
+      // partial tiles: written and read back, 8 bytes an element, at about 3000 bytes a clock for the whole device
+      const double join = s > 1 ? 4000.0 + static_cast<double>(tiles) * 128.0 * bn * s * 8.0 / 3000.0 : 0.0;
+      const double cost = waves * (ceil_div(kblocks, s) * block + TILE_CLOCKS) + join;
+      if (cost < best_cost * 0.999) best_cost = cost, best = {bn, s};
+    }
+  }
+  return best;
+}
+
+struct ForwardPlan {
+  bool pad_x, pad_w;
+  int kp;
+  size_t x_off, w_off, total;
+};
+static ForwardPlan plan_forward(const Forward& a) {
+  ForwardPlan f{};
+  const int es = a.e4m3 ? 1 : 2;
+  f.kp = pitch_of(a.K, es);
+  f.pad_x = !tma::mappable(a.x, a.T, a.xs, es);
+  f.pad_w = !tma::mappable(a.w, a.N, a.ws, es);
+  if (f.pad_x) f.x_off = f.total, f.total += align256(static_cast<size_t>(a.T) * f.kp * es);
+  if (f.pad_w) f.w_off = f.total, f.total += align256(static_cast<size_t>(a.N) * f.kp * es);
+  return f;
+}
+
+size_t forward_workspace(const Forward& a, int) { return plan_forward(a).total; }
+
+cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
+  const ForwardPlan f = plan_forward(a);
+  const int es = a.e4m3 ? 1 : 2, os = a.out_f32 ? 4 : 2;
+  const void *x = a.x, *w = a.w;
+  long long xs = a.xs, wst = a.ws;
+  cudaError_t e;
+  if (f.pad_x) {
+    void* d = static_cast<char*>(ws) + f.x_off;
+    if ((e = to_pitch(d, a.x, a.T, a.K, a.xs, f.kp, es, sms, stream)) != cudaSuccess) return e;
+    x = d, xs = f.kp;
+  }
+  if (f.pad_w) {
+    void* d = static_cast<char*>(ws) + f.w_off;
+    if ((e = to_pitch(d, a.w, a.N, a.K, a.ws, f.kp, es, sms, stream)) != cudaSuccess) return e;
+    w = d, wst = f.kp;
+  }
+  Gemm g{};
+  g.tiles_m = ceil_div(a.T, GEMM_BM);
+  g.kblocks = ceil_div(a.K, 128 / es);
+  const Plan pl = plan_product(g.tiles_m, a.N, g.kblocks, sms, 1);
+  g.tiles_n = ceil_div(a.N, pl.bn);
+  g.splits = 1;
+  g.M = static_cast<int>(a.T), g.N = a.N, g.act = a.act;
+  g.bias = a.bias, g.sm = a.x_scale, g.sn = a.w_scale;
+  g.y = a.y, g.r = a.r, g.p = a.p, g.ys = a.ys, g.rs = a.rs, g.ps = a.ps;
+  g.has_r = a.r != nullptr, g.has_p = a.p != nullptr;
+  g.y_plain = !tma::mappable(a.y, a.T, a.ys, os);
+  g.r_plain = a.r && !tma::mappable(a.r, a.T, a.rs, os);
+  g.p_plain = a.p && !tma::mappable(a.p, a.T, a.ps, 2);
+  g.err = err;
+  if (!tma::encode_rows(&g.ta, x, es, a.T, a.K, xs, GEMM_BM) || !tma::encode_rows(&g.tb, w, es, a.N, a.K, wst, pl.bn) ||
+      (!g.y_plain && !tma::encode_rows(&g.ty, a.y, os, a.T, a.N, a.ys, GEMM_BM)) ||
+      (g.has_r && !g.r_plain && !tma::encode_rows(&g.tr, a.r, os, a.T, a.N, a.rs, GEMM_BM)) ||
+      (g.has_p && !g.p_plain && !tma::encode_rows(&g.tp, a.p, 2, a.T, a.N, a.ps, GEMM_BM)))
+    return cudaErrorInvalidValue;
+  return gemm_forward(g, a.e4m3, a.out_f32, pl.bn, sms, stream);
+}
+
+struct BackwardPlan {
+  bool own_dp, pad_x, pad_w;
+  int np, kp, chunks;  // pitches of dp, and of x and W; db's chunks of rows
+  Plan dw;
+  int split_rows;
+  size_t dp_off, x_off, w_off, db_off, dw_off, total;
+};
+static BackwardPlan plan_backward(const Backward& a, int sms) {
+  BackwardPlan b{};
+  b.np = pitch_of(a.N, 2), b.kp = pitch_of(a.K, 2);
+  b.own_dp = (a.dx || a.dw) && (a.act != ACT_NONE || !tma::mappable(a.dy, a.T, a.dys, 2));
+  b.pad_x = a.dw && !tma::mappable(a.x, a.T, a.xs, 2);
+  b.pad_w = a.dx && !tma::mappable(a.w, a.N, a.ws, 2);
+  auto take = [&](size_t bytes) {
+    const size_t off = b.total;
+    b.total += align256(bytes);
+    return off;
+  };
+  if (b.own_dp) b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);
+  if (b.pad_x) b.x_off = take(static_cast<size_t>(a.T) * b.kp * 2);
+  if (b.pad_w) b.w_off = take(static_cast<size_t>(a.N) * b.kp * 2);
+  if (a.db || b.own_dp) {
+    const int strips = ceil_div(a.N, 256), rows = ceil_div(a.T, 16), most = (8 * sms + strips - 1) / strips;
+    b.chunks = rows < most ? rows : most;
+    if (b.chunks > 65535) b.chunks = 65535;
+    if (a.db) b.db_off = take(static_cast<size_t>(b.chunks) * a.N * 4);
+  }
+  if (a.dw) {
+    const int tiles_m = ceil_div(a.N, GEMM_BM);
+    b.dw = plan_product(tiles_m, a.K, ceil_div(a.T, 64), sms, 2 * sms);
+    b.split_rows = tiles_m * GEMM_BM;
+    if (b.dw.splits > 1) b.dw_off = take(static_cast<size_t>(b.dw.splits) * b.split_rows * pitch_of(a.K, 4) * 4);
+  }
+  return b;
+}
+
+size_t backward_workspace(const Backward& a, int sms) { return plan_backward(a, sms).total; }
+
+cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
+  const BackwardPlan b = plan_backward(a, sms);
+  char* base = static_cast<char*>(ws);
+  cudaError_t e;
+  const void* dp = a.dy;
+  long long dps = a.dys;
+  if (a.db || b.own_dp) {
+    Backward c = a;
+    __nv_bfloat16* d = b.own_dp ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
+    float* part = a.db ? reinterpret_cast<float*>(base + b.db_off) : nullptr;
+    long long np = b.np;
+    int chunks = b.chunks;
+    const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && (a.act == ACT_NONE || tma::mappable(a.p, a.T, a.ps, 2));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ceil_div(a.N, 256), chunks);
+    cfg.blockDim = dim3(THREADS_256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, al ? k_dp<true> : k_dp<false>, c, d, np, part, chunks);
+    if (e != cudaSuccess) return e;
+    if (b.own_dp) dp = d, dps = b.np;
+    if (a.db && (e = norm::add_rows(part, a.db, a.N, chunks, stream)) != cudaSuccess) return e;
+  }
+  if (a.dx) {
+    const void* w = a.w;
+    long long wst = a.ws;
+    if (b.pad_w) {
+      void* d = base + b.w_off;
+      if ((e = to_pitch(d, a.w, a.N, a.K, a.ws, b.kp, 2, sms, stream)) != cudaSuccess) return e;
+      w = d, wst = b.kp;
+    }
+    Gemm g{};
+    g.tiles_m = ceil_div(a.T, GEMM_BM);
+    g.kblocks = ceil_div(a.N, 64);
+    const Plan pl = plan_product(g.tiles_m, a.K, g.kblocks, sms, 1);
+    g.tiles_n = ceil_div(a.K, pl.bn);
+    g.splits = 1;
+    g.M = static_cast<int>(a.T), g.N = a.K;
+    g.y = a.dx, g.ys = a.dxs, g.y_plain = !tma::mappable(a.dx, a.T, a.dxs, 2);
+    g.err = err;
+    if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, GEMM_BM) || !tma::encode_rows(&g.tb, w, 2, a.N, a.K, wst, 64) ||
+        (!g.y_plain && !tma::encode_rows(&g.ty, a.dx, 2, a.T, a.K, a.dxs, GEMM_BM)))
+      return cudaErrorInvalidValue;
+    if ((e = gemm_dx(g, pl.bn, sms, stream)) != cudaSuccess) return e;
+  }
+  if (a.dw) {
+    const void* x = a.x;
+    long long xs = a.xs;
+    if (b.pad_x) {
+      void* d = base + b.x_off;
+      if ((e = to_pitch(d, a.x, a.T, a.K, a.xs, b.kp, 2, sms, stream)) != cudaSuccess) return e;
+      x = d, xs = b.kp;
+    }
+    Gemm g{};
+    g.tiles_m = ceil_div(a.N, GEMM_BM);
+    g.kblocks = ceil_div(a.T, 64);
+    g.tiles_n = ceil_div(a.K, b.dw.bn);
+    g.splits = b.dw.splits;
+    g.split_rows = b.split_rows;
+    g.M = a.N, g.N = a.K;
+    g.err = err;
+    const bool split = g.splits > 1;
+    const int kq = pitch_of(a.K, 4), os = split || a.dw_f32 ? 4 : 2;
+    void* out = split ? static_cast<void*>(base + b.dw_off) : a.dw;
+    const long long rows = split ? static_cast<long long>(g.splits) * b.split_rows : a.N, pitch = split ? kq : a.K;
+    g.y = out, g.ys = pitch, g.y_plain = !tma::mappable(out, rows, pitch, os);
+    if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, 64) || !tma::encode_rows(&g.tb, x, 2, a.T, a.K, xs, 64) ||
+        (!g.y_plain && !tma::encode_rows(&g.ty, out, os, rows, a.K, pitch, GEMM_BM)))
+      return cudaErrorInvalidValue;
+    if ((e = gemm_dw(g, os == 4, b.dw.bn, sms, stream)) != cudaSuccess) return e;
+    if (split) {
+      const float* part = static_cast<const float*>(out);
+      int rows_ = a.N, cols = a.K, pitch_ = kq, sr = b.split_rows, splits = g.splits;
+      void* dw = a.dw;
+      void* args[] = {&dw, &part, &rows_, &cols, &pitch_, &sr, &splits};
+      const long long n = static_cast<long long>(a.N) * ceil_div(a.K, 4), need = (n + THREADS_256 - 1) / THREADS_256;
+      e = launch_pdl(a.dw_f32 ? reinterpret_cast<const void*>(k_sum_splits<float>) : reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16>),
+                     static_cast<unsigned>(need < 8ll * sms ? need : 8ll * sms), THREADS_256, 0, stream, args);
+      if (e != cudaSuccess) return e;
+    }
+  }
+  return cudaSuccess;
+}
+
+}  // namespace linear
+}  // namespace whtmix

@@ -1,0 +1,517 @@
+// whtmix_norm.cu -- RMS norm with the residual's addition, its 8-bit output, and its backward.
+//
+//   h = x + r,   y_d = h_d w_d / sqrt(mean(h^2) + eps)                              one row of D channels
+//   8 bits: s = max_d |y_d| / 448,  q_d = e4m3(y_d / s).  1 / sqrt(mean + eps) cancels in y_d / s, so that the q are taken
+//   from h_d w_d and its largest magnitude, which is found in the same reduction as the sum of squares.
+//   backward, with rstd = 1 / sqrt(mean(h^2) + eps) and a = dy w:
+//     dx = rstd a - h rstd^3 mean(a h) + dh,      dw = sum over rows of dy h rstd
+//
+// All of it is bound by memory: a row is read once into registers (packed as stored), its sums meet in one reduction, and it is
+// written once.  TPR threads hold a row, NV 16-byte vectors each; up to 32 threads a row need no shared memory.  Sums are
+// float32 in a fixed order.  dw: every thread keeps its columns' sums over the rows that its CTA takes, the CTAs' partial rows
+// are added up by k_dw in a fixed order.  Rows that are not 16-byte aligned take element loads, consecutive threads consecutive
+// elements; rows beyond 2048 vectors are read twice (k_rms_long, k_rms_bwd_long).
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "whtmix_kernels.cuh"
+#include "whtmix_norm.cuh"
+
+namespace whtmix {
+namespace norm {
+
+constexpr float E4M3_MAX = 448.f;
+constexpr int MAX_VECTORS = 2048;  // vectors of a row that fit the threads' registers
+constexpr int LONG_THREADS = 512;
+
+template <typename T> struct Io;
+template <> struct Io<float> {
+  static constexpr int V = 4;
+  static __device__ __forceinline__ float get(const void* p, long long i) { return static_cast<const float*>(p)[i]; }
+  static __device__ __forceinline__ void put(void* p, long long i, float v) { static_cast<float*>(p)[i] = v; }
+  static __device__ __forceinline__ void unpack(uint4 u, float (&f)[4]) {
+    f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y), f[2] = __uint_as_float(u.z), f[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <> struct Io<__nv_bfloat16> {
+  static constexpr int V = 8;
+  static __device__ __forceinline__ float get(const void* p, long long i) {
+    return __uint_as_float(static_cast<uint32_t>(static_cast<const unsigned short*>(p)[i]) << 16);
+  }
+  static __device__ __forceinline__ void put(void* p, long long i, float v) {
+    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  }
+  static __device__ __forceinline__ void unpack(uint4 u, float (&f)[8]) {
+    const uint32_t a[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(a[j] << 16), f[2 * j + 1] = __uint_as_float(a[j] & 0xffff0000u);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    uint32_t a[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+      a[j] = *reinterpret_cast<uint32_t*>(&b);
+    }
+    return make_uint4(a[0], a[1], a[2], a[3]);
+  }
+};
+
+// The elements that thread `lane` of a row's TPR holds in vector k: with AL V consecutive ones, else one of every TPR.
+template <typename T, bool AL, int TPR>
+struct Row {
+  static constexpr int V = Io<T>::V;
+  static __device__ __forceinline__ long long at(int lane, int k, int j) {
+    return AL ? static_cast<long long>(lane + TPR * k) * V + j : lane + static_cast<long long>(TPR) * (k * V + j);
+  }
+  static __device__ __forceinline__ void load(const T* p, int lane, int k, int D, float (&f)[V]) {
+    if constexpr (AL) {
+      const long long e = at(lane, k, 0);
+      uint4 u = make_uint4(0u, 0u, 0u, 0u);
+      if (e < D) u = *reinterpret_cast<const uint4*>(p + e);
+      Io<T>::unpack(u, f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = at(lane, k, j) < D ? Io<T>::get(p, at(lane, k, j)) : 0.f;
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, int lane, int k, int D, const float (&f)[V]) {
+    if constexpr (AL) {
+      const long long e = at(lane, k, 0);
+      if (e < D) *reinterpret_cast<uint4*>(p + e) = Io<T>::pack(f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (at(lane, k, j) < D) Io<T>::put(p, at(lane, k, j), f[j]);
+    }
+  }
+  static __device__ __forceinline__ void gains(const float* w, int lane, int k, int D, float (&f)[V]) {
+    if constexpr (AL) {
+      const long long e = at(lane, k, 0);
+#pragma unroll
+      for (int j = 0; j < V; j += 4) {
+        const float4 v = e < D ? __ldg(reinterpret_cast<const float4*>(w + e + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        f[j] = v.x, f[j + 1] = v.y, f[j + 2] = v.z, f[j + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = at(lane, k, j) < D ? __ldg(w + at(lane, k, j)) : 0.f;
+    }
+  }
+  static __device__ __forceinline__ void store_e4m3(uint8_t* p, int lane, int k, int D, const float (&f)[V]) {
+    if constexpr (AL) {
+      const long long e = at(lane, k, 0);
+      uint32_t u[V / 4];
+#pragma unroll
+      for (int j = 0; j < V / 4; ++j)
+        u[j] = static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(f[4 * j], f[4 * j + 1]), __NV_SATFINITE, __NV_E4M3)) |
+               static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(f[4 * j + 2], f[4 * j + 3]), __NV_SATFINITE, __NV_E4M3))
+                   << 16;
+      if (e < D) {
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) reinterpret_cast<uint32_t*>(p + e)[j] = u[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (at(lane, k, j) < D) p[at(lane, k, j)] = __nv_cvt_float_to_fp8(f[j], __NV_SATFINITE, __NV_E4M3);
+    }
+  }
+};
+
+// Sum of a and sum of b (or, MAXB, the largest b by its bits: magnitudes, where a NaN is above infinity) over a row's TPR
+// threads, the same value in each.
+template <int TPR, bool MAXB>
+__device__ __forceinline__ void row_reduce(float& a, float& b) {
+  constexpr int W = TPR < 32 ? TPR : 32;
+  auto join = [](float u, float v) {
+    return MAXB ? __uint_as_float(max(__float_as_uint(u), __float_as_uint(v))) : u + v;
+  };
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, o);
+    b = join(b, __shfl_xor_sync(0xffffffffu, b, o));
+  }
+  if constexpr (TPR > 32) {
+    __shared__ float sa[TPR / 32], sb[TPR / 32];
+    __syncthreads();  // the previous row's values have been read
+    if ((threadIdx.x & 31) == 0) sa[threadIdx.x >> 5] = a, sb[threadIdx.x >> 5] = b;
+    __syncthreads();
+    a = sa[0], b = sb[0];
+#pragma unroll
+    for (int i = 1; i < TPR / 32; ++i) a += sa[i], b = join(b, sb[i]);
+  }
+}
+
+// 448 / top would overflow for a row of magnitudes below TINY: such a row is scaled up by a power of two first (exact).
+constexpr float TINY = 1e-30f, LIFT = 0x1p80f;
+__device__ __forceinline__ float to_e4m3_range(float top, float lift) { return top == 0.f ? 0.f : E4M3_MAX / (top * lift); }
+
+__device__ __forceinline__ float magnitude(float v) { return __uint_as_float(__float_as_uint(v) & 0x7fffffffu); }
+
+template <int TPR> constexpr int BLOCK_OF = TPR > 32 ? TPR : 256;  // threads a CTA
+
+template <typename T, bool Q8, bool AL, int TPR, int NV>
+__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a) {
+  constexpr int V = Io<T>::V, ROWS = BLOCK_OF<TPR> / TPR;
+  using R = Row<T, AL, TPR>;
+  const int lane = threadIdx.x % TPR;
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  pdl_wait();
+  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += static_cast<long long>(gridDim.x) * ROWS) {
+    const long long t = base + threadIdx.x / TPR;
+    const int D = t < a.T ? a.D : 0;  // a row past the end holds no elements
+    float h[NV][V];
+    float sq = 0.f, top = 0.f;
+    const T* x = static_cast<const T*>(a.x) + t * a.xs;
+    const T* r = static_cast<const T*>(a.r) + t * a.rs;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) R::load(x, lane, k, D, h[k]);
+    if (a.r) {
+      float f[NV][V];
+#pragma unroll
+      for (int k = 0; k < NV; ++k) R::load(r, lane, k, D, f[k]);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[k][j] += f[k][j];
+      if (a.h) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, D, h[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float w[V];
+      R::gains(a.w, lane, k, D, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        sq += h[k][j] * h[k][j];
+        h[k][j] *= w[j];
+        if (Q8) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(magnitude(h[k][j]))));
+      }
+    }
+    row_reduce<TPR, true>(sq, top);
+    const float rstd = rsqrtf(sq * inv_d + a.eps);
+    const float lift = Q8 && top < TINY ? LIFT : 1.f;
+    const float f = Q8 ? to_e4m3_range(top, lift) : rstd;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) h[k][j] = Q8 ? h[k][j] * lift * f : h[k][j] * f;
+      if constexpr (Q8)
+        R::store_e4m3(static_cast<uint8_t*>(a.y) + t * a.ys, lane, k, D, h[k]);
+      else
+        R::store(static_cast<T*>(a.y) + t * a.ys, lane, k, D, h[k]);
+    }
+    if (Q8 && lane == 0 && t < a.T) a.scale[t] = top * rstd * (1.f / E4M3_MAX);
+  }
+  pdl_trigger();
+}
+
+// Rows too long for the registers: a CTA a row, read twice (the second time from L2).  Element loads.
+template <typename T, bool Q8>
+__global__ void __launch_bounds__(LONG_THREADS) k_rms_long(const Forward a) {
+  pdl_wait();
+  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + t * a.xs;
+    const T* r = static_cast<const T*>(a.r) + t * a.rs;
+    float sq = 0.f, top = 0.f;
+    for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+      const float h = Io<T>::get(x, e) + (a.r ? Io<T>::get(r, e) : 0.f);
+      sq += h * h;
+      if (Q8) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(magnitude(h * __ldg(a.w + e)))));
+    }
+    row_reduce<LONG_THREADS, true>(sq, top);
+    const float rstd = rsqrtf(sq / static_cast<float>(a.D) + a.eps);
+    const float lift = Q8 && top < TINY ? LIFT : 1.f;
+    const float f = Q8 ? to_e4m3_range(top, lift) : rstd;
+    for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+      const float h = Io<T>::get(x, e) + (a.r ? Io<T>::get(r, e) : 0.f);
+      if (a.r && a.h) Io<T>::put(static_cast<T*>(a.h) + t * a.hs, e, h);
+      const float v = h * __ldg(a.w + e) * lift * f;
+      if constexpr (Q8)
+        (static_cast<uint8_t*>(a.y) + t * a.ys)[e] = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
+      else
+        Io<T>::put(static_cast<T*>(a.y) + t * a.ys, e, v);
+    }
+    if (Q8 && threadIdx.x == 0) a.scale[t] = top * rstd * (1.f / E4M3_MAX);
+  }
+  pdl_trigger();
+}
+
+// dx, and this CTA's partial row of dw: part[blockIdx.x][0 .. D).
+template <typename T, bool AL, int TPR, int NV>
+__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a) {
+  constexpr int V = Io<T>::V, ROWS = BLOCK_OF<TPR> / TPR;
+  using R = Row<T, AL, TPR>;
+  const int lane = threadIdx.x % TPR;
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  float acc[NV][V] = {};
+  pdl_wait();
+  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += static_cast<long long>(gridDim.x) * ROWS) {
+    const long long t = base + threadIdx.x / TPR;
+    const int D = t < a.T ? a.D : 0;
+    float h[NV][V], d[NV][V];
+    float sq = 0.f, ah = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) R::load(static_cast<const T*>(a.h) + t * a.hs, lane, k, D, h[k]);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) R::load(static_cast<const T*>(a.dy) + t * a.ys, lane, k, D, d[k]);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float w[V];
+      R::gains(a.w, lane, k, D, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        sq += h[k][j] * h[k][j];
+        ah += d[k][j] * w[j] * h[k][j];
+      }
+    }
+    row_reduce<TPR, false>(sq, ah);
+    const float rstd = rsqrtf(sq * inv_d + a.eps);
+    const float c = rstd * rstd * rstd * (ah * inv_d);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float w[V], o[V];
+      R::gains(a.w, lane, k, D, w);
+      if (a.dh) {
+        R::load(static_cast<const T*>(a.dh) + t * a.ds, lane, k, D, o);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        acc[k][j] += d[k][j] * (h[k][j] * rstd);
+        o[j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
+      }
+      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, D, o);
+    }
+  }
+  // the CTA's row groups hold the same columns: added in ascending group order, one vector at a time
+  float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.x) * a.D;
+  if constexpr (ROWS == 1) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (R::at(lane, k, j) < a.D) part[R::at(lane, k, j)] = acc[k][j];
+  } else {
+    __shared__ float s[ROWS][TPR][V + 1];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[threadIdx.x / TPR][lane][j] = acc[k][j];
+      __syncthreads();
+      for (int i = threadIdx.x; i < TPR * V; i += BLOCK_OF<TPR>) {
+        const int l = AL ? i / V : i % TPR, j = AL ? i % V : i / TPR;
+        float sum = 0.f;
+#pragma unroll
+        for (int g = 0; g < ROWS; ++g) sum += s[g][l][j];
+        if (R::at(l, k, j) < a.D) part[R::at(l, k, j)] = sum;
+      }
+    }
+  }
+  pdl_trigger();
+}
+
+// Rows too long for the registers: dx by a CTA a row; coef[t] = rstd for k_dw_long.
+template <typename T>
+__global__ void __launch_bounds__(LONG_THREADS) k_rms_bwd_long(const Backward a, float* __restrict__ coef) {
+  pdl_wait();
+  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const T* h = static_cast<const T*>(a.h) + t * a.hs;
+    const T* dy = static_cast<const T*>(a.dy) + t * a.ys;
+    float sq = 0.f, ah = 0.f;
+    for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+      const float v = Io<T>::get(h, e);
+      sq += v * v;
+      ah += Io<T>::get(dy, e) * __ldg(a.w + e) * v;
+    }
+    row_reduce<LONG_THREADS, false>(sq, ah);
+    const float inv_d = 1.f / static_cast<float>(a.D), rstd = rsqrtf(sq * inv_d + a.eps);
+    const float c = rstd * rstd * rstd * (ah * inv_d);
+    for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+      float o = a.dh ? Io<T>::get(static_cast<const T*>(a.dh) + t * a.ds, e) : 0.f;
+      o += rstd * (Io<T>::get(dy, e) * __ldg(a.w + e)) - c * Io<T>::get(h, e);
+      Io<T>::put(static_cast<T*>(a.dx) + t * a.xs, e, o);
+    }
+    if (threadIdx.x == 0) coef[t] = rstd;
+  }
+  pdl_trigger();
+}
+// part[blockIdx.y][e] = sum over the rows of chunk blockIdx.y of dy h rstd
+template <typename T>
+__global__ void __launch_bounds__(256) k_dw_long(const Backward a, const float* coef, int chunks) {
+  pdl_wait();
+  const int e = blockIdx.x * 256 + threadIdx.x;
+  const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
+  float sum = 0.f;
+  if (e < a.D) {
+    for (long long t = t0; t < t1; ++t)
+      sum += Io<T>::get(static_cast<const T*>(a.dy) + t * a.ys, e) * (Io<T>::get(static_cast<const T*>(a.h) + t * a.hs, e) * coef[t]);
+    (static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.y) * a.D)[e] = sum;
+  }
+  pdl_trigger();
+}
+
+// dw[e] = the sum of `parts` partial rows: 32 runs of consecutive rows, each in ascending order, then the run sums in
+// ascending order.  A CTA takes 32 columns.
+constexpr int DW_RUNS = 32;
+__global__ void __launch_bounds__(32 * DW_RUNS) k_dw(const float* part, float* __restrict__ dw, int D, int parts) {
+  __shared__ float s[DW_RUNS][33];
+  pdl_wait();
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+  const int p0 = parts * g / DW_RUNS, p1 = parts * (g + 1) / DW_RUNS;
+  float sum = 0.f;
+  if (e < D) {
+    int p = p0;
+    for (; p + 8 <= p1; p += 8) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = __ldcg(part + static_cast<long long>(p + u) * D + e);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum += v[u];
+    }
+    for (; p < p1; ++p) sum += __ldcg(part + static_cast<long long>(p) * D + e);
+  }
+  s[g][lane] = sum;
+  __syncthreads();
+  if (g == 0 && e < D) {
+    float total = s[0][lane];
+#pragma unroll
+    for (int i = 1; i < DW_RUNS; ++i) total += s[i][lane];
+    dw[e] = total;
+  }
+  pdl_trigger();
+}
+
+// ---- host ----
+
+// Threads a row and vectors a thread for rows of n vectors: at most 128 vectors stay within a warp (no shared memory).
+template <class F>
+cudaError_t by_length(int n, F&& f) {
+#define WHTMIX_ROW(TPR, NV) f(std::integral_constant<int, TPR>(), std::integral_constant<int, NV>())
+  if (n <= 8) return WHTMIX_ROW(8, 1);
+  if (n <= 16) return WHTMIX_ROW(16, 1);
+  if (n <= 32) return WHTMIX_ROW(32, 1);
+  if (n <= 64) return WHTMIX_ROW(32, 2);
+  if (n <= 128) return WHTMIX_ROW(32, 4);
+  if (n <= 256) return WHTMIX_ROW(128, 2);
+  if (n <= 512) return WHTMIX_ROW(128, 4);
+  if (n <= 1024) return WHTMIX_ROW(256, 4);
+  return WHTMIX_ROW(512, 4);
+#undef WHTMIX_ROW
+}
+
+int vectors(int D, bool bf16) { return bf16 ? (D + 7) / 8 : (D + 3) / 4; }
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// rows of `es`-byte elements at p, `stride` elements apart, all start on a 16-byte boundary
+bool rows_aligned(const void* p, long long stride, size_t es, size_t to = 16) {
+  return !p || (aligned(p, to) && (static_cast<unsigned long long>(stride) * es) % to == 0);
+}
+
+unsigned grid_rows(long long T, int rows, int block, int sms) {
+  const long long need = (T + rows - 1) / rows, most = static_cast<long long>(sms) * (2048 / block);
+  return static_cast<unsigned>(need < most ? need : most);
+}
+
+template <typename T, bool Q8>
+cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
+  const size_t es = sizeof(T);
+  const int n = vectors(a.D, es == 2);
+  if (n > MAX_VECTORS) {
+    Forward c = a;
+    void* args[] = {&c};
+    return launch_pdl(reinterpret_cast<const void*>(k_rms_long<T, Q8>), grid_rows(a.T, 1, LONG_THREADS, sms), LONG_THREADS, 0, stream, args);
+  }
+  const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.x, a.xs, es) && rows_aligned(a.r, a.rs, es) &&
+                  rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, 4) : rows_aligned(a.y, a.ys, es));
+  return by_length(n, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
+    const void* k = al ? reinterpret_cast<const void*>(k_rms<T, Q8, true, TPR, NV>)
+                       : reinterpret_cast<const void*>(k_rms<T, Q8, false, TPR, NV>);
+    Forward c = a;
+    void* args[] = {&c};
+    return launch_pdl(k, grid_rows(a.T, BLOCK / TPR, BLOCK, sms), BLOCK, 0, stream, args);
+  });
+}
+
+cudaError_t forward(const Forward& a, bool bf16, bool to_e4m3, int sms, cudaStream_t stream) {
+  if (a.T <= 0) return cudaSuccess;
+  if (bf16) return to_e4m3 ? forward_t<__nv_bfloat16, true>(a, sms, stream) : forward_t<__nv_bfloat16, false>(a, sms, stream);
+  return to_e4m3 ? forward_t<float, true>(a, sms, stream) : forward_t<float, false>(a, sms, stream);
+}
+
+// Partial rows of dw: one a CTA of k_rms_bwd (at most 512 resident threads an SM, which hold the sums of their columns), or one a
+// chunk of rows for k_dw_long.
+int dw_parts(long long T, int n, int sms) {
+  if (n > MAX_VECTORS) {
+    const long long most = 64;
+    return static_cast<int>(T < most ? T : most);
+  }
+  int parts = 0;
+  by_length(n, [&](auto tpr, auto) {
+    constexpr int TPR = decltype(tpr)::value, BLOCK = BLOCK_OF<TPR>;
+    const long long need = (T + BLOCK / TPR - 1) / (BLOCK / TPR), most = static_cast<long long>(sms) * (1024 / BLOCK);
+    parts = static_cast<int>(need < most ? need : most);
+    return cudaSuccess;
+  });
+  return parts;
+}
+
+size_t backward_workspace(long long T, int D, bool bf16, int sms) {
+  const int n = vectors(D, bf16);
+  return static_cast<size_t>(dw_parts(T, n, sms)) * D * 4 + (n > MAX_VECTORS ? static_cast<size_t>(T) * 4 : 0);
+}
+
+cudaError_t add_rows(const float* part, float* out, int D, int parts, cudaStream_t stream) {
+  void* args[] = {&part, &out, &D, &parts};
+  return launch_pdl(reinterpret_cast<const void*>(k_dw), static_cast<unsigned>((D + 31) / 32), 32 * DW_RUNS, 0, stream, args);
+}
+
+template <typename T>
+cudaError_t backward_t(const Backward& a, int sms, cudaStream_t stream) {
+  const size_t es = sizeof(T);
+  const int n = vectors(a.D, es == 2), parts = dw_parts(a.T, n, sms);
+  Backward c = a;
+  cudaError_t e;
+  if (n > MAX_VECTORS) {
+    float* coef = static_cast<float*>(a.ws) + static_cast<size_t>(parts) * a.D;
+    void* args[] = {&c, &coef};
+    e = launch_pdl(reinterpret_cast<const void*>(k_rms_bwd_long<T>), grid_rows(a.T, 1, LONG_THREADS, sms), LONG_THREADS, 0, stream, args);
+    if (e != cudaSuccess) return e;
+    k_dw_long<T><<<dim3((a.D + 255) / 256, parts), 256, 0, stream>>>(c, coef, parts);
+    e = cudaGetLastError();
+  } else {
+    const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.h, a.hs, es) && rows_aligned(a.dy, a.ys, es) &&
+                    rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es);
+    e = by_length(n, [&](auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+      const void* k = al ? reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>)
+                         : reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
+      void* args[] = {&c};
+      return launch_pdl(k, static_cast<unsigned>(parts), BLOCK_OF<TPR>, 0, stream, args);
+    });
+  }
+  if (e != cudaSuccess) return e;
+  return add_rows(static_cast<const float*>(a.ws), a.dw, a.D, parts, stream);
+}
+
+cudaError_t backward(const Backward& a, bool bf16, int sms, cudaStream_t stream) {
+  return bf16 ? backward_t<__nv_bfloat16>(a, sms, stream) : backward_t<float>(a, sms, stream);
+}
+
+}  // namespace norm
+}  // namespace whtmix

@@ -1,0 +1,72 @@
+// whtmix_tma.cuh -- TMA pieces of the matrix products: tensor maps of row-major matrices (host), tile loads and stores (device).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "whtmix_tc.cuh"
+
+namespace whtmix {
+namespace tma {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// cuTensorMapEncodeTiled through the runtime's driver entry point (no link against libcuda); null where it is missing.
+inline EncodeTiledFn encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                    q == cudaDriverEntryPointSuccess;
+    return reinterpret_cast<EncodeTiledFn>(ok ? p : nullptr);
+  }();
+  return fn;
+}
+
+// A row-major matrix can be a tensor map: 16-byte aligned rows (one row needs no stride).
+inline bool mappable(const void* base, long long rows, long long stride, int es) {
+  return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && (rows == 1 || (static_cast<unsigned long long>(stride) * es) % 16 == 0);
+}
+
+// [rows, cols] of es-byte elements (1: bytes, 2: bf16, 4: float), `stride` elements a row; boxes of box_rows rows x 128 bytes,
+// 128-byte swizzle.  What lies outside reads as zero and is not written.
+inline bool encode_rows(CUtensorMap* tm, const void* base, int es, long long rows, long long cols, long long stride, int box_rows) {
+  const EncodeTiledFn f = encode_fn();
+  if (!f) return false;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t pitch = rows == 1 ? (static_cast<cuuint64_t>(cols) * es + 15) / 16 * 16 : static_cast<cuuint64_t>(stride) * es;
+  const cuuint64_t strides[1] = {pitch};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t steps[2] = {1, 1};
+  const CUtensorMapDataType type =
+      es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  return f(tm, type, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+__device__ __forceinline__ void arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void expect_tx(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc::smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void load_2d(uint32_t sdst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(sdst), "l"(tm), "r"(x), "r"(y), "r"(tc::smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void store_2d(const CUtensorMap* tm, int x, int y, uint32_t ssrc) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+               ::"l"(tm), "r"(x), "r"(y), "r"(ssrc) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void wait_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void prefetch(const CUtensorMap* tm) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory");
+}
+
+}  // namespace tma
+}  // namespace whtmix

@@ -21,7 +21,8 @@ __all__ = ["forward", "backward", "forward_ex", "backward_ex", "forward_noalloc"
            "backward_separable",
            "forward_padded", "backward_padded", "project", "block_forward",
            "block_backward", "workspace_bytes", "sync", "plan", "release_workspaces", "WhtmixError", "WHTMixFunction",
-           "WHTMixSeparableFunction", "WHTMixBlockFunction", "pad_tokens", "EXPORTS", "library"]
+           "WHTMixSeparableFunction", "WHTMixBlockFunction", "pad_tokens", "EXPORTS", "library",
+           "rms_norm", "rms_norm_backward", "linear", "linear_backward", "quantize_rows", "RMSNormFunction", "LinearFunction"]
 
 # status codes and dtype codes of include/whtmix.h
 OK = 0
@@ -35,7 +36,14 @@ EXPORTS = ("whtmix_forward", "whtmix_backward", "whtmix_workspace_bytes", "whtmi
            "whtmix_backward_ex", "whtmix_sync", "whtmix_release_workspaces", "whtmix_status_string",
            "whtmix_last_cuda_error", "whtmix_plan", "whtmix_forward_noalloc", "whtmix_forward_separable",
            "whtmix_backward_separable", "whtmix_forward_padded", "whtmix_backward_padded", "whtmix_project",
-           "whtmix_block_forward", "whtmix_block_backward", "whtmix_forward_x16")
+           "whtmix_block_forward", "whtmix_block_backward", "whtmix_forward_x16", "whtmix_rms_norm",
+           "whtmix_rms_norm_backward", "whtmix_linear", "whtmix_linear_backward")
+
+E4M3 = torch.float8_e4m3fn
+E4M3_MAX = 448.0
+# dtype and activation codes of the layer operators
+LAYER_CODE = {torch.float32: 0, torch.bfloat16: 1, E4M3: 3}
+ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
 class WhtmixError(RuntimeError):
@@ -78,6 +86,11 @@ def library(path: str | None = None) -> ctypes.CDLL:
             lib.whtmix_block_forward.argtypes = [p, p, p, p, p, i64, i64, i64, i, p]
             lib.whtmix_block_backward.argtypes = [p, p, p, p, p, p, p, p, p, i64, i64, i64, i, p]
             lib.whtmix_backward_padded.argtypes = [p, p, p, p, p, i64, i64, i64, i64, i, p]
+            f = ctypes.c_float
+            lib.whtmix_rms_norm.argtypes = [p] * 6 + [i64] * 6 + [f, i, i, p]
+            lib.whtmix_rms_norm_backward.argtypes = [p] * 6 + [i64] * 6 + [f, i, p]
+            lib.whtmix_linear.argtypes = [p] * 8 + [i64] * 8 + [i, i, i, p]
+            lib.whtmix_linear_backward.argtypes = [p] * 7 + [i64] * 8 + [i, i, p]
             for name in EXPORTS:
                 if name != "whtmix_status_string":
                     getattr(lib, name).restype = ctypes.c_int
@@ -332,6 +345,225 @@ def block_backward(x: torch.Tensor, w_in: torch.Tensor, g: torch.Tensor, w_out: 
     return dx, dw_in, dg, dw_out
 
 
+# ---- the layer around the mixer: RMS norm and the matrix product with its epilogue ----
+
+def _rows(t: torch.Tensor, name: str, device: torch.device):
+    """(rows, channels, stride) of a tensor [..., C] whose channels are contiguous and whose other axes
+    step through memory with one stride (any contiguous tensor, a slice of channels of one, a view of
+    every k-th token)."""
+    if t.device != device or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor on {device} (WHTMix runs on CUDA tensors only)")
+    shape = t.shape
+    if len(shape) < 1 or shape[-1] < 1:
+        raise ValueError(f"{name} must have at least one channel, got shape {list(shape)}")
+    C = shape[-1]
+    rows = t.numel() // C
+    if t.is_contiguous() or rows == 0:
+        return rows, C, C
+    strides = t.stride()
+    if C > 1 and strides[-1] != 1:
+        raise ValueError(f"{name} must have contiguous channels, got strides {list(strides)}")
+    step, expect = 0, 0
+    for n, st in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n == 1:
+            continue
+        if step == 0:
+            step = st
+        elif st != expect:
+            raise ValueError(f"the rows of {name} must lie at one stride, got shape {list(shape)}, strides {list(strides)}")
+        expect = st * n
+    if rows > 1 and step < C:
+        raise ValueError(f"the rows of {name} overlap: shape {list(shape)}, strides {list(strides)}")
+    return rows, C, step or C
+
+
+def _vector(t: torch.Tensor, n: int, name: str, device: torch.device) -> int:
+    """The address of a contiguous float32 vector of n elements."""
+    if t.dtype != torch.float32 or t.numel() != n or t.dim() != 1:
+        raise ValueError(f"{name} must be float32 [{n}], got {t.dtype} {list(t.shape)}")
+    _on_device(t, device, name)
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, shape, dtype: torch.dtype, name: str, device: torch.device):
+    """(address, stride) of a row matrix of the given shape and dtype."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return t.data_ptr(), _rows(t, name, device)[2]
+
+
+def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
+             out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None, h: torch.Tensor | None = None,
+             scale: torch.Tensor | None = None, stream=None):
+    """h = x + residual; y = h w / sqrt(mean(h^2) + eps) over the last axis (x float32 or bfloat16, w float32).
+
+    Returns y, or with out_dtype float8_e4m3fn (values, scales): y = values * scales[..., None], one float32 scale a
+    token; with a residual h is appended."""
+    dtype = x.dtype
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError(f"rms_norm takes float32 or bfloat16, got {dtype}")
+    out_dtype = dtype if out_dtype is None else out_dtype
+    if out_dtype != dtype and out_dtype != E4M3:
+        raise TypeError(f"rms_norm of {dtype} writes {dtype} or {E4M3}, not {out_dtype}")
+    device, shape = x.device, x.shape
+    T, D, xs = _rows(x, "x", device)
+    wp = _vector(w, D, "w", device)
+    rp = rs = hp = hs = sp = 0
+    if residual is not None:
+        rp, rs = _matrix(residual, shape, dtype, "residual", device)
+        if h is None:
+            h = torch.empty(shape, dtype=dtype, device=device)
+        hp, hs = _matrix(h, shape, dtype, "h", device)
+    elif h is not None:
+        raise ValueError("h is the sum of x and the residual: it needs a residual")
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=device)
+        ys = D
+    else:
+        ys = _matrix(out, shape, out_dtype, "out", device)[1]
+    if out_dtype == E4M3:
+        if scale is None:
+            scale = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+        elif scale.dtype != torch.float32 or scale.shape != shape[:-1]:
+            raise ValueError(f"scale must be float32 {list(shape[:-1])}, got {scale.dtype} {list(scale.shape)}")
+        else:
+            _on_device(scale, device, "scale")
+        sp = scale.data_ptr()
+    elif scale is not None:
+        raise ValueError(f"scale belongs to an output of {E4M3}")
+    _call("whtmix_rms_norm", device, stream, library().whtmix_rms_norm, x.data_ptr(), rp, wp, hp, out.data_ptr(), sp,
+          T, D, xs, rs, hs, ys, eps, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
+    if out_dtype == E4M3:
+        return (out, scale) if residual is None else (out, scale, h)
+    return out if residual is None else (out, h)
+
+
+def rms_norm_backward(h: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, dh: torch.Tensor | None = None,
+                      eps: float = 1e-6, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, stream=None):
+    """(dx, dw) of rms_norm from its sum h (x where it had no residual); dh is the gradient that reaches h
+    directly.  dx is the gradient of x and of the residual; dw is float32."""
+    dtype = h.dtype
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError(f"rms_norm_backward takes float32 or bfloat16, got {dtype}")
+    device, shape = h.device, h.shape
+    T, D, hs = _rows(h, "h", device)
+    wp = _vector(w, D, "w", device)
+    dyp, dys = _matrix(dy, shape, dtype, "dy", device)
+    dhp, dhs = (0, 0) if dh is None else _matrix(dh, shape, dtype, "dh", device)
+    if dx is None:
+        dx = torch.empty(shape, dtype=dtype, device=device)
+    dxp, dxs = _matrix(dx, shape, dtype, "dx", device)
+    if dw is None:
+        dw = torch.empty(D, dtype=torch.float32, device=device)
+    _call("whtmix_rms_norm_backward", device, stream, library().whtmix_rms_norm_backward, h.data_ptr(), wp, dyp, dhp, dxp,
+          _vector(dw, D, "dw", device), T, D, hs, dys, dhs, dxs, eps, LAYER_CODE[dtype])
+    return dx, dw
+
+
+def _activation(name: str) -> int:
+    code = ACTIVATION.get(name)
+    if code is None:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATION)}, got {name!r}")
+    return code
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, activation: str = "none",
+           residual: torch.Tensor | None = None, x_scale: torch.Tensor | None = None,
+           w_scale: torch.Tensor | None = None, preact: torch.Tensor | bool | None = None,
+           out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, stream=None):
+    """y = act(x w^T + bias) + residual over the last axis: x [..., K] and w [N, K] bfloat16, or both float8_e4m3fn
+    with float32 scales x_scale [...] and w_scale [N]; bias [N] float32; residual and y [..., N] of out_dtype
+    (bfloat16 or float32).  preact=True, or a bfloat16 tensor, also returns the pre-activation: (y, preact)."""
+    dtype, device = x.dtype, x.device
+    if dtype != torch.bfloat16 and dtype != E4M3:
+        raise TypeError(f"linear takes bfloat16 or {E4M3}, got {dtype}")
+    if out_dtype != torch.bfloat16 and out_dtype != torch.float32:
+        raise TypeError(f"linear writes bfloat16 or float32, not {out_dtype}")
+    act = _activation(activation)
+    if w.dim() != 2 or w.dtype != dtype or w.shape[1] != x.shape[-1]:
+        raise ValueError(f"w must be {dtype} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
+    T, K, xs = _rows(x, "x", device)
+    N, _, ws = _rows(w, "w", device)
+    shape = x.shape[:-1] + (N,)
+    xsp = wsp = bp = rp = rs = pp = ps = 0
+    if dtype == E4M3:
+        if x_scale is None or w_scale is None:
+            raise ValueError(f"{E4M3} needs x_scale and w_scale")
+        if x_scale.dtype != torch.float32 or x_scale.shape != x.shape[:-1]:
+            raise ValueError(f"x_scale must be float32 {list(x.shape[:-1])}, got {x_scale.dtype} {list(x_scale.shape)}")
+        _on_device(x_scale, device, "x_scale")
+        xsp, wsp = x_scale.data_ptr(), _vector(w_scale, N, "w_scale", device)
+    elif x_scale is not None or w_scale is not None:
+        raise ValueError(f"scales belong to {E4M3} operands")
+    if bias is not None:
+        bp = _vector(bias, N, "bias", device)
+    if residual is not None:
+        rp, rs = _matrix(residual, shape, out_dtype, "residual", device)
+    save = preact is not None and preact is not False
+    if save:
+        if out_dtype != torch.bfloat16:
+            raise ValueError("preact is bfloat16 and goes with a bfloat16 output")
+        if preact is True:
+            preact = torch.empty(shape, dtype=torch.bfloat16, device=device)
+        pp, ps = _matrix(preact, shape, torch.bfloat16, "preact", device)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=device)
+        ys = N
+    else:
+        ys = _matrix(out, shape, out_dtype, "out", device)[1]
+    _call("whtmix_linear", device, stream, library().whtmix_linear, x.data_ptr(), w.data_ptr(), xsp, wsp, bp, rp, pp,
+          out.data_ptr(), T, N, K, xs, ws, rs, ps, ys, act, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
+    return (out, preact) if save else out
+
+
+def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch.Tensor | None = None,
+                    activation: str = "none", need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
+                    dw_dtype: torch.dtype = torch.bfloat16, dx: torch.Tensor | None = None,
+                    dw: torch.Tensor | None = None, db: torch.Tensor | None = None, stream=None):
+    """(dx, dw, db) of linear for the upstream gradient dy of y (bfloat16), from the stored pre-activation p (needed
+    unless the activation is "none"); None in the place of a gradient that is not needed.  The residual's gradient is
+    dy itself.  dw is bfloat16 or float32, db float32."""
+    device = x.device
+    if x.dtype != torch.bfloat16:
+        raise TypeError(f"linear_backward takes bfloat16, got {x.dtype}")
+    if dw_dtype != torch.bfloat16 and dw_dtype != torch.float32:
+        raise TypeError(f"dw is bfloat16 or float32, not {dw_dtype}")
+    act = _activation(activation)
+    if w.dim() != 2 or w.dtype != torch.bfloat16 or w.shape[1] != x.shape[-1]:
+        raise ValueError(f"w must be {torch.bfloat16} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
+    T, K, xs = _rows(x, "x", device)
+    N, _, ws = _rows(w, "w", device)
+    shape = x.shape[:-1] + (N,)
+    dyp, dys = _matrix(dy, shape, torch.bfloat16, "dy", device)
+    pp = ps = dxp = dxs = dwp = dbp = 0
+    if act:
+        if p is None:
+            raise ValueError(f"the backward of {activation} needs the pre-activation p")
+        pp, ps = _matrix(p, shape, torch.bfloat16, "p", device)
+    if need_dx or dx is not None:
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=torch.bfloat16, device=device)
+        dxp, dxs = _matrix(dx, x.shape, torch.bfloat16, "dx", device)
+    if need_dw or dw is not None:
+        dw = _out(dw, (N, K), dw_dtype, device, "dw")
+        dwp = dw.data_ptr()
+    if need_db or db is not None:
+        db = torch.empty(N, dtype=torch.float32, device=device) if db is None else db
+        dbp = _vector(db, N, "db", device)
+    _call("whtmix_linear_backward", device, stream, library().whtmix_linear_backward, x.data_ptr(), w.data_ptr(), dyp, pp,
+          dxp, dwp, dbp, T, N, K, xs, ws, dys, ps, dxs, act, LAYER_CODE[dw_dtype])
+    return dx, dw, db
+
+
+def quantize_rows(w: torch.Tensor):
+    """(values, scales) of a weight [N, K] in 8 bits, laid out once when it is loaded: values float8_e4m3fn,
+    scales [N] float32 = max |row| / 448 (1 for a row of zeros), w = values * scales[:, None] to rounding."""
+    w = w.float()
+    scale = w.abs().amax(1) / E4M3_MAX
+    scale = torch.where(scale == 0, torch.ones_like(scale), scale)
+    return (w / scale[:, None]).to(E4M3), scale
+
+
 def workspace_bytes(B: int, N: int, C: int, dtype: torch.dtype, backward: bool = False) -> int:
     out = ctypes.c_size_t(0)
     _check(library().whtmix_workspace_bytes(B, N, C, DTYPE_CODE[dtype], int(backward), ctypes.byref(out)),
@@ -436,3 +668,49 @@ class WHTMixBlockFunction(torch.autograd.Function):
         x, w_in, g, w_out = ctx.saved_tensors
         dx, dw_in, dg, dw_out = block_backward(x, w_in, g, w_out, dy.contiguous())
         return dx, dw_in.to(w_in.dtype), dg, dw_out.to(w_out.dtype)
+
+
+class RMSNormFunction(torch.autograd.Function):
+    """autograd wrapper of rms_norm: (x, w, residual, eps) -> (y, h), h = x where there is no residual."""
+
+    @staticmethod
+    def forward(ctx, x, w, residual=None, eps=1e-6):
+        if residual is None:
+            y, h = rms_norm(x, w, eps=eps), x
+        else:
+            y, h = rms_norm(x, w, residual=residual, eps=eps)
+        ctx.save_for_backward(h, w)
+        ctx.eps, ctx.with_residual = eps, residual is not None
+        return y, h
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        h, w = ctx.saved_tensors
+        dx, dw = rms_norm_backward(h, w, dy.contiguous(), dh=None if dh is None else dh.contiguous(), eps=ctx.eps)
+        return dx, dw, dx if ctx.with_residual else None, None
+
+
+class LinearFunction(torch.autograd.Function):
+    """autograd wrapper of linear in bfloat16: (x, w, bias, residual, activation) -> y; dw comes in bfloat16."""
+
+    @staticmethod
+    def forward(ctx, x, w, bias=None, residual=None, activation="none"):
+        p = None
+        if activation == "none":
+            y = linear(x, w, bias, residual=residual)
+        else:
+            y, p = linear(x, w, bias, activation, residual, preact=True)
+        ctx.save_for_backward(x, w, p)
+        ctx.activation, ctx.with_bias, ctx.with_residual = activation, bias is not None, residual is not None
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w, p = ctx.saved_tensors
+        dy = dy.contiguous()
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if need[0] or need[1] or (ctx.with_bias and need[2]):
+            dx, dw, db = linear_backward(x, w, dy, p, ctx.activation, need_dx=need[0], need_dw=need[1],
+                                         need_db=ctx.with_bias and need[2])
+        return dx, dw, db, dy if ctx.with_residual else None, None
