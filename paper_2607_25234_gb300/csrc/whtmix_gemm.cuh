@@ -47,7 +47,7 @@ struct Gemm {
 constexpr int GEMM_THREADS = 384;
 constexpr int GEMM_BM = 128;
 constexpr uint32_t RING_BYTES = 192 * 1024, PANEL_BYTES = 128 * 128;
-constexpr size_t GEMM_SMEM = RING_BYTES + 2 * PANEL_BYTES + 1024;  // 1024: alignment slack
+constexpr size_t GEMM_SMEM = RING_BYTES + 2 * PANEL_BYTES;  // + 3 KB static: all of an SM's 227 KB
 
 template <int BN>
 struct Ring {
@@ -80,11 +80,19 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uin
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// 1 / (1 + 2^t): two operations of the special-function unit; 0 where 2^t overflows, NaN for NaN
+__device__ __forceinline__ float logistic2(float t) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+constexpr float LOG2E = 1.4426950408889634f;
 __device__ __forceinline__ float activate(float z, int act) {
   switch (act) {
     case ACT_RELU: return z < 0.f ? 0.f : z;
-    case ACT_GELU: return __fdividef(z, 1.f + __expf(-GELU_2A * (z + GELU_B * z * z * z)));
-    case ACT_SILU: return __fdividef(z, 1.f + __expf(-z));
+    case ACT_GELU: return z * logistic2(z * (-GELU_2A * LOG2E - GELU_2A * LOG2E * GELU_B * (z * z)));
+    case ACT_SILU: return z * logistic2(z * -LOG2E);
     default: return z;
   }
 }
@@ -104,21 +112,36 @@ __device__ __forceinline__ uint32_t panel_at(int r, int c) {
   return r * 128 + (((c / E) ^ (r & 7)) << 4) + (c % E) * static_cast<int>(sizeof(O));
 }
 
-// The group's 128 threads copy a panel between shared memory and rows m0 .. of an unaligned matrix.
+// The group's 128 threads copy a panel between shared memory and rows m0 .. of an unaligned matrix, up to 16 elements a thread
+// in flight.
 template <typename O, bool STORE>
 __device__ __forceinline__ void panel_plain(unsigned char* s, void* g, long long stride, int m0, int M, int col0, int N, int gt) {
-  constexpr int W = Panel<O>::W;
-  const int lane = gt & 31, warp = gt >> 5;
-  for (int r = warp; r < GEMM_BM; r += 4) {
-    if (m0 + r >= M) break;
-    O* row = static_cast<O*>(g) + (m0 + r) * stride + col0;
+  constexpr int C = Panel<O>::W / 32, ROWS = 16 / C;
+  const int lane = gt & 31, warp = gt >> 5, rows = min(GEMM_BM, M - m0);
+  O* base = static_cast<O*>(g) + static_cast<long long>(m0) * stride + col0 + lane;
+  for (int r0 = warp; r0 < rows; r0 += 4 * ROWS) {
+    O v[ROWS][C];
 #pragma unroll
-    for (int c = lane; c < W; c += 32) {
-      if (col0 + c < N) {
-        O* q = reinterpret_cast<O*>(s + panel_at<O>(r, c));
-        if (STORE) row[c] = *q; else *q = row[c];
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int r = r0 + 4 * i;
+        const bool in = r < rows && col0 + lane + 32 * c < N;
+        if (STORE)
+          v[i][c] = *reinterpret_cast<O*>(s + panel_at<O>(r & (GEMM_BM - 1), lane + 32 * c));
+        else
+          v[i][c] = in ? base[r * stride + 32 * c] : O(0.f);
       }
-    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int r = r0 + 4 * i;
+        if (!STORE)
+          *reinterpret_cast<O*>(s + panel_at<O>(r & (GEMM_BM - 1), lane + 32 * c)) = v[i][c];
+        else if (r < rows && col0 + lane + 32 * c < N)
+          base[r * stride + 32 * c] = v[i][c];
+      }
   }
 }
 
@@ -175,11 +198,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   constexpr int S = R::STAGES, BK = E4M3 ? 128 : 64, PW = Panel<O>::W, PANELS = BN / PW;
   constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                              (static_cast<uint32_t>(BN >> 3) << 17) | ((128u >> 4) << 24);
-  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ GemmBars<BN> bars;
   __shared__ uint32_t tmem_slot;
-  __shared__ float s_bias[2][64], s_scale[2][64];
-  unsigned char* smem = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
+  __shared__ __align__(16) float s_bias[2][BN / 2 < PW ? PW : BN / 2], s_scale[2][BN / 2 < PW ? PW : BN / 2];
   const uint32_t ring = tc::smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (warp == 0) tc::tmem_alloc(&tmem_slot, 2 * BN);
@@ -292,14 +314,19 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       const int panels = min(PANELS, (a.N - n0 + PW - 1) / PW);
       const float sm = a.sm && m0 + row < a.M ? a.sm[m0 + row] : 1.f;
       bool waited = false;
+      // the columns of this group's panels (a panel's reads of the last tile's are behind a barrier of the group)
+      for (int j = gt; j < BN / 2 || j < PW; j += 128) {
+        const int c = n0 + (g + 2 * (j / PW)) * PW + j % PW;
+        s_bias[g][j] = a.bias && c < a.N ? a.bias[c] : 0.f;
+        s_scale[g][j] = a.sn && c < a.N ? a.sn[c] : 1.f;
+      }
+      sync_group();
       for (int p = g; p < panels; p += 2) {
         const int col0 = n0 + p * PW;
-        if (gt == 0) tma::wait_read();
-        if (gt < PW) {
-          s_bias[g][gt] = a.bias && col0 + gt < a.N ? a.bias[col0 + gt] : 0.f;
-          s_scale[g][gt] = a.sn && col0 + gt < a.N ? a.sn[col0 + gt] : 1.f;
-        }
-        sync_group();  // the panel is free, its bias has arrived
+        auto panel_free = [&] {  // the last store has read the panel
+          if (gt == 0) tma::wait_read();
+          sync_group();
+        };
         auto load_r = [&] {
           if (a.r_plain) {
             panel_plain<O, false>(st, const_cast<void*>(a.r), a.rs, m0, a.M, col0, a.N, gt);
@@ -308,7 +335,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
             tma::load_2d(st_u, &a.tr, col0, m0, &bars.rfull[g]);
           }
         };
-        if (a.has_r && !a.has_p) load_r();
+        if (a.has_r && !a.has_p) {
+          panel_free();
+          load_r();
+        }
         if (!waited) {
           wait(&bars.dfull[d], (i >> 1) & 1);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -324,16 +354,17 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
           __syncwarp();
           if (lane == 0) tma::arrive(&bars.dempty[d]);
         }
+        const float *sb = &s_bias[g][p / 2 * PW], *ss = &s_scale[g][p / 2 * PW];
         if (a.sm) {
 #pragma unroll
-          for (int c = 0; c < PW; ++c) v[c] *= sm * s_scale[g][c];
-        }
-        if (a.bias) {
+          for (int c = 0; c < PW; ++c) v[c] = v[c] * sm * ss[c] + sb[c];
+        } else if (a.bias) {
 #pragma unroll
-          for (int c = 0; c < PW; ++c) v[c] += s_bias[g][c];
+          for (int c = 0; c < PW; ++c) v[c] += sb[c];
         }
         if constexpr (PW == 64) {
           if (a.has_p) {
+            panel_free();
             panel_put<__nv_bfloat16>(st, row, v);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             sync_group();
@@ -365,6 +396,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
           else
             wait(&bars.rfull[g], loads++ & 1);
           panel_add<O>(st, row, v);
+        } else if (!a.has_p) {
+          panel_free();
         }
         panel_put<O>(st, row, v);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -393,20 +426,25 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   if (warp == 0) tc::tmem_dealloc(tmem, 2 * BN);
 }
 
-// One instance's launch: a persistent grid of at most one CTA per SM.
-template <bool E4M3, bool A_MN, bool B_MN, int BN, typename O>
-cudaError_t launch_gemm(const Gemm& g, int sms, cudaStream_t stream) {
-  const void* k = reinterpret_cast<const void*>(k_gemm<E4M3, A_MN, B_MN, BN, O>);
-  static std::atomic<uint64_t> raised{0};  // devices (of the first 64) where the shared-memory limit is raised
+// Raises a kernel's shared-memory limit once a device; `raised` holds the devices (of the first 64) where that is done.
+inline cudaError_t raise_smem(const void* kernel, size_t bytes, std::atomic<uint64_t>& raised) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (!bit || !(raised.load(std::memory_order_relaxed) & bit)) {
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(GEMM_SMEM));
-    if (e != cudaSuccess) return e;
-    raised.fetch_or(bit, std::memory_order_relaxed);
-  }
+  if (bit && (raised.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess) raised.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+// One instance's launch: a persistent grid of at most one CTA per SM.
+template <bool E4M3, bool A_MN, bool B_MN, int BN, typename O>
+cudaError_t launch_gemm(const Gemm& g, int sms, cudaStream_t stream) {
+  const void* k = reinterpret_cast<const void*>(k_gemm<E4M3, A_MN, B_MN, BN, O>);
+  static std::atomic<uint64_t> raised{0};
+  const cudaError_t e = raise_smem(k, GEMM_SMEM, raised);
+  if (e != cudaSuccess) return e;
   const long long items = static_cast<long long>(g.tiles_m) * g.tiles_n * g.splits;
   Gemm c = g;
   void* args[] = {&c};

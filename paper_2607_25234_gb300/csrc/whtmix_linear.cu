@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "whtmix_few.cuh"
 #include "whtmix_gemm.cuh"
 #include "whtmix_linear.cuh"
 #include "whtmix_norm.cuh"
@@ -49,8 +50,7 @@ __device__ __forceinline__ float slope(float z, int act) {
   if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
   const float u2 = act == ACT_GELU ? GELU_2A * (z + GELU_B * z * z * z) : z;
   const float du2 = act == ACT_GELU ? GELU_2A * (1.f + 3.f * GELU_B * z * z) : 1.f;
-  const float e = __expf(-u2), s = __fdividef(1.f, 1.f + e);
-  // s (1 + z (1 - s) du2); far below zero 1 - s is 1 and s is 0
+  const float s = logistic2(-LOG2E * u2);
   return s * (1.f + z * (1.f - s) * du2);
 }
 
@@ -192,9 +192,10 @@ static ForwardPlan plan_forward(const Forward& a) {
   return f;
 }
 
-size_t forward_workspace(const Forward& a, int) { return plan_forward(a).total; }
+size_t forward_workspace(const Forward& a, int) { return a.T <= FEW_TOKENS ? 0 : plan_forward(a).total; }
 
 cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
+  if (a.T <= FEW_TOKENS) return forward_few(a, sms, stream);
   const ForwardPlan f = plan_forward(a);
   const int es = a.e4m3 ? 1 : 2, os = a.out_f32 ? 4 : 2;
   const void *x = a.x, *w = a.w;
