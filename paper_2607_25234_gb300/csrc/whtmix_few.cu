@@ -14,6 +14,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "whtmix_few.cuh"
 #include "whtmix_gemm.cuh"
@@ -25,7 +26,8 @@ namespace linear {
 constexpr int FEW_WARPS = 8, FEW_THREADS = 32 * FEW_WARPS;
 template <int NT>
 struct Few {
-  static constexpr int MT = NT <= 4 ? 4 : 2, ROWS = 16 * MT, TOKENS = 8 * NT, PITCH = ROWS + 4;
+  static constexpr int MT = 2, ROWS = 16 * MT, TOKENS = 8 * NT, PITCH = ROWS + 4;
+  static constexpr int DEPTH = NT == 1 ? 4 : NT == 2 ? 3 : 2;  // 64-byte blocks of k a warp has in flight
   static constexpr size_t SMEM = static_cast<size_t>(FEW_WARPS) * TOKENS * PITCH * 4;
 };
 
@@ -41,7 +43,7 @@ __device__ __forceinline__ void mma_few(float (&d)[4], uint32_t a0, uint32_t a1,
 
 // VEC: rows of x and W are 16-byte aligned and whole multiples of 16 bytes.
 template <bool E4M3, int NT, bool VEC, typename O>
-__global__ void __launch_bounds__(FEW_THREADS, 1) k_few(const Forward a, int splits) {
+__global__ void __launch_bounds__(FEW_THREADS, NT <= 4 && VEC ? 2 : 1) k_few(const Forward a, int splits) {
   using F = Few<NT>;
   constexpr int MT = F::MT, ES = E4M3 ? 1 : 2;
   extern __shared__ __align__(16) float s_sum[];
@@ -53,53 +55,70 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) k_few(const Forward a, int spl
   const int blocks = static_cast<int>((row_bytes + 63) / 64);
   const int b0 = static_cast<int>(static_cast<long long>(blocks) * rank / splits), b1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / splits);
   const uint8_t *x = static_cast<const uint8_t*>(a.x), *w = static_cast<const uint8_t*>(a.w);
-  const Span sx{x, x + ((a.T - 1) * a.xs + a.K) * ES}, sw{w, w + ((a.N - 1) * a.ws + a.K) * ES};
-  auto fetch = [&](const uint8_t* base, long long pitch, int row, int rows, int block, const Span& span) -> uint4 {
+  const Span sx = span_of(x, a.T, a.xs, a.K, ES), sw = span_of(w, a.N, a.ws, a.K, ES);
+  using Raw = typename std::conditional<VEC, uint4, Granules>::type;
+  auto fetch = [&](Raw& u, const uint8_t* base, long long pitch, int row, int rows, int block, const Span& span) {
     const long long at = 64ll * block + 16 * c;
-    if (row >= rows || at >= row_bytes) return make_uint4(0u, 0u, 0u, 0u);
+    u = Raw{};
+    if (row >= rows || at >= row_bytes) return;
     const uint8_t* p = base + row * pitch * ES + at;
+    if constexpr (VEC)
+      u = *reinterpret_cast<const uint4*>(p);
+    else
+      u = fetch16(p, span);
+  };
+  auto finish = [&](const Raw& u, const uint8_t* base, long long pitch, int row, int rows, int block, const Span& span) -> uint4 {
     if constexpr (VEC) {
-      return *reinterpret_cast<const uint4*>(p);
+      return u;
     } else {
-      const uint4 u = load16(p, span);
-      return row_bytes - at >= 16 ? u : keep(u, static_cast<int>(row_bytes - at));
+      const long long at = 64ll * block + 16 * c;
+      if (row >= rows || at >= row_bytes) return make_uint4(0u, 0u, 0u, 0u);
+      const uint4 v = finish16(u, base + row * pitch * ES + at, span);
+      return row_bytes - at >= 16 ? v : keep(v, static_cast<int>(row_bytes - at));
     }
   };
   float acc[MT][NT][4] = {};
-  struct Block {
-    uint4 w[MT][2], x[NT];
-  };
-  auto load_w = [&](Block& b, int block) {
+  constexpr int DEPTH = VEC ? F::DEPTH : 1;
+  Raw wr[DEPTH][MT][2], xr[DEPTH][NT];
+  auto load = [&](Raw (&wb)[MT][2], Raw (&xb)[NT], int block) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) b.w[m][h] = fetch(w, a.ws, n0 + 16 * m + 8 * h + g, a.N, block, sw);
-  };
-  auto load_x = [&](Block& b, int block) {
+      for (int h = 0; h < 2; ++h) fetch(wb[m][h], w, a.ws, n0 + 16 * m + 8 * h + g, a.N, block, sw);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) b.x[n] = fetch(x, a.xs, 8 * n + g, T, block, sx);
+    for (int n = 0; n < NT; ++n) fetch(xb[n], x, a.xs, 8 * n + g, T, block, sx);
   };
-  auto multiply = [&](const Block& b) {
+  auto multiply = [&](const Raw (&wb)[MT][2], const Raw (&xb)[NT], int block) {
+    uint4 u[MT][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mma_few<E4M3>(acc[m][n], b.w[m][0].x, b.w[m][1].x, b.w[m][0].y, b.w[m][1].y, b.x[n].x, b.x[n].y);
-        mma_few<E4M3>(acc[m][n], b.w[m][0].z, b.w[m][1].z, b.w[m][0].w, b.w[m][1].w, b.x[n].z, b.x[n].w);
+      for (int h = 0; h < 2; ++h) u[m][h] = finish(wb[m][h], w, a.ws, n0 + 16 * m + 8 * h + g, a.N, block, sw);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint4 v = finish(xb[n], x, a.xs, 8 * n + g, T, block, sx);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        mma_few<E4M3>(acc[m][n], u[m][0].x, u[m][1].x, u[m][0].y, u[m][1].y, v.x, v.y);
+        mma_few<E4M3>(acc[m][n], u[m][0].z, u[m][1].z, u[m][0].w, u[m][1].w, v.z, v.w);
       }
+    }
   };
   pdl_wait();
-  // two blocks of W in flight while one is multiplied
-  int block = b0 + warp;
-  Block u, v;
-  if (block < b1) load_w(u, block), load_x(u, block);
-  while (block < b1) {
-    const int next = block + FEW_WARPS;
-    if (next < b1) load_w(v, next), load_x(v, next);
-    multiply(u);
-    if (next + FEW_WARPS < b1) load_w(u, next + FEW_WARPS), load_x(u, next + FEW_WARPS);
-    if (next < b1) multiply(v);
-    block = next + FEW_WARPS;
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) {
+    const int block = b0 + warp + FEW_WARPS * d;
+    if (block < b1) load(wr[d], xr[d], block);
+  }
+  for (int first = b0 + warp; first < b1; first += FEW_WARPS * DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int block = first + FEW_WARPS * d, next = block + FEW_WARPS * DEPTH;
+      if (block < b1) {
+        multiply(wr[d], xr[d], block);
+        if (next < b1) load(wr[d], xr[d], next);
+      }
+    }
   }
   // the warps' sums, then the cluster's
   float* mine = s_sum + warp * F::TOKENS * F::PITCH;
@@ -147,7 +166,7 @@ static cudaError_t launch_few(const Forward& a, int sms, cudaStream_t stream) {
   static std::atomic<uint64_t> raised{0};
   cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), F::SMEM, raised);
   if (e != cudaSuccess) return e;
-  // as many CTAs along K (1, 2, 4 or 8) as there are SMs for, each with two blocks of k a warp at least
+  // the K axis over 1, 2, 4 or 8 CTAs where the rows alone leave SMs idle, with a block of k a warp at least
   const long long tiles = (a.N + F::ROWS - 1) / F::ROWS, blocks = (static_cast<long long>(a.K) * (E4M3 ? 1 : 2) + 63) / 64;
   int splits = 1;
   while (splits < 8 && tiles * splits * 2 <= 2ll * sms && blocks >= 2ll * FEW_WARPS * splits) splits *= 2;

@@ -147,10 +147,9 @@ int whtmix_rms_norm_backward(const void* h, const float* w, const void* dy, cons
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     if (none) return zero(dw, static_cast<size_t>(D) * 4, stream);
     const bool bf16 = dtype == WHTMIX_BF16;
-    void* ws = nullptr;
-    rc = host::workspace(dev, stream, norm::backward_workspace(T, static_cast<int>(D), bf16, sms), 1, &ws);
+    norm::Backward a{h, w, dy, dh, dx, dw, nullptr, T, h_stride, dy_stride, dh_stride, dx_stride, static_cast<int>(D), eps};
+    rc = host::workspace(dev, stream, norm::backward_workspace(a, bf16, sms), 1, &a.ws);
     if (rc != WHTMIX_OK) return rc;
-    norm::Backward a{h, w, dy, dh, dx, dw, ws, T, h_stride, dy_stride, dh_stride, dx_stride, static_cast<int>(D), eps};
     return done(norm::backward(a, bf16, sms, stream));
   });
 }

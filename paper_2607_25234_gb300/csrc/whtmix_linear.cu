@@ -9,6 +9,7 @@
 #include "whtmix_gemm.cuh"
 #include "whtmix_linear.cuh"
 #include "whtmix_norm.cuh"
+#include "whtmix_unaligned.cuh"
 
 namespace whtmix {
 namespace linear {
@@ -16,33 +17,43 @@ namespace linear {
 constexpr int THREADS_256 = 256;
 
 // ---- rows to a 16-byte pitch ----
-// dst [rows, pitch] = src [rows, cols] (stride elements a row), zeros beyond cols; a thread writes 16 bytes.  pitch * sizeof(E) is
-// a multiple of 16.
-template <typename E>
-__global__ void __launch_bounds__(THREADS_256) k_pitch(E* __restrict__ dst, const E* __restrict__ src, long long rows, int cols,
-                                                       long long stride, int pitch) {
-  constexpr int V = 16 / sizeof(E);
+// dst [rows, pitch] = src [rows, cols] (stride elements a row), zeros beyond cols; a thread writes 16 bytes.  pitch is a multiple of
+// 16 bytes.  Up to two matrices a launch.
+struct Copy {
+  uint8_t* dst;
+  const uint8_t* src;
+  long long rows, stride, cols, pitch;  // stride, cols, pitch in bytes
+  long long chunks() const { return rows * (pitch / 16); }
+};
+__global__ void __launch_bounds__(THREADS_256) k_pitch(const Copy a, const Copy b, long long na, long long n) {
   pdl_wait();
-  const int per_row = pitch / V;
-  const long long n = rows * per_row, step = static_cast<long long>(gridDim.x) * THREADS_256;
+  const long long step = static_cast<long long>(gridDim.x) * THREADS_256;
+#pragma unroll 2
   for (long long i = static_cast<long long>(blockIdx.x) * THREADS_256 + threadIdx.x; i < n; i += step) {
-    const long long r = i / per_row;
-    const int c = static_cast<int>(i - r * per_row) * V;
-    const E* s = src + r * stride + c;
-    __align__(16) E v[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = c + j < cols ? s[j] : E(0);
-    *reinterpret_cast<uint4*>(dst + r * pitch + c) = *reinterpret_cast<const uint4*>(v);
+    const bool first = i < na;
+    const long long j = first ? i : i - na;
+    const long long pitch = first ? a.pitch : b.pitch, stride = first ? a.stride : b.stride, cols = first ? a.cols : b.cols;
+    const uint8_t* src = first ? a.src : b.src;
+    const uint32_t per_row = static_cast<uint32_t>(pitch / 16);
+    const long long r = j / per_row, c = (j - r * per_row) * 16, rows = first ? a.rows : b.rows;
+    const Span span{src, src + (rows - 1) * stride + cols};
+    const uint4 u = load16(src + r * stride + c, span);
+    *reinterpret_cast<uint4*>((first ? a.dst : b.dst) + r * pitch + c) = keep(u, static_cast<int>(cols - c < 16 ? cols - c : 16));
   }
   pdl_trigger();
 }
 
-static cudaError_t to_pitch(void* dst, const void* src, long long rows, int cols, long long stride, int pitch, int es, int sms,
-                            cudaStream_t stream) {
-  const long long n = rows * (pitch / (16 / es)), need = (n + THREADS_256 - 1) / THREADS_256, most = 8ll * sms;
-  void* args[] = {&dst, &src, &rows, &cols, &stride, &pitch};
-  return launch_pdl(es == 1 ? reinterpret_cast<const void*>(k_pitch<uint8_t>) : reinterpret_cast<const void*>(k_pitch<uint16_t>),
-                    static_cast<unsigned>(need < most ? need : most), THREADS_256, 0, stream, args);
+static Copy copy_of(void* dst, const void* src, long long rows, int cols, long long stride, int pitch, int es) {
+  return {static_cast<uint8_t*>(dst), static_cast<const uint8_t*>(src), rows, stride * es, static_cast<long long>(cols) * es,
+          static_cast<long long>(pitch) * es};
+}
+static cudaError_t to_pitch(const Copy& a, const Copy& b, int sms, cudaStream_t stream) {
+  long long na = a.dst ? a.chunks() : 0, n = na + (b.dst ? b.chunks() : 0);
+  if (n == 0) return cudaSuccess;
+  const long long need = (n + THREADS_256 - 1) / THREADS_256, most = 8ll * sms;
+  Copy ca = a, cb = b;
+  void* args[] = {&ca, &cb, &na, &n};
+  return launch_pdl(reinterpret_cast<const void*>(k_pitch), static_cast<unsigned>(need < most ? need : most), THREADS_256, 0, stream, args);
 }
 
 // ---- dp and db ----
@@ -55,63 +66,58 @@ __device__ __forceinline__ float slope(float z, int act) {
 }
 
 // dp[t, n] = bf16(dy act'(p)); part[chunk][n] = the chunk's rows' float32 sum of dy act'(p), before the rounding.  A CTA takes 256
-// columns (a thread 8: consecutive with AL, else every 32nd) and the rows of chunk blockIdx.y, 8 at a time.  dp, part: or null.
+// columns (a thread 8) and the rows of chunk blockIdx.y, 8 at a time.  dp, part: or null.
 template <bool AL>
 __global__ void __launch_bounds__(THREADS_256) k_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
   __shared__ float s[8][32][9];
-  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c0 = blockIdx.x * 256 + (AL ? 8 * lane : lane);
-  constexpr int STEP = AL ? 1 : 32;
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c0 = blockIdx.x * 256 + 8 * lane;
   const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
   float acc[8] = {};
   pdl_wait();
   const uint16_t *dy = static_cast<const uint16_t*>(a.dy), *p = static_cast<const uint16_t*>(a.p);
-  auto load = [&](const uint16_t* row, float (&f)[8]) {
-    if constexpr (AL) {
-      const uint4 u = c0 < a.N ? *reinterpret_cast<const uint4*>(row + c0) : make_uint4(0u, 0u, 0u, 0u);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = c0 + 32 * j < a.N ? __uint_as_float(static_cast<uint32_t>(row[c0 + 32 * j]) << 16) : 0.f;
+  const Span sd = span_of(a.dy, a.T, a.dys, a.N, 2), sp = span_of(a.p, a.T, a.ps, a.N, 2);
+  auto load = [&](const uint16_t* row, const Span& s, float (&f)[8]) {
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if (c0 < a.N) {
+      if constexpr (AL)
+        u = *reinterpret_cast<const uint4*>(row + c0);
+      else
+        u = keep(load16(reinterpret_cast<const uint8_t*>(row + c0), s), min(16, 2 * (a.N - c0)));
     }
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
   };
 #pragma unroll 2
   for (long long t = t0 + g; t < t1; t += 8) {
     float d[8], z[8];
-    load(dy + t * a.dys, d);
+    load(dy + t * a.dys, sd, d);
     if (a.act != ACT_NONE) {
-      load(p + t * a.ps, z);
+      load(p + t * a.ps, sp, z);
 #pragma unroll
       for (int j = 0; j < 8; ++j) d[j] *= slope(z[j], a.act);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] += d[j];
-    if (dp) {
-      if constexpr (AL) {
-        uint32_t h[4];
+    if (dp) {  // (its pitch holds whole vectors)
+      uint32_t h[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          __nv_bfloat162 b = __floats2bfloat162_rn(d[2 * j], d[2 * j + 1]);
-          h[j] = *reinterpret_cast<uint32_t*>(&b);
-        }
-        if (c0 < a.N) *reinterpret_cast<uint4*>(dp + t * dps + c0) = make_uint4(h[0], h[1], h[2], h[3]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c0 + 32 * j < a.N) dp[t * dps + c0 + 32 * j] = __float2bfloat16_rn(d[j]);
+      for (int j = 0; j < 4; ++j) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(d[2 * j], d[2 * j + 1]);
+        h[j] = *reinterpret_cast<uint32_t*>(&b);
       }
+      if (c0 < a.N) *reinterpret_cast<uint4*>(dp + t * dps + c0) = make_uint4(h[0], h[1], h[2], h[3]);
     }
   }
   if (part) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[g][lane][j] = acc[j];
     __syncthreads();
-    const int l = AL ? threadIdx.x >> 3 : threadIdx.x & 31, j = AL ? threadIdx.x & 7 : threadIdx.x >> 5;
+    const int l = threadIdx.x >> 3, j = threadIdx.x & 7;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum += s[i][l][j];
-    const int c = blockIdx.x * 256 + (AL ? 8 * l + j : l + STEP * j);
+    const int c = blockIdx.x * 256 + threadIdx.x;
     if (c < a.N) part[static_cast<long long>(blockIdx.y) * a.N + c] = sum;
   }
   pdl_trigger();
@@ -201,16 +207,16 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
   const void *x = a.x, *w = a.w;
   long long xs = a.xs, wst = a.ws;
   cudaError_t e;
+  Copy cx{}, cw{};
   if (f.pad_x) {
-    void* d = static_cast<char*>(ws) + f.x_off;
-    if ((e = to_pitch(d, a.x, a.T, a.K, a.xs, f.kp, es, sms, stream)) != cudaSuccess) return e;
-    x = d, xs = f.kp;
+    x = static_cast<char*>(ws) + f.x_off, xs = f.kp;
+    cx = copy_of(static_cast<char*>(ws) + f.x_off, a.x, a.T, a.K, a.xs, f.kp, es);
   }
   if (f.pad_w) {
-    void* d = static_cast<char*>(ws) + f.w_off;
-    if ((e = to_pitch(d, a.w, a.N, a.K, a.ws, f.kp, es, sms, stream)) != cudaSuccess) return e;
-    w = d, wst = f.kp;
+    w = static_cast<char*>(ws) + f.w_off, wst = f.kp;
+    cw = copy_of(static_cast<char*>(ws) + f.w_off, a.w, a.N, a.K, a.ws, f.kp, es);
   }
+  if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
   Gemm g{};
   g.tiles_m = ceil_div(a.T, GEMM_BM);
   g.kblocks = ceil_div(a.K, 128 / es);
@@ -277,6 +283,9 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
   cudaError_t e;
   const void* dp = a.dy;
   long long dps = a.dys;
+  const Copy cx = b.pad_x ? copy_of(base + b.x_off, a.x, a.T, a.K, a.xs, b.kp, 2) : Copy{};
+  const Copy cw = b.pad_w ? copy_of(base + b.w_off, a.w, a.N, a.K, a.ws, b.kp, 2) : Copy{};
+  if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
   if (a.db || b.own_dp) {
     Backward c = a;
     __nv_bfloat16* d = b.own_dp ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
@@ -299,13 +308,8 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     if (a.db && (e = norm::add_rows(part, a.db, a.N, chunks, stream)) != cudaSuccess) return e;
   }
   if (a.dx) {
-    const void* w = a.w;
-    long long wst = a.ws;
-    if (b.pad_w) {
-      void* d = base + b.w_off;
-      if ((e = to_pitch(d, a.w, a.N, a.K, a.ws, b.kp, 2, sms, stream)) != cudaSuccess) return e;
-      w = d, wst = b.kp;
-    }
+    const void* w = b.pad_w ? base + b.w_off : a.w;
+    const long long wst = b.pad_w ? b.kp : a.ws;
     Gemm g{};
     g.tiles_m = ceil_div(a.T, GEMM_BM);
     g.kblocks = ceil_div(a.N, 64);
@@ -321,13 +325,8 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     if ((e = gemm_dx(g, pl.bn, sms, stream)) != cudaSuccess) return e;
   }
   if (a.dw) {
-    const void* x = a.x;
-    long long xs = a.xs;
-    if (b.pad_x) {
-      void* d = base + b.x_off;
-      if ((e = to_pitch(d, a.x, a.T, a.K, a.xs, b.kp, 2, sms, stream)) != cudaSuccess) return e;
-      x = d, xs = b.kp;
-    }
+    const void* x = b.pad_x ? base + b.x_off : a.x;
+    const long long xs = b.pad_x ? b.kp : a.xs;
     Gemm g{};
     g.tiles_m = ceil_div(a.N, GEMM_BM);
     g.kblocks = ceil_div(a.T, 64);

@@ -9,8 +9,8 @@
 // All of it is bound by memory: a row is read once into registers (packed as stored), its sums meet in one reduction, and it is
 // written once.  TPR threads hold a row, NV 16-byte vectors each; up to 32 threads a row need no shared memory.  Sums are
 // float32 in a fixed order.  dw: every thread keeps its columns' sums over the rows that its CTA takes, the CTAs' partial rows
-// are added up by k_dw in a fixed order.  Rows that are not 16-byte aligned take element loads, consecutive threads consecutive
-// elements; rows beyond 2048 vectors are read twice (k_rms_long, k_rms_bwd_long).
+// are added up by k_dw in a fixed order.  Rows that are not 16-byte aligned are read and written in aligned 16-byte accesses
+// all the same, but for their ends; rows beyond 2048 vectors are read twice (k_rms_long, k_rms_bwd_long).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
@@ -64,37 +64,54 @@ template <> struct Io<__nv_bfloat16> {
   }
 };
 
-// The elements that thread `lane` of a row's TPR holds in vector k: with AL V consecutive ones, else one of every TPR.
+// Vector k of thread `lane` of a row's TPR: V consecutive elements, from at(lane, k) - off on.  AL: rows are 16-byte aligned, whole
+// vectors (off = 0).  Otherwise off is the row's distance from the 16-byte boundary before it, so that the vectors lie on such
+// boundaries all the same: the first and the last of a row are cut, and go element by element.  So do all vectors of a matrix
+// whose rows do not lie like the others' (same = false).
 template <typename T, bool AL, int TPR>
 struct Row {
   static constexpr int V = Io<T>::V;
-  static __device__ __forceinline__ long long at(int lane, int k, int j) {
-    return AL ? static_cast<long long>(lane + TPR * k) * V + j : lane + static_cast<long long>(TPR) * (k * V + j);
+  static __device__ __forceinline__ int at(int lane, int k) { return (lane + TPR * k) * V; }
+  static __device__ __forceinline__ int offset(const T* p) {
+    return AL ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
   }
-  static __device__ __forceinline__ void load(const T* p, int lane, int k, int D, float (&f)[V]) {
-    if constexpr (AL) {
-      const long long e = at(lane, k, 0);
-      uint4 u = make_uint4(0u, 0u, 0u, 0u);
-      if (e < D) u = *reinterpret_cast<const uint4*>(p + e);
-      Io<T>::unpack(u, f);
-    } else {
+  static __device__ __forceinline__ bool whole(int e, int D, bool same) { return AL ? e < D : same && e >= 0 && e + V <= D; }
+  // the NV vectors of a row: all loads first
+  template <int NV>
+  static __device__ __forceinline__ void load(const T* p, int lane, int off, bool same, int D, float (&f)[NV][V]) {
+    uint4 u[NV];
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = at(lane, k, j) < D ? Io<T>::get(p, at(lane, k, j)) : 0.f;
+    for (int k = 0; k < NV; ++k) {
+      const int e = at(lane, k) - off;
+      u[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (whole(e, D, same)) u[k] = *reinterpret_cast<const uint4*>(p + e);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      Io<T>::unpack(u[k], f[k]);
+      if constexpr (!AL) {
+        const int e = at(lane, k) - off;
+        if (!whole(e, D, same)) {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (e + j >= 0 && e + j < D) f[k][j] = Io<T>::get(p, e + j);
+        }
+      }
     }
   }
-  static __device__ __forceinline__ void store(T* p, int lane, int k, int D, const float (&f)[V]) {
-    if constexpr (AL) {
-      const long long e = at(lane, k, 0);
-      if (e < D) *reinterpret_cast<uint4*>(p + e) = Io<T>::pack(f);
-    } else {
+  static __device__ __forceinline__ void store(T* p, int lane, int k, int off, bool same, int D, const float (&f)[V]) {
+    const int e = at(lane, k) - off;
+    if (whole(e, D, same)) {
+      *reinterpret_cast<uint4*>(p + e) = Io<T>::pack(f);
+    } else if constexpr (!AL) {
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (at(lane, k, j) < D) Io<T>::put(p, at(lane, k, j), f[j]);
+        if (e + j >= 0 && e + j < D) Io<T>::put(p, e + j, f[j]);
     }
   }
-  static __device__ __forceinline__ void gains(const float* w, int lane, int k, int D, float (&f)[V]) {
+  static __device__ __forceinline__ void gains(const float* w, int lane, int k, int off, int D, float (&f)[V]) {
+    const int e = at(lane, k) - off;
     if constexpr (AL) {
-      const long long e = at(lane, k, 0);
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
         const float4 v = e < D ? __ldg(reinterpret_cast<const float4*>(w + e + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -102,28 +119,31 @@ struct Row {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = at(lane, k, j) < D ? __ldg(w + at(lane, k, j)) : 0.f;
+      for (int j = 0; j < V; ++j) f[j] = e + j >= 0 && e + j < D ? __ldg(w + e + j) : 0.f;
     }
   }
-  static __device__ __forceinline__ void store_e4m3(uint8_t* p, int lane, int k, int D, const float (&f)[V]) {
-    if constexpr (AL) {
-      const long long e = at(lane, k, 0);
-      uint32_t u[V / 4];
+  static __device__ __forceinline__ void store_e4m3(uint8_t* p, int lane, int k, int off, bool same, int D, const float (&f)[V]) {
+    const int e = at(lane, k) - off;
+    uint32_t u[V / 4];
 #pragma unroll
-      for (int j = 0; j < V / 4; ++j)
-        u[j] = static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(f[4 * j], f[4 * j + 1]), __NV_SATFINITE, __NV_E4M3)) |
-               static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(f[4 * j + 2], f[4 * j + 3]), __NV_SATFINITE, __NV_E4M3))
-                   << 16;
-      if (e < D) {
-#pragma unroll
-        for (int j = 0; j < V / 4; ++j) reinterpret_cast<uint32_t*>(p + e)[j] = u[j];
-      }
-    } else {
+    for (int j = 0; j < V / 4; ++j)
+      u[j] = static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(f[4 * j], f[4 * j + 1]), __NV_SATFINITE, __NV_E4M3)) |
+             static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(f[4 * j + 2], f[4 * j + 3]), __NV_SATFINITE, __NV_E4M3)) << 16;
+    if (whole(e, D, same)) {
+      if constexpr (V == 8)
+        *reinterpret_cast<uint2*>(p + e) = make_uint2(u[0], u[1]);
+      else
+        *reinterpret_cast<uint32_t*>(p + e) = u[0];
+    } else if constexpr (!AL) {
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (at(lane, k, j) < D) p[at(lane, k, j)] = __nv_cvt_float_to_fp8(f[j], __NV_SATFINITE, __NV_E4M3);
+        if (e + j >= 0 && e + j < D) p[e + j] = static_cast<uint8_t>(u[j / 4] >> (8 * (j & 3)));
     }
   }
+};
+// Which matrices of an unaligned call lie like the first one (x; h in the backward).
+struct Same {
+  bool a, b, c;
 };
 
 // Sum of a and sum of b (or, MAXB, the largest b by its bits: magnitudes, where a NaN is above infinity) over a row's TPR
@@ -159,7 +179,7 @@ __device__ __forceinline__ float magnitude(float v) { return __uint_as_float(__f
 template <int TPR> constexpr int BLOCK_OF = TPR > 32 ? TPR : 256;  // threads a CTA
 
 template <typename T, bool Q8, bool AL, int TPR, int NV>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a) {
+__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a, const Same same) {
   constexpr int V = Io<T>::V, ROWS = BLOCK_OF<TPR> / TPR;
   using R = Row<T, AL, TPR>;
   const int lane = threadIdx.x % TPR;
@@ -172,25 +192,24 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a) {
     float sq = 0.f, top = 0.f;
     const T* x = static_cast<const T*>(a.x) + t * a.xs;
     const T* r = static_cast<const T*>(a.r) + t * a.rs;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) R::load(x, lane, k, D, h[k]);
+    const int off = R::offset(x);
+    R::load(x, lane, off, true, D, h);
     if (a.r) {
       float f[NV][V];
-#pragma unroll
-      for (int k = 0; k < NV; ++k) R::load(r, lane, k, D, f[k]);
+      R::load(r, lane, off, same.a, D, f);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) h[k][j] += f[k][j];
       if (a.h) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, D, h[k]);
+        for (int k = 0; k < NV; ++k) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, off, same.b, D, h[k]);
       }
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
-      R::gains(a.w, lane, k, D, w);
+      R::gains(a.w, lane, k, off, D, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         sq += h[k][j] * h[k][j];
@@ -207,9 +226,9 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) h[k][j] = Q8 ? h[k][j] * lift * f : h[k][j] * f;
       if constexpr (Q8)
-        R::store_e4m3(static_cast<uint8_t*>(a.y) + t * a.ys, lane, k, D, h[k]);
+        R::store_e4m3(static_cast<uint8_t*>(a.y) + t * a.ys, lane, k, off, same.c, D, h[k]);
       else
-        R::store(static_cast<T*>(a.y) + t * a.ys, lane, k, D, h[k]);
+        R::store(static_cast<T*>(a.y) + t * a.ys, lane, k, off, same.c, D, h[k]);
     }
     if (Q8 && lane == 0 && t < a.T) a.scale[t] = top * rstd * (1.f / E4M3_MAX);
   }
@@ -247,77 +266,102 @@ __global__ void __launch_bounds__(LONG_THREADS) k_rms_long(const Forward a) {
   pdl_trigger();
 }
 
-// dx, and this CTA's partial row of dw: part[blockIdx.x][0 .. D).
+// Where element c of a row's sums lies in shared memory (unaligned rows): vectors' places apart, so that a warp's lanes, whose
+// vectors follow one another, touch consecutive words whatever the row's offset.
+template <int V>
+__device__ __forceinline__ int column_at(int c, int D) { return c % V * ((D + V - 1) / V) + c / V; }
+template <int V>
+__host__ __device__ constexpr int columns_of(int D) { return (D + V - 1) / V * V; }
+
+// dx, and this CTA's partial row of dw: part[blockIdx.x][0 .. D).  Aligned rows: a thread's columns are the same in every row,
+// their sums stay in its registers.  Unaligned ones: in shared memory, one set for each of the CTA's row groups (dynamic).
 template <typename T, bool AL, int TPR, int NV>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a) {
-  constexpr int V = Io<T>::V, ROWS = BLOCK_OF<TPR> / TPR;
+__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, const Same same) {
+  constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
-  const int lane = threadIdx.x % TPR;
+  extern __shared__ float s_acc[];
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
-  float acc[NV][V] = {};
+  float acc[AL ? NV : 1][V] = {};
+  float* mine = s_acc + (AL ? 0 : group * columns_of<V>(a.D));
+  if constexpr (!AL) {
+    for (int i = lane; i < columns_of<V>(a.D); i += TPR) mine[i] = 0.f;
+    __syncthreads();
+  }
   pdl_wait();
   for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += static_cast<long long>(gridDim.x) * ROWS) {
-    const long long t = base + threadIdx.x / TPR;
+    const long long t = base + group;
     const int D = t < a.T ? a.D : 0;
     float h[NV][V], d[NV][V];
     float sq = 0.f, ah = 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) R::load(static_cast<const T*>(a.h) + t * a.hs, lane, k, D, h[k]);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) R::load(static_cast<const T*>(a.dy) + t * a.ys, lane, k, D, d[k]);
+    const T* hp = static_cast<const T*>(a.h) + t * a.hs;
+    const int off = R::offset(hp);
+    R::load(hp, lane, off, true, D, h);
+    R::load(static_cast<const T*>(a.dy) + t * a.ys, lane, off, same.a, D, d);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
-      R::gains(a.w, lane, k, D, w);
+      R::gains(a.w, lane, k, off, D, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         sq += h[k][j] * h[k][j];
         ah += d[k][j] * w[j] * h[k][j];
       }
     }
-    row_reduce<TPR, false>(sq, ah);
+    row_reduce<TPR, false>(sq, ah);  // (more than a warp a row: a barrier, behind which the last row's columns are added)
+    if constexpr (!AL && TPR <= 32) __syncwarp();
     const float rstd = rsqrtf(sq * inv_d + a.eps);
     const float c = rstd * rstd * rstd * (ah * inv_d);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      float w[V], o[V];
-      R::gains(a.w, lane, k, D, w);
-      if (a.dh) {
-        R::load(static_cast<const T*>(a.dh) + t * a.ds, lane, k, D, o);
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = 0.f;
-      }
+      float w[V], o[1][V] = {};
+      R::gains(a.w, lane, k, off, D, w);
+      if (a.dh) R::load(static_cast<const T*>(a.dh) + t * a.ds, lane + TPR * k, off, same.b, D, o);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        acc[k][j] += d[k][j] * (h[k][j] * rstd);
-        o[j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
+        const float g = d[k][j] * (h[k][j] * rstd);
+        if constexpr (AL) {
+          acc[k][j] += g;
+        } else {
+          const int e = R::at(lane, k) - off + j;
+          if (e >= 0 && e < D) mine[column_at<V>(e, a.D)] += g;
+        }
+        o[0][j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
       }
-      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, D, o);
+      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o[0]);
     }
   }
-  // the CTA's row groups hold the same columns: added in ascending group order, one vector at a time
+  // the CTA's row groups hold the same columns: added in ascending group order
   float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.x) * a.D;
-  if constexpr (ROWS == 1) {
+  if constexpr (!AL) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.D; e += BLOCK) {
+      const float* s = s_acc + column_at<V>(e, a.D);
+      float sum = s[0];
+#pragma unroll 4
+      for (int g = 1; g < ROWS; ++g) sum += s[g * columns_of<V>(a.D)];
+      part[e] = sum;
+    }
+  } else if constexpr (ROWS == 1) {
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (R::at(lane, k, j) < a.D) part[R::at(lane, k, j)] = acc[k][j];
+        if (R::at(lane, k) + j < a.D) part[R::at(lane, k) + j] = acc[k][j];
   } else {
     __shared__ float s[ROWS][TPR][V + 1];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[threadIdx.x / TPR][lane][j] = acc[k][j];
+      for (int j = 0; j < V; ++j) s[group][lane][j] = acc[k][j];
       __syncthreads();
-      for (int i = threadIdx.x; i < TPR * V; i += BLOCK_OF<TPR>) {
-        const int l = AL ? i / V : i % TPR, j = AL ? i % V : i / TPR;
+      for (int i = threadIdx.x; i < TPR * V; i += BLOCK) {
+        const int l = i / V, j = i % V;
         float sum = 0.f;
 #pragma unroll
         for (int g = 0; g < ROWS; ++g) sum += s[g][l][j];
-        if (R::at(l, k, j) < a.D) part[R::at(l, k, j)] = sum;
+        if (R::at(l, k) + j < a.D) part[R::at(l, k) + j] = sum;
       }
     }
   }
@@ -397,29 +441,43 @@ __global__ void __launch_bounds__(32 * DW_RUNS) k_dw(const float* part, float* _
 
 // ---- host ----
 
-// Threads a row and vectors a thread for rows of n vectors: at most 128 vectors stay within a warp (no shared memory).
+// Threads a row and vectors a thread for rows of n vectors: at most 128 vectors stay within a warp (no shared memory).  Few rows
+// (fewer than SMs) take more threads each: a row's latency is the call's.
 template <class F>
-cudaError_t by_length(int n, F&& f) {
+cudaError_t by_length(int n, bool few, F&& f) {
 #define WHTMIX_ROW(TPR, NV) f(std::integral_constant<int, TPR>(), std::integral_constant<int, NV>())
   if (n <= 8) return WHTMIX_ROW(8, 1);
   if (n <= 16) return WHTMIX_ROW(16, 1);
   if (n <= 32) return WHTMIX_ROW(32, 1);
+  if (few) {
+    if (n <= 128) return WHTMIX_ROW(128, 1);
+    if (n <= 512) return WHTMIX_ROW(512, 1);
+  }
   if (n <= 64) return WHTMIX_ROW(32, 2);
   if (n <= 128) return WHTMIX_ROW(32, 4);
   if (n <= 256) return WHTMIX_ROW(128, 2);
-  if (n <= 512) return WHTMIX_ROW(128, 4);
-  if (n <= 1024) return WHTMIX_ROW(256, 4);
+  if (n <= 512) return WHTMIX_ROW(256, 2);
+  if (n <= 1024) return WHTMIX_ROW(512, 2);
   return WHTMIX_ROW(512, 4);
 #undef WHTMIX_ROW
 }
 
-int vectors(int D, bool bf16) { return bf16 ? (D + 7) / 8 : (D + 3) / 4; }
+// 16-byte vectors of a row; an unaligned one may touch one more
+int vectors(int D, bool bf16, bool al) {
+  const int v = bf16 ? 8 : 4;
+  return (D + v - 1) / v + (al ? 0 : 1);
+}
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // rows of `es`-byte elements at p, `stride` elements apart, all start on a 16-byte boundary
 bool rows_aligned(const void* p, long long stride, size_t es, size_t to = 16) {
   return !p || (aligned(p, to) && (static_cast<unsigned long long>(stride) * es) % to == 0);
+}
+
+// rows q lie like rows p: the same distance from a 16-byte boundary, row for row
+bool rows_same(const void* p, long long ps, const void* q, long long qs, size_t es) {
+  return !q || (((reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(q)) & 15u) == 0 && (ps - qs) * static_cast<long long>(es) % 16 == 0);
 }
 
 unsigned grid_rows(long long T, int rows, int block, int sms) {
@@ -429,21 +487,25 @@ unsigned grid_rows(long long T, int rows, int block, int sms) {
 
 template <typename T, bool Q8>
 cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
+  constexpr int V = Io<T>::V;
   const size_t es = sizeof(T);
-  const int n = vectors(a.D, es == 2);
+  const bool al = a.D % V == 0 && aligned(a.w, 16) && rows_aligned(a.x, a.xs, es) && rows_aligned(a.r, a.rs, es) &&
+                  rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, V) : rows_aligned(a.y, a.ys, es));
+  const int n = vectors(a.D, es == 2, al);
+  Forward c = a;
   if (n > MAX_VECTORS) {
-    Forward c = a;
     void* args[] = {&c};
     return launch_pdl(reinterpret_cast<const void*>(k_rms_long<T, Q8>), grid_rows(a.T, 1, LONG_THREADS, sms), LONG_THREADS, 0, stream, args);
   }
-  const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.x, a.xs, es) && rows_aligned(a.r, a.rs, es) &&
-                  rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, 4) : rows_aligned(a.y, a.ys, es));
-  return by_length(n, [&](auto tpr, auto nv) {
+  // (8 bits: a vector's V bytes start on a multiple of V)
+  const bool same_y = Q8 ? (reinterpret_cast<uintptr_t>(a.y) - reinterpret_cast<uintptr_t>(a.x) / es) % V == 0 && (a.ys - a.xs) % V == 0
+                         : rows_same(a.x, a.xs, a.y, a.ys, es);
+  Same same{rows_same(a.x, a.xs, a.r, a.rs, es), rows_same(a.x, a.xs, a.r ? a.h : nullptr, a.hs, es), same_y};
+  return by_length(n, a.T < sms, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
     const void* k = al ? reinterpret_cast<const void*>(k_rms<T, Q8, true, TPR, NV>)
                        : reinterpret_cast<const void*>(k_rms<T, Q8, false, TPR, NV>);
-    Forward c = a;
-    void* args[] = {&c};
+    void* args[] = {&c, &same};
     return launch_pdl(k, grid_rows(a.T, BLOCK / TPR, BLOCK, sms), BLOCK, 0, stream, args);
   });
 }
@@ -454,7 +516,7 @@ cudaError_t forward(const Forward& a, bool bf16, bool to_e4m3, int sms, cudaStre
   return to_e4m3 ? forward_t<float, true>(a, sms, stream) : forward_t<float, false>(a, sms, stream);
 }
 
-// Partial rows of dw: one a CTA of k_rms_bwd (at most 512 resident threads an SM, which hold the sums of their columns), or one a
+// Partial rows of dw: one a CTA of k_rms_bwd (at most 1024 threads an SM), or one a
 // chunk of rows for k_dw_long.
 int dw_parts(long long T, int n, int sms) {
   if (n > MAX_VECTORS) {
@@ -462,7 +524,7 @@ int dw_parts(long long T, int n, int sms) {
     return static_cast<int>(T < most ? T : most);
   }
   int parts = 0;
-  by_length(n, [&](auto tpr, auto) {
+  by_length(n, T < sms, [&](auto tpr, auto) {
     constexpr int TPR = decltype(tpr)::value, BLOCK = BLOCK_OF<TPR>;
     const long long need = (T + BLOCK / TPR - 1) / (BLOCK / TPR), most = static_cast<long long>(sms) * (1024 / BLOCK);
     parts = static_cast<int>(need < most ? need : most);
@@ -471,9 +533,16 @@ int dw_parts(long long T, int n, int sms) {
   return parts;
 }
 
-size_t backward_workspace(long long T, int D, bool bf16, int sms) {
-  const int n = vectors(D, bf16);
-  return static_cast<size_t>(dw_parts(T, n, sms)) * D * 4 + (n > MAX_VECTORS ? static_cast<size_t>(T) * 4 : 0);
+template <typename T>
+bool backward_aligned(const Backward& a) {
+  const size_t es = sizeof(T);
+  return a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.h, a.hs, es) && rows_aligned(a.dy, a.ys, es) &&
+         rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es);
+}
+
+size_t backward_workspace(const Backward& a, bool bf16, int sms) {
+  const int n = vectors(a.D, bf16, bf16 ? backward_aligned<__nv_bfloat16>(a) : backward_aligned<float>(a));
+  return static_cast<size_t>(dw_parts(a.T, n, sms)) * a.D * 4 + (n > MAX_VECTORS ? static_cast<size_t>(a.T) * 4 : 0);
 }
 
 cudaError_t add_rows(const float* part, float* out, int D, int parts, cudaStream_t stream) {
@@ -484,7 +553,8 @@ cudaError_t add_rows(const float* part, float* out, int D, int parts, cudaStream
 template <typename T>
 cudaError_t backward_t(const Backward& a, int sms, cudaStream_t stream) {
   const size_t es = sizeof(T);
-  const int n = vectors(a.D, es == 2), parts = dw_parts(a.T, n, sms);
+  const bool al = backward_aligned<T>(a);
+  const int n = vectors(a.D, es == 2, al), parts = dw_parts(a.T, n, sms);
   Backward c = a;
   cudaError_t e;
   if (n > MAX_VECTORS) {
@@ -495,14 +565,18 @@ cudaError_t backward_t(const Backward& a, int sms, cudaStream_t stream) {
     k_dw_long<T><<<dim3((a.D + 255) / 256, parts), 256, 0, stream>>>(c, coef, parts);
     e = cudaGetLastError();
   } else {
-    const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.h, a.hs, es) && rows_aligned(a.dy, a.ys, es) &&
-                    rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es);
-    e = by_length(n, [&](auto tpr, auto nv) {
-      constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-      const void* k = al ? reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>)
-                         : reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
-      void* args[] = {&c};
-      return launch_pdl(k, static_cast<unsigned>(parts), BLOCK_OF<TPR>, 0, stream, args);
+    Same same{rows_same(a.h, a.hs, a.dy, a.ys, es), rows_same(a.h, a.hs, a.dh, a.ds, es), rows_same(a.h, a.hs, a.dx, a.xs, es)};
+    e = by_length(n, a.T < sms, [&](auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
+      void* args[] = {&c, &same};
+      if (al) return launch_pdl(reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>), static_cast<unsigned>(parts), BLOCK, 0, stream, args);
+      const void* k = reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
+      const size_t smem = static_cast<size_t>(BLOCK / TPR) * columns_of<Io<T>::V>(a.D) * 4;  // at most 64 KB
+      if (smem > 48 * 1024) {
+        const cudaError_t f = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (f != cudaSuccess) return f;
+      }
+      return launch_pdl(k, static_cast<unsigned>(parts), BLOCK, smem, stream, args);
     });
   }
   if (e != cudaSuccess) return e;

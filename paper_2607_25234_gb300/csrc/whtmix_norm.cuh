@@ -33,7 +33,7 @@ struct Backward {
 };
 
 cudaError_t forward(const Forward& a, bool bf16, bool to_e4m3, int sms, cudaStream_t stream);
-size_t backward_workspace(long long T, int D, bool bf16, int sms);
+size_t backward_workspace(const Backward& a, bool bf16, int sms);  // (of a its ws is not read)
 // out[e] = the sum over `parts` of part[p][e], e < D, in a fixed order (also the linear layer's bias gradient)
 cudaError_t add_rows(const float* part, float* out, int D, int parts, cudaStream_t stream);
 cudaError_t backward(const Backward& a, bool bf16, int sms, cudaStream_t stream);
