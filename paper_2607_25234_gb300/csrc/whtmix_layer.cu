@@ -148,7 +148,9 @@ int whtmix_rms_norm_backward(const void* h, const float* w, const void* dy, cons
     if (none) return zero(dw, static_cast<size_t>(D) * 4, stream);
     const bool bf16 = dtype == WHTMIX_BF16;
     norm::Backward a{h, w, dy, dh, dx, dw, nullptr, T, h_stride, dy_stride, dh_stride, dx_stride, static_cast<int>(D), eps};
-    rc = host::workspace(dev, stream, norm::backward_workspace(a, bf16, sms), 1, &a.ws);
+    size_t need = 0;
+    rc = done(norm::backward_workspace(a, bf16, sms, &need));
+    if (rc == WHTMIX_OK) rc = host::workspace(dev, stream, need, 1, &a.ws);
     if (rc != WHTMIX_OK) return rc;
     return done(norm::backward(a, bf16, sms, stream));
   });

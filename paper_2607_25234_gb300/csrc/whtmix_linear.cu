@@ -198,10 +198,9 @@ static ForwardPlan plan_forward(const Forward& a) {
   return f;
 }
 
-size_t forward_workspace(const Forward& a, int) { return a.T <= FEW_TOKENS ? 0 : plan_forward(a).total; }
+size_t forward_workspace(const Forward& a, int) { return plan_forward(a).total; }
 
 cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
-  if (a.T <= FEW_TOKENS) return forward_few(a, sms, stream);
   const ForwardPlan f = plan_forward(a);
   const int es = a.e4m3 ? 1 : 2, os = a.out_f32 ? 4 : 2;
   const void *x = a.x, *w = a.w;
@@ -217,6 +216,7 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
     cw = copy_of(static_cast<char*>(ws) + f.w_off, a.w, a.N, a.K, a.ws, f.kp, es);
   }
   if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
+  if (a.T <= FEW_TOKENS) return forward_few(a, x, xs, w, wst, err, sms, stream);
   Gemm g{};
   g.tiles_m = ceil_div(a.T, GEMM_BM);
   g.kblocks = ceil_div(a.K, 128 / es);

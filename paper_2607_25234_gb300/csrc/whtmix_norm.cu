@@ -16,6 +16,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <map>
+#include <mutex>
+#include <tuple>
 #include <type_traits>
 
 #include "whtmix_kernels.cuh"
@@ -64,6 +67,23 @@ template <> struct Io<__nv_bfloat16> {
   }
 };
 
+// Where element c of a row lies in shared memory (unaligned rows' gains and sums): the places of a vector apart, so that a warp's
+// lanes, whose vectors follow one another, touch consecutive words whatever the row's offset.
+template <int V>
+__device__ __forceinline__ int column_at(int c, int D) { return c % V * ((D + V - 1) / V) + c / V; }
+template <int V>
+__host__ __device__ constexpr int columns_of(int D) { return (D + V - 1) / V * V; }
+
+// The addresses of a matrix, first to one past its last.
+struct Bounds {
+  uintptr_t lo, hi;
+};
+template <typename T>
+__device__ __forceinline__ Bounds bounds_of(const void* p, long long rows, long long stride, int D) {
+  const T* b = static_cast<const T*>(p);
+  return {reinterpret_cast<uintptr_t>(b), reinterpret_cast<uintptr_t>(b + (rows - 1) * stride + D)};
+}
+
 // Vector k of thread `lane` of a row's TPR: V consecutive elements, from at(lane, k) - off on.  AL: rows are 16-byte aligned, whole
 // vectors (off = 0).  Otherwise off is the row's distance from the 16-byte boundary before it, so that the vectors lie on such
 // boundaries all the same: the first and the last of a row are cut, and go element by element.  So do all vectors of a matrix
@@ -76,25 +96,35 @@ struct Row {
     return AL ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
   }
   static __device__ __forceinline__ bool whole(int e, int D, bool same) { return AL ? e < D : same && e >= 0 && e + V <= D; }
-  // the NV vectors of a row: all loads first
+  // a vector of the row that lies in the matrix whole, cut or not
+  static __device__ __forceinline__ bool loadable(const T* p, int e, const Bounds& b, bool same, int D) {
+    const uintptr_t q = reinterpret_cast<uintptr_t>(p + e);
+    return AL ? e < D : same && e > -V && e < D && q >= b.lo && q + 16 <= b.hi;
+  }
+  // the NV vectors of a row as they lie in memory, and their values (what a cut one holds of other rows is zero; element by element
+  // only at the ends of the matrix)
   template <int NV>
-  static __device__ __forceinline__ void load(const T* p, int lane, int off, bool same, int D, float (&f)[NV][V]) {
-    uint4 u[NV];
+  static __device__ __forceinline__ void fetch(const T* p, const Bounds& b, int lane, int off, bool same, int D, uint4 (&u)[NV]) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int e = at(lane, k) - off;
       u[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (whole(e, D, same)) u[k] = *reinterpret_cast<const uint4*>(p + e);
+      if (loadable(p, e, b, same, D)) u[k] = *reinterpret_cast<const uint4*>(p + e);
     }
+  }
+  static __device__ __forceinline__ void values(const T* p, const Bounds& b, int lane, int k, int off, bool same, int D, uint4 u,
+                                                float (&f)[V]) {
+    Io<T>::unpack(u, f);
+    if constexpr (!AL) {
+      const int e = at(lane, k) - off;
+      if (!whole(e, D, same)) {
+        const bool loaded = loadable(p, e, b, same, D);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      Io<T>::unpack(u[k], f[k]);
-      if constexpr (!AL) {
-        const int e = at(lane, k) - off;
-        if (!whole(e, D, same)) {
-#pragma unroll
-          for (int j = 0; j < V; ++j)
-            if (e + j >= 0 && e + j < D) f[k][j] = Io<T>::get(p, e + j);
+        for (int j = 0; j < V; ++j) {
+          if (e + j < 0 || e + j >= D)
+            f[j] = 0.f;
+          else if (!loaded)
+            f[j] = Io<T>::get(p, e + j);
         }
       }
     }
@@ -109,6 +139,7 @@ struct Row {
         if (e + j >= 0 && e + j < D) Io<T>::put(p, e + j, f[j]);
     }
   }
+  // AL: w itself; otherwise its copy in shared memory (gains_to_shared)
   static __device__ __forceinline__ void gains(const float* w, int lane, int k, int off, int D, float (&f)[V]) {
     const int e = at(lane, k) - off;
     if constexpr (AL) {
@@ -119,7 +150,7 @@ struct Row {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = e + j >= 0 && e + j < D ? __ldg(w + e + j) : 0.f;
+      for (int j = 0; j < V; ++j) f[j] = e + j >= 0 && e + j < D ? w[column_at<V>(e + j, D)] : 0.f;
     }
   }
   static __device__ __forceinline__ void store_e4m3(uint8_t* p, int lane, int k, int off, bool same, int D, const float (&f)[V]) {
@@ -141,6 +172,10 @@ struct Row {
     }
   }
 };
+template <int V, int BLOCK>
+__device__ __forceinline__ void gains_to_shared(float* s, const float* w, int D) {
+  for (int i = threadIdx.x; i < D; i += BLOCK) s[column_at<V>(i, D)] = __ldg(w + i);
+}
 // Which matrices of an unaligned call lie like the first one (x; h in the backward).
 struct Same {
   bool a, b, c;
@@ -178,38 +213,76 @@ __device__ __forceinline__ float magnitude(float v) { return __uint_as_float(__f
 
 template <int TPR> constexpr int BLOCK_OF = TPR > 32 ? TPR : 256;  // threads a CTA
 
+// A thread's gains, where its columns are the same in every row and they are few (else they come again with each row).
+template <typename R, bool AL, int NV>
+struct Kept {
+  static constexpr bool KEEP = AL && NV <= 2;
+  float w[KEEP ? NV : 1][R::V];
+  __device__ __forceinline__ void fill(const float* g, int lane, int D) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) R::gains(g, lane, k, 0, D, w[k]);
+    }
+  }
+  __device__ __forceinline__ void get(const float* g, int lane, int k, int off, int D, float (&f)[R::V]) const {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int j = 0; j < R::V; ++j) f[j] = w[k][j];
+    } else {
+      R::gains(g, lane, k, off, D, f);
+    }
+  }
+};
+
+// The next row's loads are issued before this row's sums are complete.
 template <typename T, bool Q8, bool AL, int TPR, int NV>
 __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a, const Same same) {
-  constexpr int V = Io<T>::V, ROWS = BLOCK_OF<TPR> / TPR;
+  constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
-  const int lane = threadIdx.x % TPR;
+  extern __shared__ float s_w[];  // unaligned rows: the gains
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
   pdl_wait();
-  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += static_cast<long long>(gridDim.x) * ROWS) {
-    const long long t = base + threadIdx.x / TPR;
+  if constexpr (!AL) {
+    gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
+    __syncthreads();
+  }
+  const float* gains = AL ? a.w : s_w;
+  Kept<R, AL, NV> kept;
+  kept.fill(gains, lane, a.D);
+  const long long step = static_cast<long long>(gridDim.x) * ROWS;
+  const Bounds bx = bounds_of<T>(a.x, a.T, a.xs, a.D), br = bounds_of<T>(a.r, a.T, a.rs, a.D);
+  uint4 ux[NV], ur[NV];
+  auto fetch = [&](long long t) {
+    const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
     const int D = t < a.T ? a.D : 0;  // a row past the end holds no elements
+    R::fetch(x, bx, lane, R::offset(x), true, D, ux);
+    if (a.r) R::fetch(r, br, lane, R::offset(x), same.a, D, ur);
+  };
+  fetch(static_cast<long long>(blockIdx.x) * ROWS + group);
+  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += step) {
+    const long long t = base + group;
+    const int D = t < a.T ? a.D : 0;
+    const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
+    const int off = R::offset(x);
     float h[NV][V];
     float sq = 0.f, top = 0.f;
-    const T* x = static_cast<const T*>(a.x) + t * a.xs;
-    const T* r = static_cast<const T*>(a.r) + t * a.rs;
-    const int off = R::offset(x);
-    R::load(x, lane, off, true, D, h);
-    if (a.r) {
-      float f[NV][V];
-      R::load(r, lane, off, same.a, D, f);
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      R::values(x, bx, lane, k, off, true, D, ux[k], h[k]);
+      if (a.r) {
+        float f[V];
+        R::values(r, br, lane, k, off, same.a, D, ur[k], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) h[k][j] += f[k][j];
-      if (a.h) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, off, same.b, D, h[k]);
+        for (int j = 0; j < V; ++j) h[k][j] += f[j];
+        if (a.h) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, off, same.b, D, h[k]);
       }
     }
+    fetch(t + step);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
-      R::gains(a.w, lane, k, off, D, w);
+      kept.get(gains, lane, k, off, a.D, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         sq += h[k][j] * h[k][j];
@@ -266,42 +339,59 @@ __global__ void __launch_bounds__(LONG_THREADS) k_rms_long(const Forward a) {
   pdl_trigger();
 }
 
-// Where element c of a row's sums lies in shared memory (unaligned rows): vectors' places apart, so that a warp's lanes, whose
-// vectors follow one another, touch consecutive words whatever the row's offset.
-template <int V>
-__device__ __forceinline__ int column_at(int c, int D) { return c % V * ((D + V - 1) / V) + c / V; }
-template <int V>
-__host__ __device__ constexpr int columns_of(int D) { return (D + V - 1) / V * V; }
-
 // dx, and this CTA's partial row of dw: part[blockIdx.x][0 .. D).  Aligned rows: a thread's columns are the same in every row,
 // their sums stay in its registers.  Unaligned ones: in shared memory, one set for each of the CTA's row groups (dynamic).
 template <typename T, bool AL, int TPR, int NV>
 __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, const Same same) {
   constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
-  extern __shared__ float s_acc[];
+  extern __shared__ float s_acc[];  // unaligned rows: the sums, then the gains
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
   float acc[AL ? NV : 1][V] = {};
   float* mine = s_acc + (AL ? 0 : group * columns_of<V>(a.D));
   if constexpr (!AL) {
     for (int i = lane; i < columns_of<V>(a.D); i += TPR) mine[i] = 0.f;
+  }
+  float* s_w = s_acc + ROWS * columns_of<V>(a.D);
+  pdl_wait();
+  if constexpr (!AL) {
+    gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
     __syncthreads();
   }
-  pdl_wait();
-  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += static_cast<long long>(gridDim.x) * ROWS) {
+  const float* gains = AL ? a.w : s_w;
+  Kept<R, AL, NV> kept;
+  kept.fill(gains, lane, a.D);
+  const long long step = static_cast<long long>(gridDim.x) * ROWS;
+  const Bounds bh = bounds_of<T>(a.h, a.T, a.hs, a.D), bd = bounds_of<T>(a.dy, a.T, a.ys, a.D), bg = bounds_of<T>(a.dh, a.T, a.ds, a.D);
+  uint4 uh[NV], ud[NV];
+  auto fetch = [&](long long t) {
+    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
+    const int D = t < a.T ? a.D : 0;
+    R::fetch(hp, bh, lane, R::offset(hp), true, D, uh);
+    R::fetch(dp, bd, lane, R::offset(hp), same.a, D, ud);
+  };
+  fetch(static_cast<long long>(blockIdx.x) * ROWS + group);
+  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += step) {
     const long long t = base + group;
     const int D = t < a.T ? a.D : 0;
     float h[NV][V], d[NV][V];
     float sq = 0.f, ah = 0.f;
-    const T* hp = static_cast<const T*>(a.h) + t * a.hs;
+    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
     const int off = R::offset(hp);
-    R::load(hp, lane, off, true, D, h);
-    R::load(static_cast<const T*>(a.dy) + t * a.ys, lane, off, same.a, D, d);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      R::values(hp, bh, lane, k, off, true, D, uh[k], h[k]);
+      R::values(dp, bd, lane, k, off, same.a, D, ud[k], d[k]);
+    }
+    uint4 ug[NV];
+    const T* gp = static_cast<const T*>(a.dh) + t * a.ds;
+    if (a.dh) R::fetch(gp, bg, lane, off, same.b, D, ug);
+    fetch(t + step);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
-      R::gains(a.w, lane, k, off, D, w);
+      kept.get(gains, lane, k, off, a.D, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         sq += h[k][j] * h[k][j];
@@ -314,9 +404,9 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
     const float c = rstd * rstd * rstd * (ah * inv_d);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      float w[V], o[1][V] = {};
-      R::gains(a.w, lane, k, off, D, w);
-      if (a.dh) R::load(static_cast<const T*>(a.dh) + t * a.ds, lane + TPR * k, off, same.b, D, o);
+      float w[V], o[V] = {};
+      kept.get(gains, lane, k, off, a.D, w);
+      if (a.dh) R::values(gp, bg, lane, k, off, same.b, D, ug[k], o);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float g = d[k][j] * (h[k][j] * rstd);
@@ -326,9 +416,9 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
           const int e = R::at(lane, k) - off + j;
           if (e >= 0 && e < D) mine[column_at<V>(e, a.D)] += g;
         }
-        o[0][j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
+        o[j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
       }
-      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o[0]);
+      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o);
     }
   }
   // the CTA's row groups hold the same columns: added in ascending group order
@@ -456,8 +546,11 @@ cudaError_t by_length(int n, bool few, F&& f) {
   if (n <= 64) return WHTMIX_ROW(32, 2);
   if (n <= 128) return WHTMIX_ROW(32, 4);
   if (n <= 256) return WHTMIX_ROW(128, 2);
+  if (n <= 384) return WHTMIX_ROW(128, 3);
   if (n <= 512) return WHTMIX_ROW(256, 2);
-  if (n <= 1024) return WHTMIX_ROW(512, 2);
+  if (n <= 768) return WHTMIX_ROW(256, 3);
+  if (n <= 1024) return WHTMIX_ROW(256, 4);
+  if (n <= 1536) return WHTMIX_ROW(512, 3);
   return WHTMIX_ROW(512, 4);
 #undef WHTMIX_ROW
 }
@@ -480,9 +573,30 @@ bool rows_same(const void* p, long long ps, const void* q, long long qs, size_t 
   return !q || (((reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(q)) & 15u) == 0 && (ps - qs) * static_cast<long long>(es) % 16 == 0);
 }
 
-unsigned grid_rows(long long T, int rows, int block, int sms) {
-  const long long need = (T + rows - 1) / rows, most = static_cast<long long>(sms) * (2048 / block);
-  return static_cast<unsigned>(need < most ? need : most);
+// CTAs for T rows, `rows` at a time: at most as many as are resident at once, so that each takes its even share (with four
+// times the SMs where three fit, a backward of 131072 rows of 256 took 66 us).
+unsigned grid_rows(long long T, int rows, int resident) {
+  const long long need = (T + rows - 1) / rows;
+  return static_cast<unsigned>(need < resident ? need : resident);
+}
+// Resident CTAs of a kernel on the whole device, its shared-memory limit raised first; asked once for each kernel and size.
+cudaError_t resident_ctas(const void* kernel, int block, size_t smem, int sms, int* out) {
+  static std::mutex mu;
+  static std::map<std::tuple<int, const void*, size_t>, int> known;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> lock(mu);
+  int& n = known[{dev, kernel, smem}];
+  if (n == 0) {
+    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) != cudaSuccess)
+      return e;
+    int per_sm = 0;
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, smem)) != cudaSuccess) return e;
+    n = (per_sm < 1 ? 1 : per_sm) * sms;
+  }
+  *out = n;
+  return cudaSuccess;
 }
 
 template <typename T, bool Q8>
@@ -495,7 +609,7 @@ cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
   Forward c = a;
   if (n > MAX_VECTORS) {
     void* args[] = {&c};
-    return launch_pdl(reinterpret_cast<const void*>(k_rms_long<T, Q8>), grid_rows(a.T, 1, LONG_THREADS, sms), LONG_THREADS, 0, stream, args);
+    return launch_pdl(reinterpret_cast<const void*>(k_rms_long<T, Q8>), grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args);
   }
   // (8 bits: a vector's V bytes start on a multiple of V)
   const bool same_y = Q8 ? (reinterpret_cast<uintptr_t>(a.y) - reinterpret_cast<uintptr_t>(a.x) / es) % V == 0 && (a.ys - a.xs) % V == 0
@@ -506,7 +620,11 @@ cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
     const void* k = al ? reinterpret_cast<const void*>(k_rms<T, Q8, true, TPR, NV>)
                        : reinterpret_cast<const void*>(k_rms<T, Q8, false, TPR, NV>);
     void* args[] = {&c, &same};
-    return launch_pdl(k, grid_rows(a.T, BLOCK / TPR, BLOCK, sms), BLOCK, 0, stream, args);
+    const size_t smem = al ? 0 : static_cast<size_t>(columns_of<V>(a.D)) * 4;  // at most 64 KB
+    int resident = 0;
+    const cudaError_t e = resident_ctas(k, BLOCK, smem, sms, &resident);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(k, grid_rows(a.T, BLOCK / TPR, resident), BLOCK, smem, stream, args);
   });
 }
 
@@ -516,22 +634,8 @@ cudaError_t forward(const Forward& a, bool bf16, bool to_e4m3, int sms, cudaStre
   return to_e4m3 ? forward_t<float, true>(a, sms, stream) : forward_t<float, false>(a, sms, stream);
 }
 
-// Partial rows of dw: one a CTA of k_rms_bwd (at most 1024 threads an SM), or one a
-// chunk of rows for k_dw_long.
-int dw_parts(long long T, int n, int sms) {
-  if (n > MAX_VECTORS) {
-    const long long most = 64;
-    return static_cast<int>(T < most ? T : most);
-  }
-  int parts = 0;
-  by_length(n, T < sms, [&](auto tpr, auto) {
-    constexpr int TPR = decltype(tpr)::value, BLOCK = BLOCK_OF<TPR>;
-    const long long need = (T + BLOCK / TPR - 1) / (BLOCK / TPR), most = static_cast<long long>(sms) * (1024 / BLOCK);
-    parts = static_cast<int>(need < most ? need : most);
-    return cudaSuccess;
-  });
-  return parts;
-}
+// Chunks of rows of k_dw_long.
+int long_parts(long long T) { return static_cast<int>(T < 64 ? T : 64); }
 
 template <typename T>
 bool backward_aligned(const Backward& a) {
@@ -540,9 +644,41 @@ bool backward_aligned(const Backward& a) {
          rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es);
 }
 
-size_t backward_workspace(const Backward& a, bool bf16, int sms) {
-  const int n = vectors(a.D, bf16, bf16 ? backward_aligned<__nv_bfloat16>(a) : backward_aligned<float>(a));
-  return static_cast<size_t>(dw_parts(a.T, n, sms)) * a.D * 4 + (n > MAX_VECTORS ? static_cast<size_t>(a.T) * 4 : 0);
+// A call's kernel, its shared memory and its CTAs, each of which leaves a partial row of dw.
+struct BackwardPlan {
+  const void* kernel;
+  size_t smem;
+  int block, parts;
+};
+template <typename T>
+cudaError_t backward_plan(const Backward& a, int n, bool al, int sms, BackwardPlan* p) {
+  return by_length(n, a.T < sms, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
+    p->kernel = al ? reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>) : reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
+    p->smem = al ? 0 : static_cast<size_t>(BLOCK / TPR + 1) * columns_of<Io<T>::V>(a.D) * 4;  // at most 128 KB
+    p->block = BLOCK;
+    int resident = 0;
+    const cudaError_t e = resident_ctas(p->kernel, BLOCK, p->smem, sms, &resident);
+    if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, BLOCK / TPR, resident));
+    return e;
+  });
+}
+
+template <typename T>
+static cudaError_t workspace_t(const Backward& a, int sms, size_t* bytes) {
+  const bool al = backward_aligned<T>(a);
+  const int n = vectors(a.D, sizeof(T) == 2, al);
+  if (n > MAX_VECTORS) {
+    *bytes = static_cast<size_t>(long_parts(a.T)) * a.D * 4 + static_cast<size_t>(a.T) * 4;
+    return cudaSuccess;
+  }
+  BackwardPlan p;
+  const cudaError_t e = backward_plan<T>(a, n, al, sms, &p);
+  if (e == cudaSuccess) *bytes = static_cast<size_t>(p.parts) * a.D * 4;
+  return e;
+}
+cudaError_t backward_workspace(const Backward& a, bool bf16, int sms, size_t* bytes) {
+  return bf16 ? workspace_t<__nv_bfloat16>(a, sms, bytes) : workspace_t<float>(a, sms, bytes);
 }
 
 cudaError_t add_rows(const float* part, float* out, int D, int parts, cudaStream_t stream) {
@@ -554,30 +690,24 @@ template <typename T>
 cudaError_t backward_t(const Backward& a, int sms, cudaStream_t stream) {
   const size_t es = sizeof(T);
   const bool al = backward_aligned<T>(a);
-  const int n = vectors(a.D, es == 2, al), parts = dw_parts(a.T, n, sms);
+  const int n = vectors(a.D, es == 2, al);
+  int parts = long_parts(a.T);
   Backward c = a;
   cudaError_t e;
   if (n > MAX_VECTORS) {
     float* coef = static_cast<float*>(a.ws) + static_cast<size_t>(parts) * a.D;
     void* args[] = {&c, &coef};
-    e = launch_pdl(reinterpret_cast<const void*>(k_rms_bwd_long<T>), grid_rows(a.T, 1, LONG_THREADS, sms), LONG_THREADS, 0, stream, args);
+    e = launch_pdl(reinterpret_cast<const void*>(k_rms_bwd_long<T>), grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args);
     if (e != cudaSuccess) return e;
     k_dw_long<T><<<dim3((a.D + 255) / 256, parts), 256, 0, stream>>>(c, coef, parts);
     e = cudaGetLastError();
   } else {
     Same same{rows_same(a.h, a.hs, a.dy, a.ys, es), rows_same(a.h, a.hs, a.dh, a.ds, es), rows_same(a.h, a.hs, a.dx, a.xs, es)};
-    e = by_length(n, a.T < sms, [&](auto tpr, auto nv) {
-      constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
-      void* args[] = {&c, &same};
-      if (al) return launch_pdl(reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>), static_cast<unsigned>(parts), BLOCK, 0, stream, args);
-      const void* k = reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
-      const size_t smem = static_cast<size_t>(BLOCK / TPR) * columns_of<Io<T>::V>(a.D) * 4;  // at most 64 KB
-      if (smem > 48 * 1024) {
-        const cudaError_t f = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-        if (f != cudaSuccess) return f;
-      }
-      return launch_pdl(k, static_cast<unsigned>(parts), BLOCK, smem, stream, args);
-    });
+    BackwardPlan p;
+    if ((e = backward_plan<T>(a, n, al, sms, &p)) != cudaSuccess) return e;
+    parts = p.parts;
+    void* args[] = {&c, &same};
+    e = launch_pdl(p.kernel, static_cast<unsigned>(parts), p.block, p.smem, stream, args);
   }
   if (e != cudaSuccess) return e;
   return add_rows(static_cast<const float*>(a.ws), a.dw, a.D, parts, stream);

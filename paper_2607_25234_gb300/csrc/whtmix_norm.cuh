@@ -26,14 +26,14 @@ struct Backward {
   const void* dh;  // gradient that reaches h directly, or null
   void* dx;
   float* dw;
-  void* ws;  // backward_workspace() bytes
+  void* ws;  // as many bytes as backward_workspace says
   long long T, hs, ys, ds, xs;  // strides of h, dy, dh, dx
   int D;
   float eps;
 };
 
 cudaError_t forward(const Forward& a, bool bf16, bool to_e4m3, int sms, cudaStream_t stream);
-size_t backward_workspace(const Backward& a, bool bf16, int sms);  // (of a its ws is not read)
+cudaError_t backward_workspace(const Backward& a, bool bf16, int sms, size_t* bytes);  // (of a its ws is not read)
 // out[e] = the sum over `parts` of part[p][e], e < D, in a fixed order (also the linear layer's bias gradient)
 cudaError_t add_rows(const float* part, float* out, int D, int parts, cudaStream_t stream);
 cudaError_t backward(const Backward& a, bool bf16, int sms, cudaStream_t stream);
