@@ -1,11 +1,11 @@
-// whtmix_few.cu -- the linear layer's product for few tokens (up to 128): y = act(s_x s_w x W^T + b) + r, bound by reading W once.
+// whtmix_few.cu -- the linear layer's product where whtmix_gemm.cuh's tiles are fewer than the SMs, few tokens above all:
+// y = act(s_x s_w x W^T + b) + r, bound by reading W and the latencies of one short chain.
 //
-// The roles of whtmix_gemm.cuh exchanged: 128 rows of W are the product's M, the tokens (rounded up to 16, 32, 64 or 128) its N, so
-// that every byte of shared memory and every load in flight is a weight's.  A CTA takes 128 rows of W and a share of K; the
-// CTAs that share the rows form a cluster (up to 8), so that a small W occupies every SM too.  Warp 4 keeps a ring of TMA loads
-// full (five blocks of 16 KB of W with the tokens' 128 bytes of k each), warp 5 issues the products into tensor memory, warps 0-3
-// are the epilogue, a thread a row of W: alone it stores its channel of every token (32 lanes, 32 consecutive channels); in a
-// cluster the sums go to shared memory, and each CTA adds its part of the tile from all of them, in rank order.
+// The roles of whtmix_gemm.cuh exchanged: 128 rows of W are the product's M, 16, 32, 64 or 128 tokens its N, so that with few
+// tokens every load in flight is a weight's.  A CTA takes 128 rows of W, the tokens of one tile and a share of K; the CTAs that
+// share a tile form a cluster (up to 8), two CTAs fit an SM.  Warp 4 keeps a ring of TMA loads full, warp 5 issues the products
+// into tensor memory, warps 0-3 move the accumulator (a thread a row of W) to shared memory; then each CTA of the cluster adds
+// its share of the tile's tokens from all of them, in rank order, applies the epilogue and stores 128 consecutive channels a warp.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -17,7 +17,7 @@
 namespace whtmix {
 namespace linear {
 
-constexpr int FEW_THREADS = 192, FEW_ROWS = 128, FEW_STAGES = 5;
+constexpr int FEW_THREADS = 192, FEW_ROWS = 128;
 
 struct Few {
   CUtensorMap tw, tx;
@@ -26,19 +26,49 @@ struct Few {
   void* p;
   long long ys, rs, ps;
   const float *bias, *sx, *sw;  // scales of the rows of x and W, or null
-  int T, N, kblocks, splits, act;
+  int T, N, kblocks, splits, tiles_n, act;
+  bool vec;  // rows of y, r and p lie on whole fours of channels
   unsigned int* err;
 };
 
 template <int TN>
 constexpr uint32_t FEW_STAGE = (FEW_ROWS + TN) * 128;
+template <int TN>
+constexpr int FEW_STAGES = TN <= 32 ? 5 : TN == 64 ? 4 : 3;  // at most 100 KB: two CTAs an SM
 template <int TN>  // the ring, or the tile's sums that take its place
-constexpr size_t FEW_SMEM = FEW_STAGES * FEW_STAGE<TN>;
+constexpr size_t FEW_SMEM = FEW_STAGES<TN> * FEW_STAGE<TN>;
 static_assert(FEW_SMEM<128> >= 128 * FEW_ROWS * 4 && FEW_SMEM<16> >= 16 * FEW_ROWS * 4, "a tile's sums fit the ring");
+
+// four consecutive channels
+template <typename O>
+struct Four;
+template <>
+struct Four<float> {
+  static __device__ __forceinline__ void load(const void* p, long long i, float (&f)[4]) {
+    const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+    f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+  }
+  static __device__ __forceinline__ void store(void* p, long long i, const float (&f)[4]) {
+    *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(f[0], f[1], f[2], f[3]);
+  }
+};
+template <>
+struct Four<__nv_bfloat16> {
+  static __device__ __forceinline__ void load(const void* p, long long i, float (&f)[4]) {
+    const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + i);
+    f[0] = __uint_as_float(u.x << 16), f[1] = __uint_as_float(u.x & 0xffff0000u);
+    f[2] = __uint_as_float(u.y << 16), f[3] = __uint_as_float(u.y & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(void* p, long long i, const float (&f)[4]) {
+    __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p) + i) =
+        make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+  }
+};
 
 template <bool E4M3, int TN, typename O>
 __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few a) {
-  constexpr int BK = E4M3 ? 128 : 64, S = FEW_STAGES;
+  constexpr int BK = E4M3 ? 128 : 64, S = FEW_STAGES<TN>;
   constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (static_cast<uint32_t>(TN >> 3) << 17) | ((128u >> 4) << 24);
   constexpr int COLS = TN < 32 ? 32 : TN;  // tensor-memory columns
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -47,7 +77,8 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   namespace cg = cooperative_groups;
   const uint32_t ring = tc::smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = blockIdx.x % a.splits, n0 = blockIdx.x / a.splits * FEW_ROWS;
+  const int rank = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
+  const int n0 = tile % a.tiles_n * FEW_ROWS, t0 = tile / a.tiles_n * TN, tokens = min(TN, a.T - t0);
   const int k0 = static_cast<int>(static_cast<long long>(a.kblocks) * rank / a.splits);
   const int k1 = static_cast<int>(static_cast<long long>(a.kblocks) * (rank + 1) / a.splits);
   if (warp == 0) tc::tmem_alloc(&tmem_slot, COLS);
@@ -76,7 +107,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
         const uint32_t st = ring + s * FEW_STAGE<TN>;
         tma::expect_tx(&full[s], FEW_STAGE<TN>);
         tma::load_2d(st, &a.tw, (k0 + i) * BK, n0, &full[s]);
-        tma::load_2d(st + FEW_ROWS * 128, &a.tx, (k0 + i) * BK, 0, &full[s]);
+        tma::load_2d(st + FEW_ROWS * 128, &a.tx, (k0 + i) * BK, t0, &full[s]);
       }
       if (bad)  // the copies in flight have landed before the CTA can end (otherwise the products have waited for them)
         for (int j = i > S ? i - S : 0; j < i; ++j) tc::mbar_wait(&full[j % S], (j / S) & 1);
@@ -104,54 +135,81 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
       tc::mma_commit(&dfull);
     }
   }
-  auto finish = [&](int t, int n, float z) {
-    if (a.sx) z *= a.sx[t] * a.sw[n];
-    if (a.bias) z += a.bias[n];
-    if (a.p) static_cast<__nv_bfloat16*>(a.p)[t * a.ps + n] = __float2bfloat16_rn(z);
-    z = activate(z, a.act);
-    if (a.r) z += static_cast<float>(static_cast<const O*>(a.r)[t * a.rs + n]);
-    static_cast<O*>(a.y)[t * a.ys + n] = static_cast<O>(z);
-  };
   float* sums = reinterpret_cast<float*>(smem);  // [token][row of W]
   if (warp < 4) {
     // the products have completed: the accumulator can be read, the ring is free
     if (!tc::mbar_wait(&dfull, 0)) bad |= 4;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     __syncwarp();
-    const int n = n0 + tid;
 #pragma unroll
     for (int c = 0; c < TN; c += 16) {
-      if (c < a.T) {
+      if (c < tokens) {
         float v[16];
         tc::tmem_ld16(tmem + (static_cast<uint32_t>(32 * warp) << 16) + c, v);
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (a.splits > 1) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) sums[(c + j) * FEW_ROWS + tid] = v[j];
-        } else if (n < a.N) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (c + j < a.T) finish(c + j, n, v[j]);
-        }
+        for (int j = 0; j < 16; ++j) sums[(c + j) * FEW_ROWS + tid] = v[j];
       }
     }
   }
-  if (a.splits > 1) {
-    cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
-    const int live = a.T * FEW_ROWS, i1 = live * (rank + 1) / a.splits;
-    for (int i = live * rank / a.splits + tid; i < i1; i += FEW_THREADS) {
-      float part[8];
+  cg::cluster_group cluster = cg::this_cluster();
+  if (a.splits > 1) cluster.sync(); else __syncthreads();
+  const int n = n0 + 4 * lane, live = min(4, a.N - n);
+  float bias[4] = {}, sw[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) part[k] = k < a.splits ? *cluster.map_shared_rank(sums + i, k) : 0.f;
-      float z = part[0];
-#pragma unroll
-      for (int k = 1; k < 8; ++k) z += part[k];
-      const int t = i / FEW_ROWS, n = n0 + i % FEW_ROWS;
-      if (n < a.N) finish(t, n, z);
-    }
-    cluster.sync();  // the others have read this CTA's sums
+  for (int j = 0; j < 4; ++j) {
+    if (j < live && a.bias) bias[j] = a.bias[n + j];
+    if (j < live && a.sw) sw[j] = a.sw[n + j];
   }
+  const bool vec = a.vec && live == 4;
+  for (int tt = tokens * rank / a.splits + warp; tt < tokens * (rank + 1) / a.splits; tt += FEW_THREADS / 32) {
+    const long long t = t0 + tt;
+    float z[4], r[4] = {};
+    if (a.r) {
+      if (vec) {
+        Four<O>::load(a.r, t * a.rs + n, r);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < live) r[j] = static_cast<float>(static_cast<const O*>(a.r)[t * a.rs + n + j]);
+      }
+    }
+    const int at = tt * FEW_ROWS + 4 * lane;
+    if (a.splits == 1) {
+      Four<float>::load(sums, at, z);
+    } else {
+      float4 part[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < a.splits) part[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums + at, k));
+      z[0] = part[0].x, z[1] = part[0].y, z[2] = part[0].z, z[3] = part[0].w;
+#pragma unroll
+      for (int k = 1; k < 8; ++k)
+        if (k < a.splits) z[0] += part[k].x, z[1] += part[k].y, z[2] += part[k].z, z[3] += part[k].w;
+    }
+    const float sx = a.sx ? a.sx[t] : 1.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = (a.sx ? z[j] * sx * sw[j] : z[j]) + bias[j];
+    if (a.p) {
+      if (vec) {
+        Four<__nv_bfloat16>::store(a.p, t * a.ps + n, z);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < live) static_cast<__nv_bfloat16*>(a.p)[t * a.ps + n + j] = __float2bfloat16_rn(z[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = activate(z[j], a.act) + r[j];
+    if (vec) {
+      Four<O>::store(a.y, t * a.ys + n, z);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < live) static_cast<O*>(a.y)[t * a.ys + n + j] = static_cast<O>(z[j]);
+    }
+  }
+  if (a.splits > 1) cluster.sync();  // the others have read this CTA's sums
   if (bad) atomicOr(a.err, bad << 24);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -167,7 +225,7 @@ static cudaError_t launch_few(const Few& f, int sms, cudaStream_t stream) {
   cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), FEW_SMEM<TN>, raised);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((f.N + FEW_ROWS - 1) / FEW_ROWS * f.splits));
+  cfg.gridDim = dim3(static_cast<unsigned>(f.tiles_n * ((f.T + TN - 1) / TN) * f.splits));
   cfg.blockDim = dim3(FEW_THREADS);
   cfg.dynamicSmemBytes = FEW_SMEM<TN>;
   cfg.stream = stream;
@@ -192,16 +250,26 @@ static cudaError_t by_tokens(const Few& f, int tn, int sms, cudaStream_t stream)
   }
 }
 
+bool use_few(long long T, int N, int sms) {
+  const long long tiles = (T + 127) / 128 * ((N + 127) / 128);
+  return T <= 128 || tiles < sms;
+}
+
 cudaError_t forward_few(const Forward& a, const void* x, long long xs, const void* w, long long ws, unsigned int* err, int sms,
                         cudaStream_t stream) {
-  const int es = a.e4m3 ? 1 : 2, tn = a.T <= 16 ? 16 : a.T <= 32 ? 32 : a.T <= 64 ? 64 : 128;
+  const int es = a.e4m3 ? 1 : 2, os = a.out_f32 ? 4 : 2, tn = a.T <= 16 ? 16 : a.T <= 32 ? 32 : a.T <= 64 ? 64 : 128;
   Few f{};
   f.y = a.y, f.r = a.r, f.p = a.p, f.ys = a.ys, f.rs = a.rs, f.ps = a.ps;
   f.bias = a.bias, f.sx = a.x_scale, f.sw = a.w_scale;
   f.T = static_cast<int>(a.T), f.N = a.N, f.act = a.act, f.err = err;
+  auto fours = [&](const void* p, long long stride, int size) {
+    return !p || (reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && (a.T == 1 || stride % 4 == 0));
+  };
+  f.vec = fours(a.y, a.ys, os) && fours(a.r, a.rs, os) && fours(a.p, a.ps, 2);
   f.kblocks = static_cast<int>((static_cast<long long>(a.K) * es + 127) / 128);
-  // the K axis over 1, 2, 4 or 8 CTAs while SMs are idle and each keeps two blocks
-  const long long tiles = (a.N + FEW_ROWS - 1) / FEW_ROWS;
+  f.tiles_n = (a.N + FEW_ROWS - 1) / FEW_ROWS;
+  // the K axis over 1, 2, 4 or 8 CTAs while two CTAs an SM are not reached and each keeps two blocks
+  const long long tiles = static_cast<long long>(f.tiles_n) * ((a.T + tn - 1) / tn);
   f.splits = 1;
   while (f.splits < 8 && tiles * f.splits * 2 <= 2ll * sms && f.kblocks >= 4 * f.splits) f.splits *= 2;
   if (!tma::encode_rows(&f.tw, w, es, a.N, a.K, ws, FEW_ROWS) || !tma::encode_rows(&f.tx, x, es, a.T, a.K, xs, tn))

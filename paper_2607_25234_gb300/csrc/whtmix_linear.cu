@@ -216,7 +216,7 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
     cw = copy_of(static_cast<char*>(ws) + f.w_off, a.w, a.N, a.K, a.ws, f.kp, es);
   }
   if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
-  if (a.T <= FEW_TOKENS) return forward_few(a, x, xs, w, wst, err, sms, stream);
+  if (use_few(a.T, a.N, sms)) return forward_few(a, x, xs, w, wst, err, sms, stream);
   Gemm g{};
   g.tiles_m = ceil_div(a.T, GEMM_BM);
   g.kblocks = ceil_div(a.K, 128 / es);

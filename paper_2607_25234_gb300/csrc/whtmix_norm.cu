@@ -67,12 +67,22 @@ template <> struct Io<__nv_bfloat16> {
   }
 };
 
-// Where element c of a row lies in shared memory (unaligned rows' gains and sums): the places of a vector apart, so that a warp's
-// lanes, whose vectors follow one another, touch consecutive words whatever the row's offset.
+// Unaligned rows' gains and sums in shared memory: the places of a vector slots_of() words apart, so that a warp's lanes, whose
+// vectors follow one another, touch consecutive words whatever the row's offset; a slot before and one after take the elements of a
+// cut vector that are not the row's.
 template <int V>
-__device__ __forceinline__ int column_at(int c, int D) { return c % V * ((D + V - 1) / V) + c / V; }
+__host__ __device__ constexpr int slots_of(int D) { return (D + V - 1) / V + 2; }
 template <int V>
-__host__ __device__ constexpr int columns_of(int D) { return (D + V - 1) / V * V; }
+__device__ __forceinline__ int column_at(int c, int D) { return c % V * slots_of<V>(D) + c / V + 1; }
+// Where elements 0 .. V - 1 of the vector that starts at -off lie; V elements on each is the next word.
+template <int V>
+struct Places {
+  int at[V];
+  __device__ __forceinline__ Places(int off, int D) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) at[j] = ((j - off) & (V - 1)) * slots_of<V>(D) + (j < off ? 0 : 1);
+  }
+};
 
 // The addresses of a matrix, first to one past its last.
 struct Bounds {
@@ -139,8 +149,8 @@ struct Row {
         if (e + j >= 0 && e + j < D) Io<T>::put(p, e + j, f[j]);
     }
   }
-  // AL: w itself; otherwise its copy in shared memory (gains_to_shared)
-  static __device__ __forceinline__ void gains(const float* w, int lane, int k, int off, int D, float (&f)[V]) {
+  // AL: from w; otherwise from its copy in shared memory (gains_to_shared)
+  static __device__ __forceinline__ void gains(const float* w, const Places<V>& at_, int lane, int k, int off, int D, float (&f)[V]) {
     const int e = at(lane, k) - off;
     if constexpr (AL) {
 #pragma unroll
@@ -150,7 +160,7 @@ struct Row {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = e + j >= 0 && e + j < D ? w[column_at<V>(e + j, D)] : 0.f;
+      for (int j = 0; j < V; ++j) f[j] = e < D ? w[at_.at[j] + lane + TPR * k] : 0.f;
     }
   }
   static __device__ __forceinline__ void store_e4m3(uint8_t* p, int lane, int k, int off, bool same, int D, const float (&f)[V]) {
@@ -174,6 +184,8 @@ struct Row {
 };
 template <int V, int BLOCK>
 __device__ __forceinline__ void gains_to_shared(float* s, const float* w, int D) {
+  for (int i = threadIdx.x; i < V * slots_of<V>(D); i += BLOCK) s[i] = 0.f;
+  __syncthreads();
   for (int i = threadIdx.x; i < D; i += BLOCK) s[column_at<V>(i, D)] = __ldg(w + i);
 }
 // Which matrices of an unaligned call lie like the first one (x; h in the backward).
@@ -221,15 +233,15 @@ struct Kept {
   __device__ __forceinline__ void fill(const float* g, int lane, int D) {
     if constexpr (KEEP) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) R::gains(g, lane, k, 0, D, w[k]);
+      for (int k = 0; k < NV; ++k) R::gains(g, Places<R::V>(0, D), lane, k, 0, D, w[k]);
     }
   }
-  __device__ __forceinline__ void get(const float* g, int lane, int k, int off, int D, float (&f)[R::V]) const {
+  __device__ __forceinline__ void get(const float* g, const Places<R::V>& at, int lane, int k, int off, int D, float (&f)[R::V]) const {
     if constexpr (KEEP) {
 #pragma unroll
       for (int j = 0; j < R::V; ++j) f[j] = w[k][j];
     } else {
-      R::gains(g, lane, k, off, D, f);
+      R::gains(g, at, lane, k, off, D, f);
     }
   }
 };
@@ -265,6 +277,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a, const Sa
     const int D = t < a.T ? a.D : 0;
     const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
     const int off = R::offset(x);
+    const Places<V> places(off, a.D);
     float h[NV][V];
     float sq = 0.f, top = 0.f;
 #pragma unroll
@@ -282,7 +295,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a, const Sa
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
-      kept.get(gains, lane, k, off, a.D, w);
+      kept.get(gains, places, lane, k, off, a.D, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         sq += h[k][j] * h[k][j];
@@ -349,11 +362,12 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
   float acc[AL ? NV : 1][V] = {};
-  float* mine = s_acc + (AL ? 0 : group * columns_of<V>(a.D));
+  const int set = V * slots_of<V>(a.D);
+  float* mine = s_acc + (AL ? 0 : group * set);
   if constexpr (!AL) {
-    for (int i = lane; i < columns_of<V>(a.D); i += TPR) mine[i] = 0.f;
+    for (int i = lane; i < set; i += TPR) mine[i] = 0.f;
   }
-  float* s_w = s_acc + ROWS * columns_of<V>(a.D);
+  float* s_w = s_acc + ROWS * set;
   pdl_wait();
   if constexpr (!AL) {
     gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
@@ -379,6 +393,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
     float sq = 0.f, ah = 0.f;
     const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
     const int off = R::offset(hp);
+    const Places<V> places(off, a.D);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       R::values(hp, bh, lane, k, off, true, D, uh[k], h[k]);
@@ -391,7 +406,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
-      kept.get(gains, lane, k, off, a.D, w);
+      kept.get(gains, places, lane, k, off, a.D, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         sq += h[k][j] * h[k][j];
@@ -405,7 +420,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V], o[V] = {};
-      kept.get(gains, lane, k, off, a.D, w);
+      kept.get(gains, places, lane, k, off, a.D, w);
       if (a.dh) R::values(gp, bg, lane, k, off, same.b, D, ug[k], o);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -413,8 +428,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
         if constexpr (AL) {
           acc[k][j] += g;
         } else {
-          const int e = R::at(lane, k) - off + j;
-          if (e >= 0 && e < D) mine[column_at<V>(e, a.D)] += g;
+          if (R::at(lane, k) - off < D) mine[places.at[j] + lane + TPR * k] += g;
         }
         o[j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
       }
@@ -429,7 +443,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
       const float* s = s_acc + column_at<V>(e, a.D);
       float sum = s[0];
 #pragma unroll 4
-      for (int g = 1; g < ROWS; ++g) sum += s[g * columns_of<V>(a.D)];
+      for (int g = 1; g < ROWS; ++g) sum += s[g * set];
       part[e] = sum;
     }
   } else if constexpr (ROWS == 1) {
@@ -552,6 +566,20 @@ cudaError_t by_length(int n, bool few, F&& f) {
   if (n <= 1024) return WHTMIX_ROW(256, 4);
   if (n <= 1536) return WHTMIX_ROW(512, 3);
   return WHTMIX_ROW(512, 4);
+}
+// The backward's: more registers a vector (its sums and two inputs), so one a thread up to 512 vectors.
+template <class F>
+cudaError_t by_length_backward(int n, F&& f) {
+  if (n <= 8) return WHTMIX_ROW(8, 1);
+  if (n <= 16) return WHTMIX_ROW(16, 1);
+  if (n <= 32) return WHTMIX_ROW(32, 1);
+  if (n <= 64) return WHTMIX_ROW(32, 2);
+  if (n <= 128) return WHTMIX_ROW(128, 1);
+  if (n <= 256) return WHTMIX_ROW(256, 1);
+  if (n <= 512) return WHTMIX_ROW(512, 1);
+  if (n <= 1024) return WHTMIX_ROW(512, 2);
+  if (n <= 1536) return WHTMIX_ROW(512, 3);
+  return WHTMIX_ROW(512, 4);
 #undef WHTMIX_ROW
 }
 
@@ -620,7 +648,7 @@ cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
     const void* k = al ? reinterpret_cast<const void*>(k_rms<T, Q8, true, TPR, NV>)
                        : reinterpret_cast<const void*>(k_rms<T, Q8, false, TPR, NV>);
     void* args[] = {&c, &same};
-    const size_t smem = al ? 0 : static_cast<size_t>(columns_of<V>(a.D)) * 4;  // at most 64 KB
+    const size_t smem = al ? 0 : static_cast<size_t>(V) * slots_of<V>(a.D) * 4;  // at most 64 KB
     int resident = 0;
     const cudaError_t e = resident_ctas(k, BLOCK, smem, sms, &resident);
     if (e != cudaSuccess) return e;
@@ -652,10 +680,10 @@ struct BackwardPlan {
 };
 template <typename T>
 cudaError_t backward_plan(const Backward& a, int n, bool al, int sms, BackwardPlan* p) {
-  return by_length(n, a.T < sms, [&](auto tpr, auto nv) {
+  return by_length_backward(n, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
     p->kernel = al ? reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>) : reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
-    p->smem = al ? 0 : static_cast<size_t>(BLOCK / TPR + 1) * columns_of<Io<T>::V>(a.D) * 4;  // at most 128 KB
+    p->smem = al ? 0 : static_cast<size_t>(BLOCK / TPR + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 129 KB
     p->block = BLOCK;
     int resident = 0;
     const cudaError_t e = resident_ctas(p->kernel, BLOCK, p->smem, sms, &resident);
