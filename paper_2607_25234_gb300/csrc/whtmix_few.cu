@@ -11,6 +11,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "whtmix_few.cuh"
 #include "whtmix_gemm.cuh"
 
@@ -162,9 +164,10 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
     if (j < live && a.sw) sw[j] = a.sw[n + j];
   }
   const bool vec = a.vec && live == 4;
-  for (int tt = tokens * rank / a.splits + warp; tt < tokens * (rank + 1) / a.splits; tt += FEW_THREADS / 32) {
+  const int tt0 = tokens * rank / a.splits, tt1 = tokens * (rank + 1) / a.splits;
+  auto finish = [&](int tt, float4 sum) {
     const long long t = t0 + tt;
-    float z[4], r[4] = {};
+    float z[4] = {sum.x, sum.y, sum.z, sum.w}, r[4] = {};
     if (a.r) {
       if (vec) {
         Four<O>::load(a.r, t * a.rs + n, r);
@@ -173,19 +176,6 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
         for (int j = 0; j < 4; ++j)
           if (j < live) r[j] = static_cast<float>(static_cast<const O*>(a.r)[t * a.rs + n + j]);
       }
-    }
-    const int at = tt * FEW_ROWS + 4 * lane;
-    if (a.splits == 1) {
-      Four<float>::load(sums, at, z);
-    } else {
-      float4 part[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < a.splits) part[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums + at, k));
-      z[0] = part[0].x, z[1] = part[0].y, z[2] = part[0].z, z[3] = part[0].w;
-#pragma unroll
-      for (int k = 1; k < 8; ++k)
-        if (k < a.splits) z[0] += part[k].x, z[1] += part[k].y, z[2] += part[k].z, z[3] += part[k].w;
     }
     const float sx = a.sx ? a.sx[t] : 1.f;
 #pragma unroll
@@ -200,7 +190,10 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
       }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] = activate(z[j], a.act) + r[j];
+    for (int j = 0; j < 4; j += 2) {
+      activate(z[j], z[j + 1], a.act);
+      z[j] += r[j], z[j + 1] += r[j + 1];
+    }
     if (vec) {
       Four<O>::store(a.y, t * a.ys + n, z);
     } else {
@@ -208,6 +201,39 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
       for (int j = 0; j < 4; ++j)
         if (j < live) static_cast<O*>(a.y)[t * a.ys + n + j] = static_cast<O>(z[j]);
     }
+  };
+  // 16 loads of the cluster's sums in flight: 16 / splits tokens at a time
+  auto add_up = [&](auto splits) {
+    constexpr int SPLITS = decltype(splits)::value, U = 16 / SPLITS < 4 ? 16 / SPLITS : 4;
+    const float* from[SPLITS];
+#pragma unroll
+    for (int k = 0; k < SPLITS; ++k) from[k] = SPLITS == 1 ? sums : cluster.map_shared_rank(sums, k);
+    for (int base = tt0 + warp; base < tt1; base += U * (FEW_THREADS / 32)) {
+      float4 part[U][SPLITS];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < SPLITS; ++k) {
+          const int tt = base + u * (FEW_THREADS / 32);
+          if (tt < tt1) part[u][k] = *reinterpret_cast<const float4*>(from[k] + tt * FEW_ROWS + 4 * lane);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int tt = base + u * (FEW_THREADS / 32);
+        if (tt < tt1) {
+          float4 z = part[u][0];
+#pragma unroll
+          for (int k = 1; k < SPLITS; ++k) z.x += part[u][k].x, z.y += part[u][k].y, z.z += part[u][k].z, z.w += part[u][k].w;
+          finish(tt, z);
+        }
+      }
+    }
+  };
+  switch (a.splits) {
+    case 1: add_up(std::integral_constant<int, 1>()); break;
+    case 2: add_up(std::integral_constant<int, 2>()); break;
+    case 4: add_up(std::integral_constant<int, 4>()); break;
+    default: add_up(std::integral_constant<int, 8>()); break;
   }
   if (a.splits > 1) cluster.sync();  // the others have read this CTA's sums
   if (bad) atomicOr(a.err, bad << 24);
@@ -250,10 +276,7 @@ static cudaError_t by_tokens(const Few& f, int tn, int sms, cudaStream_t stream)
   }
 }
 
-bool use_few(long long T, int N, int sms) {
-  const long long tiles = (T + 127) / 128 * ((N + 127) / 128);
-  return T <= 128 || tiles < sms;
-}
+bool use_few(long long T, int kblocks) { return T <= 64 || (T <= 128 && kblocks >= 8) || (T <= 256 && kblocks >= 32); }
 
 cudaError_t forward_few(const Forward& a, const void* x, long long xs, const void* w, long long ws, unsigned int* err, int sms,
                         cudaStream_t stream) {

@@ -12,8 +12,8 @@
 // contraction down the rows): the panels are multiplied as they lie.  What lies past an edge reads as zero and is not stored, so
 // that every size runs; rows that are not 16-byte aligned are stored (and the residual read) with plain accesses, through the
 // same shared-memory panel.
-// Splits: item s of a split tile takes its share of the K blocks and stores fp32 partial rows [s * split_rows + m]; the caller
-// adds them up in a fixed order.
+// Splits: item s of a split tile takes its share of the K blocks and stores fp32 partial rows [s * split_rows + m] (added to a
+// residual that lies the same way); the caller adds them up in a fixed order.
 #pragma once
 
 #include <cuda.h>
@@ -80,20 +80,64 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uin
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// 1 / (1 + 2^t): two operations of the special-function unit; 0 where 2^t overflows, NaN for NaN
-__device__ __forceinline__ float logistic2(float t) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+// Two values at once (packed float32 arithmetic: half the instructions).
+struct Pair {
+  uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float a, float b) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
   return r;
 }
-constexpr float LOG2E = 1.4426950408889634f;
-__device__ __forceinline__ float activate(float z, int act) {
-  switch (act) {
-    case ACT_RELU: return z < 0.f ? 0.f : z;
-    case ACT_GELU: return z * logistic2(z * (-GELU_2A * LOG2E - GELU_2A * LOG2E * GELU_B * (z * z)));
-    case ACT_SILU: return z * logistic2(z * -LOG2E);
-    default: return z;
+__device__ __forceinline__ void unpair(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
+// 1 / (1 + 2^t) for both of t.  The special-function unit takes 16 operations a clock, an exponential and a reciprocal for each
+// value bound the short products' epilogues; here one reciprocal serves two: 1 / (d0 d1) times the other.  t is cut at 60, so that
+// the product stays finite and a NaN becomes a number that leaves the other value alone (the caller multiplies by its own z, which
+// is NaN then too).
+__device__ __forceinline__ Pair logistic2(Pair t) {
+  float t0, t1, e0, e1, d0, d1, r;
+  unpair(t, t0, t1);
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(t0, 60.f)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(t1, 60.f)));
+  unpair(pair(e0, e1) + pair(1.f, 1.f), d0, d1);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
+  return pair(r, r) * pair(d1, d0);
+}
+// max(z, lo), NaN for NaN: below lo the products with logistic2 (at least 2^-60) stay next to nothing, infinities too
+__device__ __forceinline__ float above(float z, float lo) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(lo));
+  return r;
+}
+constexpr float LOG2E = 1.4426950408889634f, GATE_LOW = -64.f;
+// the exponent of two in gelu's and silu's z / (1 + 2^t)
+__device__ __forceinline__ Pair gate_exponent(Pair z, int act) {
+  constexpr float A = -GELU_2A * LOG2E, B = A * GELU_B;
+  if (act == ACT_GELU) return z * fma(z * z, pair(B, B), pair(A, A));
+  return z * pair(-LOG2E, -LOG2E);
+}
+__device__ __forceinline__ void activate(float& z0, float& z1, int act) {
+  if (act == ACT_RELU) {
+    z0 = z0 < 0.f ? 0.f : z0, z1 = z1 < 0.f ? 0.f : z1;
+  } else if (act != ACT_NONE) {
+    const Pair z = pair(above(z0, GATE_LOW), above(z1, GATE_LOW));
+    unpair(z * logistic2(gate_exponent(z, act)), z0, z1);
   }
 }
 
@@ -311,6 +355,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       int m0, n0, split;
       place(item, m0, n0, split);
       const int d = i & 1, yrow = split * a.split_rows + m0;
+      const bool none = first_block(split) == first_block(split + 1);  // no K block: a sum of nothing
       const int panels = min(PANELS, (a.N - n0 + PW - 1) / PW);
       const float sm = a.sm && m0 + row < a.M ? a.sm[m0 + row] : 1.f;
       bool waited = false;
@@ -332,7 +377,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
             panel_plain<O, false>(st, const_cast<void*>(a.r), a.rs, m0, a.M, col0, a.N, gt);
           } else if (gt == 0) {
             tma::expect_tx(&bars.rfull[g], PANEL_BYTES);
-            tma::load_2d(st_u, &a.tr, col0, m0, &bars.rfull[g]);
+            tma::load_2d(st_u, &a.tr, col0, yrow, &bars.rfull[g]);
           }
         };
         if (a.has_r && !a.has_p) {
@@ -349,18 +394,28 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
 #pragma unroll
         for (int c = 0; c < PW; c += 32) tmem_ld32(tmem + lanes + d * BN + p * PW + c, v + c);
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (none) {
+#pragma unroll
+          for (int c = 0; c < PW; ++c) v[c] = 0.f;
+        }
         if (p + 2 >= panels) {  // the accumulator has been read
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) tma::arrive(&bars.dempty[d]);
         }
         const float *sb = &s_bias[g][p / 2 * PW], *ss = &s_scale[g][p / 2 * PW];
-        if (a.sm) {
+        if (a.sm || a.bias) {
+          const float f = a.sm ? sm : 1.f;
 #pragma unroll
-          for (int c = 0; c < PW; ++c) v[c] = v[c] * sm * ss[c] + sb[c];
-        } else if (a.bias) {
-#pragma unroll
-          for (int c = 0; c < PW; ++c) v[c] += sb[c];
+          for (int c = 0; c < PW; c += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(sb + c);
+            if (a.sm) {
+              const float4 s = *reinterpret_cast<const float4*>(ss + c);
+              v[c] *= f * s.x, v[c + 1] *= f * s.y, v[c + 2] *= f * s.z, v[c + 3] *= f * s.w;
+            }
+            unpair(pair(v[c], v[c + 1]) + pair(b.x, b.y), v[c], v[c + 1]);
+            unpair(pair(v[c + 2], v[c + 3]) + pair(b.z, b.w), v[c + 2], v[c + 3]);
+          }
         }
         if constexpr (PW == 64) {
           if (a.has_p) {
@@ -382,7 +437,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
         switch (a.act) {
 #define WHTMIX_ACT(A)                                             \
   case A:                                                         \
-    _Pragma("unroll") for (int c = 0; c < PW; ++c) v[c] = activate(v[c], A); \
+    _Pragma("unroll") for (int c = 0; c < PW; c += 2) activate(v[c], v[c + 1], A); \
     break
           WHTMIX_ACT(ACT_RELU);
           WHTMIX_ACT(ACT_GELU);

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "whtmix_few.cuh"
 #include "whtmix_gemm.cuh"
 #include "whtmix_linear.cuh"
@@ -25,20 +27,36 @@ struct Copy {
   long long rows, stride, cols, pitch;  // stride, cols, pitch in bytes
   long long chunks() const { return rows * (pitch / 16); }
 };
+template <typename I>  // 32-bit places where they suffice
 __global__ void __launch_bounds__(THREADS_256) k_pitch(const Copy a, const Copy b, long long na, long long n) {
+  constexpr int U = 4;
   pdl_wait();
-  const long long step = static_cast<long long>(gridDim.x) * THREADS_256;
-#pragma unroll 2
-  for (long long i = static_cast<long long>(blockIdx.x) * THREADS_256 + threadIdx.x; i < n; i += step) {
-    const bool first = i < na;
-    const long long j = first ? i : i - na;
-    const long long pitch = first ? a.pitch : b.pitch, stride = first ? a.stride : b.stride, cols = first ? a.cols : b.cols;
-    const uint8_t* src = first ? a.src : b.src;
-    const uint32_t per_row = static_cast<uint32_t>(pitch / 16);
-    const long long r = j / per_row, c = (j - r * per_row) * 16, rows = first ? a.rows : b.rows;
-    const Span span{src, src + (rows - 1) * stride + cols};
-    const uint4 u = load16(src + r * stride + c, span);
-    *reinterpret_cast<uint4*>((first ? a.dst : b.dst) + r * pitch + c) = keep(u, static_cast<int>(cols - c < 16 ? cols - c : 16));
+  const I step = static_cast<I>(gridDim.x) * THREADS_256;
+  for (I i0 = static_cast<I>(blockIdx.x) * THREADS_256 + threadIdx.x; i0 < static_cast<I>(n); i0 += U * step) {
+    Granules g[U];
+    const uint8_t* p[U];
+    uint8_t* q[U];
+    int left[U];
+    Span span[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const I i = i0 + u * step;
+      left[u] = -1;
+      if (i < static_cast<I>(n)) {
+        const bool first = i < static_cast<I>(na);
+        const Copy& m = first ? a : b;
+        const I j = first ? i : i - static_cast<I>(na), per_row = static_cast<I>(m.pitch >> 4), r = j / per_row;
+        const long long c = static_cast<long long>(j - r * per_row) * 16;
+        p[u] = m.src + static_cast<long long>(r) * m.stride + c;
+        q[u] = m.dst + static_cast<long long>(r) * m.pitch + c;
+        left[u] = static_cast<int>(m.cols - c < 16 ? m.cols - c : 16);
+        span[u] = Span{m.src, m.src + (m.rows - 1) * m.stride + m.cols};
+        g[u] = fetch16(p[u], span[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (left[u] >= 0) *reinterpret_cast<uint4*>(q[u]) = keep(finish16(g[u], p[u], span[u]), left[u]);
   }
   pdl_trigger();
 }
@@ -50,25 +68,29 @@ static Copy copy_of(void* dst, const void* src, long long rows, int cols, long l
 static cudaError_t to_pitch(const Copy& a, const Copy& b, int sms, cudaStream_t stream) {
   long long na = a.dst ? a.chunks() : 0, n = na + (b.dst ? b.chunks() : 0);
   if (n == 0) return cudaSuccess;
-  const long long need = (n + THREADS_256 - 1) / THREADS_256, most = 8ll * sms;
+  const long long need = (n + 4 * THREADS_256 - 1) / (4 * THREADS_256), most = 4ll * sms;
   Copy ca = a, cb = b;
   void* args[] = {&ca, &cb, &na, &n};
-  return launch_pdl(reinterpret_cast<const void*>(k_pitch), static_cast<unsigned>(need < most ? need : most), THREADS_256, 0, stream, args);
+  return launch_pdl(n < (1ll << 30) ? reinterpret_cast<const void*>(k_pitch<uint32_t>) : reinterpret_cast<const void*>(k_pitch<unsigned long long>), static_cast<unsigned>(need < most ? need : most), THREADS_256, 0, stream, args);
 }
 
 // ---- dp and db ----
-__device__ __forceinline__ float slope(float z, int act) {
-  if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  const float u2 = act == ACT_GELU ? GELU_2A * (z + GELU_B * z * z * z) : z;
-  const float du2 = act == ACT_GELU ? GELU_2A * (1.f + 3.f * GELU_B * z * z) : 1.f;
-  const float s = logistic2(-LOG2E * u2);
-  return s * (1.f + z * (1.f - s) * du2);
+// d0 *= act'(z0), d1 *= act'(z1).  gelu and silu: s (1 + z (1 - s) u'), s = 1 / (1 + e^-u)
+__device__ __forceinline__ void times_slope(float& d0, float& d1, float z0, float z1, int act) {
+  if (act == ACT_RELU) {
+    d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
+    return;
+  }
+  const Pair z = pair(z0, z1), s = logistic2(gate_exponent(pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), act));
+  Pair g = z * fma(s, pair(-1.f, -1.f), pair(1.f, 1.f));
+  if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
+  unpair(pair(d0, d1) * (s * (g + pair(1.f, 1.f))), d0, d1);
 }
 
 // dp[t, n] = bf16(dy act'(p)); part[chunk][n] = the chunk's rows' float32 sum of dy act'(p), before the rounding.  A CTA takes 256
 // columns (a thread 8) and the rows of chunk blockIdx.y, 8 at a time.  dp, part: or null.
 template <bool AL>
-__global__ void __launch_bounds__(THREADS_256) k_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
+__global__ void __launch_bounds__(THREADS_256, AL ? 4 : 3) k_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
   __shared__ float s[8][32][9];
   const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c0 = blockIdx.x * 256 + 8 * lane;
   const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
@@ -76,37 +98,61 @@ __global__ void __launch_bounds__(THREADS_256) k_dp(const Backward a, __nv_bfloa
   pdl_wait();
   const uint16_t *dy = static_cast<const uint16_t*>(a.dy), *p = static_cast<const uint16_t*>(a.p);
   const Span sd = span_of(a.dy, a.T, a.dys, a.N, 2), sp = span_of(a.p, a.T, a.ps, a.N, 2);
-  auto load = [&](const uint16_t* row, const Span& s, float (&f)[8]) {
-    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+  using Raw = typename std::conditional<AL, uint4, Granules>::type;
+  auto fetch = [&](const uint16_t* row, const Span& s) {
+    Raw u = Raw{};
     if (c0 < a.N) {
       if constexpr (AL)
         u = *reinterpret_cast<const uint4*>(row + c0);
       else
-        u = keep(load16(reinterpret_cast<const uint8_t*>(row + c0), s), min(16, 2 * (a.N - c0)));
+        u = fetch16(reinterpret_cast<const uint8_t*>(row + c0), s);
     }
+    return u;
+  };
+  auto values = [&](const Raw& raw, const uint16_t* row, const Span& s, float (&f)[8]) {
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (AL)
+      u = raw;
+    else if (c0 < a.N)
+      u = keep(finish16(raw, reinterpret_cast<const uint8_t*>(row + c0), s), min(16, 2 * (a.N - c0)));
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
   };
-#pragma unroll 2
-  for (long long t = t0 + g; t < t1; t += 8) {
-    float d[8], z[8];
-    load(dy + t * a.dys, sd, d);
-    if (a.act != ACT_NONE) {
-      load(p + t * a.ps, sp, z);
+  constexpr int U = 2;  // rows in flight
+  for (long long first = t0 + g; first < t1; first += 8 * U) {
+    Raw ud[U], uz[U];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) d[j] *= slope(z[j], a.act);
+    for (int r = 0; r < U; ++r) {
+      const long long t = first + 8 * r;
+      if (t < t1) {
+        ud[r] = fetch(dy + t * a.dys, sd);
+        if (a.act != ACT_NONE) uz[r] = fetch(p + t * a.ps, sp);
+      }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += d[j];
-    if (dp) {  // (its pitch holds whole vectors)
-      uint32_t h[4];
+    for (int r = 0; r < U; ++r) {
+      const long long t = first + 8 * r;
+      if (t >= t1) break;
+      float d[8];
+      values(ud[r], dy + t * a.dys, sd, d);
+      if (a.act != ACT_NONE) {
+        float z[8];
+        values(uz[r], p + t * a.ps, sp, z);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        __nv_bfloat162 b = __floats2bfloat162_rn(d[2 * j], d[2 * j + 1]);
-        h[j] = *reinterpret_cast<uint32_t*>(&b);
+        for (int j = 0; j < 8; j += 2) times_slope(d[j], d[j + 1], z[j], z[j + 1], a.act);
       }
-      if (c0 < a.N) *reinterpret_cast<uint4*>(dp + t * dps + c0) = make_uint4(h[0], h[1], h[2], h[3]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += d[j];
+      if (dp) {  // (its pitch holds whole vectors)
+        uint32_t h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          __nv_bfloat162 b = __floats2bfloat162_rn(d[2 * j], d[2 * j + 1]);
+          h[j] = *reinterpret_cast<uint32_t*>(&b);
+        }
+        if (c0 < a.N) *reinterpret_cast<uint4*>(dp + t * dps + c0) = make_uint4(h[0], h[1], h[2], h[3]);
+      }
     }
   }
   if (part) {
@@ -154,9 +200,10 @@ static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
 static int pitch_of(int cols, int es) { return (cols + 16 / es - 1) / (16 / es) * (16 / es); }
 static int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
 
-// Tile width and splits of a product of tiles_m rows of tiles, N columns and kblocks K blocks.  A tile's block takes the larger of
-// its products (2 BN clocks) and its operands' way out of shared memory ((128 + BN) clocks at 128 bytes a clock); a tile costs
-// about TILE_CLOCKS besides, and a split product's partial tiles their way through memory.
+// Tile width and splits of a product of tiles_m rows of tiles, N columns and kblocks K blocks.  A block of 128 x BN costs BLOCK
+// clocks of one SM, not in proportion to BN: the operands' way from L2 and out of shared memory bounds the narrow tiles (measured
+// at [8192, 4096] x [4096, 4096]: 545 clocks at 256, 450 at 128).  A tile costs about TILE_CLOCKS besides, a split product's partial
+// tiles their way through memory.
 struct Plan {
   int bn, splits;
 };
@@ -166,7 +213,7 @@ static Plan plan_product(long long tiles_m, int N, int kblocks, int sms, int max
   double best_cost = 1e300;
   for (int bn = 256; bn >= 64; bn >>= 1) {
     const long long tiles = tiles_m * ceil_div(N, bn);
-    const double block = 2 * bn > 128 + bn ? 2 * bn : 128 + bn;
+    const double block = bn == 256 ? 545.0 : bn == 128 ? 450.0 : 400.0;
     // one split, or as many as fill 1 .. 4 waves
     for (int w = 0; w <= 4; ++w) {
       const long long fill = w == 0 ? 1 : static_cast<long long>(w) * sms / tiles;
@@ -216,7 +263,7 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
     cw = copy_of(static_cast<char*>(ws) + f.w_off, a.w, a.N, a.K, a.ws, f.kp, es);
   }
   if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
-  if (use_few(a.T, a.N, sms)) return forward_few(a, x, xs, w, wst, err, sms, stream);
+  if (use_few(a.T, ceil_div(a.K, 128 / es))) return forward_few(a, x, xs, w, wst, err, sms, stream);
   Gemm g{};
   g.tiles_m = ceil_div(a.T, GEMM_BM);
   g.kblocks = ceil_div(a.K, 128 / es);
@@ -261,10 +308,11 @@ static BackwardPlan plan_backward(const Backward& a, int sms) {
   if (b.pad_x) b.x_off = take(static_cast<size_t>(a.T) * b.kp * 2);
   if (b.pad_w) b.w_off = take(static_cast<size_t>(a.N) * b.kp * 2);
   if (a.db || b.own_dp) {
-    const int strips = ceil_div(a.N, 256), rows = ceil_div(a.T, 16), most = (8 * sms + strips - 1) / strips;
+    const int strips = ceil_div(a.N, 256), rows = ceil_div(a.T, 16), most = (4 * sms + strips - 1) / strips;  // one wave
     b.chunks = rows < most ? rows : most;
     if (b.chunks > 65535) b.chunks = 65535;
-    if (a.db) b.db_off = take(static_cast<size_t>(b.chunks) * a.N * 4);
+    if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
+    if (a.db && b.chunks > 1) b.db_off = take(static_cast<size_t>(b.chunks) * a.N * 4);
   }
   if (a.dw) {
     const int tiles_m = ceil_div(a.N, GEMM_BM);
@@ -280,16 +328,16 @@ size_t backward_workspace(const Backward& a, int sms) { return plan_backward(a, 
 cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
   const BackwardPlan b = plan_backward(a, sms);
   char* base = static_cast<char*>(ws);
-  cudaError_t e;
-  const void* dp = a.dy;
-  long long dps = a.dys;
   const Copy cx = b.pad_x ? copy_of(base + b.x_off, a.x, a.T, a.K, a.xs, b.kp, 2) : Copy{};
   const Copy cw = b.pad_w ? copy_of(base + b.w_off, a.w, a.N, a.K, a.ws, b.kp, 2) : Copy{};
-  if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
+  cudaError_t e = to_pitch(cx, cw, sms, stream);
+  if (e != cudaSuccess) return e;
+  const void* dp = a.dy;
+  long long dps = a.dys;
   if (a.db || b.own_dp) {
     Backward c = a;
     __nv_bfloat16* d = b.own_dp ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
-    float* part = a.db ? reinterpret_cast<float*>(base + b.db_off) : nullptr;
+    float* part = !a.db ? nullptr : b.chunks > 1 ? reinterpret_cast<float*>(base + b.db_off) : a.db;
     long long np = b.np;
     int chunks = b.chunks;
     const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && (a.act == ACT_NONE || tma::mappable(a.p, a.T, a.ps, 2));
@@ -305,11 +353,9 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     e = cudaLaunchKernelEx(&cfg, al ? k_dp<true> : k_dp<false>, c, d, np, part, chunks);
     if (e != cudaSuccess) return e;
     if (b.own_dp) dp = d, dps = b.np;
-    if (a.db && (e = norm::add_rows(part, a.db, a.N, chunks, stream)) != cudaSuccess) return e;
+    if (a.db && chunks > 1 && (e = norm::add_rows(part, a.db, a.N, chunks, stream)) != cudaSuccess) return e;
   }
   if (a.dx) {
-    const void* w = b.pad_w ? base + b.w_off : a.w;
-    const long long wst = b.pad_w ? b.kp : a.ws;
     Gemm g{};
     g.tiles_m = ceil_div(a.T, GEMM_BM);
     g.kblocks = ceil_div(a.N, 64);
@@ -319,14 +365,13 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     g.M = static_cast<int>(a.T), g.N = a.K;
     g.y = a.dx, g.ys = a.dxs, g.y_plain = !tma::mappable(a.dx, a.T, a.dxs, 2);
     g.err = err;
-    if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, GEMM_BM) || !tma::encode_rows(&g.tb, w, 2, a.N, a.K, wst, 64) ||
+    if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, GEMM_BM) ||
+        !tma::encode_rows(&g.tb, b.pad_w ? base + b.w_off : a.w, 2, a.N, a.K, b.pad_w ? b.kp : a.ws, 64) ||
         (!g.y_plain && !tma::encode_rows(&g.ty, a.dx, 2, a.T, a.K, a.dxs, GEMM_BM)))
       return cudaErrorInvalidValue;
     if ((e = gemm_dx(g, pl.bn, sms, stream)) != cudaSuccess) return e;
   }
   if (a.dw) {
-    const void* x = b.pad_x ? base + b.x_off : a.x;
-    const long long xs = b.pad_x ? b.kp : a.xs;
     Gemm g{};
     g.tiles_m = ceil_div(a.N, GEMM_BM);
     g.kblocks = ceil_div(a.T, 64);
@@ -336,26 +381,27 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     g.M = a.N, g.N = a.K;
     g.err = err;
     const bool split = g.splits > 1;
-    const int kq = pitch_of(a.K, 4), os = split || a.dw_f32 ? 4 : 2;
+    const int os = split || a.dw_f32 ? 4 : 2;
     void* out = split ? static_cast<void*>(base + b.dw_off) : a.dw;
-    const long long rows = split ? static_cast<long long>(g.splits) * b.split_rows : a.N, pitch = split ? kq : a.K;
+    const long long rows = split ? static_cast<long long>(g.splits) * b.split_rows : a.N;
+    int pitch = split ? pitch_of(a.K, 4) : a.K;
     g.y = out, g.ys = pitch, g.y_plain = !tma::mappable(out, rows, pitch, os);
-    if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, 64) || !tma::encode_rows(&g.tb, x, 2, a.T, a.K, xs, 64) ||
+    if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, 64) ||
+        !tma::encode_rows(&g.tb, b.pad_x ? base + b.x_off : a.x, 2, a.T, a.K, b.pad_x ? b.kp : a.xs, 64) ||
         (!g.y_plain && !tma::encode_rows(&g.ty, out, os, rows, a.K, pitch, GEMM_BM)))
       return cudaErrorInvalidValue;
     if ((e = gemm_dw(g, os == 4, b.dw.bn, sms, stream)) != cudaSuccess) return e;
     if (split) {
       const float* part = static_cast<const float*>(out);
-      int rows_ = a.N, cols = a.K, pitch_ = kq, sr = b.split_rows, splits = g.splits;
+      int rows_ = a.N, cols = a.K, sr = b.split_rows, splits = g.splits;
       void* dw = a.dw;
-      void* args[] = {&dw, &part, &rows_, &cols, &pitch_, &sr, &splits};
+      void* args[] = {&dw, &part, &rows_, &cols, &pitch, &sr, &splits};
       const long long n = static_cast<long long>(a.N) * ceil_div(a.K, 4), need = (n + THREADS_256 - 1) / THREADS_256;
       e = launch_pdl(a.dw_f32 ? reinterpret_cast<const void*>(k_sum_splits<float>) : reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16>),
                      static_cast<unsigned>(need < 8ll * sms ? need : 8ll * sms), THREADS_256, 0, stream, args);
-      if (e != cudaSuccess) return e;
     }
   }
-  return cudaSuccess;
+  return e;
 }
 
 }  // namespace linear

@@ -354,7 +354,7 @@ def _rows(t: torch.Tensor, name: str, device: torch.device):
     if t.device != device or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor on {device} (WHTMix runs on CUDA tensors only)")
     shape = t.shape
-    if len(shape) < 1 or shape[-1] < 1:
+    if not shape or shape[-1] < 1:
         raise ValueError(f"{name} must have at least one channel, got shape {list(shape)}")
     C = shape[-1]
     rows = t.numel() // C
@@ -379,17 +379,29 @@ def _rows(t: torch.Tensor, name: str, device: torch.device):
 
 def _vector(t: torch.Tensor, n: int, name: str, device: torch.device) -> int:
     """The address of a contiguous float32 vector of n elements."""
-    if t.dtype != torch.float32 or t.numel() != n or t.dim() != 1:
+    if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n:
         raise ValueError(f"{name} must be float32 [{n}], got {t.dtype} {list(t.shape)}")
-    _on_device(t, device, name)
+    if t.device != device or not t.is_contiguous():
+        _on_device(t, device, name)
     return t.data_ptr()
 
 
-def _matrix(t: torch.Tensor, shape, dtype: torch.dtype, name: str, device: torch.device):
-    """(address, stride) of a row matrix of the given shape and dtype."""
+def _stride(t: torch.Tensor, shape, dtype: torch.dtype, name: str, device: torch.device) -> int:
+    """The row stride of a row matrix of the given shape and dtype."""
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    return t.data_ptr(), _rows(t, name, device)[2]
+    if t.is_contiguous() and t.device == device:
+        return shape[-1]
+    return _rows(t, name, device)[2]
+
+
+def _token_scale(t: torch.Tensor, shape, name: str, device: torch.device) -> int:
+    """The address of contiguous float32 scales, one a token."""
+    if t.dtype != torch.float32 or t.shape != shape:
+        raise ValueError(f"{name} must be float32 {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if t.device != device or not t.is_contiguous():
+        _on_device(t, device, name)
+    return t.data_ptr()
 
 
 def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
@@ -398,42 +410,48 @@ def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = N
     """h = x + residual; y = h w / sqrt(mean(h^2) + eps) over the last axis (x float32 or bfloat16, w float32).
 
     Returns y, or with out_dtype float8_e4m3fn (values, scales): y = values * scales[..., None], one float32 scale a
-    token; with a residual h is appended."""
+    token; with a residual h is appended.  8-bit values that are allocated here have rows at a 16-byte pitch (a view
+    of a wider tensor where the last axis is no multiple of 16)."""
     dtype = x.dtype
     if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError(f"rms_norm takes float32 or bfloat16, got {dtype}")
-    out_dtype = dtype if out_dtype is None else out_dtype
-    if out_dtype != dtype and out_dtype != E4M3:
+    eight = out_dtype == E4M3
+    if not eight and out_dtype is not None and out_dtype != dtype:
         raise TypeError(f"rms_norm of {dtype} writes {dtype} or {E4M3}, not {out_dtype}")
     device, shape = x.device, x.shape
     T, D, xs = _rows(x, "x", device)
     wp = _vector(w, D, "w", device)
     rp = rs = hp = hs = sp = 0
     if residual is not None:
-        rp, rs = _matrix(residual, shape, dtype, "residual", device)
+        rs = _stride(residual, shape, dtype, "residual", device)
+        rp = residual.data_ptr()
         if h is None:
-            h = torch.empty(shape, dtype=dtype, device=device)
-        hp, hs = _matrix(h, shape, dtype, "h", device)
+            h, hs = torch.empty(shape, dtype=dtype, device=device), D
+        else:
+            hs = _stride(h, shape, dtype, "h", device)
+        hp = h.data_ptr()
     elif h is not None:
         raise ValueError("h is the sum of x and the residual: it needs a residual")
-    if out is None:
-        out = torch.empty(shape, dtype=out_dtype, device=device)
-        ys = D
+    if out is not None:
+        ys = _stride(out, shape, E4M3 if eight else dtype, "out", device)
+    elif eight and D % 16:
+        # rows at a 16-byte pitch, as the tensor cores' loads want them: linear takes them as they lie
+        ys = (D + 15) // 16 * 16
+        out = torch.empty((*shape[:-1], ys), dtype=E4M3, device=device)[..., :D]
     else:
-        ys = _matrix(out, shape, out_dtype, "out", device)[1]
-    if out_dtype == E4M3:
+        out, ys = torch.empty(shape, dtype=E4M3 if eight else dtype, device=device), D
+    if eight:
         if scale is None:
             scale = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-        elif scale.dtype != torch.float32 or scale.shape != shape[:-1]:
-            raise ValueError(f"scale must be float32 {list(shape[:-1])}, got {scale.dtype} {list(scale.shape)}")
+            sp = scale.data_ptr()
         else:
-            _on_device(scale, device, "scale")
-        sp = scale.data_ptr()
+            sp = _token_scale(scale, shape[:-1], "scale", device)
     elif scale is not None:
         raise ValueError(f"scale belongs to an output of {E4M3}")
-    _call("whtmix_rms_norm", device, stream, library().whtmix_rms_norm, x.data_ptr(), rp, wp, hp, out.data_ptr(), sp,
-          T, D, xs, rs, hs, ys, eps, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
-    if out_dtype == E4M3:
+    code = LAYER_CODE[dtype]
+    _call("whtmix_rms_norm", device, stream, (_lib or library()).whtmix_rms_norm, x.data_ptr(), rp, wp, hp, out.data_ptr(),
+          sp, T, D, xs, rs, hs, ys, eps, code, 3 if eight else code)
+    if eight:
         return (out, scale) if residual is None else (out, scale, h)
     return out if residual is None else (out, h)
 
@@ -448,15 +466,17 @@ def rms_norm_backward(h: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, dh: to
     device, shape = h.device, h.shape
     T, D, hs = _rows(h, "h", device)
     wp = _vector(w, D, "w", device)
-    dyp, dys = _matrix(dy, shape, dtype, "dy", device)
-    dhp, dhs = (0, 0) if dh is None else _matrix(dh, shape, dtype, "dh", device)
+    dys = _stride(dy, shape, dtype, "dy", device)
+    dhs = 0 if dh is None else _stride(dh, shape, dtype, "dh", device)
     if dx is None:
-        dx = torch.empty(shape, dtype=dtype, device=device)
-    dxp, dxs = _matrix(dx, shape, dtype, "dx", device)
+        dx, dxs = torch.empty(shape, dtype=dtype, device=device), D
+    else:
+        dxs = _stride(dx, shape, dtype, "dx", device)
     if dw is None:
         dw = torch.empty(D, dtype=torch.float32, device=device)
-    _call("whtmix_rms_norm_backward", device, stream, library().whtmix_rms_norm_backward, h.data_ptr(), wp, dyp, dhp, dxp,
-          _vector(dw, D, "dw", device), T, D, hs, dys, dhs, dxs, eps, LAYER_CODE[dtype])
+    _call("whtmix_rms_norm_backward", device, stream, (_lib or library()).whtmix_rms_norm_backward, h.data_ptr(), wp,
+          dy.data_ptr(), 0 if dh is None else dh.data_ptr(), dx.data_ptr(), _vector(dw, D, "dw", device), T, D, hs, dys, dhs,
+          dxs, eps, LAYER_CODE[dtype])
     return dx, dw
 
 
@@ -480,39 +500,40 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
     if out_dtype != torch.bfloat16 and out_dtype != torch.float32:
         raise TypeError(f"linear writes bfloat16 or float32, not {out_dtype}")
     act = _activation(activation)
-    if w.dim() != 2 or w.dtype != dtype or w.shape[1] != x.shape[-1]:
+    N, K = w.shape if w.dim() == 2 else (0, 0)
+    if w.dtype != dtype or K != x.shape[-1]:
         raise ValueError(f"w must be {dtype} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
-    T, K, xs = _rows(x, "x", device)
-    N, _, ws = _rows(w, "w", device)
-    shape = x.shape[:-1] + (N,)
+    T, _, xs = _rows(x, "x", device)
+    ws = _rows(w, "w", device)[2]
+    lead = x.shape[:-1]
+    shape = lead + (N,)
     xsp = wsp = bp = rp = rs = pp = ps = 0
     if dtype == E4M3:
         if x_scale is None or w_scale is None:
             raise ValueError(f"{E4M3} needs x_scale and w_scale")
-        if x_scale.dtype != torch.float32 or x_scale.shape != x.shape[:-1]:
-            raise ValueError(f"x_scale must be float32 {list(x.shape[:-1])}, got {x_scale.dtype} {list(x_scale.shape)}")
-        _on_device(x_scale, device, "x_scale")
-        xsp, wsp = x_scale.data_ptr(), _vector(w_scale, N, "w_scale", device)
+        xsp, wsp = _token_scale(x_scale, lead, "x_scale", device), _vector(w_scale, N, "w_scale", device)
     elif x_scale is not None or w_scale is not None:
         raise ValueError(f"scales belong to {E4M3} operands")
     if bias is not None:
         bp = _vector(bias, N, "bias", device)
     if residual is not None:
-        rp, rs = _matrix(residual, shape, out_dtype, "residual", device)
+        rs = _stride(residual, shape, out_dtype, "residual", device)
+        rp = residual.data_ptr()
     save = preact is not None and preact is not False
     if save:
         if out_dtype != torch.bfloat16:
             raise ValueError("preact is bfloat16 and goes with a bfloat16 output")
         if preact is True:
-            preact = torch.empty(shape, dtype=torch.bfloat16, device=device)
-        pp, ps = _matrix(preact, shape, torch.bfloat16, "preact", device)
+            preact, ps = torch.empty(shape, dtype=torch.bfloat16, device=device), N
+        else:
+            ps = _stride(preact, shape, torch.bfloat16, "preact", device)
+        pp = preact.data_ptr()
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype, device=device)
-        ys = N
+        out, ys = torch.empty(shape, dtype=out_dtype, device=device), N
     else:
-        ys = _matrix(out, shape, out_dtype, "out", device)[1]
-    _call("whtmix_linear", device, stream, library().whtmix_linear, x.data_ptr(), w.data_ptr(), xsp, wsp, bp, rp, pp,
-          out.data_ptr(), T, N, K, xs, ws, rs, ps, ys, act, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
+        ys = _stride(out, shape, out_dtype, "out", device)
+    _call("whtmix_linear", device, stream, (_lib or library()).whtmix_linear, x.data_ptr(), w.data_ptr(), xsp, wsp, bp, rp,
+          pp, out.data_ptr(), T, N, K, xs, ws, rs, ps, ys, act, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
     return (out, preact) if save else out
 
 
@@ -529,29 +550,33 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch
     if dw_dtype != torch.bfloat16 and dw_dtype != torch.float32:
         raise TypeError(f"dw is bfloat16 or float32, not {dw_dtype}")
     act = _activation(activation)
-    if w.dim() != 2 or w.dtype != torch.bfloat16 or w.shape[1] != x.shape[-1]:
+    N, K = w.shape if w.dim() == 2 else (0, 0)
+    if w.dtype != torch.bfloat16 or K != x.shape[-1]:
         raise ValueError(f"w must be {torch.bfloat16} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
-    T, K, xs = _rows(x, "x", device)
-    N, _, ws = _rows(w, "w", device)
+    T, _, xs = _rows(x, "x", device)
+    ws = _rows(w, "w", device)[2]
     shape = x.shape[:-1] + (N,)
-    dyp, dys = _matrix(dy, shape, torch.bfloat16, "dy", device)
+    dys = _stride(dy, shape, torch.bfloat16, "dy", device)
     pp = ps = dxp = dxs = dwp = dbp = 0
     if act:
         if p is None:
             raise ValueError(f"the backward of {activation} needs the pre-activation p")
-        pp, ps = _matrix(p, shape, torch.bfloat16, "p", device)
-    if need_dx or dx is not None:
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=torch.bfloat16, device=device)
-        dxp, dxs = _matrix(dx, x.shape, torch.bfloat16, "dx", device)
-    if need_dw or dw is not None:
+        ps = _stride(p, shape, torch.bfloat16, "p", device)
+        pp = p.data_ptr()
+    if dx is not None:
+        dxs = _stride(dx, x.shape, torch.bfloat16, "dx", device)
+        dxp = dx.data_ptr()
+    elif need_dx:
+        dx, dxs = torch.empty(x.shape, dtype=torch.bfloat16, device=device), K
+        dxp = dx.data_ptr()
+    if dw is not None or need_dw:
         dw = _out(dw, (N, K), dw_dtype, device, "dw")
         dwp = dw.data_ptr()
-    if need_db or db is not None:
+    if db is not None or need_db:
         db = torch.empty(N, dtype=torch.float32, device=device) if db is None else db
         dbp = _vector(db, N, "db", device)
-    _call("whtmix_linear_backward", device, stream, library().whtmix_linear_backward, x.data_ptr(), w.data_ptr(), dyp, pp,
-          dxp, dwp, dbp, T, N, K, xs, ws, dys, ps, dxs, act, LAYER_CODE[dw_dtype])
+    _call("whtmix_linear_backward", device, stream, (_lib or library()).whtmix_linear_backward, x.data_ptr(), w.data_ptr(),
+          dy.data_ptr(), pp, dxp, dwp, dbp, T, N, K, xs, ws, dys, ps, dxs, act, LAYER_CODE[dw_dtype])
     return dx, dw, db
 
 
