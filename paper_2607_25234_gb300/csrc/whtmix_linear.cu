@@ -274,9 +274,9 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
   g.bias = a.bias, g.sm = a.x_scale, g.sn = a.w_scale;
   g.y = a.y, g.r = a.r, g.p = a.p, g.ys = a.ys, g.rs = a.rs, g.ps = a.ps;
   g.has_r = a.r != nullptr, g.has_p = a.p != nullptr;
-  g.y_plain = !tma::mappable(a.y, a.T, a.ys, os);
+  g.y_plain = !tma::storable(a.y, a.T, a.N, a.ys, os);
   g.r_plain = a.r && !tma::mappable(a.r, a.T, a.rs, os);
-  g.p_plain = a.p && !tma::mappable(a.p, a.T, a.ps, 2);
+  g.p_plain = a.p && !tma::storable(a.p, a.T, a.N, a.ps, 2);
   g.err = err;
   if (!tma::encode_rows(&g.ta, x, es, a.T, a.K, xs, GEMM_BM) || !tma::encode_rows(&g.tb, w, es, a.N, a.K, wst, pl.bn) ||
       (!g.y_plain && !tma::encode_rows(&g.ty, a.y, os, a.T, a.N, a.ys, GEMM_BM)) ||
@@ -363,7 +363,7 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     g.tiles_n = ceil_div(a.K, pl.bn);
     g.splits = 1;
     g.M = static_cast<int>(a.T), g.N = a.K;
-    g.y = a.dx, g.ys = a.dxs, g.y_plain = !tma::mappable(a.dx, a.T, a.dxs, 2);
+    g.y = a.dx, g.ys = a.dxs, g.y_plain = !tma::storable(a.dx, a.T, a.K, a.dxs, 2);
     g.err = err;
     if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, GEMM_BM) ||
         !tma::encode_rows(&g.tb, b.pad_w ? base + b.w_off : a.w, 2, a.N, a.K, b.pad_w ? b.kp : a.ws, 64) ||
@@ -385,7 +385,7 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     void* out = split ? static_cast<void*>(base + b.dw_off) : a.dw;
     const long long rows = split ? static_cast<long long>(g.splits) * b.split_rows : a.N;
     int pitch = split ? pitch_of(a.K, 4) : a.K;
-    g.y = out, g.ys = pitch, g.y_plain = !tma::mappable(out, rows, pitch, os);
+    g.y = out, g.ys = pitch, g.y_plain = !split && !tma::storable(out, rows, a.K, pitch, os);  // (a partial row's end may be written over)
     if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, 64) ||
         !tma::encode_rows(&g.tb, b.pad_x ? base + b.x_off : a.x, 2, a.T, a.K, b.pad_x ? b.kp : a.xs, 64) ||
         (!g.y_plain && !tma::encode_rows(&g.ty, out, os, rows, a.K, pitch, GEMM_BM)))

@@ -31,6 +31,12 @@ inline bool mappable(const void* base, long long rows, long long stride, int es)
   return (reinterpret_cast<uintptr_t>(base) & 15u) == 0 && (rows == 1 || (static_cast<unsigned long long>(stride) * es) % 16 == 0);
 }
 
+// A tensor map of it can be stored to: a store writes whole 16-byte pieces, zeros beyond the last column (a load's columns end
+// where the map's do), so that only rows of whole pieces leave what follows them alone.
+inline bool storable(const void* base, long long rows, long long cols, long long stride, int es) {
+  return mappable(base, rows, stride, es) && static_cast<unsigned long long>(cols) * es % 16 == 0;
+}
+
 // [rows, cols] of es-byte elements (1: bytes, 2: bf16, 4: float), `stride` elements a row; boxes of box_rows rows x 128 bytes,
 // 128-byte swizzle.  What lies outside reads as zero and is not written.
 inline bool encode_rows(CUtensorMap* tm, const void* base, int es, long long rows, long long cols, long long stride, int box_rows) {

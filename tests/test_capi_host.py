@@ -309,3 +309,142 @@ def test_x16_checks_its_arguments_as_the_forward_does(lib):
         assert xfwd(lib, **kw) == fwd(lib, **kw), kw
     passes_every_check(lambda: xfwd(lib, y=FAKE))                     # exact in place
     passes_every_check(lambda: xfwd(lib, N=65536, C=128, dtype=1, x=FAKE, g=(1 << 40), y=(1 << 41)))
+
+
+# ---- the layer operators ----
+
+def norm(lib, x=FAKE, r=2 * FAKE, w=3 * FAKE, h=4 * FAKE, y=5 * FAKE, s=None, T=4, D=8, xs=8, rs=8, hs=8, ys=8, eps=1e-6, dt=1, odt=1):
+    return lib.whtmix_rms_norm(x, r, w, h, y, s, T, D, xs, rs, hs, ys, eps, dt, odt, None)
+
+
+def norm_bwd(lib, h=FAKE, w=2 * FAKE, dy=3 * FAKE, dh=4 * FAKE, dx=5 * FAKE, dw=6 * FAKE, T=4, D=8, hs=8, ys=8, gs=8, xs=8, eps=1e-6, dt=1):
+    return lib.whtmix_rms_norm_backward(h, w, dy, dh, dx, dw, T, D, hs, ys, gs, xs, eps, dt, None)
+
+
+def lin(lib, x=FAKE, w=2 * FAKE, sx=None, sw=None, b=3 * FAKE, r=4 * FAKE, p=5 * FAKE, y=6 * FAKE, T=4, N=8, K=16, xs=16, ws=16, rs=8, ps=8,
+        ys=8, act=2, dt=1, odt=1):
+    return lib.whtmix_linear(x, w, sx, sw, b, r, p, y, T, N, K, xs, ws, rs, ps, ys, act, dt, odt, None)
+
+
+def lin_bwd(lib, x=FAKE, w=2 * FAKE, dy=3 * FAKE, p=4 * FAKE, dx=5 * FAKE, dw=6 * FAKE, db=7 * FAKE, T=4, N=8, K=16, xs=16, ws=16, ys=8,
+            ps=8, dxs=16, act=2, wdt=1):
+    return lib.whtmix_linear_backward(x, w, dy, p, dx, dw, db, T, N, K, xs, ws, ys, ps, dxs, act, wdt, None)
+
+
+def test_layer_calls_reject_bad_arguments(lib):
+    for call in (norm, norm_bwd):
+        assert call(lib, w=None) == 1
+        assert call(lib, T=-1) == 1
+        assert call(lib, D=0) == 1
+        assert call(lib, eps=-1.0) == 1
+        assert call(lib, eps=float("nan")) == 1
+        assert call(lib, D=(1 << 24) + 1) == 2
+        assert call(lib, T=(1 << 31) - 255) == 2
+        assert call(lib, T=1 << 30, D=1 << 11) == 2  # 2^41 elements
+        assert call(lib, xs=7) == 1                # rows that overlap
+        assert call(lib, xs=1 << 41) == 2
+        assert call(lib, dt=2) == 3
+        assert call(lib, dt=3) == 3
+        assert call(lib, w=3 * FAKE + 2) == 4
+        passes_every_check(lambda c=call: c(lib))
+        passes_every_check(lambda c=call: c(lib, T=1, xs=0))  # one row has no stride
+    assert norm(lib, x=None) == 1
+    assert norm(lib, y=None) == 1
+    assert norm(lib, odt=0) == 3
+    assert norm(lib, odt=3) == 1                    # 8 bits without scales
+    assert norm(lib, x=FAKE + 1) == 4
+    assert norm(lib, odt=3, s=7 * FAKE + 2) == 4
+    passes_every_check(lambda: norm(lib, odt=3, s=7 * FAKE, y=5 * FAKE + 1))
+    passes_every_check(lambda: norm(lib, r=None, h=None))
+    assert norm_bwd(lib, dy=None) == 1
+    assert norm_bwd(lib, dw=None) == 1
+    assert norm_bwd(lib, dw=None, T=0) == 1
+    passes_every_check(lambda: norm_bwd(lib, dh=None))
+    assert norm(lib, x=None, r=None, w=None, h=None, y=None, T=0) == 0
+
+    assert lin(lib, x=None) == 1
+    assert lin(lib, w=None) == 1
+    assert lin(lib, y=None) == 1
+    assert lin(lib, K=0) == 1
+    assert lin(lib, N=0) == 1
+    assert lin(lib, act=4) == 1
+    assert lin(lib, act=-1) == 1
+    assert lin(lib, sx=8 * FAKE) == 1               # scales belong to 8-bit operands
+    assert lin(lib, dt=3) == 1                      # which need them
+    passes_every_check(lambda: lin(lib, dt=3, sx=8 * FAKE, sw=9 * FAKE))
+    assert lin(lib, dt=0) == 3
+    assert lin(lib, odt=2) == 3
+    assert lin(lib, odt=0) == 3                     # the pre-activation goes with a bf16 output
+    passes_every_check(lambda: lin(lib, odt=0, p=None))
+    assert lin(lib, xs=15) == 1
+    assert lin(lib, ys=7) == 1
+    assert lin(lib, N=1 << 22, K=1 << 22) == 2
+    assert lin(lib, b=3 * FAKE + 2) == 4
+    assert lin(lib, y=6 * FAKE + 1) == 4
+    passes_every_check(lambda: lin(lib, b=None, r=None, p=None))
+    assert lin(lib, x=None, w=None, y=None, T=0) == 0
+
+    assert lin_bwd(lib, dy=None) == 1
+    assert lin_bwd(lib, p=None) == 1                # gelu's slope needs the pre-activation
+    passes_every_check(lambda: lin_bwd(lib, p=None, act=0))
+    assert lin_bwd(lib, x=None) == 1
+    passes_every_check(lambda: lin_bwd(lib, x=None, dw=None))
+    assert lin_bwd(lib, w=None) == 1
+    passes_every_check(lambda: lin_bwd(lib, w=None, dx=None))
+    assert lin_bwd(lib, dx=None, dw=None, db=None) == 1
+    assert lin_bwd(lib, wdt=3) == 3
+    assert lin_bwd(lib, act=9) == 1
+    assert lin_bwd(lib, dw=6 * FAKE + 1) == 4
+
+
+def test_layer_alias_rules(lib):
+    row = 8 * 2                                     # bytes of a row of 8 bf16
+    assert norm(lib, y=FAKE + row) == 5             # part of x
+    assert norm(lib, h=4 * FAKE, y=4 * FAKE) == 5   # two outputs
+    assert norm(lib, y=3 * FAKE) == 5               # over the gains
+    assert norm(lib, y=FAKE, ys=16) == 5            # x's address, another stride
+    passes_every_check(lambda: norm(lib, y=FAKE))
+    passes_every_check(lambda: norm(lib, h=2 * FAKE))
+    assert norm(lib, odt=3, s=7 * FAKE, y=FAKE) == 5  # 8 bits over x
+    assert norm_bwd(lib, dx=FAKE) == 5              # h is read again
+    assert norm_bwd(lib, dw=FAKE + 16) == 5
+    passes_every_check(lambda: norm_bwd(lib, dx=3 * FAKE))
+    passes_every_check(lambda: norm_bwd(lib, dx=4 * FAKE))
+    assert lin(lib, y=FAKE) == 5
+    assert lin(lib, y=2 * FAKE + 16) == 5
+    assert lin(lib, p=6 * FAKE) == 5
+    assert lin(lib, p=4 * FAKE) == 5                # the pre-activation over the residual
+    assert lin(lib, y=4 * FAKE + 2) == 5
+    passes_every_check(lambda: lin(lib, y=4 * FAKE))
+    assert lin_bwd(lib, dx=FAKE) == 5
+    assert lin_bwd(lib, dx=3 * FAKE) == 5
+    assert lin_bwd(lib, db=6 * FAKE + 4) == 5
+
+
+def test_layer_binding_checks_what_a_pointer_cannot_carry():
+    bf, f32, e4 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+    x, w, gain = torch.zeros(4, 16, dtype=bf), torch.zeros(8, 16, dtype=bf), torch.ones(16)
+    with pytest.raises(ValueError, match="CUDA"):
+        whtmix.rms_norm(x, gain)
+    with pytest.raises(ValueError, match="CUDA"):
+        whtmix.linear(x, w)
+    with pytest.raises(TypeError):
+        whtmix.rms_norm(x.to(torch.float16), gain)
+    with pytest.raises(TypeError):
+        whtmix.rms_norm(x, gain, out_dtype=f32)
+    with pytest.raises(TypeError):
+        whtmix.linear(x.float(), w.float())
+    with pytest.raises(TypeError):
+        whtmix.linear(x, w, out_dtype=torch.float16)
+    with pytest.raises(ValueError, match="activation"):
+        whtmix.linear(x, w, activation="tanh")
+    with pytest.raises(ValueError, match="w must be"):
+        whtmix.linear(x, torch.zeros(8, 15, dtype=bf))
+    with pytest.raises(ValueError, match="w must be"):
+        whtmix.linear(x.to(e4), w)
+    with pytest.raises(TypeError):
+        whtmix.linear_backward(x.float(), w, x)
+    with pytest.raises(ValueError, match="activation"):
+        whtmix.linear_backward(x, w, x, activation="elu")
+    q, s = whtmix.quantize_rows(torch.tensor([[1.0, -448.0, 0.25], [0.0, 0.0, 0.0]]))
+    assert q.dtype == e4 and q.float().tolist() == [[1.0, -448.0, 0.25], [0.0, 0.0, 0.0]] and s.tolist() == [1.0, 1.0]
