@@ -87,12 +87,13 @@ __device__ __forceinline__ void times_slope(float& d0, float& d1, float z0, floa
   unpair(pair(d0, d1) * (s * (g + pair(1.f, 1.f))), d0, d1);
 }
 
-// dp[t, n] = bf16(dy act'(p)); part[chunk][n] = the chunk's rows' float32 sum of dy act'(p), before the rounding.  A CTA takes 256
-// columns (a thread 8) and the rows of chunk blockIdx.y, 8 at a time.  dp, part: or null.
-template <bool AL>
+// dp[t, n] = bf16(dy act'(p)); part[chunk][n] = the chunk's rows' float32 sum of dy act'(p), before the rounding.  A CTA takes
+// 8 TX columns (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.
+template <bool AL, int TX>
 __global__ void __launch_bounds__(THREADS_256, AL ? 4 : 3) k_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
-  __shared__ float s[8][32][9];
-  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c0 = blockIdx.x * 256 + 8 * lane;
+  constexpr int G = THREADS_256 / TX;  // rows at a time
+  __shared__ float s[G][TX][9];
+  const int lane = threadIdx.x % TX, g = threadIdx.x / TX, c0 = (blockIdx.x * TX + lane) * 8;
   const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
   float acc[8] = {};
   pdl_wait();
@@ -120,11 +121,11 @@ __global__ void __launch_bounds__(THREADS_256, AL ? 4 : 3) k_dp(const Backward a
     for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
   };
   constexpr int U = 2;  // rows in flight
-  for (long long first = t0 + g; first < t1; first += 8 * U) {
+  for (long long first = t0 + g; first < t1; first += G * U) {
     Raw ud[U], uz[U];
 #pragma unroll
     for (int r = 0; r < U; ++r) {
-      const long long t = first + 8 * r;
+      const long long t = first + G * r;
       if (t < t1) {
         ud[r] = fetch(dy + t * a.dys, sd);
         if (a.act != ACT_NONE) uz[r] = fetch(p + t * a.ps, sp);
@@ -132,7 +133,7 @@ __global__ void __launch_bounds__(THREADS_256, AL ? 4 : 3) k_dp(const Backward a
     }
 #pragma unroll
     for (int r = 0; r < U; ++r) {
-      const long long t = first + 8 * r;
+      const long long t = first + G * r;
       if (t >= t1) break;
       float d[8];
       values(ud[r], dy + t * a.dys, sd, d);
@@ -159,37 +160,68 @@ __global__ void __launch_bounds__(THREADS_256, AL ? 4 : 3) k_dp(const Backward a
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[g][lane][j] = acc[j];
     __syncthreads();
-    const int l = threadIdx.x >> 3, j = threadIdx.x & 7;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum += s[i][l][j];
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c < a.N) part[static_cast<long long>(blockIdx.y) * a.N + c] = sum;
+    if (threadIdx.x < 8 * TX) {
+      float sum = 0.f;
+#pragma unroll 8
+      for (int i = 0; i < G; ++i) sum += s[i][threadIdx.x >> 3][threadIdx.x & 7];
+      const int c = blockIdx.x * 8 * TX + threadIdx.x;
+      if (c < a.N) part[static_cast<long long>(blockIdx.y) * a.N + c] = sum;
+    }
   }
   pdl_trigger();
 }
 
 // ---- the sum of a split product ----
-// out [rows, cols] contiguous = sum over s of part[s * split_rows + row][pitch], in ascending s
-template <typename O>
+// out [rows, cols] contiguous = sum over s of part[s * split_rows + row][pitch].  A CTA takes 256 / G fours of columns; its G groups
+// of threads sum runs of consecutive splits, each in ascending order, then the run sums are added in ascending order.  Many splits
+// take G = 8: with a thread for all the splits of its four, 152 splits of [77, 488] took 12.5 us.
+template <typename O, int G>
 __global__ void __launch_bounds__(THREADS_256) k_sum_splits(O* __restrict__ out, const float* part, int rows, int cols, int pitch,
                                                             int split_rows, int splits) {
+  constexpr int L = THREADS_256 / G;
+  __shared__ float4 s[G][L];
   pdl_wait();
-  const int quads = (cols + 3) / 4;
-  const long long n = static_cast<long long>(rows) * quads, step = static_cast<long long>(gridDim.x) * THREADS_256;
-  for (long long i = static_cast<long long>(blockIdx.x) * THREADS_256 + threadIdx.x; i < n; i += step) {
+  const int lane = threadIdx.x % L, g = threadIdx.x / L, quads = (cols + 3) / 4;
+  const int s0 = splits * g / G, s1 = splits * (g + 1) / G;
+  const long long n = static_cast<long long>(rows) * quads;
+  for (long long base = static_cast<long long>(blockIdx.x) * L; base < n; base += static_cast<long long>(gridDim.x) * L) {
+    const long long i = base + lane;
     const int r = static_cast<int>(i / quads), c = static_cast<int>(i - static_cast<long long>(r) * quads) * 4;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(part + (static_cast<long long>(s) * split_rows + r) * pitch + c));
-      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-    }
-    const float f[4] = {sum.x, sum.y, sum.z, sum.w};
-    O* o = out + static_cast<long long>(r) * cols + c;
+    if (i < n) {
+      const float4* p = reinterpret_cast<const float4*>(part + (static_cast<long long>(s0) * split_rows + r) * pitch + c);
+      const long long step = static_cast<long long>(split_rows) * pitch / 4;
+      int k = s0;
+      for (; k + 8 <= s1; k += 8, p += 8 * step) {
+        float4 v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (c + j < cols) o[j] = static_cast<O>(f[j]);
+        for (int u = 0; u < 8; ++u) v[u] = __ldcg(p + u * step);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum.x += v[u].x, sum.y += v[u].y, sum.z += v[u].z, sum.w += v[u].w;
+      }
+#pragma unroll 4
+      for (; k < s1; ++k, p += step) {
+        const float4 v = __ldcg(p);
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+      }
+    }
+    if constexpr (G > 1) {
+      __syncthreads();  // the last round's sums have been read
+      s[g][lane] = sum;
+      __syncthreads();
+    }
+    if (g == 0 && i < n) {
+#pragma unroll
+      for (int k = 1; k < G; ++k) {
+        const float4 v = s[k][lane];
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+      }
+      const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+      O* o = out + static_cast<long long>(r) * cols + c;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < cols) o[j] = static_cast<O>(f[j]);
+    }
   }
   pdl_trigger();
 }
@@ -286,6 +318,9 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
   return gemm_forward(g, a.e4m3, a.out_f32, pl.bn, sms, stream);
 }
 
+// Threads a row of k_dp, eight columns each.
+static int dp_lanes(int N) { return N <= 64 ? 8 : N <= 128 ? 16 : 32; }
+
 struct BackwardPlan {
   bool own_dp, pad_x, pad_w;
   int np, kp, chunks;  // pitches of dp, and of x and W; db's chunks of rows
@@ -308,7 +343,7 @@ static BackwardPlan plan_backward(const Backward& a, int sms) {
   if (b.pad_x) b.x_off = take(static_cast<size_t>(a.T) * b.kp * 2);
   if (b.pad_w) b.w_off = take(static_cast<size_t>(a.N) * b.kp * 2);
   if (a.db || b.own_dp) {
-    const int strips = ceil_div(a.N, 256), rows = ceil_div(a.T, 16), most = (4 * sms + strips - 1) / strips;  // one wave
+    const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (4 * sms + strips - 1) / strips;  // one wave
     b.chunks = rows < most ? rows : most;
     if (b.chunks > 65535) b.chunks = 65535;
     if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
@@ -342,7 +377,8 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     int chunks = b.chunks;
     const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && (a.act == ACT_NONE || tma::mappable(a.p, a.T, a.ps, 2));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ceil_div(a.N, 256), chunks);
+    const int tx = dp_lanes(a.N);
+    cfg.gridDim = dim3(ceil_div(a.N, 8 * tx), chunks);
     cfg.blockDim = dim3(THREADS_256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -350,7 +386,11 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, al ? k_dp<true> : k_dp<false>, c, d, np, part, chunks);
+    e = cudaLaunchKernelEx(&cfg,
+                           tx == 8    ? (al ? k_dp<true, 8> : k_dp<false, 8>)
+                           : tx == 16 ? (al ? k_dp<true, 16> : k_dp<false, 16>)
+                                      : (al ? k_dp<true, 32> : k_dp<false, 32>),
+                           c, d, np, part, chunks);
     if (e != cudaSuccess) return e;
     if (b.own_dp) dp = d, dps = b.np;
     if (a.db && chunks > 1 && (e = norm::add_rows(part, a.db, a.N, chunks, stream)) != cudaSuccess) return e;
@@ -396,8 +436,11 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
       int rows_ = a.N, cols = a.K, sr = b.split_rows, splits = g.splits;
       void* dw = a.dw;
       void* args[] = {&dw, &part, &rows_, &cols, &pitch, &sr, &splits};
-      const long long n = static_cast<long long>(a.N) * ceil_div(a.K, 4), need = (n + THREADS_256 - 1) / THREADS_256;
-      e = launch_pdl(a.dw_f32 ? reinterpret_cast<const void*>(k_sum_splits<float>) : reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16>),
+      const long long n = static_cast<long long>(a.N) * ceil_div(a.K, 4), need = (n + (splits >= 16 ? 31 : 255)) / (splits >= 16 ? 32 : 256);
+      const bool many = splits >= 16;
+      e = launch_pdl(a.dw_f32 ? (many ? reinterpret_cast<const void*>(k_sum_splits<float, 8>) : reinterpret_cast<const void*>(k_sum_splits<float, 1>))
+                              : (many ? reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16, 8>)
+                                      : reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16, 1>)),
                      static_cast<unsigned>(need < 8ll * sms ? need : 8ll * sms), THREADS_256, 0, stream, args);
     }
   }

@@ -347,18 +347,19 @@ def block_backward(x: torch.Tensor, w_in: torch.Tensor, g: torch.Tensor, w_out: 
 
 # ---- the layer around the mixer: RMS norm and the matrix product with its epilogue ----
 
-def _rows(t: torch.Tensor, name: str, device: torch.device):
-    """(rows, channels, stride) of a tensor [..., C] whose channels are contiguous and whose other axes
-    step through memory with one stride (any contiguous tensor, a slice of channels of one, a view of
+def _rows(t: torch.Tensor, name: str, index: int):
+    """(rows, channels, stride) of a tensor [..., C] on CUDA device `index` whose channels are contiguous and whose
+    other axes step through memory with one stride (any contiguous tensor, a slice of channels of one, a view of
     every k-th token)."""
-    if t.device != device or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor on {device} (WHTMix runs on CUDA tensors only)")
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} must be a CUDA tensor on the first tensor's device (WHTMix runs on CUDA tensors only), "
+                         f"it is on {t.device}")
     shape = t.shape
     if not shape or shape[-1] < 1:
         raise ValueError(f"{name} must have at least one channel, got shape {list(shape)}")
     C = shape[-1]
-    rows = t.numel() // C
-    if t.is_contiguous() or rows == 0:
+    rows = shape[0] if len(shape) == 2 else t.numel() // C
+    if rows == 0 or t.is_contiguous():
         return rows, C, C
     strides = t.stride()
     if C > 1 and strides[-1] != 1:
@@ -377,31 +378,22 @@ def _rows(t: torch.Tensor, name: str, device: torch.device):
     return rows, C, step or C
 
 
-def _vector(t: torch.Tensor, n: int, name: str, device: torch.device) -> int:
-    """The address of a contiguous float32 vector of n elements."""
-    if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n:
-        raise ValueError(f"{name} must be float32 [{n}], got {t.dtype} {list(t.shape)}")
-    if t.device != device or not t.is_contiguous():
-        _on_device(t, device, name)
+def _vector(t: torch.Tensor, shape, name: str, index: int) -> int:
+    """The address of a contiguous float32 tensor of the given shape."""
+    if t.dtype != torch.float32 or t.shape != shape:
+        raise ValueError(f"{name} must be float32 {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the first tensor's device")
     return t.data_ptr()
 
 
-def _stride(t: torch.Tensor, shape, dtype: torch.dtype, name: str, device: torch.device) -> int:
+def _stride(t: torch.Tensor, shape, dtype: torch.dtype, name: str, index: int) -> int:
     """The row stride of a row matrix of the given shape and dtype."""
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.is_contiguous() and t.device == device:
+    if t.is_contiguous() and t.get_device() == index:
         return shape[-1]
-    return _rows(t, name, device)[2]
-
-
-def _token_scale(t: torch.Tensor, shape, name: str, device: torch.device) -> int:
-    """The address of contiguous float32 scales, one a token."""
-    if t.dtype != torch.float32 or t.shape != shape:
-        raise ValueError(f"{name} must be float32 {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.device != device or not t.is_contiguous():
-        _on_device(t, device, name)
-    return t.data_ptr()
+    return _rows(t, name, index)[2]
 
 
 def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
@@ -418,22 +410,23 @@ def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = N
     eight = out_dtype == E4M3
     if not eight and out_dtype is not None and out_dtype != dtype:
         raise TypeError(f"rms_norm of {dtype} writes {dtype} or {E4M3}, not {out_dtype}")
-    device, shape = x.device, x.shape
-    T, D, xs = _rows(x, "x", device)
-    wp = _vector(w, D, "w", device)
+    shape, index = x.shape, x.get_device()
+    T, D, xs = _rows(x, "x", index)
+    wp = _vector(w, (D,), "w", index)
+    device = x.device
     rp = rs = hp = hs = sp = 0
     if residual is not None:
-        rs = _stride(residual, shape, dtype, "residual", device)
+        rs = _stride(residual, shape, dtype, "residual", index)
         rp = residual.data_ptr()
         if h is None:
             h, hs = torch.empty(shape, dtype=dtype, device=device), D
         else:
-            hs = _stride(h, shape, dtype, "h", device)
+            hs = _stride(h, shape, dtype, "h", index)
         hp = h.data_ptr()
     elif h is not None:
         raise ValueError("h is the sum of x and the residual: it needs a residual")
     if out is not None:
-        ys = _stride(out, shape, E4M3 if eight else dtype, "out", device)
+        ys = _stride(out, shape, E4M3 if eight else dtype, "out", index)
     elif eight and D % 16:
         # rows at a 16-byte pitch, as the tensor cores' loads want them: linear takes them as they lie
         ys = (D + 15) // 16 * 16
@@ -445,7 +438,7 @@ def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = N
             scale = torch.empty(shape[:-1], dtype=torch.float32, device=device)
             sp = scale.data_ptr()
         else:
-            sp = _token_scale(scale, shape[:-1], "scale", device)
+            sp = _vector(scale, shape[:-1], "scale", index)
     elif scale is not None:
         raise ValueError(f"scale belongs to an output of {E4M3}")
     code = LAYER_CODE[dtype]
@@ -463,19 +456,20 @@ def rms_norm_backward(h: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, dh: to
     dtype = h.dtype
     if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError(f"rms_norm_backward takes float32 or bfloat16, got {dtype}")
-    device, shape = h.device, h.shape
-    T, D, hs = _rows(h, "h", device)
-    wp = _vector(w, D, "w", device)
-    dys = _stride(dy, shape, dtype, "dy", device)
-    dhs = 0 if dh is None else _stride(dh, shape, dtype, "dh", device)
+    shape, index = h.shape, h.get_device()
+    T, D, hs = _rows(h, "h", index)
+    wp = _vector(w, (D,), "w", index)
+    device = h.device
+    dys = _stride(dy, shape, dtype, "dy", index)
+    dhs = 0 if dh is None else _stride(dh, shape, dtype, "dh", index)
     if dx is None:
         dx, dxs = torch.empty(shape, dtype=dtype, device=device), D
     else:
-        dxs = _stride(dx, shape, dtype, "dx", device)
+        dxs = _stride(dx, shape, dtype, "dx", index)
     if dw is None:
         dw = torch.empty(D, dtype=torch.float32, device=device)
     _call("whtmix_rms_norm_backward", device, stream, (_lib or library()).whtmix_rms_norm_backward, h.data_ptr(), wp,
-          dy.data_ptr(), 0 if dh is None else dh.data_ptr(), dx.data_ptr(), _vector(dw, D, "dw", device), T, D, hs, dys, dhs,
+          dy.data_ptr(), 0 if dh is None else dh.data_ptr(), dx.data_ptr(), _vector(dw, (D,), "dw", index), T, D, hs, dys, dhs,
           dxs, eps, LAYER_CODE[dtype])
     return dx, dw
 
@@ -494,7 +488,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
     """y = act(x w^T + bias) + residual over the last axis: x [..., K] and w [N, K] bfloat16, or both float8_e4m3fn
     with float32 scales x_scale [...] and w_scale [N]; bias [N] float32; residual and y [..., N] of out_dtype
     (bfloat16 or float32).  preact=True, or a bfloat16 tensor, also returns the pre-activation: (y, preact)."""
-    dtype, device = x.dtype, x.device
+    dtype, device, index = x.dtype, x.device, x.get_device()
     if dtype != torch.bfloat16 and dtype != E4M3:
         raise TypeError(f"linear takes bfloat16 or {E4M3}, got {dtype}")
     if out_dtype != torch.bfloat16 and out_dtype != torch.float32:
@@ -503,21 +497,21 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
     N, K = w.shape if w.dim() == 2 else (0, 0)
     if w.dtype != dtype or K != x.shape[-1]:
         raise ValueError(f"w must be {dtype} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
-    T, _, xs = _rows(x, "x", device)
-    ws = _rows(w, "w", device)[2]
+    T, _, xs = _rows(x, "x", index)
+    ws = _rows(w, "w", index)[2]
     lead = x.shape[:-1]
     shape = lead + (N,)
     xsp = wsp = bp = rp = rs = pp = ps = 0
     if dtype == E4M3:
         if x_scale is None or w_scale is None:
             raise ValueError(f"{E4M3} needs x_scale and w_scale")
-        xsp, wsp = _token_scale(x_scale, lead, "x_scale", device), _vector(w_scale, N, "w_scale", device)
+        xsp, wsp = _vector(x_scale, lead, "x_scale", index), _vector(w_scale, (N,), "w_scale", index)
     elif x_scale is not None or w_scale is not None:
         raise ValueError(f"scales belong to {E4M3} operands")
     if bias is not None:
-        bp = _vector(bias, N, "bias", device)
+        bp = _vector(bias, (N,), "bias", index)
     if residual is not None:
-        rs = _stride(residual, shape, out_dtype, "residual", device)
+        rs = _stride(residual, shape, out_dtype, "residual", index)
         rp = residual.data_ptr()
     save = preact is not None and preact is not False
     if save:
@@ -526,12 +520,12 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
         if preact is True:
             preact, ps = torch.empty(shape, dtype=torch.bfloat16, device=device), N
         else:
-            ps = _stride(preact, shape, torch.bfloat16, "preact", device)
+            ps = _stride(preact, shape, torch.bfloat16, "preact", index)
         pp = preact.data_ptr()
     if out is None:
         out, ys = torch.empty(shape, dtype=out_dtype, device=device), N
     else:
-        ys = _stride(out, shape, out_dtype, "out", device)
+        ys = _stride(out, shape, out_dtype, "out", index)
     _call("whtmix_linear", device, stream, (_lib or library()).whtmix_linear, x.data_ptr(), w.data_ptr(), xsp, wsp, bp, rp,
           pp, out.data_ptr(), T, N, K, xs, ws, rs, ps, ys, act, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
     return (out, preact) if save else out
@@ -544,7 +538,7 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch
     """(dx, dw, db) of linear for the upstream gradient dy of y (bfloat16), from the stored pre-activation p (needed
     unless the activation is "none"); None in the place of a gradient that is not needed.  The residual's gradient is
     dy itself.  dw is bfloat16 or float32, db float32."""
-    device = x.device
+    device, index = x.device, x.get_device()
     if x.dtype != torch.bfloat16:
         raise TypeError(f"linear_backward takes bfloat16, got {x.dtype}")
     if dw_dtype != torch.bfloat16 and dw_dtype != torch.float32:
@@ -553,18 +547,18 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch
     N, K = w.shape if w.dim() == 2 else (0, 0)
     if w.dtype != torch.bfloat16 or K != x.shape[-1]:
         raise ValueError(f"w must be {torch.bfloat16} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
-    T, _, xs = _rows(x, "x", device)
-    ws = _rows(w, "w", device)[2]
+    T, _, xs = _rows(x, "x", index)
+    ws = _rows(w, "w", index)[2]
     shape = x.shape[:-1] + (N,)
-    dys = _stride(dy, shape, torch.bfloat16, "dy", device)
+    dys = _stride(dy, shape, torch.bfloat16, "dy", index)
     pp = ps = dxp = dxs = dwp = dbp = 0
     if act:
         if p is None:
             raise ValueError(f"the backward of {activation} needs the pre-activation p")
-        ps = _stride(p, shape, torch.bfloat16, "p", device)
+        ps = _stride(p, shape, torch.bfloat16, "p", index)
         pp = p.data_ptr()
     if dx is not None:
-        dxs = _stride(dx, x.shape, torch.bfloat16, "dx", device)
+        dxs = _stride(dx, x.shape, torch.bfloat16, "dx", index)
         dxp = dx.data_ptr()
     elif need_dx:
         dx, dxs = torch.empty(x.shape, dtype=torch.bfloat16, device=device), K
@@ -574,7 +568,7 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch
         dwp = dw.data_ptr()
     if db is not None or need_db:
         db = torch.empty(N, dtype=torch.float32, device=device) if db is None else db
-        dbp = _vector(db, N, "db", device)
+        dbp = _vector(db, (N,), "db", index)
     _call("whtmix_linear_backward", device, stream, (_lib or library()).whtmix_linear_backward, x.data_ptr(), w.data_ptr(),
           dy.data_ptr(), pp, dxp, dwp, dbp, T, N, K, xs, ws, dys, ps, dxs, act, LAYER_CODE[dw_dtype])
     return dx, dw, db
