@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
       int i = 0;
       for (const int n = k1 - k0; i < n; ++i) {
         const int s = i % S;
-        if (!tc::mbar_wait(&empty[s], ((i / S) & 1) ^ 1)) {
+        if (!tma::wait(&empty[s], ((i / S) & 1) ^ 1)) {
           bad |= 1;
           break;
         }
@@ -112,13 +112,13 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
         tma::load_2d(st + FEW_ROWS * 128, &a.tx, (k0 + i) * BK, t0, &full[s]);
       }
       if (bad)  // the copies in flight have landed before the CTA can end (otherwise the products have waited for them)
-        for (int j = i > S ? i - S : 0; j < i; ++j) tc::mbar_wait(&full[j % S], (j / S) & 1);
+        for (int j = i > S ? i - S : 0; j < i; ++j) tma::wait(&full[j % S], (j / S) & 1);
     }
   } else if (warp == 5) {
     if (lane == 0) {
       for (int kb = k0; kb < k1; ++kb) {
         const int i = kb - k0, s = i % S;
-        if (!tc::mbar_wait(&full[s], (i / S) & 1)) {
+        if (!tma::wait(&full[s], (i / S) & 1)) {
           bad |= 2;
           break;
         }
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   float* sums = reinterpret_cast<float*>(smem);  // [token][row of W]
   if (warp < 4) {
     // the products have completed: the accumulator can be read, the ring is free
-    if (!tc::mbar_wait(&dfull, 0)) bad |= 4;
+    if (!tma::wait(&dfull, 0)) bad |= 4;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     __syncwarp();
 #pragma unroll

@@ -6,8 +6,10 @@
 //   warp 0     TMA loads of A and B blocks into a ring of stages (192 KB in all);
 //   warp 1     four tcgen05.mma a block (fp32 accumulators in tensor memory, two tiles' worth: the next tile's products run
 //              while the last one's accumulator is read);
-//   warps 4-11 epilogue, two groups of four warps; a group takes every other panel of 128 bytes of a row: accumulator ->
-//              registers, the epilogue, a 128 x 128-byte panel in shared memory, TMA store.
+//   warps 4-11 epilogue, two groups of four warps, which take every other tile (a CTA with one tile: every other panel of it); a
+//              panel is 128 bytes of each of the 128 rows: accumulator -> registers, the epilogue, shared memory, TMA store.
+//              Of a panel's 3300 clocks with gelu 1850 are the special-function unit's where both groups work on panels of one
+//              tile, in step; apart, one's stores cover the other's arithmetic.
 // A and B may lie with k along a row (the forward; A of dx = dp W) or with m / n along a row (B of dx; both of dw = dp^T x, the
 // contraction down the rows): the panels are multiplied as they lie.  What lies past an edge reads as zero and is not stored, so
 // that every size runs; rows that are not 16-byte aligned are stored (and the residual read) with plain accesses, through the
@@ -141,6 +143,18 @@ __device__ __forceinline__ void activate(float& z0, float& z1, int act) {
   }
 }
 
+// d0 *= act'(z0), d1 *= act'(z1).  gelu and silu: s (1 + z (1 - s) u'), s = 1 / (1 + e^-u)
+__device__ __forceinline__ void times_slope(float& d0, float& d1, float z0, float z1, int act) {
+  if (act == ACT_RELU) {
+    d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
+    return;
+  }
+  const Pair z = pair(z0, z1), s = logistic2(gate_exponent(pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), act));
+  Pair g = z * fma(s, pair(-1.f, -1.f), pair(1.f, 1.f));
+  if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
+  unpair(pair(d0, d1) * (s * (g + pair(1.f, 1.f))), d0, d1);
+}
+
 template <typename O> struct Panel;  // a 128-byte row of the output
 template <> struct Panel<__nv_bfloat16> {
   static constexpr int W = 64;
@@ -245,13 +259,15 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ GemmBars<BN> bars;
   __shared__ uint32_t tmem_slot;
-  __shared__ __align__(16) float s_bias[2][BN / 2 < PW ? PW : BN / 2], s_scale[2][BN / 2 < PW ? PW : BN / 2];
+  __shared__ __align__(16) float s_bias[2][2][PW], s_scale[2][2][PW];  // of a group's panel and its next
   const uint32_t ring = tc::smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int items = a.tiles_m * a.tiles_n * a.splits;
+  const bool alternate = items > static_cast<int>(gridDim.x);
   if (warp == 0) tc::tmem_alloc(&tmem_slot, 2 * BN);
   if (tid == 32) {
     for (int s = 0; s < S; ++s) tc::mbar_init(&bars.full[s], 1), tc::mbar_init(&bars.empty[s], 1);
-    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], 8), tc::mbar_init(&bars.rfull[s], 1);
+    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], alternate ? 4 : 8), tc::mbar_init(&bars.rfull[s], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma::prefetch(&a.ta);
     tma::prefetch(&a.tb);
@@ -261,7 +277,6 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_wait();
   const uint32_t tmem = tmem_slot;
-  const int items = a.tiles_m * a.tiles_n * a.splits;
   // item -> tile (n fastest) and split (slowest)
   auto place = [&](int item, int& m0, int& n0, int& split) {
     const int tile = item % (a.tiles_m * a.tiles_n);
@@ -280,7 +295,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
         const int k1 = first_block(split + 1);
         for (int kb = first_block(split); kb < k1; ++kb, ++it) {
           const int s = it % S;
-          if (!tc::mbar_wait(&bars.empty[s], ((it / S) & 1) ^ 1)) {
+          if (!tma::wait(&bars.empty[s], ((it / S) & 1) ^ 1)) {
             bad |= 1;
             break;
           }
@@ -302,7 +317,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       }
       // the copies in flight have landed before the CTA can end
       for (uint32_t j = it > S ? it - S : 0; j < it; ++j)
-        if (!tc::mbar_wait(&bars.full[j % S], (j / S) & 1)) bad |= 1;
+        if (!tma::wait(&bars.full[j % S], (j / S) & 1)) bad |= 1;
     }
   } else if (warp == 1) {
     if (lane == 0) {
@@ -311,14 +326,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
         int m0, n0, split;
         place(item, m0, n0, split);
         const int d = i & 1, k0 = first_block(split), k1 = first_block(split + 1);
-        if (!tc::mbar_wait(&bars.dempty[d], ((i >> 1) & 1) ^ 1)) {
+        if (!tma::wait(&bars.dempty[d], ((i >> 1) & 1) ^ 1)) {
           bad |= 2;
           break;
         }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         for (int kb = k0; kb < k1; ++kb, ++it) {
           const int s = it % S;
-          if (!tc::mbar_wait(&bars.full[s], (it / S) & 1)) {
+          if (!tma::wait(&bars.full[s], (it / S) & 1)) {
             bad |= 4;
             break;
           }
@@ -340,7 +355,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       }
       // every product has completed before the tensor memory is freed
       for (uint32_t j = i > 2 ? i - 2 : 0; j < i; ++j)
-        if (!tc::mbar_wait(&bars.dfull[j & 1], (j >> 1) & 1)) bad |= 2;
+        if (!tma::wait(&bars.dfull[j & 1], (j >> 1) & 1)) bad |= 2;
     }
   } else if (warp >= 4) {
     const int g = (warp - 4) >> 2, gt = tid - 128 - 128 * g, row = 32 * (warp & 3) + lane;
@@ -349,25 +364,53 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
     uint32_t i = 0, loads = 0;
     auto sync_group = [&] { asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory"); };
     auto wait = [&](uint64_t* b, uint32_t parity) {  // (after one wait has given up none is waited for)
-      if (!bad && !tc::mbar_wait(b, parity)) bad |= 8;
+      if (!bad && !tma::wait(b, parity)) bad |= 8;
     };
-    for (int item = blockIdx.x; item < items; item += gridDim.x, ++i) {
+    // the group's tiles, and of the next one's columns gt, gt + 128 the bias and scale, of its row the scale: on their way while a
+    // tile is stored
+    const int step = alternate ? 1 : 2, p0 = alternate ? 0 : g, stride = alternate ? 2 * gridDim.x : gridDim.x;
+    constexpr int HELD = (BN + 127) / 128;
+    float next_bias[HELD], next_scale[HELD], next_sm = 1.f;
+    auto fetch = [&](int item) {
+      if (item >= items) return;
+      int m0, n0, split;
+      place(item, m0, n0, split);
+#pragma unroll
+      for (int j = 0; j < HELD; ++j) {
+        const int c = n0 + 128 * j + gt;
+        next_bias[j] = a.bias && c < a.N ? __ldg(a.bias + c) : 0.f;
+        next_scale[j] = a.sn && c < a.N ? __ldg(a.sn + c) : 1.f;
+      }
+      if (a.sm) next_sm = m0 + row < a.M ? __ldg(a.sm + m0 + row) : 1.f;
+    };
+    const int first = blockIdx.x + (alternate ? g * gridDim.x : 0);
+    if (alternate) i = g;
+    fetch(first);
+    for (int item = first; item < items; item += stride, i += step == 1 ? 2 : 1) {
       int m0, n0, split;
       place(item, m0, n0, split);
       const int d = i & 1, yrow = split * a.split_rows + m0;
       const bool none = first_block(split) == first_block(split + 1);  // no K block: a sum of nothing
       const int panels = min(PANELS, (a.N - n0 + PW - 1) / PW);
-      const float sm = a.sm && m0 + row < a.M ? a.sm[m0 + row] : 1.f;
+      const float sm = next_sm;
       bool waited = false;
-      // the columns of this group's panels (a panel's reads of the last tile's are behind a barrier of the group)
-      for (int j = gt; j < BN / 2 || j < PW; j += 128) {
-        const int c = n0 + (g + 2 * (j / PW)) * PW + j % PW;
-        s_bias[g][j] = a.bias && c < a.N ? a.bias[c] : 0.f;
-        s_scale[g][j] = a.sn && c < a.N ? a.sn[c] : 1.f;
-      }
+      int turn = 0;
+      float bias[HELD], scale[HELD];
+#pragma unroll
+      for (int j = 0; j < HELD; ++j) bias[j] = next_bias[j], scale[j] = next_scale[j];
+      fetch(item + stride);
+      auto put_cols = [&](int p, int b) {  // of panel p, by the threads that hold its columns
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+          const int c = 128 * j + gt - p * PW;
+          if (c >= 0 && c < PW) s_bias[g][b][c] = bias[j], s_scale[g][b][c] = scale[j];
+        }
+      };
+      put_cols(p0, 0);
       sync_group();
-      for (int p = g; p < panels; p += 2) {
+      for (int p = p0; p < panels; p += step, turn ^= 1) {
         const int col0 = n0 + p * PW;
+        put_cols(p + step, turn ^ 1);  // (the last panel's readers are behind its barrier)
         auto panel_free = [&] {  // the last store has read the panel
           if (gt == 0) tma::wait_read();
           sync_group();
@@ -398,21 +441,24 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
 #pragma unroll
           for (int c = 0; c < PW; ++c) v[c] = 0.f;
         }
-        if (p + 2 >= panels) {  // the accumulator has been read
+        if (p + step >= panels) {  // the accumulator has been read
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) tma::arrive(&bars.dempty[d]);
         }
-        const float *sb = &s_bias[g][p / 2 * PW], *ss = &s_scale[g][p / 2 * PW];
-        if (a.sm || a.bias) {
-          const float f = a.sm ? sm : 1.f;
+        const float *sb = s_bias[g][turn], *ss = s_scale[g][turn];
+        if (a.sm) {
+#pragma unroll
+          for (int c = 0; c < PW; c += 4) {
+            const float4 s = *reinterpret_cast<const float4*>(ss + c);
+            unpair(pair(v[c], v[c + 1]) * (pair(sm, sm) * pair(s.x, s.y)), v[c], v[c + 1]);
+            unpair(pair(v[c + 2], v[c + 3]) * (pair(sm, sm) * pair(s.z, s.w)), v[c + 2], v[c + 3]);
+          }
+        }
+        if (a.bias) {
 #pragma unroll
           for (int c = 0; c < PW; c += 4) {
             const float4 b = *reinterpret_cast<const float4*>(sb + c);
-            if (a.sm) {
-              const float4 s = *reinterpret_cast<const float4*>(ss + c);
-              v[c] *= f * s.x, v[c + 1] *= f * s.y, v[c + 2] *= f * s.z, v[c + 3] *= f * s.w;
-            }
             unpair(pair(v[c], v[c + 1]) + pair(b.x, b.y), v[c], v[c + 1]);
             unpair(pair(v[c + 2], v[c + 3]) + pair(b.z, b.w), v[c + 2], v[c + 3]);
           }
@@ -471,7 +517,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       }
     }
     if (gt == 0) tma::wait_done();
-    if (bad && loads && !tc::mbar_wait(&bars.rfull[g], (loads - 1) & 1)) bad |= 16;  // a residual panel in flight
+    if (bad && loads && !tma::wait(&bars.rfull[g], (loads - 1) & 1)) bad |= 16;  // a residual panel in flight
   }
   if (bad) atomicOr(a.err, bad << 16);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -510,6 +556,20 @@ cudaError_t launch_gemm(const Gemm& g, int sms, cudaStream_t stream) {
 cudaError_t gemm_forward(const Gemm& g, bool e4m3, bool out_f32, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dx(const Gemm& g, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dw(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
+
+// whtmix_gemm_dp.cu: dp = dy act'(p), its column sums and dx = dp W in one pass, for K <= 256 (one tile of columns) and an
+// activation.  part [tiles_m, N]: the 128-token tiles' sums of unrounded dp, or null; tdp's map is written where store_dp.
+struct DpProduct {
+  CUtensorMap tdy, tp, tw, tdp, tdx;
+  float* part;
+  void* dx;
+  long long dxs;
+  int M, N, K, tiles_m, kblocks, act;
+  bool store_dp, dx_plain;
+  unsigned int* err;
+};
+cudaError_t gemm_dp(const DpProduct& g, int sms, cudaStream_t stream);
+
 
 }  // namespace linear
 }  // namespace whtmix

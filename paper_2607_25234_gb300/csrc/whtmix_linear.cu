@@ -75,18 +75,6 @@ static cudaError_t to_pitch(const Copy& a, const Copy& b, int sms, cudaStream_t 
 }
 
 // ---- dp and db ----
-// d0 *= act'(z0), d1 *= act'(z1).  gelu and silu: s (1 + z (1 - s) u'), s = 1 / (1 + e^-u)
-__device__ __forceinline__ void times_slope(float& d0, float& d1, float z0, float z1, int act) {
-  if (act == ACT_RELU) {
-    d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
-    return;
-  }
-  const Pair z = pair(z0, z1), s = logistic2(gate_exponent(pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), act));
-  Pair g = z * fma(s, pair(-1.f, -1.f), pair(1.f, 1.f));
-  if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
-  unpair(pair(d0, d1) * (s * (g + pair(1.f, 1.f))), d0, d1);
-}
-
 // dp[t, n] = bf16(dy act'(p)); part[chunk][n] = the chunk's rows' float32 sum of dy act'(p), before the rounding.  A CTA takes
 // 8 TX columns (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.
 template <bool AL, int TX>
@@ -322,6 +310,7 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
 static int dp_lanes(int N) { return N <= 64 ? 8 : N <= 128 ? 16 : 32; }
 
 struct BackwardPlan {
+  bool fused;  // dp, db's partial sums and dx in one kernel (whtmix_gemm_dp.cu)
   bool own_dp, pad_x, pad_w;
   int np, kp, chunks;  // pitches of dp, and of x and W; db's chunks of rows
   Plan dw;
@@ -332,6 +321,9 @@ static BackwardPlan plan_backward(const Backward& a, int sms) {
   BackwardPlan b{};
   b.np = pitch_of(a.N, 2), b.kp = pitch_of(a.K, 2);
   b.own_dp = (a.dx || a.dw) && (a.act != ACT_NONE || !tma::mappable(a.dy, a.T, a.dys, 2));
+  // one pass over dy and p instead of a kernel for dp and a product that reads it again; tiles of 128 tokens on half the SMs at least
+  b.fused = a.dx && a.act != ACT_NONE && a.K <= 256 && tma::mappable(a.dy, a.T, a.dys, 2) && tma::mappable(a.p, a.T, a.ps, 2) &&
+            2ll * ceil_div(a.T, GEMM_BM) >= sms;
   b.pad_x = a.dw && !tma::mappable(a.x, a.T, a.xs, 2);
   b.pad_w = a.dx && !tma::mappable(a.w, a.N, a.ws, 2);
   auto take = [&](size_t bytes) {
@@ -339,10 +331,13 @@ static BackwardPlan plan_backward(const Backward& a, int sms) {
     b.total += align256(bytes);
     return off;
   };
-  if (b.own_dp) b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);
+  if (b.fused ? a.dw != nullptr : b.own_dp) b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);
   if (b.pad_x) b.x_off = take(static_cast<size_t>(a.T) * b.kp * 2);
   if (b.pad_w) b.w_off = take(static_cast<size_t>(a.N) * b.kp * 2);
-  if (a.db || b.own_dp) {
+  if (b.fused) {
+    b.chunks = ceil_div(a.T, GEMM_BM);
+    if (a.db) b.db_off = take(static_cast<size_t>(b.chunks) * a.N * 4);
+  } else if (a.db || b.own_dp) {
     const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (4 * sms + strips - 1) / strips;  // one wave
     b.chunks = rows < most ? rows : most;
     if (b.chunks > 65535) b.chunks = 65535;
@@ -369,7 +364,23 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
   if (e != cudaSuccess) return e;
   const void* dp = a.dy;
   long long dps = a.dys;
-  if (a.db || b.own_dp) {
+  if (b.fused) {
+    void* d = a.dw ? base + b.dp_off : nullptr;
+    DpProduct g{};
+    g.M = static_cast<int>(a.T), g.N = a.N, g.K = a.K, g.tiles_m = b.chunks, g.kblocks = ceil_div(a.N, 64), g.act = a.act;
+    g.part = a.db ? reinterpret_cast<float*>(base + b.db_off) : nullptr;
+    g.store_dp = d != nullptr;
+    g.dx = a.dx, g.dxs = a.dxs, g.dx_plain = !tma::storable(a.dx, a.T, a.K, a.dxs, 2);
+    g.err = err;
+    if (!tma::encode_rows(&g.tdy, a.dy, 2, a.T, a.N, a.dys, GEMM_BM) || !tma::encode_rows(&g.tp, a.p, 2, a.T, a.N, a.ps, GEMM_BM) ||
+        !tma::encode_rows(&g.tw, b.pad_w ? base + b.w_off : a.w, 2, a.N, a.K, b.pad_w ? b.kp : a.ws, 64) ||
+        (d && !tma::encode_rows(&g.tdp, d, 2, a.T, b.np, b.np, GEMM_BM)) ||
+        (!g.dx_plain && !tma::encode_rows(&g.tdx, a.dx, 2, a.T, a.K, a.dxs, GEMM_BM)))
+      return cudaErrorInvalidValue;
+    if ((e = gemm_dp(g, sms, stream)) != cudaSuccess) return e;
+    if (d) dp = d, dps = b.np;
+    if (a.db && (e = norm::add_rows(g.part, a.db, a.N, b.chunks, stream)) != cudaSuccess) return e;
+  } else if (a.db || b.own_dp) {
     Backward c = a;
     __nv_bfloat16* d = b.own_dp ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
     float* part = !a.db ? nullptr : b.chunks > 1 ? reinterpret_cast<float*>(base + b.db_off) : a.db;
@@ -395,7 +406,7 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
     if (b.own_dp) dp = d, dps = b.np;
     if (a.db && chunks > 1 && (e = norm::add_rows(part, a.db, a.N, chunks, stream)) != cudaSuccess) return e;
   }
-  if (a.dx) {
+  if (a.dx && !b.fused) {
     Gemm g{};
     g.tiles_m = ceil_div(a.T, GEMM_BM);
     g.kblocks = ceil_div(a.N, 64);

@@ -53,6 +53,28 @@ inline bool encode_rows(CUtensorMap* tm, const void* base, int es, long long row
            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Phase `parity` of an mbarrier, waited for at most WAIT_NS; false if it did not complete by then.
+constexpr unsigned long long WAIT_NS = 1000000000ull;  // 1 s
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity) {
+  const uint32_t bar = tc::smem_u32(b);
+  if (try_wait(bar, parity)) return true;
+  unsigned long long t0, t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+  do {
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i)
+      if (try_wait(bar, parity)) return true;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  } while (t - t0 < WAIT_NS);
+  return false;
+}
+
 __device__ __forceinline__ void arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc::smem_u32(b)) : "memory");
 }

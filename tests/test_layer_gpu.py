@@ -465,6 +465,32 @@ def test_linear_backward_against_float64(T, N, K, act):
     check_linear_backward(T, N, K, act, dw_dtype=F32)
 
 
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("T,N,K", [(9729, 1024, 256), (12000, 200, 130), (20001, 72, 64), (10240, 520, 33)])
+def test_linear_backward_of_many_tokens_and_few_channels(T, N, K, act):
+    """dp, its sums and dx in one pass."""
+    check_linear_backward(T, N, K, act)
+
+
+def test_linear_backward_of_many_tokens_leaves_out_what_is_not_wanted():
+    T, N, K = 10000, 136, 100
+    x, w, dy, p, (dx, dw, db) = check_linear_backward(T, N, K, "gelu")
+    again = whtmix.linear_backward(x, w, dy, p, "gelu")
+    assert torch.equal(dx, again[0]) and torch.equal(dw, again[1]) and torch.equal(db, again[2])
+    one = whtmix.linear_backward(x, w, dy, p, "gelu", need_dw=False, need_db=False)
+    assert torch.equal(one[0], dx) and one[1] is None and one[2] is None
+    two = whtmix.linear_backward(x, w, dy, p, "gelu", need_dw=False)
+    assert torch.equal(two[0], dx) and torch.equal(two[2], db)
+    bad = dy.clone()
+    bad[5000, 3] = math.nan
+    got = whtmix.linear_backward(x, w, bad, p, "gelu")
+    rest = [i for i in range(T) if i != 5000]
+    cols = [i for i in range(N) if i != 3]
+    assert bool(torch.isnan(got[0][5000]).all()) and torch.equal(got[0][rest], dx[rest])
+    assert bool(torch.isnan(got[1][3]).all()) and torch.equal(got[1][cols], dw[cols])
+    assert bool(torch.isnan(got[2][3])) and torch.equal(got[2][cols], db[cols])
+
+
 def test_linear_backward_repeats_bit_for_bit_and_leaves_out_what_is_not_wanted():
     x, w, dy, p, (dx, dw, db) = check_linear_backward(3000, 200, 128, "gelu")
     again = whtmix.linear_backward(x, w, dy, p, "gelu")
