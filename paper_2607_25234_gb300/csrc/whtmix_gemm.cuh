@@ -14,6 +14,9 @@
 // contraction down the rows): the panels are multiplied as they lie.  What lies past an edge reads as zero and is not stored, so
 // that every size runs; rows that are not 16-byte aligned are stored (and the residual read) with plain accesses, through the
 // same shared-memory panel.
+// PAIR: the two CTAs of a cluster share a tile of 256 x 256.  Each loads its 128 rows of A and 128 of the 256 rows of B, the first
+// one's warp 1 issues cta_group::2 products that read both CTAs' shared memory, and each CTA's tensor memory takes its 128 rows:
+// a third less comes from L2 and out of shared memory than with two tiles of 128 x 256.
 // Splits: item s of a split tile takes its share of the K blocks and stores fp32 partial rows [s * split_rows + m] (added to a
 // residual that lies the same way); the caller adds them up in a fixed order.
 #pragma once
@@ -51,15 +54,15 @@ constexpr int GEMM_BM = 128;
 constexpr uint32_t RING_BYTES = 192 * 1024, PANEL_BYTES = 128 * 128;
 constexpr size_t GEMM_SMEM = RING_BYTES + 2 * PANEL_BYTES;  // + 3 KB static: all of an SM's 227 KB
 
-template <int BN>
+template <int BN, bool PAIR>
 struct Ring {
-  static constexpr uint32_t A = GEMM_BM * 128, B = BN * 128, STAGE = A + B;
-  static constexpr int STAGES = RING_BYTES / STAGE;  // 4, 6, 8
+  static constexpr uint32_t A = GEMM_BM * 128, B = (PAIR ? BN / 2 : BN) * 128, STAGE = A + B;
+  static constexpr int STAGES = RING_BYTES / STAGE;  // 4, 6, 8; a pair's 6
 };
 
-template <int BN>
+template <int BN, bool PAIR>
 struct GemmBars {
-  uint64_t full[Ring<BN>::STAGES], empty[Ring<BN>::STAGES], dfull[2], dempty[2], rfull[2];
+  uint64_t full[Ring<BN, PAIR>::STAGES], empty[Ring<BN, PAIR>::STAGES], dfull[2], dempty[2], rfull[2];
 };
 
 __device__ __forceinline__ void tmem_ld32(uint32_t ta, float* r) {
@@ -76,6 +79,20 @@ __device__ __forceinline__ void tmem_ld32(uint32_t ta, float* r) {
 __device__ __forceinline__ uint64_t mn_major_desc(uint32_t addr, uint32_t panel) {
   return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(panel >> 4) << 16) |
          (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+template <bool E4M3>
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (E4M3)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The products so far have completed: an arrival at this barrier in both CTAs.
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(tc::smem_u32(bar)), "h"(static_cast<uint16_t>(3)) : "memory");
 }
 __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
@@ -249,31 +266,42 @@ __device__ __forceinline__ void panel_add<float>(const unsigned char* s, int row
 }
 
 // E4M3: A and B are e4m3 (else bf16); A_MN, B_MN: m / n along the rows of A / B (bf16 only); O: the output's type.
-template <bool E4M3, bool A_MN, bool B_MN, int BN, typename O>
+template <bool E4M3, bool A_MN, bool B_MN, int BN, bool PAIR, typename O>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant__ Gemm a) {
   static_assert(!E4M3 || (!A_MN && !B_MN), "8-bit operands lie with k along their rows");
-  using R = Ring<BN>;
+  static_assert(!PAIR || BN == 256, "a pair's tile is 256 x 256");
+  using R = Ring<BN, PAIR>;
+  constexpr int CTAS = PAIR ? 2 : 1, TILE_M = CTAS * GEMM_BM;
   constexpr int S = R::STAGES, BK = E4M3 ? 128 : 64, PW = Panel<O>::W, PANELS = BN / PW;
   constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
-                             (static_cast<uint32_t>(BN >> 3) << 17) | ((128u >> 4) << 24);
+                             (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>(TILE_M >> 4) << 24);
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ GemmBars<BN> bars;
+  __shared__ GemmBars<BN, PAIR> bars;
   __shared__ uint32_t tmem_slot;
   __shared__ __align__(16) float s_bias[2][2][PW], s_scale[2][2][PW];  // of a group's panel and its next
   const uint32_t ring = tc::smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.tiles_m * a.tiles_n * a.splits;
-  const bool alternate = items > static_cast<int>(gridDim.x);
-  if (warp == 0) tc::tmem_alloc(&tmem_slot, 2 * BN);
+  const int unit = blockIdx.x / CTAS, units = gridDim.x / CTAS, rank = PAIR ? blockIdx.x % 2 : 0;
+  const bool alternate = items > units;
+  if (warp == 0) {
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&tmem_slot)), "r"(2 * BN) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      tc::tmem_alloc(&tmem_slot, 2 * BN);
+    }
+  }
   if (tid == 32) {
     for (int s = 0; s < S; ++s) tc::mbar_init(&bars.full[s], 1), tc::mbar_init(&bars.empty[s], 1);
-    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], alternate ? 4 : 8), tc::mbar_init(&bars.rfull[s], 1);
+    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], CTAS * (alternate ? 4 : 8)), tc::mbar_init(&bars.rfull[s], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma::prefetch(&a.ta);
     tma::prefetch(&a.tb);
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if constexpr (PAIR) tma::cluster_sync();  // the other CTA's barriers are set up
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_wait();
   const uint32_t tmem = tmem_slot;
@@ -281,7 +309,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   auto place = [&](int item, int& m0, int& n0, int& split) {
     const int tile = item % (a.tiles_m * a.tiles_n);
     split = item / (a.tiles_m * a.tiles_n);
-    m0 = tile / a.tiles_n * GEMM_BM;
+    m0 = tile / a.tiles_n * TILE_M + rank * GEMM_BM;  // this CTA's rows
     n0 = tile % a.tiles_n * BN;
   };
   auto first_block = [&](int split) { return static_cast<int>(static_cast<long long>(a.kblocks) * split / a.splits); };
@@ -289,10 +317,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0;
-      for (int item = blockIdx.x; item < items && !bad; item += gridDim.x) {
+      for (int item = unit; item < items && !bad; item += units) {
         int m0, n0, split;
         place(item, m0, n0, split);
-        const int k1 = first_block(split + 1);
+        const int k1 = first_block(split + 1), b0 = PAIR ? n0 + rank * (BN / 2) : n0;
         for (int kb = first_block(split); kb < k1; ++kb, ++it) {
           const int s = it % S;
           if (!tma::wait(&bars.empty[s], ((it / S) & 1) ^ 1)) {
@@ -300,29 +328,36 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
             break;
           }
           const uint32_t sa = ring + s * R::STAGE, sb = sa + R::A;
-          tma::expect_tx(&bars.full[s], R::STAGE);
+          if (rank == 0) tma::expect_tx(&bars.full[s], CTAS * R::STAGE);
+          const uint32_t full = PAIR ? tma::in_cta(tc::smem_u32(&bars.full[s]), 0) : 0;
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y) {
+            if constexpr (PAIR)
+              tma::load_2d_pair(dst, tm, x, y, full);
+            else
+              tma::load_2d(dst, tm, x, y, &bars.full[s]);
+          };
           if constexpr (A_MN) {
 #pragma unroll
-            for (int i = 0; i < GEMM_BM / 64; ++i) tma::load_2d(sa + i * 8192, &a.ta, m0 + 64 * i, kb * BK, &bars.full[s]);
+            for (int i = 0; i < GEMM_BM / 64; ++i) load(sa + i * 8192, &a.ta, m0 + 64 * i, kb * BK);
           } else {
-            tma::load_2d(sa, &a.ta, kb * BK, m0, &bars.full[s]);
+            load(sa, &a.ta, kb * BK, m0);
           }
           if constexpr (B_MN) {
 #pragma unroll
-            for (int i = 0; i < BN / 64; ++i) tma::load_2d(sb + i * 8192, &a.tb, n0 + 64 * i, kb * BK, &bars.full[s]);
+            for (int i = 0; i < BN / CTAS / 64; ++i) load(sb + i * 8192, &a.tb, b0 + 64 * i, kb * BK);
           } else {
-            tma::load_2d(sb, &a.tb, kb * BK, n0, &bars.full[s]);
+            load(sb, &a.tb, kb * BK, b0);
           }
         }
       }
       // the copies in flight have landed before the CTA can end
-      for (uint32_t j = it > S ? it - S : 0; j < it; ++j)
+      for (uint32_t j = it > S ? it - S : 0; rank == 0 && j < it; ++j)
         if (!tma::wait(&bars.full[j % S], (j / S) & 1)) bad |= 1;
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       uint32_t it = 0, i = 0;
-      for (int item = blockIdx.x; item < items && !bad; item += gridDim.x, ++i) {
+      for (int item = unit; item < items && !bad; item += units, ++i) {
         int m0, n0, split;
         place(item, m0, n0, split);
         const int d = i & 1, k0 = first_block(split), k1 = first_block(split + 1);
@@ -344,14 +379,16 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
             const uint64_t da = A_MN ? mn_major_desc(sa + ks * 2048, 8192) : tc::sw128_desc(sa + ks * 32);
             const uint64_t db = B_MN ? mn_major_desc(sb + ks * 2048, 8192) : tc::sw128_desc(sb + ks * 32);
             const uint32_t acc = kb > k0 || ks > 0;
-            if constexpr (E4M3)
+            if constexpr (PAIR)
+              mma_pair<E4M3>(tmem + d * BN, da, db, IDESC, acc);
+            else if constexpr (E4M3)
               mma_e4m3(tmem + d * BN, da, db, IDESC, acc);
             else
               tc::mma_bf16(tmem + d * BN, da, db, IDESC, acc);
           }
-          tc::mma_commit(&bars.empty[s]);
+          if constexpr (PAIR) commit_pair(&bars.empty[s]); else tc::mma_commit(&bars.empty[s]);
         }
-        tc::mma_commit(&bars.dfull[d]);
+        if constexpr (PAIR) commit_pair(&bars.dfull[d]); else tc::mma_commit(&bars.dfull[d]);
       }
       // every product has completed before the tensor memory is freed
       for (uint32_t j = i > 2 ? i - 2 : 0; j < i; ++j)
@@ -368,7 +405,17 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
     };
     // the group's tiles, and of the next one's columns gt, gt + 128 the bias and scale, of its row the scale: on their way while a
     // tile is stored
-    const int step = alternate ? 1 : 2, p0 = alternate ? 0 : g, stride = alternate ? 2 * gridDim.x : gridDim.x;
+    const int step = alternate ? 1 : 2, p0 = alternate ? 0 : g, stride = alternate ? 2 * units : units;
+    auto accumulator_read = [&](int d) {
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (PAIR)
+          tma::arrive_in(tma::in_cta(tc::smem_u32(&bars.dempty[d]), 0));
+        else
+          tma::arrive(&bars.dempty[d]);
+      }
+    };
     constexpr int HELD = (BN + 127) / 128;
     float next_bias[HELD], next_scale[HELD], next_sm = 1.f;
     auto fetch = [&](int item) {
@@ -383,7 +430,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       }
       if (a.sm) next_sm = m0 + row < a.M ? __ldg(a.sm + m0 + row) : 1.f;
     };
-    const int first = blockIdx.x + (alternate ? g * gridDim.x : 0);
+    const int first = unit + (alternate ? g * units : 0);
     if (alternate) i = g;
     fetch(first);
     for (int item = first; item < items; item += stride, i += step == 1 ? 2 : 1) {
@@ -441,11 +488,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
 #pragma unroll
           for (int c = 0; c < PW; ++c) v[c] = 0.f;
         }
-        if (p + step >= panels) {  // the accumulator has been read
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) tma::arrive(&bars.dempty[d]);
-        }
+        if (p + step >= panels) accumulator_read(d);
         const float *sb = s_bias[g][turn], *ss = s_scale[g][turn];
         if (a.sm) {
 #pragma unroll
@@ -471,7 +514,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
             sync_group();
             if (a.p_plain) {
               panel_plain<__nv_bfloat16, true>(st, a.p, a.ps, m0, a.M, col0, a.N, gt);
-            } else if (gt == 0) {
+            } else if (gt == 0 && (!PAIR || m0 < a.M)) {
               tma::store_2d(&a.tp, col0, m0, st_u);
               tma::commit();
               tma::wait_read();
@@ -505,15 +548,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
         sync_group();
         if (a.y_plain) {
           panel_plain<O, true>(st, a.y, a.ys, m0, a.M, col0, a.N, gt);
-        } else if (gt == 0) {
+        } else if (gt == 0 && (!PAIR || m0 < a.M)) {
           tma::store_2d(&a.ty, col0, yrow, st_u);
           tma::commit();
         }
       }
       if (!waited) {  // no panel of this tile for this group
         wait(&bars.dfull[d], (i >> 1) & 1);
-        __syncwarp();
-        if (lane == 0) tma::arrive(&bars.dempty[d]);
+        accumulator_read(d);
       }
     }
     if (gt == 0) tma::wait_done();
@@ -522,9 +564,15 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   if (bad) atomicOr(a.err, bad << 16);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if constexpr (PAIR) tma::cluster_sync();  // neither CTA ends while the other's products or arrivals reach into it
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_trigger();
-  if (warp == 0) tc::tmem_dealloc(tmem, 2 * BN);
+  if (warp == 0) {
+    if constexpr (PAIR)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
+    else
+      tc::tmem_dealloc(tmem, 2 * BN);
+  }
 }
 
 // Raises a kernel's shared-memory limit once a device; `raised` holds the devices (of the first 64) where that is done.
@@ -540,20 +588,49 @@ inline cudaError_t raise_smem(const void* kernel, size_t bytes, std::atomic<uint
 }
 
 // One instance's launch: a persistent grid of at most one CTA per SM.
-template <bool E4M3, bool A_MN, bool B_MN, int BN, typename O>
+template <bool E4M3, bool A_MN, bool B_MN, int BN, bool PAIR, typename O>
 cudaError_t launch_gemm(const Gemm& g, int sms, cudaStream_t stream) {
-  const void* k = reinterpret_cast<const void*>(k_gemm<E4M3, A_MN, B_MN, BN, O>);
+  auto k = k_gemm<E4M3, A_MN, B_MN, BN, PAIR, O>;
   static std::atomic<uint64_t> raised{0};
-  const cudaError_t e = raise_smem(k, GEMM_SMEM, raised);
+  const cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), GEMM_SMEM, raised);
   if (e != cudaSuccess) return e;
-  const long long items = static_cast<long long>(g.tiles_m) * g.tiles_n * g.splits;
-  Gemm c = g;
-  void* args[] = {&c};
-  return launch_pdl(k, static_cast<unsigned>(items < sms ? items : sms), GEMM_THREADS, GEMM_SMEM, stream, args);
+  constexpr int CTAS = PAIR ? 2 : 1;
+  const long long items = static_cast<long long>(g.tiles_m) * g.tiles_n * g.splits, most = sms / CTAS;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(CTAS * (items < most ? items : most)));
+  cfg.blockDim = dim3(GEMM_THREADS);
+  cfg.dynamicSmemBytes = GEMM_SMEM;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CTAS;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CTAS;
+  return cudaLaunchKernelEx(&cfg, k, g);
 }
 
-// whtmix_gemm_fwd.cu: y from x and W; whtmix_gemm_bwd.cu: dx (A with k, B with n along its rows) and dw (both m / n)
-cudaError_t gemm_forward(const Gemm& g, bool e4m3, bool out_f32, int bn, int sms, cudaStream_t stream);
+// The products by tile width: 64, 128, 256, or TILE_PAIR, two CTAs on 256 x 256.
+constexpr int TILE_PAIR = 512;
+inline int tile_rows(int bn) { return bn == TILE_PAIR ? 2 * GEMM_BM : GEMM_BM; }
+inline int tile_cols(int bn) { return bn == TILE_PAIR ? 256 : bn; }
+inline int tile_b_rows(int bn) { return bn == TILE_PAIR ? 128 : bn; }  // of B that a CTA loads
+template <bool E4M3, bool A_MN, bool B_MN, typename O>
+cudaError_t gemm_by_width(const Gemm& g, int bn, int sms, cudaStream_t stream) {
+  switch (bn) {
+    case 64: return launch_gemm<E4M3, A_MN, B_MN, 64, false, O>(g, sms, stream);
+    case 128: return launch_gemm<E4M3, A_MN, B_MN, 128, false, O>(g, sms, stream);
+    case 256: return launch_gemm<E4M3, A_MN, B_MN, 256, false, O>(g, sms, stream);
+    default: return launch_gemm<E4M3, A_MN, B_MN, 256, true, O>(g, sms, stream);
+  }
+}
+
+// whtmix_gemm_fwd.cu, whtmix_gemm_e4m3.cu: y from x and W; whtmix_gemm_dx.cu (A with k, B with n along its rows); whtmix_gemm_dw.cu
+// (both m / n)
+cudaError_t gemm_forward(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
+cudaError_t gemm_e4m3(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dx(const Gemm& g, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dw(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 
@@ -569,7 +646,6 @@ struct DpProduct {
   unsigned int* err;
 };
 cudaError_t gemm_dp(const DpProduct& g, int sms, cudaStream_t stream);
-
 
 }  // namespace linear
 }  // namespace whtmix

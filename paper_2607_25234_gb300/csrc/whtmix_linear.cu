@@ -220,29 +220,32 @@ static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
 static int pitch_of(int cols, int es) { return (cols + 16 / es - 1) / (16 / es) * (16 / es); }
 static int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
 
-// Tile width and splits of a product of tiles_m rows of tiles, N columns and kblocks K blocks.  A block of 128 x BN costs BLOCK
-// clocks of one SM, not in proportion to BN: the operands' way from L2 and out of shared memory bounds the narrow tiles (measured
-// at [8192, 4096] x [4096, 4096]: 545 clocks at 256, 450 at 128).  A tile costs about TILE_CLOCKS besides, a split product's partial
-// tiles their way through memory.
+// Tile width and splits of a product of M rows, N columns and kblocks K blocks.  A block of a tile costs BLOCK clocks of an SM (of a
+// pair of them), not in proportion to its width: the operands' way from L2 and out of shared memory bounds the narrow tiles
+// (measured at [8192, 4096] x [4096, 4096]: 545 clocks at 256 columns, 450 at 128; a pair's 256 x 256 takes 470).  A tile costs about
+// TILE_CLOCKS besides, more where two CTAs wait for each other, a split product's partial tiles their way through memory.  Pairs
+// against single tiles, us: that product 157.7 and 168.5; [8192, 1024] x [1024, 1024] 18.7 and 17.2; 64800 tokens of 128 channels to
+// 512 32.2 and 28.6: long K axes take pairs, short ones do not.
 struct Plan {
   int bn, splits;
 };
-static Plan plan_product(long long tiles_m, int N, int kblocks, int sms, int max_splits) {
-  constexpr double TILE_CLOCKS = 1500.0;
+static Plan plan_product(long long M, int N, int kblocks, int sms, int max_splits) {
+  constexpr double TILE_CLOCKS = 1500.0, PAIR_TILE_CLOCKS = 3700.0;
   Plan best{256, 1};
   double best_cost = 1e300;
-  for (int bn = 256; bn >= 64; bn >>= 1) {
-    const long long tiles = tiles_m * ceil_div(N, bn);
-    const double block = bn == 256 ? 545.0 : bn == 128 ? 450.0 : 400.0;
+  for (int bn = TILE_PAIR; bn >= 64; bn >>= 1) {
+    const int units = bn == TILE_PAIR ? sms / 2 : sms;  // tiles at a time
+    const long long tiles = static_cast<long long>(ceil_div(M, tile_rows(bn))) * ceil_div(N, tile_cols(bn));
+    const double block = bn == TILE_PAIR ? 470.0 : bn == 256 ? 545.0 : bn == 128 ? 450.0 : 400.0;
     // one split, or as many as fill 1 .. 4 waves
     for (int w = 0; w <= 4; ++w) {
-      const long long fill = w == 0 ? 1 : static_cast<long long>(w) * sms / tiles;
+      const long long fill = w == 0 ? 1 : static_cast<long long>(w) * units / tiles;
       const int s = static_cast<int>(fill < max_splits ? (fill < kblocks ? fill : kblocks) : (max_splits < kblocks ? max_splits : kblocks));
       if (s < 1 || (w > 0 && s == 1)) continue;
-      const double waves = ceil_div(tiles * s, sms);
+      const double waves = ceil_div(tiles * s, units);
       // partial tiles: written and read back, 8 bytes an element, at about 3000 bytes a clock for the whole device
-      const double join = s > 1 ? 4000.0 + static_cast<double>(tiles) * 128.0 * bn * s * 8.0 / 3000.0 : 0.0;
-      const double cost = waves * (ceil_div(kblocks, s) * block + TILE_CLOCKS) + join;
+      const double join = s > 1 ? 4000.0 + static_cast<double>(tiles) * tile_rows(bn) * tile_cols(bn) * s * 8.0 / 3000.0 : 0.0;
+      const double cost = waves * (ceil_div(kblocks, s) * block + (bn == TILE_PAIR ? PAIR_TILE_CLOCKS : TILE_CLOCKS)) + join;
       if (cost < best_cost * 0.999) best_cost = cost, best = {bn, s};
     }
   }
@@ -285,10 +288,9 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
   if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
   if (use_few(a.T, ceil_div(a.K, 128 / es))) return forward_few(a, x, xs, w, wst, err, sms, stream);
   Gemm g{};
-  g.tiles_m = ceil_div(a.T, GEMM_BM);
   g.kblocks = ceil_div(a.K, 128 / es);
-  const Plan pl = plan_product(g.tiles_m, a.N, g.kblocks, sms, 1);
-  g.tiles_n = ceil_div(a.N, pl.bn);
+  const Plan pl = plan_product(a.T, a.N, g.kblocks, sms, 1);
+  g.tiles_m = ceil_div(a.T, tile_rows(pl.bn)), g.tiles_n = ceil_div(a.N, tile_cols(pl.bn));
   g.splits = 1;
   g.M = static_cast<int>(a.T), g.N = a.N, g.act = a.act;
   g.bias = a.bias, g.sm = a.x_scale, g.sn = a.w_scale;
@@ -298,12 +300,12 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
   g.r_plain = a.r && !tma::mappable(a.r, a.T, a.rs, os);
   g.p_plain = a.p && !tma::storable(a.p, a.T, a.N, a.ps, 2);
   g.err = err;
-  if (!tma::encode_rows(&g.ta, x, es, a.T, a.K, xs, GEMM_BM) || !tma::encode_rows(&g.tb, w, es, a.N, a.K, wst, pl.bn) ||
+  if (!tma::encode_rows(&g.ta, x, es, a.T, a.K, xs, GEMM_BM) || !tma::encode_rows(&g.tb, w, es, a.N, a.K, wst, tile_b_rows(pl.bn)) ||
       (!g.y_plain && !tma::encode_rows(&g.ty, a.y, os, a.T, a.N, a.ys, GEMM_BM)) ||
       (g.has_r && !g.r_plain && !tma::encode_rows(&g.tr, a.r, os, a.T, a.N, a.rs, GEMM_BM)) ||
       (g.has_p && !g.p_plain && !tma::encode_rows(&g.tp, a.p, 2, a.T, a.N, a.ps, GEMM_BM)))
     return cudaErrorInvalidValue;
-  return gemm_forward(g, a.e4m3, a.out_f32, pl.bn, sms, stream);
+  return a.e4m3 ? gemm_e4m3(g, a.out_f32, pl.bn, sms, stream) : gemm_forward(g, a.out_f32, pl.bn, sms, stream);
 }
 
 // Threads a row of k_dp, eight columns each.
@@ -345,9 +347,8 @@ static BackwardPlan plan_backward(const Backward& a, int sms) {
     if (a.db && b.chunks > 1) b.db_off = take(static_cast<size_t>(b.chunks) * a.N * 4);
   }
   if (a.dw) {
-    const int tiles_m = ceil_div(a.N, GEMM_BM);
-    b.dw = plan_product(tiles_m, a.K, ceil_div(a.T, 64), sms, 2 * sms);
-    b.split_rows = tiles_m * GEMM_BM;
+    b.dw = plan_product(a.N, a.K, ceil_div(a.T, 64), sms, 2 * sms);
+    b.split_rows = ceil_div(a.N, tile_rows(b.dw.bn)) * tile_rows(b.dw.bn);
     if (b.dw.splits > 1) b.dw_off = take(static_cast<size_t>(b.dw.splits) * b.split_rows * pitch_of(a.K, 4) * 4);
   }
   return b;
@@ -408,10 +409,9 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
   }
   if (a.dx && !b.fused) {
     Gemm g{};
-    g.tiles_m = ceil_div(a.T, GEMM_BM);
     g.kblocks = ceil_div(a.N, 64);
-    const Plan pl = plan_product(g.tiles_m, a.K, g.kblocks, sms, 1);
-    g.tiles_n = ceil_div(a.K, pl.bn);
+    const Plan pl = plan_product(a.T, a.K, g.kblocks, sms, 1);
+    g.tiles_m = ceil_div(a.T, tile_rows(pl.bn)), g.tiles_n = ceil_div(a.K, tile_cols(pl.bn));
     g.splits = 1;
     g.M = static_cast<int>(a.T), g.N = a.K;
     g.y = a.dx, g.ys = a.dxs, g.y_plain = !tma::storable(a.dx, a.T, a.K, a.dxs, 2);
@@ -424,9 +424,8 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
   }
   if (a.dw) {
     Gemm g{};
-    g.tiles_m = ceil_div(a.N, GEMM_BM);
     g.kblocks = ceil_div(a.T, 64);
-    g.tiles_n = ceil_div(a.K, b.dw.bn);
+    g.tiles_m = ceil_div(a.N, tile_rows(b.dw.bn)), g.tiles_n = ceil_div(a.K, tile_cols(b.dw.bn));
     g.splits = b.dw.splits;
     g.split_rows = b.split_rows;
     g.M = a.N, g.N = a.K;

@@ -331,11 +331,19 @@ def test_eight_bit_linear_against_float64(T, N, K):
     check_linear(T, N, K, "none", False, False, True, F32, False)
 
 
+@pytest.mark.parametrize("T,N,K", [(8192, 4096, 1024), (5000, 4100, 2000), (9001, 2048, 1003)])
+def test_large_products_against_float64(T, N, K):
+    """Long K axes: two CTAs on a tile; the last tiles of rows and columns cut."""
+    check_linear(T, N, K, "gelu", True, True, False, BF, True)
+    check_linear(T, N, K, "none", True, False, True, F32, False)
+    check_linear_backward(T, N, K, "silu")
+
+
 def test_linear_of_integers_is_exact():
     """Small integers: every product and sum is exact in float32, so that one wrong element shows."""
     g = torch.Generator(device="cuda")
     g.manual_seed(7)
-    for T, N, K in [(1, 300, 200), (50, 129, 77), (120, 256, 1024), (300, 777, 333), (2000, 520, 128)]:
+    for T, N, K in [(1, 300, 200), (50, 129, 77), (120, 256, 1024), (300, 777, 333), (2000, 520, 128), (8000, 4096, 1500)]:
         x = torch.randint(-3, 4, (T, K), generator=g, device="cuda").to(BF)
         w = torch.randint(-3, 4, (N, K), generator=g, device="cuda").to(BF)
         b = torch.randint(-9, 10, (N,), generator=g, device="cuda").float()
