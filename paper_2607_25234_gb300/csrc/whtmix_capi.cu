@@ -175,6 +175,7 @@ std::map<std::tuple<int, cudaStream_t, int>, WsEntry> g_ws;
 
 int cached_workspace(int dev, cudaStream_t stream, size_t need, void** out, int slot = 0) {
   std::lock_guard<std::mutex> lk(g_mu);
+  if (need < HEADER_BYTES) need = HEADER_BYTES;  // the memset below
   WsEntry& w = g_ws[std::make_tuple(dev, stream, slot)];
   if (w.bytes < need) {
     if (w.ptr) {

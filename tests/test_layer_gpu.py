@@ -588,6 +588,24 @@ def test_on_another_stream_and_in_a_graph():
     assert all(torch.equal(a, b_) for a, b_ in zip(got, want))
 
 
+def test_a_streams_first_call_may_be_the_smallest():
+    """A stream's first workspace for a call that needs a few bytes."""
+    x, w, dy = rand(1, 1, 1), torch.ones(1, device="cuda"), rand(2, 1, 1)
+    whtmix.release_workspaces()
+    check_norm_backward(x, w, dy, None)
+    for T, N, K in ((1, 1, 1), (3, 2, 5)):
+        a, b, g = rand(1, T, K).to(BF), rand(2, N, K).to(BF), rand(3, T, N).to(BF)
+        whtmix.release_workspaces()
+        y = whtmix.linear(a, b)
+        whtmix.release_workspaces()
+        dx, dw, db = whtmix.linear_backward(a, b, g, need_db=True)
+        whtmix.sync()
+        A, B, G = a.double(), b.double(), g.double()
+        for got, left, right in ((y, A, B.T), (dx, G, B), (dw, G.T, A), (db, torch.ones(1, T, device="cuda").double(), G)):
+            ref = (left @ right).reshape(got.shape)
+            close(got, ref, U16 * 1.01 * ref.abs() + 2.0 ** -18 * (left.abs() @ right.abs()).reshape(got.shape))
+
+
 def test_offsets_beyond_32_bits():
     """Rows at more than 2^31 and 2^32 elements: the first, one past each and the last are right."""
     T, D = (1 << 32) // 4096 + 70, 4096
