@@ -8,8 +8,8 @@
 //              while the last one's accumulator is read);
 //   warps 4-11 epilogue, two groups of four warps, which take every other tile (a CTA with one tile: every other panel of it); a
 //              panel is 128 bytes of each of the 128 rows: accumulator -> registers, the epilogue, shared memory, TMA store.
-//              Of a panel's 3300 clocks with gelu 1850 are the special-function unit's where both groups work on panels of one
-//              tile, in step; apart, one's stores cover the other's arithmetic.
+//              On panels of one tile both groups work in step and wait for the special-function unit together; a tile apart,
+//              one's stores cover the other's arithmetic.
 // A and B may lie with k along a row (the forward; A of dx = dp W) or with m / n along a row (B of dx; both of dw = dp^T x, the
 // contraction down the rows): the panels are multiplied as they lie.  What lies past an edge reads as zero and is not stored, so
 // that every size runs; rows that are not 16-byte aligned are stored (and the residual read) with plain accesses, through the
@@ -125,10 +125,9 @@ __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
   return r;
 }
 
-// 1 / (1 + 2^t) for both of t.  The special-function unit takes 16 operations a clock, an exponential and a reciprocal for each
-// value bound the short products' epilogues; here one reciprocal serves two: 1 / (d0 d1) times the other.  t is cut at 60, so that
-// the product stays finite and a NaN becomes a number that leaves the other value alone (the caller multiplies by its own z, which
-// is NaN then too).
+// 1 / (1 + 2^t) for both of t.  A reciprocal takes the special-function unit twice an exponential's time (measured: 16 and 32
+// results a clock and SM), so one serves two values: 1 / (d0 d1) times the other.  t is cut at 60, so that the product stays finite
+// and a NaN becomes a number that leaves the other value alone (the caller multiplies by its own z, which is NaN then too).
 __device__ __forceinline__ Pair logistic2(Pair t) {
   float t0, t1, e0, e1, d0, d1, r;
   unpair(t, t0, t1);

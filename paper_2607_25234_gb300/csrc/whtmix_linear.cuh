@@ -1,5 +1,5 @@
-// whtmix_linear.cuh -- the matrix products' arguments and launches (whtmix_gemm*.cu, whtmix_linear.cu), shared with the host side
-// of the C ABI, and the activations of their epilogues.
+// whtmix_linear.cuh -- the linear layer's arguments and launches (whtmix_linear.cu, which calls the products of whtmix_gemm*.cu and
+// whtmix_few.cu), shared with the host side of the C ABI.
 #pragma once
 
 #include <cuda_runtime.h>

@@ -61,7 +61,6 @@ __device__ __forceinline__ uint4 finish16(const Granules g, const uint8_t* p, co
   shift_bytes<4>(w, m);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint4 load16(const uint8_t* p, const Span s) { return finish16(fetch16(p, s), p, s); }
 
 // The first `bytes` (0 .. 16) of u, zeros beyond.
 __device__ __forceinline__ uint4 keep(uint4 u, int bytes) {

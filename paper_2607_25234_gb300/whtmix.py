@@ -1,7 +1,8 @@
 """Python binding of the WHTMix C ABI (``include/whtmix.h``): argument marshalling only.
 
 Every step of the mixer runs in the CUDA library ``_lib/libwhtmix.so``; this module passes device
-pointers, sizes and the current CUDA stream through ctypes.  torch supplies device memory and
+pointers, sizes and the current CUDA stream through ctypes, the layer operators' plain calls through a
+compiled module that does the same (``_lib/whtmix_torch.so``).  torch supplies device memory and
 streams.  There is no CPU path: a missing library or a CPU tensor raises.
 
 The operation (paper Section III-B, Eq. 1-4): Y_b = H_N (G (.) H_N X_b H_C) H_C / (N C) for every
@@ -10,6 +11,8 @@ plane X_b [N, C] of X [B, N, C]; the backward returns dX and dG = sum_b (H X_b H
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 import threading
 
@@ -96,6 +99,26 @@ def library(path: str | None = None) -> ctypes.CDLL:
                     getattr(lib, name).restype = ctypes.c_int
             _lib = lib
     return _lib
+
+
+_quick = None
+
+
+def _quick_path():
+    """The compiled quick path of the layer operators (csrc/whtmix_torch.cpp): a call with plain tensors and no result
+    given runs there; each of its functions returns None for any other call."""
+    global _quick
+    library()
+    with _lock:
+        if _quick is None:
+            if not os.path.exists(_build.QUICK):
+                raise RuntimeError(f"WHTMix binding not built ({_build.QUICK}); run __graft_entry__.build()")
+            loader = importlib.machinery.ExtensionFileLoader("whtmix_torch", _build.QUICK)
+            module = importlib.util.module_from_spec(importlib.util.spec_from_loader("whtmix_torch", loader))
+            loader.exec_module(module)
+            module.bind(_check)
+            _quick = module
+    return _quick
 
 
 def _check(rc: int, what: str):
@@ -404,6 +427,10 @@ def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = N
     Returns y, or with out_dtype float8_e4m3fn (values, scales): y = values * scales[..., None], one float32 scale a
     token; with a residual h is appended.  8-bit values that are allocated here have rows at a 16-byte pitch (a view
     of a wider tensor where the last axis is no multiple of 16)."""
+    if x.is_cuda and out is None and h is None and scale is None and stream is None:
+        done = (_quick or _quick_path()).rms_norm(x, w, residual, eps, out_dtype)
+        if done is not None:
+            return done
     dtype = x.dtype
     if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError(f"rms_norm takes float32 or bfloat16, got {dtype}")
@@ -453,6 +480,10 @@ def rms_norm_backward(h: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, dh: to
                       eps: float = 1e-6, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None, stream=None):
     """(dx, dw) of rms_norm from its sum h (x where it had no residual); dh is the gradient that reaches h
     directly.  dx is the gradient of x and of the residual; dw is float32."""
+    if h.is_cuda and dx is None and dw is None and stream is None:
+        done = (_quick or _quick_path()).rms_norm_backward(h, w, dy, dh, eps)
+        if done is not None:
+            return done
     dtype = h.dtype
     if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError(f"rms_norm_backward takes float32 or bfloat16, got {dtype}")
@@ -488,12 +519,16 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
     """y = act(x w^T + bias) + residual over the last axis: x [..., K] and w [N, K] bfloat16, or both float8_e4m3fn
     with float32 scales x_scale [...] and w_scale [N]; bias [N] float32; residual and y [..., N] of out_dtype
     (bfloat16 or float32).  preact=True, or a bfloat16 tensor, also returns the pre-activation: (y, preact)."""
+    act = _activation(activation)
+    if x.is_cuda and out is None and stream is None and (preact is None or preact.__class__ is bool):
+        done = (_quick or _quick_path()).linear(x, w, bias, act, residual, x_scale, w_scale, preact, out_dtype)
+        if done is not None:
+            return done
     dtype, device, index = x.dtype, x.device, x.get_device()
     if dtype != torch.bfloat16 and dtype != E4M3:
         raise TypeError(f"linear takes bfloat16 or {E4M3}, got {dtype}")
     if out_dtype != torch.bfloat16 and out_dtype != torch.float32:
         raise TypeError(f"linear writes bfloat16 or float32, not {out_dtype}")
-    act = _activation(activation)
     N, K = w.shape if w.dim() == 2 else (0, 0)
     if w.dtype != dtype or K != x.shape[-1]:
         raise ValueError(f"w must be {dtype} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")
@@ -538,12 +573,16 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch
     """(dx, dw, db) of linear for the upstream gradient dy of y (bfloat16), from the stored pre-activation p (needed
     unless the activation is "none"); None in the place of a gradient that is not needed.  The residual's gradient is
     dy itself.  dw is bfloat16 or float32, db float32."""
+    act = _activation(activation)
+    if x.is_cuda and dx is None and dw is None and db is None and stream is None:
+        done = (_quick or _quick_path()).linear_backward(x, w, dy, p, act, need_dx, need_dw, need_db, dw_dtype)
+        if done is not None:
+            return done
     device, index = x.device, x.get_device()
     if x.dtype != torch.bfloat16:
         raise TypeError(f"linear_backward takes bfloat16, got {x.dtype}")
     if dw_dtype != torch.bfloat16 and dw_dtype != torch.float32:
         raise TypeError(f"dw is bfloat16 or float32, not {dw_dtype}")
-    act = _activation(activation)
     N, K = w.shape if w.dim() == 2 else (0, 0)
     if w.dtype != torch.bfloat16 or K != x.shape[-1]:
         raise ValueError(f"w must be {torch.bfloat16} [N, {x.shape[-1]}], got {w.dtype} {list(w.shape)}")

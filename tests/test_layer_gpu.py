@@ -588,6 +588,39 @@ def test_on_another_stream_and_in_a_graph():
     assert all(torch.equal(a, b_) for a, b_ in zip(got, want))
 
 
+@pytest.mark.parametrize("lead", [(1,), (5, 7), (130,)])
+def test_calls_with_and_without_given_results_agree(lead):
+    """The compiled path of plain calls and the step-by-step one (results given) launch the same work."""
+    K, N = 96, 80
+    x, r = rand(1, *lead, K).to(BF), rand(2, *lead, K).to(BF)
+    gain = 1.0 + 0.1 * rand(3, K)
+    new = lambda *shape, dtype=BF: torch.empty(*shape, dtype=dtype, device="cuda")
+    y, h = whtmix.rms_norm(x, gain, residual=r)
+    y2, h2 = whtmix.rms_norm(x, gain, residual=r, out=new(*lead, K), h=new(*lead, K))
+    assert torch.equal(y, y2) and torch.equal(h, h2)
+    assert torch.equal(whtmix.rms_norm(h, gain), whtmix.rms_norm(h, gain, out=new(*lead, K)))
+    q, s, h3 = whtmix.rms_norm(x, gain, residual=r, out_dtype=E4M3)
+    q2, s2, _ = whtmix.rms_norm(x, gain, residual=r, out_dtype=E4M3, scale=new(*lead, dtype=F32))
+    assert torch.equal(q.float(), q2.float()) and torch.equal(s, s2) and torch.equal(h, h3)
+    dx, dw = whtmix.rms_norm_backward(h, gain, x, dh=r)
+    dx2, dw2 = whtmix.rms_norm_backward(h, gain, x, dh=r, dx=new(*lead, K))
+    assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    w, b, res = rand(4, N, K).to(BF), rand(5, N), rand(6, *lead, N).to(BF)
+    z, p = whtmix.linear(x, w, b, "gelu", residual=res, preact=True)
+    z2, p2 = whtmix.linear(x, w, b, "gelu", residual=res, preact=True, out=new(*lead, N))
+    assert torch.equal(z, z2) and torch.equal(p, p2) and z.shape == (*lead, N)
+    assert torch.equal(whtmix.linear(x, w, b, "gelu", residual=res, preact=False), z)
+    wq, ws = whtmix.quantize_rows(w)
+    eight = whtmix.linear(q, wq, b, "silu", x_scale=s, w_scale=ws, out_dtype=F32)
+    again = whtmix.linear(q, wq, b, "silu", x_scale=s, w_scale=ws, out_dtype=F32, out=new(*lead, N, dtype=F32))
+    assert eight.dtype == F32 and torch.equal(eight, again)
+    for need in ((True, True, True), (1, 0, 1), (False, True, False)):
+        got = whtmix.linear_backward(x, w, res, p, "gelu", *need, dw_dtype=F32)
+        all_given = whtmix.linear_backward(x, w, res, p, "gelu", dw_dtype=F32, dx=new(*lead, K))
+        for g, a, wanted in zip(got, all_given, need):
+            assert (g is None) if not wanted else torch.equal(g, a)
+
+
 def test_a_streams_first_call_may_be_the_smallest():
     """A stream's first workspace for a call that needs a few bytes."""
     x, w, dy = rand(1, 1, 1), torch.ones(1, device="cuda"), rand(2, 1, 1)
