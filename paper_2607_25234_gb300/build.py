@@ -23,7 +23,7 @@ QUICK_SOURCE = "whtmix_torch.cpp"
 SOURCES = ["whtmix_capi.cu", "whtmix_fast_f32.cu", "whtmix_fast_bf16.cu", "whtmix_fast_sep_f32.cu", "whtmix_block.cu", "whtmix_plane.cu", "whtmix_small.cu",
            "whtmix_fast_sep_bf16.cu", "whtmix_fast_x16.cu", "whtmix_noalloc.cu", "whtmix_proj.cu", "whtmix_block_bwd.cu",
            "whtmix_layer.cu", "whtmix_norm.cu", "whtmix_linear.cu", "whtmix_gemm_fwd.cu", "whtmix_gemm_e4m3.cu",
-           "whtmix_gemm_dx.cu", "whtmix_gemm_dw.cu",
+           "whtmix_gemm_four.cu", "whtmix_gemm_e4m3_four.cu", "whtmix_gemm_dx.cu", "whtmix_gemm_dw.cu",
            "whtmix_few.cu", "whtmix_gemm_dp.cu"]
 OBJDIR = os.path.join(LIBDIR, "obj")
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"

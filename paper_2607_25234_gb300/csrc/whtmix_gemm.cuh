@@ -2,12 +2,13 @@
 //
 //   C[m, n] = sum over k of A[m, k] B[n, k]        y = act(s_m s_n C + b_n) + r
 //
-// One persistent CTA per SM, 384 threads, tiles of 128 x BN (BN = 64, 128, 256) in turn, the K axis in blocks of 128 bytes:
-//   warp 0     TMA loads of A and B blocks into a ring of stages (192 KB in all);
+// One persistent CTA per SM, 384 or 640 threads, tiles of 128 x BN (BN = 64, 128, 256) in turn, the K axis in blocks of 128 bytes:
+//   warp 0     TMA loads of A and B blocks into a ring of stages (192 or 144 KB in all);
 //   warp 1     four tcgen05.mma a block (fp32 accumulators in tensor memory, two tiles' worth: the next tile's products run
 //              while the last one's accumulator is read);
 //   warps 4-11 epilogue, two groups of four warps, which take every other tile (a CTA with one tile: every other panel of it); a
-//              panel is 128 bytes of each of the 128 rows: accumulator -> registers, the epilogue, shared memory, TMA store.
+//   (4-19)     panel is 128 bytes of each of the 128 rows: accumulator -> registers, the epilogue, shared memory, TMA store.  Four
+//              groups: two to a tile, 32 columns at a time in registers.
 //              On panels of one tile both groups work in step and wait for the special-function unit together; a tile apart,
 //              one's stores cover the other's arithmetic.
 // A and B may lie with k along a row (the forward; A of dx = dp W) or with m / n along a row (B of dx; both of dw = dp^T x, the
@@ -49,20 +50,25 @@ struct Gemm {
   unsigned int* err;
 };
 
-constexpr int GEMM_THREADS = 384;
 constexpr int GEMM_BM = 128;
-constexpr uint32_t RING_BYTES = 192 * 1024, PANEL_BYTES = 128 * 128;
-constexpr size_t GEMM_SMEM = RING_BYTES + 2 * PANEL_BYTES;  // + 3 KB static: all of an SM's 227 KB
+constexpr uint32_t PANEL_BYTES = 128 * 128;
+template <int GROUPS>
+constexpr int GEMM_THREADS = 128 + 128 * GROUPS;
+// the stages' bytes, a panel for each epilogue group behind them: with 3 or 5 KB static an SM's 227 KB at most
+template <int GROUPS>
+constexpr uint32_t RING_BYTES = (GROUPS == 2 ? 192 : 144) * 1024;
+template <int GROUPS>
+constexpr size_t GEMM_SMEM = RING_BYTES<GROUPS> + GROUPS * PANEL_BYTES;
 
-template <int BN, bool PAIR>
+template <int BN, bool PAIR, int GROUPS>
 struct Ring {
   static constexpr uint32_t A = GEMM_BM * 128, B = (PAIR ? BN / 2 : BN) * 128, STAGE = A + B;
-  static constexpr int STAGES = RING_BYTES / STAGE;  // 4, 6, 8; a pair's 6
+  static constexpr int STAGES = RING_BYTES<GROUPS> / STAGE;  // two groups: 4, 6, 8, a pair's 6; four: 3, 4
 };
 
-template <int BN, bool PAIR>
+template <int BN, bool PAIR, int GROUPS>
 struct GemmBars {
-  uint64_t full[Ring<BN, PAIR>::STAGES], empty[Ring<BN, PAIR>::STAGES], dfull[2], dempty[2], rfull[2];
+  uint64_t full[Ring<BN, PAIR, GROUPS>::STAGES], empty[Ring<BN, PAIR, GROUPS>::STAGES], dfull[2], dempty[2], rfull[GROUPS];
 };
 
 __device__ __forceinline__ void tmem_ld32(uint32_t ta, float* r) {
@@ -219,34 +225,31 @@ __device__ __forceinline__ void panel_plain(unsigned char* s, void* g, long long
   }
 }
 
-template <typename O>
-__device__ __forceinline__ void panel_put(unsigned char* s, int row, const float* v);
-template <>
-__device__ __forceinline__ void panel_put<__nv_bfloat16>(unsigned char* s, int row, const float* v) {
+// 16-byte pieces q0 .. q0 + Q - 1 of a row of a panel
+template <int Q>
+__device__ __forceinline__ void panel_put(unsigned char* s, int row, int q0, const float* v, __nv_bfloat16) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
+  for (int q = 0; q < Q; ++q) {
     uint32_t h[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * q + 2 * j], v[8 * q + 2 * j + 1]);
       h[j] = *reinterpret_cast<uint32_t*>(&b);
     }
-    *reinterpret_cast<uint4*>(s + row * 128 + ((q ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4*>(s + row * 128 + (((q0 + q) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
   }
 }
-template <>
-__device__ __forceinline__ void panel_put<float>(unsigned char* s, int row, const float* v) {
+template <int Q>
+__device__ __forceinline__ void panel_put(unsigned char* s, int row, int q0, const float* v, float) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
-    *reinterpret_cast<float4*>(s + row * 128 + ((q ^ (row & 7)) << 4)) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  for (int q = 0; q < Q; ++q)
+    *reinterpret_cast<float4*>(s + row * 128 + (((q0 + q) ^ (row & 7)) << 4)) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
 }
-template <typename O>
-__device__ __forceinline__ void panel_add(const unsigned char* s, int row, float* v);
-template <>
-__device__ __forceinline__ void panel_add<__nv_bfloat16>(const unsigned char* s, int row, float* v) {
+template <int Q>
+__device__ __forceinline__ void panel_add(const unsigned char* s, int row, int q0, float* v, __nv_bfloat16) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const uint4 u = *reinterpret_cast<const uint4*>(s + row * 128 + ((q ^ (row & 7)) << 4));
+  for (int q = 0; q < Q; ++q) {
+    const uint4 u = *reinterpret_cast<const uint4*>(s + row * 128 + (((q0 + q) ^ (row & 7)) << 4));
     const uint32_t a[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -255,29 +258,33 @@ __device__ __forceinline__ void panel_add<__nv_bfloat16>(const unsigned char* s,
     }
   }
 }
-template <>
-__device__ __forceinline__ void panel_add<float>(const unsigned char* s, int row, float* v) {
+template <int Q>
+__device__ __forceinline__ void panel_add(const unsigned char* s, int row, int q0, float* v, float) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const float4 u = *reinterpret_cast<const float4*>(s + row * 128 + ((q ^ (row & 7)) << 4));
+  for (int q = 0; q < Q; ++q) {
+    const float4 u = *reinterpret_cast<const float4*>(s + row * 128 + (((q0 + q) ^ (row & 7)) << 4));
     v[4 * q] += u.x, v[4 * q + 1] += u.y, v[4 * q + 2] += u.z, v[4 * q + 3] += u.w;
   }
 }
 
 // E4M3: A and B are e4m3 (else bf16); A_MN, B_MN: m / n along the rows of A / B (bf16 only); O: the output's type.
-template <bool E4M3, bool A_MN, bool B_MN, int BN, bool PAIR, typename O>
-__global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant__ Gemm a) {
+// GROUPS: epilogue groups.
+template <bool E4M3, bool A_MN, bool B_MN, int BN, bool PAIR, int GROUPS, typename O>
+__global__ void __launch_bounds__(GEMM_THREADS<GROUPS>, 1) k_gemm(const __grid_constant__ Gemm a) {
   static_assert(!E4M3 || (!A_MN && !B_MN), "8-bit operands lie with k along their rows");
   static_assert(!PAIR || BN == 256, "a pair's tile is 256 x 256");
-  using R = Ring<BN, PAIR>;
+  static_assert(GROUPS == 2 || (GROUPS == 4 && !PAIR), "two or four epilogue groups");
+  using R = Ring<BN, PAIR, GROUPS>;
   constexpr int CTAS = PAIR ? 2 : 1, TILE_M = CTAS * GEMM_BM;
   constexpr int S = R::STAGES, BK = E4M3 ? 128 : 64, PW = Panel<O>::W, PANELS = BN / PW;
   constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                              (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>(TILE_M >> 4) << 24);
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ GemmBars<BN, PAIR> bars;
+  constexpr int TEAM = GROUPS / 2;  // groups on a tile
+  constexpr int CH = GROUPS == 2 || PW < 32 ? PW : 32, Q = CH * static_cast<int>(sizeof(O)) / 16;  // columns in registers, their pieces
+  __shared__ GemmBars<BN, PAIR, GROUPS> bars;
   __shared__ uint32_t tmem_slot;
-  __shared__ __align__(16) float s_bias[2][2][PW], s_scale[2][2][PW];  // of a group's panel and its next
+  __shared__ __align__(16) float s_bias[GROUPS][2][PW], s_scale[GROUPS][2][PW];  // of a group's panel and its next
   const uint32_t ring = tc::smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = a.tiles_m * a.tiles_n * a.splits;
@@ -293,7 +300,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
   }
   if (tid == 32) {
     for (int s = 0; s < S; ++s) tc::mbar_init(&bars.full[s], 1), tc::mbar_init(&bars.empty[s], 1);
-    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], CTAS * (alternate ? 4 : 8)), tc::mbar_init(&bars.rfull[s], 1);
+    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], CTAS * (alternate ? 4 * TEAM : 4 * GROUPS));
+    for (int s = 0; s < GROUPS; ++s) tc::mbar_init(&bars.rfull[s], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma::prefetch(&a.ta);
     tma::prefetch(&a.tb);
@@ -395,7 +403,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
     }
   } else if (warp >= 4) {
     const int g = (warp - 4) >> 2, gt = tid - 128 - 128 * g, row = 32 * (warp & 3) + lane;
-    unsigned char* st = smem + RING_BYTES + g * PANEL_BYTES;
+    unsigned char* st = smem + RING_BYTES<GROUPS> + g * PANEL_BYTES;
     const uint32_t st_u = tc::smem_u32(st), lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
     uint32_t i = 0, loads = 0;
     auto sync_group = [&] { asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory"); };
@@ -404,7 +412,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
     };
     // the group's tiles, and of the next one's columns gt, gt + 128 the bias and scale, of its row the scale: on their way while a
     // tile is stored
-    const int step = alternate ? 1 : 2, p0 = alternate ? 0 : g, stride = alternate ? 2 * units : units;
+    const int step = alternate ? TEAM : GROUPS, p0 = alternate ? g % TEAM : g, stride = alternate ? 2 * units : units;
     auto accumulator_read = [&](int d) {
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -429,10 +437,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
       }
       if (a.sm) next_sm = m0 + row < a.M ? __ldg(a.sm + m0 + row) : 1.f;
     };
-    const int first = unit + (alternate ? g * units : 0);
-    if (alternate) i = g;
+    const int first = unit + (alternate ? g / TEAM * units : 0);
+    if (alternate) i = g / TEAM;
     fetch(first);
-    for (int item = first; item < items; item += stride, i += step == 1 ? 2 : 1) {
+    for (int item = first; item < items; item += stride, i += alternate ? 2 : 1) {
       int m0, n0, split;
       place(item, m0, n0, split);
       const int d = i & 1, yrow = split * a.split_rows + m0;
@@ -478,37 +486,42 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           waited = true;
         }
-        __syncwarp();
-        float v[PW];
-#pragma unroll
-        for (int c = 0; c < PW; c += 32) tmem_ld32(tmem + lanes + d * BN + p * PW + c, v + c);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (none) {
-#pragma unroll
-          for (int c = 0; c < PW; ++c) v[c] = 0.f;
-        }
-        if (p + step >= panels) accumulator_read(d);
         const float *sb = s_bias[g][turn], *ss = s_scale[g][turn];
-        if (a.sm) {
+        float v[CH];
+        auto values = [&](int c0) {  // columns c0 .. of the panel before the activation
+          __syncwarp();
 #pragma unroll
-          for (int c = 0; c < PW; c += 4) {
-            const float4 s = *reinterpret_cast<const float4*>(ss + c);
-            unpair(pair(v[c], v[c + 1]) * (pair(sm, sm) * pair(s.x, s.y)), v[c], v[c + 1]);
-            unpair(pair(v[c + 2], v[c + 3]) * (pair(sm, sm) * pair(s.z, s.w)), v[c + 2], v[c + 3]);
-          }
-        }
-        if (a.bias) {
+          for (int c = 0; c < CH; c += 32) tmem_ld32(tmem + lanes + d * BN + p * PW + c0 + c, v + c);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (none) {
 #pragma unroll
-          for (int c = 0; c < PW; c += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(sb + c);
-            unpair(pair(v[c], v[c + 1]) + pair(b.x, b.y), v[c], v[c + 1]);
-            unpair(pair(v[c + 2], v[c + 3]) + pair(b.z, b.w), v[c + 2], v[c + 3]);
+            for (int c = 0; c < CH; ++c) v[c] = 0.f;
           }
-        }
+          if (a.sm) {
+#pragma unroll
+            for (int c = 0; c < CH; c += 4) {
+              const float4 s = *reinterpret_cast<const float4*>(ss + c0 + c);
+              unpair(pair(v[c], v[c + 1]) * (pair(sm, sm) * pair(s.x, s.y)), v[c], v[c + 1]);
+              unpair(pair(v[c + 2], v[c + 3]) * (pair(sm, sm) * pair(s.z, s.w)), v[c + 2], v[c + 3]);
+            }
+          }
+          if (a.bias) {
+#pragma unroll
+            for (int c = 0; c < CH; c += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(sb + c0 + c);
+              unpair(pair(v[c], v[c + 1]) + pair(b.x, b.y), v[c], v[c + 1]);
+              unpair(pair(v[c + 2], v[c + 3]) + pair(b.z, b.w), v[c + 2], v[c + 3]);
+            }
+          }
+        };
         if constexpr (PW == 64) {
           if (a.has_p) {
             panel_free();
-            panel_put<__nv_bfloat16>(st, row, v);
+#pragma unroll
+            for (int c0 = 0; c0 < PW; c0 += CH) {
+              values(c0);
+              panel_put<Q>(st, row, c0 / 8, v, O());
+            }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             sync_group();
             if (a.p_plain) {
@@ -522,27 +535,34 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) k_gemm(const __grid_constant_
             if (a.has_r) load_r();
           }
         }
-        switch (a.act) {
+#pragma unroll
+        for (int c0 = 0; c0 < PW; c0 += CH) {
+          if (CH < PW || !a.has_p) values(c0);  // (a whole panel's are still there)
+          if (c0 + CH == PW && p + step >= panels) accumulator_read(d);
+          switch (a.act) {
 #define WHTMIX_ACT(A)                                             \
   case A:                                                         \
-    _Pragma("unroll") for (int c = 0; c < PW; c += 2) activate(v[c], v[c + 1], A); \
+    _Pragma("unroll") for (int c = 0; c < CH; c += 2) activate(v[c], v[c + 1], A); \
     break
-          WHTMIX_ACT(ACT_RELU);
-          WHTMIX_ACT(ACT_GELU);
-          WHTMIX_ACT(ACT_SILU);
+            WHTMIX_ACT(ACT_RELU);
+            WHTMIX_ACT(ACT_GELU);
+            WHTMIX_ACT(ACT_SILU);
 #undef WHTMIX_ACT
-          default: break;
+            default: break;
+          }
+          if (a.has_r) {
+            if (c0 == 0) {
+              if (a.r_plain)
+                sync_group();
+              else
+                wait(&bars.rfull[g], loads++ & 1);
+            }
+            panel_add<Q>(st, row, c0 * static_cast<int>(sizeof(O)) / 16, v, O());
+          } else if (c0 == 0 && !a.has_p) {
+            panel_free();
+          }
+          panel_put<Q>(st, row, c0 * static_cast<int>(sizeof(O)) / 16, v, O());
         }
-        if (a.has_r) {
-          if (a.r_plain)
-            sync_group();
-          else
-            wait(&bars.rfull[g], loads++ & 1);
-          panel_add<O>(st, row, v);
-        } else if (!a.has_p) {
-          panel_free();
-        }
-        panel_put<O>(st, row, v);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         sync_group();
         if (a.y_plain) {
@@ -587,18 +607,18 @@ inline cudaError_t raise_smem(const void* kernel, size_t bytes, std::atomic<uint
 }
 
 // One instance's launch: a persistent grid of at most one CTA per SM.
-template <bool E4M3, bool A_MN, bool B_MN, int BN, bool PAIR, typename O>
+template <bool E4M3, bool A_MN, bool B_MN, int BN, bool PAIR, typename O, int GROUPS = 2>
 cudaError_t launch_gemm(const Gemm& g, int sms, cudaStream_t stream) {
-  auto k = k_gemm<E4M3, A_MN, B_MN, BN, PAIR, O>;
+  auto k = k_gemm<E4M3, A_MN, B_MN, BN, PAIR, GROUPS, O>;
   static std::atomic<uint64_t> raised{0};
-  const cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), GEMM_SMEM, raised);
+  const cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), GEMM_SMEM<GROUPS>, raised);
   if (e != cudaSuccess) return e;
   constexpr int CTAS = PAIR ? 2 : 1;
   const long long items = static_cast<long long>(g.tiles_m) * g.tiles_n * g.splits, most = sms / CTAS;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(CTAS * (items < most ? items : most)));
-  cfg.blockDim = dim3(GEMM_THREADS);
-  cfg.dynamicSmemBytes = GEMM_SMEM;
+  cfg.blockDim = dim3(GEMM_THREADS<GROUPS>);
+  cfg.dynamicSmemBytes = GEMM_SMEM<GROUPS>;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -626,10 +646,19 @@ cudaError_t gemm_by_width(const Gemm& g, int bn, int sms, cudaStream_t stream) {
   }
 }
 
+// bn 128 or 256
+template <bool E4M3, typename O>
+cudaError_t gemm_four(const Gemm& g, int bn, int sms, cudaStream_t stream) {
+  return bn == 128 ? launch_gemm<E4M3, false, false, 128, false, O, 4>(g, sms, stream) : launch_gemm<E4M3, false, false, 256, false, O, 4>(g, sms, stream);
+}
+
 // whtmix_gemm_fwd.cu, whtmix_gemm_e4m3.cu: y from x and W; whtmix_gemm_dx.cu (A with k, B with n along its rows); whtmix_gemm_dw.cu
 // (both m / n)
 cudaError_t gemm_forward(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_e4m3(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
+// whtmix_gemm_four.cu, whtmix_gemm_e4m3_four.cu: the same with four epilogue groups
+cudaError_t gemm_forward_four(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
+cudaError_t gemm_e4m3_four(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dx(const Gemm& g, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dw(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 

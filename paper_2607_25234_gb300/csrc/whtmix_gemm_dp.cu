@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(DP_THREADS, 1) k_dx_dp(const __grid_constant__
         }
         if (gt == 0) tma::wait_read();  // the last store has read the panel
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        panel_put<__nv_bfloat16>(st, row, v);
+        panel_put<8>(st, row, 0, v, __nv_bfloat16());
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("bar.sync 1, 128;" ::: "memory");
         if (a.dx_plain) {
