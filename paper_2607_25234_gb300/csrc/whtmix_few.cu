@@ -95,6 +95,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_wait();
+  pdl_trigger();  // (tensor memory is allocated) the next kernel comes in beside this one: a chain of [1, 1024] to 4096 5.8 -> 4.8 us a link
   const uint32_t tmem = tmem_slot;
   unsigned bad = 0;
   if (warp == 4) {
@@ -240,7 +241,6 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  pdl_trigger();
   if (warp == 0) tc::tmem_dealloc(tmem, COLS);
 }
 

@@ -331,6 +331,15 @@ def test_eight_bit_linear_against_float64(T, N, K):
     check_linear(T, N, K, "none", False, False, True, F32, False)
 
 
+@pytest.mark.parametrize("T,N,K", [(20011, 304, 136), (20011, 300, 135), (40000, 512, 64), (9000, 520, 384), (9001, 129, 5), (700, 1001, 500)])
+def test_products_of_many_tokens_and_short_axes(T, N, K):
+    """Several tiles a CTA and few K blocks; residuals of odd rows."""
+    for eight in (False, True):
+        check_linear(T, N, K, "gelu", True, False, eight, BF, False)
+        check_linear(T, N, K, "silu", True, True, eight, BF, True)
+        check_linear(T, N, K, "none", False, True, eight, F32, False)
+
+
 @pytest.mark.parametrize("T,N,K", [(8192, 4096, 1024), (5000, 4100, 2000), (9001, 2048, 1003)])
 def test_large_products_against_float64(T, N, K):
     """Long K axes: two CTAs on a tile; the last tiles of rows and columns cut."""
