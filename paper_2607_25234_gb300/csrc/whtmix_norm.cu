@@ -10,7 +10,8 @@
 // written once.  TPR threads hold a row, NV 16-byte vectors each; up to 32 threads a row need no shared memory.  Sums are
 // float32 in a fixed order.  dw: every thread keeps its columns' sums over the rows that its CTA takes, the CTAs' partial rows
 // are added up by k_dw in a fixed order.  Rows that are not 16-byte aligned are read and written in aligned 16-byte accesses
-// all the same, but for their ends; rows beyond 2048 vectors are read twice (k_rms_long, k_rms_bwd_long).
+// all the same, but for their ends, short ones that lie one behind another several at a time (k_rms_flat, k_rms_bwd_flat); rows
+// beyond 2048 vectors are read twice (k_rms_long, k_rms_bwd_long).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
@@ -547,6 +548,245 @@ __global__ void __launch_bounds__(32 * DW_RUNS) k_dw(const float* part, float* _
   pdl_trigger();
 }
 
+// ---- contiguous rows of an odd length ----
+// V rows of a contiguous matrix (V elements in 16 bytes) are D whole vectors: a CTA takes them as they lie, thread v vectors v,
+// v + BLOCK, ..  A vector holds elements of one row or, cut, of two (D >= V); its row, its cut and its gains are the same in every
+// group, the gains in shared memory in the vectors' order.  Each vector leaves the sums of its part of one row and of the next one in
+// shared memory, a warp adds a row's up.  Measured against the rows' own kernels (above), us: [21680, 177] bf16 with a residual 15.9
+// and 7.5 (floor 4.5), its backward 21.4 and 15.9; [1300, 177] 3.4 and 2.8.  As many warps as rows at least: with six for 177 vectors
+// it took 9.3.
+template <typename T>
+struct Flat {
+  static constexpr int V = Io<T>::V;
+  static __device__ __forceinline__ void gains(float* s, const float* w, int D) {
+    for (int i = threadIdx.x; i < V * D; i += blockDim.x) s[(((i % V) >> 2) * D + i / V) * 4 + (i & 3)] = __ldg(w + i % D);
+  }
+  static __device__ __forceinline__ void gain(const float* s, int v, int D, float (&f)[V]) {
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const float4 u = reinterpret_cast<const float4*>(s)[q * D + v];
+      f[4 * q] = u.x, f[4 * q + 1] = u.y, f[4 * q + 2] = u.z, f[4 * q + 3] = u.w;
+    }
+  }
+  // elements e .. e + V - 1 of the group at p, those from n on zero
+  static __device__ __forceinline__ uint4 load(const T* p, int e, int n) {
+    if (e + V <= n) return *reinterpret_cast<const uint4*>(p + e);
+    float f[V] = {};
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (e + j < n) f[j] = Io<T>::get(p, e + j);
+    return Io<T>::pack(f);
+  }
+  static __device__ __forceinline__ void store(T* p, int e, int n, const float (&f)[V]) {
+    if (e + V <= n) {
+      *reinterpret_cast<uint4*>(p + e) = Io<T>::pack(f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (e + j < n) Io<T>::put(p, e + j, f[j]);
+    }
+  }
+  // row r's sum of the vectors' first parts, by one warp; the same value in each lane
+  static __device__ __forceinline__ float row_sum(const float* first, int r, int D) {
+    float sum = 0.f;
+    const int end = ((r + 1) * D + V - 1) / V;
+    for (int v = (r * D + V - 1) / V + (threadIdx.x & 31); v < end; v += 32) sum += first[v];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+  }
+};
+
+template <typename T, int BLOCK, int NV>
+__global__ void __launch_bounds__(BLOCK) k_rms_flat(const Forward a) {
+  using F = Flat<T>;
+  constexpr int V = F::V;
+  extern __shared__ __align__(16) float s_w[];  // the gains, then the vectors' sums
+  __shared__ float s_second[V], s_rstd[V];
+  const int D = a.D, warp = threadIdx.x >> 5;
+  const float inv_d = 1.f / static_cast<float>(D);
+  float* s_first = s_w + V * D;
+  int row[NV], cut[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int e = V * (static_cast<int>(threadIdx.x) + BLOCK * k);
+    row[k] = e / D;
+    cut[k] = min(V, (row[k] + 1) * D - e);
+  }
+  if (threadIdx.x < V) s_second[threadIdx.x] = 0.f;
+  pdl_wait();
+  F::gains(s_w, a.w, D);
+  __syncthreads();
+  const long long groups = (a.T + V - 1) / V;
+  auto elements = [&](long long g) { return static_cast<int>(min(static_cast<long long>(V), a.T - g * V)) * D; };
+  uint4 ux[NV], ur[NV];
+  auto fetch = [&](long long g) {
+    if (g >= groups) return;
+    const int n = elements(g);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int e = V * (static_cast<int>(threadIdx.x) + BLOCK * k);
+      if (e >= V * D) continue;
+      ux[k] = F::load(static_cast<const T*>(a.x) + g * V * D, e, n);
+      if (a.r) ur[k] = F::load(static_cast<const T*>(a.r) + g * V * D, e, n);
+    }
+  };
+  fetch(blockIdx.x);
+  for (long long g = blockIdx.x; g < groups; g += gridDim.x) {
+    const int n = elements(g);
+    float h[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = threadIdx.x + BLOCK * k;
+      if (v >= D) continue;
+      Io<T>::unpack(ux[k], h[k]);
+      if (a.r) {
+        float f[V];
+        Io<T>::unpack(ur[k], f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[k][j] += f[j];
+        if (a.h) F::store(static_cast<T*>(a.h) + g * V * D, V * v, n, h[k]);
+      }
+      float first = 0.f, second = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float s = h[k][j] * h[k][j];
+        if (j < cut[k]) first += s; else second += s;
+      }
+      s_first[v] = first;
+      if (cut[k] < V) s_second[row[k] + 1] = second;
+    }
+    fetch(g + gridDim.x);
+    __syncthreads();
+    for (int r = warp; r < V; r += BLOCK / 32) {
+      const float sum = F::row_sum(s_first, r, D) + s_second[r];
+      if ((threadIdx.x & 31) == 0) s_rstd[r] = rsqrtf(sum * inv_d + a.eps);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = threadIdx.x + BLOCK * k;
+      if (v >= D) continue;
+      const float ra = s_rstd[row[k]], rb = s_rstd[min(row[k] + 1, V - 1)];
+      float w[V];
+      F::gain(s_w, v, D, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) h[k][j] = h[k][j] * w[j] * (j < cut[k] ? ra : rb);
+      F::store(static_cast<T*>(a.y) + g * V * D, V * v, n, h[k]);
+    }
+  }
+  pdl_trigger();
+}
+
+// dw: a thread's places in the group have the same columns in every group, their sums stay in its registers; at the end the V
+// rows' sums of a column are added in ascending order.
+template <typename T, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) k_rms_bwd_flat(const Backward a) {
+  using F = Flat<T>;
+  constexpr int V = F::V, NV = 1;
+  extern __shared__ __align__(16) float s_w[];  // the gains (at the end the columns' sums), then the vectors' two sums
+  __shared__ float s_second[2][V], s_rstd[V], s_c[V];
+  const int D = a.D, warp = threadIdx.x >> 5;
+  const float inv_d = 1.f / static_cast<float>(D);
+  float *s_sq = s_w + V * D, *s_ah = s_sq + D;
+  int row[NV], cut[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int e = V * (static_cast<int>(threadIdx.x) + BLOCK * k);
+    row[k] = e / D;
+    cut[k] = min(V, (row[k] + 1) * D - e);
+  }
+  if (threadIdx.x < V) s_second[0][threadIdx.x] = s_second[1][threadIdx.x] = 0.f;
+  pdl_wait();
+  F::gains(s_w, a.w, D);
+  __syncthreads();
+  const long long groups = (a.T + V - 1) / V;
+  auto elements = [&](long long g) { return static_cast<int>(min(static_cast<long long>(V), a.T - g * V)) * D; };
+  float acc[NV][V] = {};
+  uint4 uh[NV], ud[NV];
+  auto fetch = [&](long long g) {
+    if (g >= groups) return;
+    const int n = elements(g);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int e = V * (static_cast<int>(threadIdx.x) + BLOCK * k);
+      if (e >= V * D) continue;
+      uh[k] = F::load(static_cast<const T*>(a.h) + g * V * D, e, n);
+      ud[k] = F::load(static_cast<const T*>(a.dy) + g * V * D, e, n);
+    }
+  };
+  fetch(blockIdx.x);
+  for (long long g = blockIdx.x; g < groups; g += gridDim.x) {
+    const int n = elements(g);
+    float h[NV][V], d[NV][V];
+    uint4 ug[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = threadIdx.x + BLOCK * k;
+      if (v >= D) continue;
+      Io<T>::unpack(uh[k], h[k]);
+      Io<T>::unpack(ud[k], d[k]);
+      if (a.dh) ug[k] = F::load(static_cast<const T*>(a.dh) + g * V * D, V * v, n);
+    }
+    fetch(g + gridDim.x);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = threadIdx.x + BLOCK * k;
+      if (v >= D) continue;
+      float w[V], sq[2] = {}, ah[2] = {};
+      F::gain(s_w, v, D, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float s = h[k][j] * h[k][j], t = d[k][j] * w[j] * h[k][j];
+        if (j < cut[k]) sq[0] += s, ah[0] += t; else sq[1] += s, ah[1] += t;
+      }
+      s_sq[v] = sq[0], s_ah[v] = ah[0];
+      if (cut[k] < V) s_second[0][row[k] + 1] = sq[1], s_second[1][row[k] + 1] = ah[1];
+    }
+    __syncthreads();
+    for (int r = warp; r < V; r += BLOCK / 32) {
+      const float sq = F::row_sum(s_sq, r, D) + s_second[0][r], ah = F::row_sum(s_ah, r, D) + s_second[1][r];
+      const float rstd = r * D < n ? rsqrtf(sq * inv_d + a.eps) : 0.f;  // (a row past the end adds nothing to dw)
+      if ((threadIdx.x & 31) == 0) s_rstd[r] = rstd, s_c[r] = rstd * rstd * rstd * (ah * inv_d);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = threadIdx.x + BLOCK * k;
+      if (v >= D) continue;
+      const int next = min(row[k] + 1, V - 1);
+      const float ra = s_rstd[row[k]], rb = s_rstd[next], ca = s_c[row[k]], cb = s_c[next];
+      float w[V], o[V] = {};
+      F::gain(s_w, v, D, w);
+      if (a.dh) Io<T>::unpack(ug[k], o);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float rstd = j < cut[k] ? ra : rb, c = j < cut[k] ? ca : cb;
+        acc[k][j] += d[k][j] * (h[k][j] * rstd);
+        o[j] += rstd * (d[k][j] * w[j]) - c * h[k][j];
+      }
+      F::store(static_cast<T*>(a.dx) + g * V * D, V * v, n, o);
+    }
+  }
+  __syncthreads();  // the gains have been read
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = threadIdx.x + BLOCK * k;
+    if (v >= D) continue;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s_w[V * v + j] = acc[k][j];
+  }
+  __syncthreads();
+  float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.x) * D;
+  for (int e = threadIdx.x; e < D; e += BLOCK) {
+    float sum = s_w[e];
+#pragma unroll
+    for (int r = 1; r < V; ++r) sum += s_w[r * D + e];
+    part[e] = sum;
+  }
+  pdl_trigger();
+}
+
 // ---- host ----
 
 // Threads a row and vectors a thread for rows of n vectors: at most 128 vectors stay within a warp (no shared memory).  Few rows
@@ -631,6 +871,20 @@ cudaError_t resident_ctas(const void* kernel, int block, size_t smem, int sms, i
   return cudaSuccess;
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+// The longest rows that go this way.  Row kernels and these, us: forward [20000, 1001] bf16 40.1 and 32.1, [5200, 1001] f32 16.6 and
+// 17.7; backward [21680, 177] bf16 21.4 and 15.8, [20000, 333] f32 42.3 and 49.8, [20000, 500] bf16 29.7 and 35.7.
+template <typename T>
+constexpr int FLAT_FORWARD = 2048 / sizeof(T);
+constexpr int FLAT_BACKWARD = 256;
+// A contiguous matrix of odd rows and enough groups of them, every matrix on a 16-byte boundary: k_rms_flat's and k_rms_bwd_flat's.
+template <typename T>
+bool flat(long long T_, int D, int most, int sms) {
+  constexpr int V = Io<T>::V;
+  return D % V != 0 && D >= V && D <= most && T_ >= static_cast<long long>(V) * (D > 512 ? 2 * sms : sms);
+}
+bool contiguous(const void* p, long long stride, int D) { return !p || (stride == D && aligned(p, 16)); }
 template <typename T, bool Q8>
 cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
   constexpr int V = Io<T>::V;
@@ -639,6 +893,28 @@ cudaError_t forward_t(const Forward& a, int sms, cudaStream_t stream) {
                   rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, V) : rows_aligned(a.y, a.ys, es));
   const int n = vectors(a.D, es == 2, al);
   Forward c = a;
+  if constexpr (!Q8) {
+    if (flat<T>(a.T, a.D, FLAT_FORWARD<T>, sms) && contiguous(a.x, a.xs, a.D) && contiguous(a.r, a.rs, a.D) &&
+        contiguous(a.r ? a.h : nullptr, a.hs, a.D) && contiguous(a.y, a.ys, a.D)) {
+      const void* k = nullptr;
+      int block = 0;
+      auto take = [&](auto threads, auto nv) {
+        block = decltype(threads)::value;
+        k = reinterpret_cast<const void*>(k_rms_flat<T, decltype(threads)::value, decltype(nv)::value>);
+      };
+      if (a.D <= 64) take(Int<64>(), Int<1>());
+      else if (a.D <= 128) take(Int<128>(), Int<1>());
+      else if (a.D <= 256) take(Int<256>(), Int<1>());
+      else if (a.D <= 512) take(Int<256>(), Int<2>());
+      else if constexpr (FLAT_FORWARD<T> > 512) take(Int<512>(), Int<2>());
+      const size_t smem = static_cast<size_t>(V + 1) * a.D * 4;  // at most 36 KB
+      int resident = 0;
+      const cudaError_t e = resident_ctas(k, block, smem, sms, &resident);
+      if (e != cudaSuccess) return e;
+      void* args[] = {&c};
+      return launch_pdl(k, grid_rows(a.T, V, resident), block, smem, stream, args);
+    }
+  }
   if (n > MAX_VECTORS) {
     void* args[] = {&c};
     return launch_pdl(reinterpret_cast<const void*>(k_rms_long<T, Q8>), grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args);
@@ -684,6 +960,19 @@ struct BackwardPlan {
 };
 template <typename T>
 cudaError_t backward_plan(const Backward& a, int n, bool al, int sms, BackwardPlan* p) {
+  if (flat<T>(a.T, a.D, FLAT_BACKWARD, sms) && contiguous(a.h, a.hs, a.D) && contiguous(a.dy, a.ys, a.D) && contiguous(a.dh, a.ds, a.D) &&
+      contiguous(a.dx, a.xs, a.D)) {
+    constexpr int V = Io<T>::V;
+    p->kernel = a.D <= 64    ? reinterpret_cast<const void*>(k_rms_bwd_flat<T, 64>)
+                : a.D <= 128 ? reinterpret_cast<const void*>(k_rms_bwd_flat<T, 128>)
+                             : reinterpret_cast<const void*>(k_rms_bwd_flat<T, 256>);
+    p->block = a.D <= 64 ? 64 : a.D <= 128 ? 128 : 256;
+    p->smem = static_cast<size_t>(V + 2) * a.D * 4;
+    int resident = 0;
+    const cudaError_t e = resident_ctas(p->kernel, p->block, p->smem, sms, &resident);
+    if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, V, resident));
+    return e;
+  }
   return by_length_backward(n, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
     p->kernel = al ? reinterpret_cast<const void*>(k_rms_bwd<T, true, TPR, NV>) : reinterpret_cast<const void*>(k_rms_bwd<T, false, TPR, NV>);
@@ -738,7 +1027,7 @@ cudaError_t backward_t(const Backward& a, int sms, cudaStream_t stream) {
     BackwardPlan p;
     if ((e = backward_plan<T>(a, n, al, sms, &p)) != cudaSuccess) return e;
     parts = p.parts;
-    void* args[] = {&c, &same};
+    void* args[] = {&c, &same};  // (the flat kernel takes the first alone)
     e = launch_pdl(p.kernel, static_cast<unsigned>(parts), p.block, p.smem, stream, args);
   }
   if (e != cudaSuccess) return e;

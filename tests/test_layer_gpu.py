@@ -237,6 +237,40 @@ def test_norm_backward_against_float64(T, D, dtype):
         assert torch.equal(got, dx)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(1216, 177), (1217, 177), (5000, 9), (2433, 1001), (1300, 500), (620, 257), (3001, 77), (1219, 12), (1300, 1023),
+                                 (20003, 33), (1223, 513), (1231, 5)])
+def test_norm_of_many_odd_rows(T, D, dtype):
+    """Contiguous rows that share their 16-byte pieces, both directions; also in place and beside a matrix that starts elsewhere."""
+    test_norm_against_float64(T, D, dtype)
+    w, h, dy, dh = 1.0 + 0.1 * rand(3, D), rand(1, T, D).to(dtype), rand(4, T, D).to(dtype), rand(5, T, D).to(dtype)
+    check_norm_backward(h, w, dy, None)
+    dx, dw = check_norm_backward(h, w, dy, dh)
+    again = whtmix.rms_norm_backward(h, w, dy, dh=dh, dx=dy)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+    y, s = whtmix.rms_norm(h, w, residual=dh)
+    x = h.clone()
+    y2, s2 = whtmix.rms_norm(x, w, residual=dh, h=x)
+    assert torch.equal(y, y2) and torch.equal(s, s2) and s2 is x
+    shifted = torch.empty(T * D + 1, dtype=dtype, device="cuda")[1:].view(T, D).copy_(h)
+    y3, _ = whtmix.rms_norm(shifted, w, residual=dh)
+    close(y3, y.double(), 2 * (U16 if dtype == BF else (D / 32 + 200) * U32) * y.double().abs() + 1e-37)
+
+
+def test_a_row_that_is_not_finite_leaves_its_neighbours():
+    T, D = 2000, 177
+    for dtype in (BF, F32):
+        x, w, dy = rand(1, T, D).to(dtype), 1.0 + 0.1 * rand(3, D), rand(4, T, D).to(dtype)
+        y, (dx, _) = whtmix.rms_norm(x, w), whtmix.rms_norm_backward(x, w, dy)
+        bad = x.clone()
+        bad[5, 7], bad[11, 0], bad[12, D - 1], bad[T - 1, 3] = float("nan"), float("inf"), float("nan"), float("nan")
+        rows = torch.ones(T, dtype=torch.bool, device="cuda")
+        rows[[5, 11, 12, T - 1]] = False
+        y2, (dx2, dw2) = whtmix.rms_norm(bad, w), whtmix.rms_norm_backward(bad, w, dy)
+        assert torch.equal(y[rows], y2[rows]) and torch.equal(dx[rows], dx2[rows])
+        assert bool(torch.isnan(y2[5]).all()) and bool(torch.isnan(y2[12]).all()) and bool(torch.isnan(dw2).all())
+
+
 def test_norm_gradients_by_differences():
     T, D = 3, 24
     x, r, w = rand(1, T, D), rand(2, T, D), 1.0 + 0.1 * rand(3, D)
