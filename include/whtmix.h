@@ -256,7 +256,7 @@ WHTMIX_API int whtmix_rms_norm(const void *x, const void *residual, const float 
  *     dx = r a - h r^3 mean(a h) + dh,     dw = sum over the rows of dy h r
  *   h, dy, dx  [T, D] (dtype); dh [T, D] (dtype) the gradient that reaches h directly, or NULL.  dx is the gradient of x and of
  *              the residual alike; it may be dy or dh itself (same pointer and stride).
- *   dw         [D] float32, overwritten.  Two launches. */
+ *   dw         [D] float32, overwritten.  Two launches (three for rows of more than 2048 16-byte pieces). */
 WHTMIX_API int whtmix_rms_norm_backward(const void *h, const float *w, const void *dy, const void *dh, void *dx, float *dw,
                                         int64_t T, int64_t D, int64_t h_stride, int64_t dy_stride, int64_t dh_stride,
                                         int64_t dx_stride, float eps, int dtype, void *stream);
@@ -270,7 +270,7 @@ WHTMIX_API int whtmix_rms_norm_backward(const void *h, const float *w, const voi
  *   preact     [T, N] bf16: p, rounded once, for whtmix_linear_backward; NULL if it is not wanted; out_dtype WHTMIX_BF16 only
  *   y          [T, N] of out_dtype: WHTMIX_BF16 or WHTMIX_F32; it may be the residual itself (same pointer and stride)
  *   act        a whtmix_activation_t
- * float32 accumulation and epilogue, one rounding. */
+ * float32 accumulation and epilogue, one rounding.  One launch, two where x or w has no 16-byte aligned rows (they are copied). */
 WHTMIX_API int whtmix_linear(const void *x, const void *w, const float *x_scale, const float *w_scale, const float *bias,
                              const void *residual, void *preact, void *y, int64_t T, int64_t N, int64_t K,
                              int64_t x_stride, int64_t w_stride, int64_t residual_stride, int64_t preact_stride,
@@ -282,7 +282,8 @@ WHTMIX_API int whtmix_linear(const void *x, const void *w, const float *x_scale,
  *   dx         [T, K] bf16, or NULL
  *   dw         [N, K] contiguous, of dw_dtype WHTMIX_BF16 or WHTMIX_F32, overwritten; or NULL
  *   db         [N] float32, overwritten; or NULL
- * dp is rounded to bf16 for the two products (an activation gradient, as the block's dM and dZ); db sums it unrounded. */
+ * dp is rounded to bf16 for the two products (an activation gradient, as the block's dM and dZ); db sums it unrounded.  One
+ * to six launches. */
 WHTMIX_API int whtmix_linear_backward(const void *x, const void *w, const void *dy, const void *preact, void *dx, void *dw,
                                       float *db, int64_t T, int64_t N, int64_t K, int64_t x_stride, int64_t w_stride,
                                       int64_t dy_stride, int64_t preact_stride, int64_t dx_stride, int act, int dw_dtype,
