@@ -131,17 +131,21 @@ __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
   return r;
 }
 
-// 1 / (1 + 2^t) for both of t.  A reciprocal takes the special-function unit twice an exponential's time (measured: 16 and 32
+// s = 1 / (1 + e) for both of e = 2^t.  A reciprocal takes the special-function unit twice an exponential's time (measured: 16 and 32
 // results a clock and SM), so one serves two values: 1 / (d0 d1) times the other.  t is cut at 60, so that the product stays finite
 // and a NaN becomes a number that leaves the other value alone (the caller multiplies by its own z, which is NaN then too).
-__device__ __forceinline__ Pair logistic2(Pair t) {
+struct Logistic {
+  Pair s, e;
+};
+__device__ __forceinline__ Logistic logistic2(Pair t) {
   float t0, t1, e0, e1, d0, d1, r;
   unpair(t, t0, t1);
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(t0, 60.f)));
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(t1, 60.f)));
-  unpair(pair(e0, e1) + pair(1.f, 1.f), d0, d1);
+  const Pair e = pair(e0, e1);
+  unpair(e + pair(1.f, 1.f), d0, d1);
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
-  return pair(r, r) * pair(d1, d0);
+  return {pair(r, r) * pair(d1, d0), e};
 }
 // max(z, lo), NaN for NaN: below lo the products with logistic2 (at least 2^-60) stay next to nothing, infinities too
 __device__ __forceinline__ float above(float z, float lo) {
@@ -161,20 +165,30 @@ __device__ __forceinline__ void activate(float& z0, float& z1, int act) {
     z0 = z0 < 0.f ? 0.f : z0, z1 = z1 < 0.f ? 0.f : z1;
   } else if (act != ACT_NONE) {
     const Pair z = pair(above(z0, GATE_LOW), above(z1, GATE_LOW));
-    unpair(z * logistic2(gate_exponent(z, act)), z0, z1);
+    unpair(z * logistic2(gate_exponent(z, act)).s, z0, z1);
   }
 }
 
-// d0 *= act'(z0), d1 *= act'(z1).  gelu and silu: s (1 + z (1 - s) u'), s = 1 / (1 + e^-u)
+// d0 *= act'(z0), d1 *= act'(z1).  gelu and silu: s (1 + z (1 - s) u'), s = 1 / (1 + e), e = 2^t.  1 - s is taken as e s: the shared
+// reciprocal leaves s a unit or so off 1, which z u' (of the third degree in gelu) would make 1 % at z = 100.  z is held in
+// [GATE_LOW, GATE_HIGH], beyond which the slope is 0 and 1 in float32 (e s is 0 from z = 9.8 on in gelu, from 87.4 on in silu; at
+// GATE_LOW s, cut at 2^-60, leaves 5e-14 at most): left as it is, z u' would outgrow both, and 0 times an infinity be NaN.
+constexpr float GATE_HIGH = 128.f;
+__device__ __forceinline__ float between(float z, float lo, float hi) {  // NaN for NaN
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(above(z, lo)), "f"(hi));
+  return r;
+}
 __device__ __forceinline__ void times_slope(float& d0, float& d1, float z0, float z1, int act) {
   if (act == ACT_RELU) {
     d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
     return;
   }
-  const Pair z = pair(z0, z1), s = logistic2(gate_exponent(pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), act));
-  Pair g = z * fma(s, pair(-1.f, -1.f), pair(1.f, 1.f));
+  const Pair z = pair(between(z0, GATE_LOW, GATE_HIGH), between(z1, GATE_LOW, GATE_HIGH));
+  const Logistic l = logistic2(gate_exponent(z, act));
+  Pair g = z * (l.e * l.s);
   if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
-  unpair(pair(d0, d1) * (s * (g + pair(1.f, 1.f))), d0, d1);
+  unpair(pair(d0, d1) * (l.s * (g + pair(1.f, 1.f))), d0, d1);
 }
 
 template <typename O> struct Panel;  // a 128-byte row of the output
