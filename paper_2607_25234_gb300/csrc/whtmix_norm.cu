@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
     }
     row_reduce<TPR, false>(sq, ah);  // (more than a warp a row: a barrier, behind which the last row's columns are added)
     if constexpr (!AL && TPR <= 32) __syncwarp();
-    const float rstd = rsqrtf(sq * inv_d + a.eps);
+    const float rstd = t < a.T ? rsqrtf(sq * inv_d + a.eps) : 0.f;  // (a row past the end adds nothing to dw, with eps = 0 either)
     const float c = rstd * rstd * rstd * (ah * inv_d);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {

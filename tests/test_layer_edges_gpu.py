@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2607_25234_gb300 import whtmix
-from test_layer_gpu import BF, U16, close, phi, rand
+from test_layer_gpu import BF, F32, U16, U32, close, phi, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,32 @@ def test_slopes_of_far_preactivations(T, K, act):
     _, dw, db = whtmix.linear_backward(x, w, dy, rows, act)
     close(db, ref, 2.0 ** -16)
     close(dw, ref[:, None].expand(N, K), 2.0 ** -16 + U16 * (1 + U16) * (ref.abs() + 2.0 ** -16)[:, None])
+
+
+# ---- RMS norm ----
+
+def norm_backward_ref(h, w, dy, eps):
+    H, W, G = h.double(), w.double(), dy.double()
+    D, T = h.shape[-1], h.shape[0]
+    rstd = 1.0 / torch.sqrt(H.square().mean(-1, keepdim=True) + eps)
+    a, n = G * W, H * rstd
+    dx = rstd * a - H * rstd ** 3 * (a * H).mean(-1, keepdim=True)
+    spread = rstd * a.abs() + H.abs() * rstd ** 3 * (a * H).abs().mean(-1, keepdim=True)
+    unit = U16 if h.dtype == BF else U32
+    dx_bound = unit * (1 + U16) * dx.abs() + ((D / 32 + 80) * U32 + 2.0 ** -19) * spread + 1e-37
+    dw_bound = ((T / 32 + D / 32 + 200) * U32 + 2.0 ** -19) * (G * n).abs().sum(0) + 1e-37
+    return dx, dx_bound, (G * n).sum(0), dw_bound
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(1, 1), (1, 8), (1, 256), (3, 64), (5, 128), (33, 512), (70, 65), (9, 250), (153, 77), (1219, 12), (1300, 177), (2, 5001)])
+def test_norm_backward_without_eps(T, D, dtype):
+    """eps = 0: rows are not 0, so that every gradient is finite, whatever a CTA's idle row groups hold."""
+    w, h, dy = 1.0 + 0.1 * rand(3, D), rand(1, T, D).to(dtype), rand(4, T, D).to(dtype)
+    wide = torch.zeros(T, 2 * D + 1, dtype=dtype, device="cuda")
+    wide[:, 1:D + 1] = h
+    for rows in (h, wide[:, 1:D + 1]):  # and rows at any distance from a 16-byte boundary
+        dx, dw = whtmix.rms_norm_backward(rows, w, dy, eps=0.0)
+        dx_ref, dx_bound, dw_ref, dw_bound = norm_backward_ref(h, w, dy, 0.0)
+        close(dx, dx_ref, dx_bound)
+        close(dw, dw_ref, dw_bound)
