@@ -256,7 +256,7 @@ WHTMIX_API int whtmix_rms_norm(const void *x, const void *residual, const float 
  *     dx = r a - h r^3 mean(a h) + dh,     dw = sum over the rows of dy h r
  *   h, dy, dx  [T, D] (dtype); dh [T, D] (dtype) the gradient that reaches h directly, or NULL.  dx is the gradient of x and of
  *              the residual alike; it may be dy or dh itself (same pointer and stride).
- *   dw         [D] float32, overwritten.  Two launches (three for rows of more than 2048 16-byte pieces). */
+ *   dw         [D] float32, overwritten.  Two launches (for rows of more than 2048 16-byte pieces three, four if dx is dy). */
 WHTMIX_API int whtmix_rms_norm_backward(const void *h, const float *w, const void *dy, const void *dh, void *dx, float *dw,
                                         int64_t T, int64_t D, int64_t h_stride, int64_t dy_stride, int64_t dh_stride,
                                         int64_t dx_stride, float eps, int dtype, void *stream);

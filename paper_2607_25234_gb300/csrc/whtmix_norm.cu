@@ -477,8 +477,8 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms_bwd(const Backward a, con
   pdl_trigger();
 }
 
-// Rows too long for the registers: dx by a CTA a row; coef[t] = rstd for k_dw_long.
-template <typename T>
+// Rows too long for the registers: dx (DX) by a CTA a row; coef[t] = rstd for k_dw_long.
+template <typename T, bool DX>
 __global__ void __launch_bounds__(LONG_THREADS) k_rms_bwd_long(const Backward a, float* __restrict__ coef) {
   pdl_wait();
   for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
@@ -493,10 +493,12 @@ __global__ void __launch_bounds__(LONG_THREADS) k_rms_bwd_long(const Backward a,
     row_reduce<LONG_THREADS, false>(sq, ah);
     const float inv_d = 1.f / static_cast<float>(a.D), rstd = rsqrtf(sq * inv_d + a.eps);
     const float c = rstd * rstd * rstd * (ah * inv_d);
-    for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
-      float o = a.dh ? Io<T>::get(static_cast<const T*>(a.dh) + t * a.ds, e) : 0.f;
-      o += rstd * (Io<T>::get(dy, e) * __ldg(a.w + e)) - c * Io<T>::get(h, e);
-      Io<T>::put(static_cast<T*>(a.dx) + t * a.xs, e, o);
+    if constexpr (DX) {
+      for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+        float o = a.dh ? Io<T>::get(static_cast<const T*>(a.dh) + t * a.ds, e) : 0.f;
+        o += rstd * (Io<T>::get(dy, e) * __ldg(a.w + e)) - c * Io<T>::get(h, e);
+        Io<T>::put(static_cast<T*>(a.dx) + t * a.xs, e, o);
+      }
     }
     if (threadIdx.x == 0) coef[t] = rstd;
   }
@@ -1017,11 +1019,16 @@ cudaError_t backward_t(const Backward& a, int sms, cudaStream_t stream) {
   cudaError_t e;
   if (n > MAX_VECTORS) {
     float* coef = static_cast<float*>(a.ws) + static_cast<size_t>(parts) * a.D;
+    // dw reads dy: where dx takes dy's place, the coefficients alone come first and dx last.  [1000, 20001] bf16, us: 96, and 71 where
+    // dx is another matrix; with dx written by the threads that add up a column's dw both took 139.
+    const bool over_dy = a.dx == a.dy;
+    const void *with_dx = reinterpret_cast<const void*>(k_rms_bwd_long<T, true>), *without = reinterpret_cast<const void*>(k_rms_bwd_long<T, false>);
     void* args[] = {&c, &coef};
-    e = launch_pdl(reinterpret_cast<const void*>(k_rms_bwd_long<T>), grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args);
-    if (e != cudaSuccess) return e;
+    auto rows = [&](const void* k) { return launch_pdl(k, grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args); };
+    if ((e = rows(over_dy ? without : with_dx)) != cudaSuccess) return e;
     k_dw_long<T><<<dim3((a.D + 255) / 256, parts), 256, 0, stream>>>(c, coef, parts);
-    e = cudaGetLastError();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (over_dy) e = rows(with_dx);
   } else {
     Same same{rows_same(a.h, a.hs, a.dy, a.ys, es), rows_same(a.h, a.hs, a.dh, a.ds, es), rows_same(a.h, a.hs, a.dx, a.xs, es)};
     BackwardPlan p;

@@ -74,3 +74,22 @@ def test_norm_backward_without_eps(T, D, dtype):
         dx_ref, dx_bound, dw_ref, dw_bound = norm_backward_ref(h, w, dy, 0.0)
         close(dx, dx_ref, dx_bound)
         close(dw, dw_ref, dw_bound)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(1, 16392), (3, 20001), (130, 16400), (70, 8200)])
+def test_norm_backward_of_long_rows_in_place(T, D, dtype):
+    """dx over dy and over dh: dx and dw are those of separate matrices."""
+    w, h, dy, dh = 1.0 + 0.1 * rand(3, D), rand(1, T, D).to(dtype), rand(4, T, D).to(dtype), rand(5, T, D).to(dtype)
+    for extra in (None, dh):
+        dx, dw = whtmix.rms_norm_backward(h, w, dy, dh=extra)
+        dx_ref, dx_bound, dw_ref, dw_bound = norm_backward_ref(h, w, dy, 1e-6)
+        if extra is None:
+            close(dx, dx_ref, dx_bound)
+        close(dw, dw_ref, dw_bound)
+        a = dy.clone()
+        got = whtmix.rms_norm_backward(h, w, a, dh=extra, dx=a)
+        assert got[0] is a and torch.equal(a, dx) and torch.equal(got[1], dw)
+    b = dh.clone()
+    got = whtmix.rms_norm_backward(h, w, dy, dh=b, dx=b)
+    assert torch.equal(b, dx) and torch.equal(got[1], dw)
