@@ -21,6 +21,7 @@
 #include <mutex>
 #include <tuple>
 #include <type_traits>
+#include <utility>
 
 #include "whtmix_kernels.cuh"
 #include "whtmix_norm.cuh"
@@ -853,18 +854,23 @@ unsigned grid_rows(long long T, int rows, int resident) {
   const long long need = (T + rows - 1) / rows;
   return static_cast<unsigned>(need < resident ? need : resident);
 }
-// Resident CTAs of a kernel on the whole device, its shared-memory limit raised first; asked once for each kernel and size.
+// Resident CTAs of a kernel on the whole device, asked once for each kernel and size.  Its shared-memory limit, which belongs to the
+// kernel and not to a size, is raised first and never lowered: calls of other widths, on other threads too, go on under it.
 cudaError_t resident_ctas(const void* kernel, int block, size_t smem, int sms, int* out) {
   static std::mutex mu;
   static std::map<std::tuple<int, const void*, size_t>, int> known;
+  static std::map<std::pair<int, const void*>, size_t> limits;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   std::lock_guard<std::mutex> lock(mu);
   int& n = known[{dev, kernel, smem}];
   if (n == 0) {
-    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) != cudaSuccess)
-      return e;
+    size_t& limit = limits.emplace(std::make_pair(dev, kernel), size_t{48 * 1024}).first->second;
+    if (smem > limit) {
+      if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) != cudaSuccess) return e;
+      limit = smem;
+    }
     int per_sm = 0;
     if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, smem)) != cudaSuccess) return e;
     n = (per_sm < 1 ? 1 : per_sm) * sms;

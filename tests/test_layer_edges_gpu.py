@@ -1,6 +1,9 @@
 """The layer operators on a GPU at the ends of their ranges.  References in float64; the bounds are test_layer_gpu.py's, with the same
 derivation."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -9,6 +12,7 @@ from paper_2607_25234_gb300 import whtmix
 from test_layer_gpu import BF, F32, U16, U32, close, phi, rand
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -93,3 +97,41 @@ def test_norm_backward_of_long_rows_in_place(T, D, dtype):
     b = dh.clone()
     got = whtmix.rms_norm_backward(h, w, dy, dh=b, dx=b)
     assert torch.equal(b, dx) and torch.equal(got[1], dw)
+
+
+WIDTHS = """
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import torch
+from paper_2607_25234_gb300 import whtmix
+from test_layer_gpu import close, norm_ref, rand, U16, U32
+from test_layer_edges_gpu import norm_backward_ref
+dtype = getattr(torch, {dtype!r})
+for D in {widths}:
+    w, x, dy = 1.0 + 0.1 * rand(3, D), rand(1, 5, D).to(dtype), rand(4, 5, D).to(dtype)
+    if {backward}:
+        dx, dw = whtmix.rms_norm_backward(x, w, dy)
+        dx_ref, dx_bound, dw_ref, dw_bound = norm_backward_ref(x, w, dy, 1e-6)
+        close(dx, dx_ref, dx_bound)
+        close(dw, dw_ref, dw_bound)
+    else:
+        y, ref = whtmix.rms_norm(x, w), norm_ref(x, None, w)[1]
+        close(y, ref, (U16 * (1 + U16) if dtype == torch.bfloat16 else U32) * ref.abs() + ((D / 32 + 60) * U32 + 2.0 ** -21) * ref.abs() + 1e-37)
+whtmix.sync()
+print("widths ok")
+"""
+
+
+def widths_in_a_fresh_process(dtype, backward, widths):
+    """Unaligned rows of these widths one after another, in a process that has run no others."""
+    code = WIDTHS.format(root=ROOT, tests=os.path.join(ROOT, "tests"), dtype=dtype, backward=backward, widths=widths)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0 and "widths ok" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype,backward,widths", [
+    ("bfloat16", True, [8001, 6501, 8001, 7001, 8001]), ("float32", True, [8001, 6501, 8001, 7001, 8001]),
+    ("bfloat16", False, [16001, 12501, 16001, 14001, 16001])])
+def test_odd_widths_in_any_order(dtype, backward, widths):
+    """A narrower row's launch leaves a wider one's shared memory."""
+    widths_in_a_fresh_process(dtype, backward, widths)
