@@ -866,14 +866,20 @@ cudaError_t resident_ctas(const void* kernel, int block, size_t smem, int sms, i
   std::lock_guard<std::mutex> lock(mu);
   int& n = known[{dev, kernel, smem}];
   if (n == 0) {
-    size_t& limit = limits.emplace(std::make_pair(dev, kernel), size_t{48 * 1024}).first->second;
+    size_t& limit = limits[{dev, kernel}];
+    if (limit == 0) {  // until it is raised: 48 KB less what the kernel declares itself
+      cudaFuncAttributes own;
+      if ((e = cudaFuncGetAttributes(&own, kernel)) != cudaSuccess) return e;
+      limit = 48 * 1024 - own.sharedSizeBytes;
+    }
     if (smem > limit) {
       if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) != cudaSuccess) return e;
       limit = smem;
     }
     int per_sm = 0;
     if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, smem)) != cudaSuccess) return e;
-    n = (per_sm < 1 ? 1 : per_sm) * sms;
+    if (per_sm < 1) return cudaErrorLaunchOutOfResources;
+    n = per_sm * sms;
   }
   *out = n;
   return cudaSuccess;

@@ -135,3 +135,10 @@ def widths_in_a_fresh_process(dtype, backward, widths):
 def test_odd_widths_in_any_order(dtype, backward, widths):
     """A narrower row's launch leaves a wider one's shared memory."""
     widths_in_a_fresh_process(dtype, backward, widths)
+
+
+@pytest.mark.parametrize("dtype,backward,widths", [("bfloat16", True, [6115, 6121]), ("bfloat16", True, [6127]), ("float32", True, [6121]),
+                                                   ("float32", True, [6135]), ("bfloat16", False, [12257, 12281])])
+def test_odd_widths_about_the_default_limit(dtype, backward, widths):
+    """The gains and sums alone are at most 48 KB, with the kernel's own shared memory they are more."""
+    widths_in_a_fresh_process(dtype, backward, widths)
