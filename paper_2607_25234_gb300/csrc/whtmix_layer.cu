@@ -203,9 +203,9 @@ int whtmix_linear_backward(const void* x, const void* w, const void* dy, const v
     if (rc != WHTMIX_OK) return rc;
     if (dw_dtype != WHTMIX_BF16 && dw_dtype != WHTMIX_F32) return WHTMIX_ERR_BAD_DTYPE;
     if (!is_act(act)) return WHTMIX_ERR_INVALID_ARG;
-    if (!dx && !dw && !db) return WHTMIX_ERR_INVALID_ARG;
+    const bool none = T == 0;  // (an empty dx may have no address)
+    if (!dx && !dw && !db) return none ? WHTMIX_OK : WHTMIX_ERR_INVALID_ARG;
     const int os = dw_dtype == WHTMIX_F32 ? 4 : 2;
-    const bool none = T == 0;
     if (!none && (!dy || (dw && !x) || (dx && !w) || (act != WHTMIX_ACT_NONE && !preact))) return WHTMIX_ERR_INVALID_ARG;
     if (act == WHTMIX_ACT_NONE) preact = nullptr;
     const Range out[3] = {{none ? nullptr : dx, T, K, dx_stride, 2}, {dw, N, K, K, os}, {db, 1, N, N, 4}};

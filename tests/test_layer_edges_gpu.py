@@ -142,3 +142,20 @@ def test_odd_widths_in_any_order(dtype, backward, widths):
 def test_odd_widths_about_the_default_limit(dtype, backward, widths):
     """The gains and sums alone are at most 48 KB, with the kernel's own shared memory they are more."""
     widths_in_a_fresh_process(dtype, backward, widths)
+
+
+# ---- empty batches, streams, autograd ----
+
+@pytest.mark.parametrize("lead", [(0,), (0, 4), (3, 0)])
+def test_an_empty_batch_and_each_gradient_alone(lead):
+    x, w = torch.empty(*lead, 32, dtype=BF, device="cuda"), (rand(2, 64, 32) / 5).to(BF)
+    dy = torch.empty(*lead, 64, dtype=BF, device="cuda")
+    for act, p in (("none", None), ("gelu", dy)):
+        for need in ((True, False, False), (False, True, False), (False, False, True), (True, True, True)):
+            dx, dw, db = whtmix.linear_backward(x, w, dy, p, act, *need)
+            assert (dx.shape == x.shape) if need[0] else dx is None
+            assert bool((dw == 0).all()) and dw.shape == w.shape if need[1] else dw is None
+            assert bool((db == 0).all()) and db.shape == (64,) if need[2] else db is None
+        xr = x.clone().requires_grad_(True)
+        whtmix.LinearFunction.apply(xr, w, None, None, act).sum().backward()
+        assert xr.grad.shape == x.shape
