@@ -112,8 +112,9 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
         tma::load_2d(st, &a.tw, (k0 + i) * BK, n0, &full[s]);
         tma::load_2d(st + FEW_ROWS * 128, &a.tx, (k0 + i) * BK, t0, &full[s]);
       }
-      if (bad)  // the copies in flight have landed before the CTA can end (otherwise the products have waited for them)
-        for (int j = i > S ? i - S : 0; j < i; ++j) tma::wait(&full[j % S], (j / S) & 1);
+      // the copies in flight have landed before the CTA can end, whichever warp has given up
+      for (int j = i > S ? i - S : 0; j < i; ++j)
+        if (!tma::wait(&full[j % S], (j / S) & 1)) bad |= 1;
     }
   } else if (warp == 5) {
     if (lane == 0) {
@@ -136,6 +137,8 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
         tc::mma_commit(&empty[s]);
       }
       tc::mma_commit(&dfull);
+      // every product has completed before the tensor memory is freed, also where warps 0-3 have given up
+      if (!tma::wait(&dfull, 0)) bad |= 2;
     }
   }
   float* sums = reinterpret_cast<float*>(smem);  // [token][row of W]

@@ -1,8 +1,11 @@
-"""Host-side behaviour of the layer operators at the ends of their ranges (CPU)."""
+"""What the layer operators do on the host at the ends of their ranges, and orderings that no run shows to be missing (CPU)."""
+import re
+
 import pytest
 
 from paper_2607_25234_gb300 import build as libbuild
 from paper_2607_25234_gb300 import whtmix
+from test_ordering_host import functions, read
 
 
 @pytest.fixture(scope="module")
@@ -18,3 +21,26 @@ def test_nothing_is_asked_of_an_empty_batch(lib):
     assert call(0) == 0 and call(0, act=2) == 0
     assert call(4) == 1
     assert call(0, act=9) == 1 and call(0, dtype=3) == 3 and call(-1) == 1
+
+
+LANDED = re.compile(r"(\)\s*)?for \(\w+ j = \w+ > S \? \w+ - S : 0;[^)]*?j < \w+; \+\+j\)\s*(?:if \(!)?tma::wait\(&(?:bars\.)?full\[j % S\]")
+COMPLETED = re.compile(r"mma_commit\(&(?:bars\.)?dfull\b(?:(?!warp [<>=]|else if).)*?tma::wait\(&(?:bars\.)?dfull\b", re.S)
+
+
+def waits_before_it_ends(kernel):
+    """The loading warp waits for its last copies whether or not a wait has given up, the warp that issues the products for the last of
+    them (a wait of another warp may give up earlier)."""
+    landed = LANDED.search(kernel)
+    return bool(landed and not landed.group(1)) and bool(COMPLETED.search(kernel))
+
+
+@pytest.mark.parametrize("name,kernel", [("whtmix_few.cu", "k_few"), ("whtmix_gemm.cuh", "k_gemm"), ("whtmix_gemm_dp.cu", "k_dx_dp")])
+def test_copies_and_products_in_flight_are_waited_for_whichever_wait_gave_up(name, kernel):
+    text = dict(functions(read(name)))[kernel]
+    assert waits_before_it_ends(text)
+    # and the check sees one that is missing
+    only_then = LANDED.sub(lambda m: "if (bad) " + m.group(0), text)
+    assert not waits_before_it_ends(only_then)
+    last = [m.end() for m in re.finditer(r"mma_commit\(&(?:bars\.)?dfull\b[^;]*;", text)][-1]
+    issuer = text[last:].split("else if" if "else if (warp >=" in text[last:] else "float* sums", 1)[0]
+    assert not waits_before_it_ends(text.replace(issuer, issuer.replace("tma::wait", "no_wait")))
