@@ -419,6 +419,14 @@ def _stride(t: torch.Tensor, shape, dtype: torch.dtype, name: str, index: int) -
     return _rows(t, name, index)[2]
 
 
+def _on(stream, device: torch.device):
+    """A context in which the call runs on the given stream and results are allocated as that stream's: memory of another
+    stream's may still be in use there, and goes back to it, while this one writes."""
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+    return torch.cuda.stream(stream)
+
+
 def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
              out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None, h: torch.Tensor | None = None,
              scale: torch.Tensor | None = None, stream=None):
@@ -431,6 +439,10 @@ def rms_norm(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = N
         done = (_quick or _quick_path()).rms_norm(x, w, residual, eps, out_dtype)
         if done is not None:
             return done
+    if stream is not None and x.is_cuda and (out is None or (h is None and residual is not None) or
+                                             (scale is None and out_dtype == E4M3)):
+        with _on(stream, x.device):
+            return rms_norm(x, w, residual, eps, out_dtype, out, h, scale)
     dtype = x.dtype
     if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError(f"rms_norm takes float32 or bfloat16, got {dtype}")
@@ -484,6 +496,9 @@ def rms_norm_backward(h: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, dh: to
         done = (_quick or _quick_path()).rms_norm_backward(h, w, dy, dh, eps)
         if done is not None:
             return done
+    if stream is not None and h.is_cuda and (dx is None or dw is None):
+        with _on(stream, h.device):
+            return rms_norm_backward(h, w, dy, dh, eps, dx, dw)
     dtype = h.dtype
     if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError(f"rms_norm_backward takes float32 or bfloat16, got {dtype}")
@@ -524,6 +539,9 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
         done = (_quick or _quick_path()).linear(x, w, bias, act, residual, x_scale, w_scale, preact, out_dtype)
         if done is not None:
             return done
+    if stream is not None and x.is_cuda and (out is None or preact is True):
+        with _on(stream, x.device):
+            return linear(x, w, bias, activation, residual, x_scale, w_scale, preact, out_dtype, out)
     dtype, device, index = x.dtype, x.device, x.get_device()
     if dtype != torch.bfloat16 and dtype != E4M3:
         raise TypeError(f"linear takes bfloat16 or {E4M3}, got {dtype}")
@@ -578,6 +596,9 @@ def linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch
         done = (_quick or _quick_path()).linear_backward(x, w, dy, p, act, need_dx, need_dw, need_db, dw_dtype)
         if done is not None:
             return done
+    if stream is not None and x.is_cuda and ((dx is None and need_dx) or (dw is None and need_dw) or (db is None and need_db)):
+        with _on(stream, x.device):
+            return linear_backward(x, w, dy, p, activation, need_dx, need_dw, need_db, dw_dtype, dx, dw, db)
     device, index = x.device, x.get_device()
     if x.dtype != torch.bfloat16:
         raise TypeError(f"linear_backward takes bfloat16, got {x.dtype}")

@@ -159,3 +159,34 @@ def test_an_empty_batch_and_each_gradient_alone(lead):
         xr = x.clone().requires_grad_(True)
         whtmix.LinearFunction.apply(xr, w, None, None, act).sum().backward()
         assert xr.grad.shape == x.shape
+
+
+def stream_of(t):
+    """The stream whose memory t lies in."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not in a segment of the allocator")
+
+
+def test_results_of_a_call_on_a_stream_are_that_streams():
+    """Memory that another stream may still be using, or may take back at once, is not what a call on this stream writes."""
+    s = torch.cuda.Stream()
+    T, N, K = 300, 256, 200
+    gain, w, b = torch.ones(K, device="cuda"), (rand(2, N, K) / 14).to(BF), rand(3, N)
+    x, r, dy = rand(1, T, K).to(BF), rand(4, T, K).to(BF), rand(5, T, N).to(BF)
+    torch.cuda.synchronize()
+    y, h = whtmix.rms_norm(x, gain, residual=r, stream=s)
+    q = whtmix.rms_norm(x, gain, residual=r, out_dtype=torch.float8_e4m3fn, stream=s)
+    z, p = whtmix.linear(y, w, bias=b, activation="gelu", preact=True, stream=s)
+    grads = whtmix.linear_backward(y, w, dy, p, "gelu", stream=s) + whtmix.rms_norm_backward(h, gain, y, stream=s)
+    given = torch.empty(T, N, dtype=BF, device="cuda")
+    assert whtmix.linear(y, w, out=given, stream=s) is given
+    for t in (y, h, *q, z, p, *grads):
+        assert stream_of(t) == s.cuda_stream
+    whtmix.sync(s)
+    want = whtmix.linear(whtmix.rms_norm(x, gain, residual=r)[0], w, bias=b, activation="gelu")
+    assert torch.equal(z, want) and torch.cuda.current_stream() != s
+    cpu = torch.zeros(2, 16, dtype=BF)
+    with pytest.raises(ValueError, match="CUDA"):
+        whtmix.rms_norm(cpu, torch.ones(16), stream=s)
