@@ -760,12 +760,16 @@ class RMSNormFunction(torch.autograd.Function):
             y, h = rms_norm(x, w, residual=residual, eps=eps)
         ctx.save_for_backward(h, w)
         ctx.eps, ctx.with_residual = eps, residual is not None
+        ctx.set_materialize_grads(False)  # where h (or y) is not used, no zeros are filled in and read as its gradient
         return y, h
 
     @staticmethod
     def backward(ctx, dy, dh):
         h, w = ctx.saved_tensors
-        dx, dw = rms_norm_backward(h, w, dy.contiguous(), dh=None if dh is None else dh.contiguous(), eps=ctx.eps)
+        if dy is None:
+            dx, dw = dh, None if dh is None else torch.zeros_like(w)
+        else:
+            dx, dw = rms_norm_backward(h, w, dy.contiguous(), dh=None if dh is None else dh.contiguous(), eps=ctx.eps)
         return dx, dw, dx if ctx.with_residual else None, None
 
 

@@ -190,3 +190,29 @@ def test_results_of_a_call_on_a_stream_are_that_streams():
     cpu = torch.zeros(2, 16, dtype=BF)
     with pytest.raises(ValueError, match="CUDA"):
         whtmix.rms_norm(cpu, torch.ones(16), stream=s)
+
+
+def test_norm_function_passes_only_the_gradients_that_arrive(monkeypatch):
+    T, D = 40, 48
+    x, r, w = rand(1, T, D).to(BF), rand(2, T, D).to(BF), 1.0 + 0.1 * rand(3, D)
+    gy, gh = rand(4, T, D).to(BF), rand(5, T, D).to(BF)
+    seen = []
+    plain = whtmix.rms_norm_backward
+    monkeypatch.setattr(whtmix, "rms_norm_backward", lambda h, w, dy, dh=None, **kw: (seen.append(dh is not None), plain(h, w, dy, dh=dh, **kw))[1])
+    for residual in (None, r):
+        for use_y, use_h in ((True, False), (True, True), (False, True)):
+            leaves = [x.clone().requires_grad_(True), w.clone().requires_grad_(True)]
+            if residual is not None:
+                leaves.append(residual.clone().requires_grad_(True))
+            y, h = whtmix.RMSNormFunction.apply(*leaves)
+            outs, grads = ([y] if use_y else []) + ([h] if use_h else []), ([gy] if use_y else []) + ([gh] if use_h else [])
+            seen.clear()
+            torch.autograd.backward(outs, grads)
+            if use_y:
+                dx, dw = plain(h.detach(), w, gy, dh=gh if use_h else None)
+                assert seen == [use_h]
+            else:
+                dx, dw = gh, torch.zeros_like(w)
+                assert seen == []
+            assert torch.equal(leaves[0].grad, dx) and torch.equal(leaves[1].grad, dw)
+            assert residual is None or torch.equal(leaves[2].grad, dx)
