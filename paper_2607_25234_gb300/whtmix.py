@@ -17,6 +17,7 @@ import os
 import threading
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import build as _build
 
@@ -764,6 +765,7 @@ class RMSNormFunction(torch.autograd.Function):
         return y, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh):
         h, w = ctx.saved_tensors
         if dy is None:
@@ -788,6 +790,7 @@ class LinearFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, w, p = ctx.saved_tensors
         dy = dy.contiguous()

@@ -216,3 +216,14 @@ def test_norm_function_passes_only_the_gradients_that_arrive(monkeypatch):
                 assert seen == []
             assert torch.equal(leaves[0].grad, dx) and torch.equal(leaves[1].grad, dw)
             assert residual is None or torch.equal(leaves[2].grad, dx)
+
+
+def test_second_derivatives_are_refused():
+    """A penalty on a gradient raises: it would have been left out of the second one."""
+    x, w = rand(1, 4, 16).to(BF).requires_grad_(True), torch.ones(16, device="cuda", requires_grad=True)
+    m = (rand(2, 8, 16) / 4).to(BF).requires_grad_(True)
+    for y in (whtmix.RMSNormFunction.apply(x, w)[0], whtmix.LinearFunction.apply(x, m, None, None, "gelu")):
+        loss = y.float().square().sum()
+        (g,) = torch.autograd.grad(loss, x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            (loss + g.float().square().sum()).backward()
