@@ -1,5 +1,5 @@
-"""Builds the C-ABI shared library ``_lib/libwhtmix.so`` with nvcc for sm_103a (no torch involved), and the Python
-binding's quick path ``_lib/whtmix_torch.so`` (host code, which links to it and to torch).
+"""Builds the C-ABI shared library ``_lib/libwhtmix.so`` with nvcc for sm_103a (no torch involved), and where torch is
+installed the Python binding's quick path ``_lib/whtmix_torch.so`` (host code, which links to it and to torch).
 
 Usage: ``python -m paper_2607_25234_gb300.build`` (or ``__graft_entry__.build()``).
 """
@@ -45,17 +45,16 @@ def _deps() -> list[str]:
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(QUICK):
+    made = [LIB] if _torch_dir() is None else [LIB, QUICK]
+    if not all(os.path.exists(f) for f in made):
         return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(QUICK))
+    t = min(os.path.getmtime(f) for f in made)
     return all(os.path.getmtime(f) <= t for f in _deps())
 
 
-def _torch_dir() -> str:
+def _torch_dir() -> str | None:
     spec = importlib.util.find_spec("torch")
-    if spec is None or spec.origin is None:
-        raise RuntimeError("torch not found: the Python binding cannot be built")
-    return os.path.dirname(spec.origin)
+    return None if spec is None or spec.origin is None else os.path.dirname(spec.origin)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -72,24 +71,31 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(OBJDIR, src.replace(".cu", f".{os.getpid()}.o"))
         objs.append(obj)
         procs.append((src, subprocess.Popen(common + ["-c", os.path.join(CSRC, src), "-o", obj])))
-    torch_dir, quick_obj = _torch_dir(), os.path.join(OBJDIR, f"whtmix_torch.{os.getpid()}.o")
-    procs.append((QUICK_SOURCE, subprocess.Popen(
-        [nvcc(), "-O2", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-I", INCLUDE,
-         "-isystem", os.path.join(torch_dir, "include"), "-isystem", sysconfig.get_paths()["include"],
-         "-c", os.path.join(CSRC, QUICK_SOURCE), "-o", quick_obj])))
+    torch_dir, quick_obj, quick = _torch_dir(), os.path.join(OBJDIR, f"whtmix_torch.{os.getpid()}.o"), None
+    if torch_dir is not None:
+        quick = subprocess.Popen(
+            [nvcc(), "-O2", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-I", INCLUDE,
+             "-isystem", os.path.join(torch_dir, "include"), "-isystem", sysconfig.get_paths()["include"],
+             "-c", os.path.join(CSRC, QUICK_SOURCE), "-o", quick_obj])
     failed = [src for src, p in procs if p.wait() != 0]
+    quick_failed = quick is not None and quick.wait() != 0
     if failed:
         raise RuntimeError(f"nvcc failed for {failed}")
     tmp = LIB + f".tmp{os.getpid()}"
     subprocess.run([nvcc(), ARCH, "-shared", "-o", tmp] + objs + ["-lcudart"], check=True)
     os.replace(tmp, LIB)
+    for obj in objs:
+        os.remove(obj)
+    if quick is None:
+        return LIB
+    if quick_failed:
+        raise RuntimeError(f"nvcc failed for {QUICK_SOURCE}")
     # both names found beside the module, whose own run path leads there, and in torch's folder
     subprocess.run([nvcc(), "-shared", "-o", tmp, quick_obj, "-L", LIBDIR, "-lwhtmix", "-L", os.path.join(torch_dir, "lib"),
                     "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Xlinker", "-rpath,$ORIGIN",
                     "-Xlinker", "-rpath," + os.path.join(torch_dir, "lib")], check=True)
     os.replace(tmp, QUICK)
-    for obj in objs + [quick_obj]:
-        os.remove(obj)
+    os.remove(quick_obj)
     return LIB
 
 

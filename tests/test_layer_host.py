@@ -1,4 +1,6 @@
 """What the layer operators do on the host at the ends of their ranges, and orderings that no run shows to be missing (CPU)."""
+import importlib.util
+import os
 import re
 
 import pytest
@@ -44,3 +46,24 @@ def test_copies_and_products_in_flight_are_waited_for_whichever_wait_gave_up(nam
     last = [m.end() for m in re.finditer(r"mma_commit\(&(?:bars\.)?dfull\b[^;]*;", text)][-1]
     issuer = text[last:].split("else if" if "else if (warp >=" in text[last:] else "float* sums", 1)[0]
     assert not waits_before_it_ends(text.replace(issuer, issuer.replace("tma::wait", "no_wait")))
+
+
+@pytest.mark.parametrize("with_torch", [False, True])
+def test_the_c_library_is_built_without_torch(tmp_path, monkeypatch, with_torch):
+    """With a compiler that only makes its output file and writes down what it was asked."""
+    nvcc, log = tmp_path / "nvcc", tmp_path / "log"
+    nvcc.write_text('#!/bin/sh\necho "$@" >> ' + str(log) + '\nwhile [ "$1" != -o ]; do shift; done\n: > "$2"\n')
+    nvcc.chmod(0o755)
+    monkeypatch.setenv("NVCC", str(nvcc))
+    for name, value in (("LIBDIR", tmp_path / "lib"), ("OBJDIR", tmp_path / "lib" / "obj"), ("LIB", tmp_path / "lib" / "libwhtmix.so"),
+                        ("QUICK", tmp_path / "lib" / "whtmix_torch.so")):
+        monkeypatch.setattr(libbuild, name, str(value))
+    if not with_torch:
+        find = importlib.util.find_spec
+        monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: None if name == "torch" else find(name, *a))
+    assert not libbuild.up_to_date()
+    assert libbuild.build() == libbuild.LIB and os.path.exists(libbuild.LIB)
+    assert os.path.exists(libbuild.QUICK) == with_torch and libbuild.up_to_date()
+    assert os.listdir(libbuild.OBJDIR) == []
+    for line in log.read_text().splitlines():
+        assert with_torch or "torch" not in line.replace(str(tmp_path), "")
