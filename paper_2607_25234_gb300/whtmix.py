@@ -641,7 +641,8 @@ def quantize_rows(w: torch.Tensor):
     w = w.float()
     scale = w.abs().amax(1) / E4M3_MAX
     scale = torch.where(scale == 0, torch.ones_like(scale), scale)
-    return (w / scale[:, None]).to(E4M3), scale
+    # (a scale below float32's normal numbers is rounded by more than the type's 464 / 448 allows: 2.1e-42 / 4.2e-45 = 500)
+    return (w / scale[:, None]).clamp(-E4M3_MAX, E4M3_MAX).to(E4M3), scale
 
 
 def workspace_bytes(B: int, N: int, C: int, dtype: torch.dtype, backward: bool = False) -> int:

@@ -4,6 +4,7 @@ import os
 import re
 
 import pytest
+import torch
 
 from paper_2607_25234_gb300 import build as libbuild
 from paper_2607_25234_gb300 import whtmix
@@ -67,3 +68,16 @@ def test_the_c_library_is_built_without_torch(tmp_path, monkeypatch, with_torch)
     assert os.listdir(libbuild.OBJDIR) == []
     for line in log.read_text().splitlines():
         assert with_torch or "torch" not in line.replace(str(tmp_path), "")
+
+
+@pytest.mark.parametrize("top", [1.0, 1e-30, 9.3e-41, 2.1e-42, 6e-43, 1e-43, 3e38])
+def test_rows_of_any_size_have_finite_eight_bit_values(top):
+    """Weights of a row whose scale is a float32 below the normal numbers (steps of 2^-149): within a step of 448, no NaN."""
+    q, s = whtmix.quantize_rows(torch.tensor([[top, top / 2, -top, 0.0]]))
+    v = q.double() * s.double()[:, None]
+    w = torch.tensor([[top, top / 2, -top, 0.0]]).double()
+    assert bool(torch.isfinite(q.float()).all())
+    # the scale is the nearest float32, whose step times 448 is what the largest value may be off by
+    assert bool(((v - w).abs() <= 2.0 ** -4 * w.abs() + 448 * 2.0 ** -149).all())
+    bad, _ = whtmix.quantize_rows(torch.tensor([[float("nan"), 1.0]]))
+    assert bool(torch.isnan(bad.float()).any())
