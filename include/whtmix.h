@@ -236,7 +236,7 @@ WHTMIX_API int whtmix_block_backward(const void *x, const void *w_in, const void
  * of no meaning where T <= 1).  T >= 0; channels from 1 to 2^24; T < 2^31 - 256 and every matrix at most 2^40 elements
  * (WHTMIX_ERR_BAD_SHAPE).  Any size and any alignment of the element type runs (WHTMIX_ERR_MISALIGNED below that); 16-byte
  * aligned rows are the fast ones.  An output may share no address range with an input or another output, except where stated.
- * T = 0: nothing is read, gradients of parameters are set to zero.  All sums are float32, in a fixed order. */
+ * T = 0: nothing is read, gradients of parameters that are asked for are set to zero.  All sums are float32, in a fixed order. */
 
 /* RMS norm with the residual's addition, one row of D channels at a time:
  *     h = x + residual,    y = h w / sqrt(mean(h^2) + eps)
@@ -246,7 +246,8 @@ WHTMIX_API int whtmix_block_backward(const void *x, const void *w_in, const void
  *                the residual itself (same pointer and stride).
  *   y            [T, D]: of `dtype` where out_dtype is dtype (it may then be x or the residual itself, if h is not), or
  *                WHTMIX_E4M3: y / y_scale[t], rounded to nearest, ties to even
- *   y_scale      [T] float32, WHTMIX_E4M3 only (else unused): max |y| / 448 of the row; a row of zeros has scale 0 and values 0
+ *   y_scale      [T] float32, WHTMIX_E4M3 only (else unused): max |y| / 448 of the row; a row of zeros has scale 0 (NaN if eps is
+ *                0: y is 0 / 0) and values 0
  * y is computed from the unrounded sum.  A row with an infinity or a NaN yields NaN as the formula does (and a NaN scale). */
 WHTMIX_API int whtmix_rms_norm(const void *x, const void *residual, const float *w, void *h, void *y, float *y_scale,
                                int64_t T, int64_t D, int64_t x_stride, int64_t residual_stride, int64_t h_stride,

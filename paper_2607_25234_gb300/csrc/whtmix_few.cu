@@ -1,4 +1,4 @@
-// whtmix_few.cu -- the linear layer's product where whtmix_gemm.cuh's tiles are fewer than the SMs, few tokens above all:
+// whtmix_few.cu -- the linear layer's product for few tokens (use_few), where whtmix_gemm.cuh would have few tiles or wait for W:
 // y = act(s_x s_w x W^T + b) + r, bound by reading W and the latencies of one short chain.
 //
 // The roles of whtmix_gemm.cuh exchanged: 128 rows of W are the product's M, 16, 32, 64 or 128 tokens its N, so that with few

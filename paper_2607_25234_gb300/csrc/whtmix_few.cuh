@@ -1,4 +1,4 @@
-// whtmix_few.cuh -- the linear layer's forward for few tokens or few tiles (whtmix_few.cu): x and W (at x, w) with 16-byte aligned
+// whtmix_few.cuh -- the linear layer's forward for few tokens (whtmix_few.cu): x and W (at x, w) with 16-byte aligned
 // rows, everything else as whtmix_linear.cuh has it.
 #pragma once
 

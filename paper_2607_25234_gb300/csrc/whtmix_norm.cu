@@ -11,7 +11,7 @@
 // float32 in a fixed order.  dw: every thread keeps its columns' sums over the rows that its CTA takes, the CTAs' partial rows
 // are added up by k_dw in a fixed order.  Rows that are not 16-byte aligned are read and written in aligned 16-byte accesses
 // all the same, but for their ends, short ones that lie one behind another several at a time (k_rms_flat, k_rms_bwd_flat); rows
-// beyond 2048 vectors are read twice (k_rms_long, k_rms_bwd_long).
+// beyond 2048 vectors (an unaligned row touches one more) are read twice (k_rms_long, k_rms_bwd_long).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
@@ -257,8 +257,8 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_rms(const Forward a, const Sa
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
   pdl_wait();
-  // A short launch lets the next kernel come in at once (24 rows to 8 bits and their product 12.4 -> 11.0 us); a long one would have it
-  // wait in the SMs' way.
+  // A short launch lets the next kernel come in at once (24 rows to 8 bits and their product, time on the GPU,
+  // 12.4 -> 11.0 us); a long one would have it wait in the SMs' way.
   const bool short_launch = gridDim.x < 128;
   if (short_launch) pdl_trigger();
   if constexpr (!AL) {
