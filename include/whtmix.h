@@ -231,7 +231,8 @@ WHTMIX_API int whtmix_block_backward(const void *x, const void *w_in, const void
 
 /* ---- The layer around the mixer ----
  * A transformer layer is h = x + block(norm(x)), y = h + W2 act(W1 norm(h) + b1) + b2 (Section III-B: the block is linear and
- * the feed-forward half supplies the nonlinearity).  The four calls below are its norm and its products.  They take rows: T
+ * the feed-forward half supplies the nonlinearity).  The calls below are its norms, its products and, last, the clipping of its
+ * gradients.  They take rows: T
  * tokens of D, K or N channels, channels contiguous, `*_stride` elements from one row to the next (at least a row's length;
  * of no meaning where T <= 1).  T >= 0; channels from 1 to 2^24; T < 2^31 - 256 and every matrix at most 2^40 elements
  * (WHTMIX_ERR_BAD_SHAPE).  Any size and any alignment of the element type runs (WHTMIX_ERR_MISALIGNED below that); 16-byte
@@ -290,12 +291,78 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w, const void *
                                       int64_t dy_stride, int64_t preact_stride, int64_t dx_stride, int act, int dw_dtype,
                                       void *stream);
 
+/* Layer norm with the residual's addition, one row of D channels at a time:
+ *     h = x + residual,    y = (h - mean(h)) w / sqrt(mean((h - mean(h))^2) + eps) + b
+ * Arguments, types and overlaps as whtmix_rms_norm's, and
+ *   b            [D] float32 shifts, or NULL
+ * y is computed from the unrounded sum.  A row with an infinity or a NaN yields NaN (and a NaN scale); a row of equal values yields b.
+ * WHTMIX_E4M3: a row whose y is all zero has scale 0 and values 0. */
+WHTMIX_API int whtmix_layer_norm(const void *x, const void *residual, const float *w, const float *b, void *h, void *y,
+                                 float *y_scale, int64_t T, int64_t D, int64_t x_stride, int64_t residual_stride,
+                                 int64_t h_stride, int64_t y_stride, float eps, int dtype, int out_dtype, void *stream);
+
+/* Backward of whtmix_layer_norm from the stored sum h: with r = 1 / sqrt(var(h) + eps), n = (h - mean(h)) r and a = dy w,
+ *     dx = r (a - mean(a) - n mean(a n)) + dh,     dw = sum over the rows of dy n,     db = sum over the rows of dy
+ * Arguments as whtmix_rms_norm_backward's, and
+ *   db         [D] float32, overwritten; or NULL
+ * Two launches (for rows beyond the registers three, four if dx is dy).  What a stream that is being captured needs in between
+ * belongs to the graph; so it is with the four calls below. */
+WHTMIX_API int whtmix_layer_norm_backward(const void *h, const float *w, const void *dy, const void *dh, void *dx, float *dw,
+                                          float *db, int64_t T, int64_t D, int64_t h_stride, int64_t dy_stride,
+                                          int64_t dh_stride, int64_t dx_stride, float eps, int dtype, void *stream);
+
+/* The first half of a gated feed-forward block: both products, the activation and the gating in one kernel:
+ *     g = x wg^T + bg,    u = x wu^T + bu,    y = act(g) u
+ *   x          [T, K], w [2 N, K]: N rows wg and then N rows wu, both of `dtype`: WHTMIX_BF16, or WHTMIX_E4M3 with float32 scales a
+ *              row, x_scale [T] and w_scale [2 N]; scales are NULL for WHTMIX_BF16
+ *   bias       [2 N] float32: bg, bu; or NULL
+ *   preact     [T, 2 N] bf16: g and u, each rounded once, for whtmix_gated_linear_backward; NULL if they are not wanted; out_dtype
+ *              WHTMIX_BF16 only
+ *   y          [T, N] of out_dtype: WHTMIX_BF16 or WHTMIX_F32
+ *   act        a whtmix_activation_t
+ * float32 accumulation, activation and gating, one rounding.  N at most 2^23.  No output may overlap anything.  One launch, two where
+ * x or w has no 16-byte aligned rows. */
+WHTMIX_API int whtmix_gated_linear(const void *x, const void *w, const float *x_scale, const float *w_scale, const float *bias,
+                                   void *preact, void *y, int64_t T, int64_t N, int64_t K, int64_t x_stride, int64_t w_stride,
+                                   int64_t preact_stride, int64_t y_stride, int act, int dtype, int out_dtype, void *stream);
+
+/* Backward of whtmix_gated_linear (WHTMIX_BF16) for the upstream gradient dy of y, from the stored preact = [g, u]:
+ *     dp = [dy u act'(g), dy act(g)],    dx = dp w,    dw = dp^T x,    db = sum over the rows of dp
+ *   x [T, K], w [2 N, K], dy [T, N], preact [T, 2 N] bf16
+ *   dx         [T, K] bf16, or NULL
+ *   dw         [2 N, K] contiguous, of dw_dtype WHTMIX_BF16 or WHTMIX_F32, overwritten; or NULL
+ *   db         [2 N] float32, overwritten; or NULL
+ * dp is rounded to bf16 for the two products; db sums it unrounded.  Two to six launches. */
+WHTMIX_API int whtmix_gated_linear_backward(const void *x, const void *w, const void *dy, const void *preact, void *dx, void *dw,
+                                            float *db, int64_t T, int64_t N, int64_t K, int64_t x_stride, int64_t w_stride,
+                                            int64_t dy_stride, int64_t preact_stride, int64_t dx_stride, int act, int dw_dtype,
+                                            void *stream);
+
+/* One tensor of a list: n contiguous elements of WHTMIX_F32 or WHTMIX_BF16 on the device (n = 0: no pointer needed). */
+typedef struct {
+    const void *in;
+    void *out; /* whtmix_clip_by_global_norm only: `in` itself, or memory that overlaps nothing */
+    int64_t n;
+    int dtype;
+} whtmix_tensor_t;
+
+/* The common norm of a list of tensors, and the list scaled down to at most max_norm:
+ *     norm = sqrt(sum over all tensors and elements of in^2),    out = in min(1, max_norm / (norm + 1e-6))
+ *   tensors    `count` entries in HOST memory, read during the call; count from 0 (norm = 0) to 2^20
+ *   norm       one float32 on the device; whtmix_clip_by_global_norm: or NULL
+ *   max_norm   >= 0
+ * The sum is float64; every finite list has its norm, whatever its values' size (`norm` is its float32: infinite beyond 3.4e38, where
+ * the factor is still right).  The factor is rounded to float32, its products to the tensor's type.  An infinity makes the norm infinite and the factor 0 (max_norm finite), a NaN makes both
+ * NaN: what comes out then is not to be used.  Two launches for up to 64 tensors, two for every 480 beyond. */
+WHTMIX_API int whtmix_global_norm(const whtmix_tensor_t *tensors, int64_t count, float *norm, void *stream);
+WHTMIX_API int whtmix_clip_by_global_norm(const whtmix_tensor_t *tensors, int64_t count, float max_norm, float *norm, void *stream);
+
 /* Synchronises `stream` and reports device-side failures of the calls enqueued on it since the
  * previous whtmix_sync: WHTMIX_ERR_TIMEOUT if a bounded device-wide wait gave up (the library
  * then resets that workspace's barrier), WHTMIX_ERR_CUDA if the synchronisation itself failed,
  * WHTMIX_OK otherwise.  Checked: the library-managed workspace of `stream` and, on the current
  * device, the fixed scratch of whtmix_forward_noalloc (pass the stream those calls used, so that
- * they have finished).  Caller-owned _ex workspaces are the caller's to read (error word at byte
+ * they have finished) and the error word of the gated products.  Caller-owned _ex workspaces are the caller's to read (error word at byte
  * offset 8). */
 WHTMIX_API int whtmix_sync(void *stream);
 

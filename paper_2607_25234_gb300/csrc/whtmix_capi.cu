@@ -16,6 +16,7 @@
 
 #include "whtmix.h"
 #include "whtmix_fast_launch.cuh"
+#include "whtmix_host.cuh"
 #include "whtmix_kernels.cuh"
 
 namespace whtmix {
@@ -166,7 +167,7 @@ int device_check(int* dev_out, int* sms_out) {
 
 // ---- library-managed workspaces, one per (device, stream, slot) ----
 // Slot 0 is the kernels' workspace (barrier header + plane group); slot 1 holds the block
-// backward's intermediates, which must survive the slot-0 calls made in between.
+// backward's intermediates, which must survive the slot-0 calls made in between.  Slot 2 is the scratch of host::Scratch.
 struct WsEntry {
   void* ptr = nullptr;
   size_t bytes = 0;
@@ -882,6 +883,51 @@ int device(int* dev, int* sms) { return device_check(dev, sms); }
 int workspace(int dev, cudaStream_t stream, size_t bytes, int slot, void** out) {
   return cached_workspace(dev, stream, bytes, out, slot);
 }
+
+static __device__ GridBarrier g_wait_header;
+static std::map<int, GridBarrier*> g_wait_addr;  // device -> address of g_wait_header there
+static GridBarrier* wait_header(int dev) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  auto it = g_wait_addr.find(dev);
+  return it == g_wait_addr.end() ? nullptr : it->second;
+}
+int error_word(int dev, unsigned int** err) {
+  GridBarrier* h = wait_header(dev);
+  if (!h) {
+    void* p = nullptr;
+    const cudaError_t e = cudaGetSymbolAddress(&p, g_wait_header);
+    if (e != cudaSuccess) return cuda_fail(e);
+    h = static_cast<GridBarrier*>(p);
+    std::lock_guard<std::mutex> lk(g_mu);
+    g_wait_addr[dev] = h;
+  }
+  *err = &h->err;
+  return WHTMIX_OK;
+}
+
+constexpr int SCRATCH_SLOT = 2, SCRATCH_TURNS = 64;
+static std::mutex g_turns[SCRATCH_TURNS];  // by stream
+int Scratch::take(int dev, cudaStream_t stream, size_t bytes) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(stream, &status);
+  if (e != cudaSuccess) return cuda_fail(e);
+  stream_ = stream;
+  captured_ = status != cudaStreamCaptureStatusNone;
+  if (captured_) {
+    e = cudaMallocAsync(&p_, bytes, stream);
+    return e == cudaSuccess ? WHTMIX_OK : cuda_fail(e);
+  }
+  turn_ = std::unique_lock<std::mutex>(g_turns[(reinterpret_cast<uintptr_t>(stream) >> 4) % SCRATCH_TURNS]);
+  return cached_workspace(dev, stream, bytes, &p_, SCRATCH_SLOT);
+}
+int Scratch::give_back() {
+  void* p = p_;
+  p_ = nullptr;
+  if (turn_.owns_lock()) turn_.unlock();
+  if (!p || !captured_) return WHTMIX_OK;
+  const cudaError_t e = cudaFreeAsync(p, stream_);
+  return e == cudaSuccess ? WHTMIX_OK : cuda_fail(e);
+}
 }  // namespace host
 // Device address of the fixed scratch on device `dev`, or null if no call has set it up there.
 void* noalloc_scratch_of(int dev);
@@ -1107,14 +1153,14 @@ int whtmix_sync(void* stream_v) {
   int dev = 0;
   e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_fail(e);
-  void* ptrs[3] = {nullptr, whtmix::noalloc_scratch_of(dev), pln::error_header(dev)};
+  void* ptrs[4] = {nullptr, whtmix::noalloc_scratch_of(dev), pln::error_header(dev), host::wait_header(dev)};
   {
     std::lock_guard<std::mutex> lk(g_mu);
     auto it = g_ws.find(std::make_tuple(dev, stream, 0));
     if (it != g_ws.end()) ptrs[0] = it->second.ptr;
   }
-  // the stream's library-managed workspace, then this device's no-allocation scratch and the
-  // one-plane-per-CTA kernels' header (all keep a set error word until it is reported here)
+  // the stream's library-managed workspace, then this device's no-allocation scratch and the headers of the
+  // one-plane-per-CTA kernels and of the gated products (all keep a set error word until it is reported here)
   int rc = WHTMIX_OK;
   for (void* ptr : ptrs) {
     if (!ptr) continue;

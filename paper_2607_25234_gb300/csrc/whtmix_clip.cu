@@ -1,0 +1,275 @@
+// whtmix_clip.cu -- the common norm of many tensors and their scaling by it (clipping of a step's gradients).
+//
+//   norm = sqrt(sum over all tensors and elements of g^2),   out = g min(1, max_norm / (norm + 1e-6))
+//
+// Bound by memory: the gradients are read for the norm and again for the scaling.  A tensor is cut into chunks of CHUNK 16-byte
+// vectors, counted from the 16-byte boundary at or before its first element, so that every load is aligned whatever its address; a
+// CTA takes chunks at the grid's stride.  A table of the tensors goes along as a kernel parameter (a captured graph keeps it), a
+// launch for every MAX of them.  The scaling takes the chunks in descending order: the last ones read are still in L2.
+// A thread's squares of one chunk are added in float32, those sums in float64; values whose squares leave float32's range are
+// scaled by a power of two first, so that every finite gradient has its finite norm.  Every CTA of the scaling adds up the partial
+// sums itself, in the same order: no atomics, results repeat bit for bit.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "whtmix_clip.cuh"
+#include "whtmix_kernels.cuh"
+
+namespace whtmix {
+namespace clip {
+
+constexpr int CLIP_THREADS = 256, VECTORS = 8, CHUNK = CLIP_THREADS * VECTORS;
+constexpr double CLIP_EPS = 1e-6;
+
+struct Entry {
+  const uint8_t* in;
+  uint8_t* out;
+  long long bytes;
+  int first;  // its first chunk; the top bit: bf16
+};
+constexpr int BF16_BIT = static_cast<int>(0x80000000u);
+template <int MAX>
+struct Table {
+  Entry e[MAX];
+  int count, chunks;
+};
+
+// A chunk: vectors v0 .. of the tensor, vector v at base + 16 v.
+struct Piece {
+  const uint8_t *base, *lo, *hi;  // base: the 16-byte boundary at or before lo
+  long long shift;                // out - in
+  int v0;                         // (a tensor of 2^40 elements has 2^38 vectors: v0 counts chunks)
+  bool bf16;
+};
+template <int MAX>
+__device__ __forceinline__ Piece piece(const Table<MAX>& t, int chunk) {
+  int lo = 0, hi = t.count - 1;  // the last tensor whose first chunk is not beyond this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((t.e[mid].first & ~BF16_BIT) <= chunk) lo = mid; else hi = mid - 1;
+  }
+  const Entry e = t.e[lo];
+  Piece p;
+  p.lo = e.in, p.hi = e.in + e.bytes;
+  p.base = e.in - (reinterpret_cast<uintptr_t>(e.in) & 15u);
+  p.shift = e.out - e.in;
+  p.v0 = chunk - (e.first & ~BF16_BIT);
+  p.bf16 = e.first < 0;
+  return p;
+}
+__device__ __forceinline__ const uint8_t* vector_at(const Piece& p, int u) {
+  return p.base + (static_cast<long long>(p.v0) * CHUNK + threadIdx.x + u * CLIP_THREADS) * 16;
+}
+// the vector at q, zeros outside the tensor
+__device__ __forceinline__ uint4 load(const Piece& p, const uint8_t* q) {
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (q >= p.lo && q + 16 <= p.hi) {
+    v = *reinterpret_cast<const uint4*>(q);
+  } else if (q + 16 > p.lo && q < p.hi) {  // a tensor's first or last vector, in halves of words (elements are aligned)
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (q + 2 * i >= p.lo && q + 2 * i < p.hi) w[i >> 1] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(q + 2 * i)) << (16 * (i & 1));
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return v;
+}
+
+// sum of the squares of s times the values of u, two accumulators
+__device__ __forceinline__ float squares(const uint4 (&u)[VECTORS], bool bf16, float s) {
+  float a = 0.f, b = 0.f;
+#pragma unroll
+  for (int k = 0; k < VECTORS; ++k) {
+    const uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (bf16) {
+        const float x = __uint_as_float(w[j] << 16) * s, y = __uint_as_float(w[j] & 0xffff0000u) * s;
+        a = fmaf(x, x, a), b = fmaf(y, y, b);
+      } else {
+        const float x = __uint_as_float(w[j]) * s;
+        if (j & 1) b = fmaf(x, x, b); else a = fmaf(x, x, a);
+      }
+    }
+  }
+  return a + b;
+}
+// Beyond [2^-100, 2^120] the sum is taken again with the values scaled by 2^110 (all of them are below 2^-50 then) or 2^-72.
+__device__ __forceinline__ double sum_of_squares(const uint4 (&u)[VECTORS], bool bf16) {
+  const float s = squares(u, bf16, 1.f);
+  if (s >= 0x1p-100f && s <= 0x1p120f) return s;
+  uint32_t any = 0;
+#pragma unroll
+  for (int k = 0; k < VECTORS; ++k) any |= u[k].x | u[k].y | u[k].z | u[k].w;
+  if ((any & 0x7fff7fffu) == 0 && (bf16 || (any & 0x7fffffffu) == 0)) return 0.0;
+  const bool tiny = s < 1.f;
+  return static_cast<double>(squares(u, bf16, tiny ? 0x1p110f : 0x1p-72f)) * (tiny ? 0x1p-220 : 0x1p144);
+}
+
+// The sum of a over the CTA's threads, in each of them; the same order everywhere.
+__device__ __forceinline__ double add_up(double a) {
+  __shared__ double s[CLIP_THREADS / 32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = a;
+  __syncthreads();
+  double sum = s[0];
+#pragma unroll
+  for (int i = 1; i < CLIP_THREADS / 32; ++i) sum += s[i];
+  return sum;
+}
+__device__ __forceinline__ double add_parts(const double* part, int parts) {
+  double a = 0.0;
+  for (int i = threadIdx.x; i < parts; i += CLIP_THREADS) a += __ldcg(part + i);
+  return add_up(a);
+}
+
+// part[blockIdx.x] = the sum of squares of this CTA's chunks
+template <int MAX>
+__global__ void __launch_bounds__(CLIP_THREADS) k_squares(const __grid_constant__ Table<MAX> t, double* part) {
+  pdl_wait();
+  double sum = 0.0;
+  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const Piece p = piece(t, c);
+    uint4 u[VECTORS];
+#pragma unroll
+    for (int k = 0; k < VECTORS; ++k) u[k] = load(p, vector_at(p, k));
+    sum += sum_of_squares(u, p.bf16);
+  }
+  sum = add_up(sum);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+  pdl_trigger();
+}
+
+// *total = the sum of the parts, *norm its root (each or null)
+__global__ void __launch_bounds__(CLIP_THREADS) k_total(const double* part, int parts, double* total, float* norm) {
+  pdl_wait();
+  const double sum = add_parts(part, parts);
+  if (threadIdx.x == 0) {
+    if (total) *total = sum;
+    if (norm) *norm = static_cast<float>(sqrt(sum));
+  }
+  pdl_trigger();
+}
+
+template <int MAX>
+__global__ void __launch_bounds__(CLIP_THREADS) k_scale(const __grid_constant__ Table<MAX> t, const double* part, int parts, float max_norm,
+                                                        float* norm) {
+  pdl_wait();
+  const double root = sqrt(add_parts(part, parts)), ratio = max_norm / (root + CLIP_EPS);
+  const float f = ratio >= 1.0 ? 1.f : static_cast<float>(ratio);  // (NaN stays)
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(root);
+  for (int i = blockIdx.x; i < t.chunks; i += gridDim.x) {
+    const Piece p = piece(t, t.chunks - 1 - i);
+    if (f == 1.f && p.shift == 0) continue;
+    uint4 u[VECTORS];
+#pragma unroll
+    for (int k = 0; k < VECTORS; ++k) u[k] = load(p, vector_at(p, k));
+#pragma unroll
+    for (int k = 0; k < VECTORS; ++k) {
+      uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (p.bf16) {
+          __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
+          w[j] = *reinterpret_cast<uint32_t*>(&b);
+        } else {
+          w[j] = __float_as_uint(__uint_as_float(w[j]) * f);
+        }
+      }
+      const uint8_t* q = vector_at(p, k);
+      uint8_t* o = const_cast<uint8_t*>(q) + p.shift;
+      if (q >= p.lo && q + 16 <= p.hi && (p.shift & 15) == 0) {
+        *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (q + 2 * j >= p.lo && q + 2 * j < p.hi) *reinterpret_cast<uint16_t*>(o + 2 * j) = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+      }
+    }
+  }
+  pdl_trigger();
+}
+
+// ---- host ----
+
+// Tensors a launch: a small table for the usual list, a large one (15 KB of parameters) for long ones.
+constexpr int FEW = 64, MANY = 480;
+constexpr int PARTS_AT_ONCE = 4096;  // more are added up once, before the scaling
+
+static long long chunks_of(const Item& i) {
+  const long long bytes = i.n * (i.bf16 ? 2 : 4) + static_cast<long long>(reinterpret_cast<uintptr_t>(i.in) & 15u);
+  return (bytes + 16ll * CHUNK - 1) / (16ll * CHUNK);
+}
+static int ctas(long long chunks, int sms) {
+  const long long most = 4ll * sms;
+  return static_cast<int>(chunks < most ? chunks : most);
+}
+
+// f(table, its CTAs) for each launch's tensors, in order; stops at an error
+template <int MAX, class F>
+static cudaError_t each(const Call& a, int sms, F&& f) {
+  Table<MAX> t;
+  t.count = 0, t.chunks = 0;
+  for (long long i = 0; i < a.count; ++i) {
+    const Item& m = a.items[i];
+    t.e[t.count++] = {static_cast<const uint8_t*>(m.in), static_cast<uint8_t*>(m.out ? m.out : const_cast<void*>(m.in)), m.n * (m.bf16 ? 2 : 4),
+                      t.chunks | (m.bf16 ? BF16_BIT : 0)};
+    t.chunks += static_cast<int>(chunks_of(m));
+    if (t.count == MAX || i + 1 == a.count || t.chunks + chunks_of(a.items[i + 1]) >= (1ll << 31)) {
+      const cudaError_t e = f(t, ctas(t.chunks, sms));
+      if (e != cudaSuccess) return e;
+      t.count = 0, t.chunks = 0;
+    }
+  }
+  return cudaSuccess;
+}
+template <int MAX>
+static long long parts_of(const Call& a, int sms) {
+  long long n = 0;
+  (void)each<MAX>(a, sms, [&](Table<MAX>&, int grid) {
+    n += grid;
+    return cudaSuccess;
+  });
+  return n;
+}
+static bool long_list(const Call& a) { return a.count > FEW; }
+
+size_t workspace(const Call& a, int sms) {
+  return (1 + (long_list(a) ? parts_of<MANY>(a, sms) : parts_of<FEW>(a, sms))) * sizeof(double);
+}
+
+template <int MAX>
+static cudaError_t run_t(const Call& a, void* ws, int sms, cudaStream_t stream) {
+  double *total = static_cast<double*>(ws), *part = total + 1;
+  int parts = 0;
+  cudaError_t e = each<MAX>(a, sms, [&](Table<MAX>& t, int grid) {
+    double* p = part + parts;
+    parts += grid;
+    void* args[] = {&t, &p};
+    return launch_pdl(reinterpret_cast<const void*>(k_squares<MAX>), static_cast<unsigned>(grid), CLIP_THREADS, 0, stream, args);
+  });
+  if (e != cudaSuccess) return e;
+  const double* from = part;
+  float* norm = a.norm;
+  if (!a.scale || parts > PARTS_AT_ONCE) {
+    double* to = a.scale ? total : nullptr;
+    void* args[] = {&from, &parts, &to, &norm};
+    if ((e = launch_pdl(reinterpret_cast<const void*>(k_total), 1, CLIP_THREADS, 0, stream, args)) != cudaSuccess || !a.scale) return e;
+    from = total, parts = 1, norm = nullptr;
+  }
+  float max_norm = a.max_norm;
+  return each<MAX>(a, sms, [&](Table<MAX>& t, int grid) {
+    void* args[] = {&t, &from, &parts, &max_norm, &norm};
+    const cudaError_t r = launch_pdl(reinterpret_cast<const void*>(k_scale<MAX>), static_cast<unsigned>(grid), CLIP_THREADS, 0, stream, args);
+    norm = nullptr;
+    return r;
+  });
+}
+cudaError_t run(const Call& a, void* ws, int sms, cudaStream_t stream) {
+  return long_list(a) ? run_t<MANY>(a, ws, sms, stream) : run_t<FEW>(a, ws, sms, stream);
+}
+
+}  // namespace clip
+}  // namespace whtmix

@@ -68,8 +68,11 @@ struct Four<__nv_bfloat16> {
   }
 };
 
-template <bool E4M3, int TN, typename O>
+// GATED: a tile's 128 rows of W are 64 of the gate's and the 64 of the value's that belong to the same channels; lanes 0-15 of a
+// warp take the gate's sums, lanes 16-31 the value's, and the gate's lanes store four channels of y.
+template <bool E4M3, int TN, typename O, bool GATED>
 __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few a) {
+  constexpr int OUT = GATED ? FEW_ROWS / 2 : FEW_ROWS;  // channels of a tile
   constexpr int BK = E4M3 ? 128 : 64, S = FEW_STAGES<TN>;
   constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (static_cast<uint32_t>(TN >> 3) << 17) | ((128u >> 4) << 24);
   constexpr int COLS = TN < 32 ? 32 : TN;  // tensor-memory columns
@@ -80,7 +83,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   const uint32_t ring = tc::smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
-  const int n0 = tile % a.tiles_n * FEW_ROWS, t0 = tile / a.tiles_n * TN, tokens = min(TN, a.T - t0);
+  const int n0 = tile % a.tiles_n * OUT, t0 = tile / a.tiles_n * TN, tokens = min(TN, a.T - t0);
   const int k0 = static_cast<int>(static_cast<long long>(a.kblocks) * rank / a.splits);
   const int k1 = static_cast<int>(static_cast<long long>(a.kblocks) * (rank + 1) / a.splits);
   if (warp == 0) tc::tmem_alloc(&tmem_slot, COLS);
@@ -110,6 +113,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
         const uint32_t st = ring + s * FEW_STAGE<TN>;
         tma::expect_tx(&full[s], FEW_STAGE<TN>);
         tma::load_2d(st, &a.tw, (k0 + i) * BK, n0, &full[s]);
+        if constexpr (GATED) tma::load_2d(st + OUT * 128, &a.tw, (k0 + i) * BK, a.N + n0, &full[s]);
         tma::load_2d(st + FEW_ROWS * 128, &a.tx, (k0 + i) * BK, t0, &full[s]);
       }
       // the copies in flight have landed before the CTA can end, whichever warp has given up
@@ -160,12 +164,12 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   }
   cg::cluster_group cluster = cg::this_cluster();
   if (a.splits > 1) cluster.sync(); else __syncthreads();
-  const int n = n0 + 4 * lane, live = min(4, a.N - n);
+  const int n = n0 + (4 * lane) % OUT, live = min(4, a.N - n), wn = n + (4 * lane < OUT ? 0 : a.N);  // channel, row of W
   float bias[4] = {}, sw[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if (j < live && a.bias) bias[j] = a.bias[n + j];
-    if (j < live && a.sw) sw[j] = a.sw[n + j];
+    if (j < live && a.bias) bias[j] = a.bias[wn + j];
+    if (j < live && a.sw) sw[j] = a.sw[wn + j];
   }
   const bool vec = a.vec && live == 4;
   const int tt0 = tokens * rank / a.splits, tt1 = tokens * (rank + 1) / a.splits;
@@ -186,17 +190,26 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
     for (int j = 0; j < 4; ++j) z[j] = (a.sx ? z[j] * sx * sw[j] : z[j]) + bias[j];
     if (a.p) {
       if (vec) {
-        Four<__nv_bfloat16>::store(a.p, t * a.ps + n, z);
+        Four<__nv_bfloat16>::store(a.p, t * a.ps + wn, z);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (j < live) static_cast<__nv_bfloat16*>(a.p)[t * a.ps + n + j] = __float2bfloat16_rn(z[j]);
+          if (j < live) static_cast<__nv_bfloat16*>(a.p)[t * a.ps + wn + j] = __float2bfloat16_rn(z[j]);
       }
+    }
+    float u[4] = {1.f, 1.f, 1.f, 1.f};
+    if constexpr (GATED) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) u[j] = __shfl_down_sync(0xffffffffu, z[j], 16);
+      if (lane >= 16) return;
     }
 #pragma unroll
     for (int j = 0; j < 4; j += 2) {
       activate(z[j], z[j + 1], a.act);
-      z[j] += r[j], z[j + 1] += r[j + 1];
+      if constexpr (GATED)
+        z[j] *= u[j], z[j + 1] *= u[j + 1];
+      else
+        z[j] += r[j], z[j + 1] += r[j + 1];
     }
     if (vec) {
       Four<O>::store(a.y, t * a.ys + n, z);
@@ -247,9 +260,9 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const __grid_constant__ Few
   if (warp == 0) tc::tmem_dealloc(tmem, COLS);
 }
 
-template <bool E4M3, int TN, typename O>
+template <bool E4M3, int TN, typename O, bool GATED>
 static cudaError_t launch_few(const Few& f, int sms, cudaStream_t stream) {
-  auto k = k_few<E4M3, TN, O>;
+  auto k = k_few<E4M3, TN, O, GATED>;
   static std::atomic<uint64_t> raised{0};
   cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), FEW_SMEM<TN>, raised);
   if (e != cudaSuccess) return e;
@@ -269,19 +282,24 @@ static cudaError_t launch_few(const Few& f, int sms, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, k, f);
 }
 
-template <bool E4M3, typename O>
+template <bool E4M3, typename O, bool GATED>
 static cudaError_t by_tokens(const Few& f, int tn, int sms, cudaStream_t stream) {
   switch (tn) {
-    case 16: return launch_few<E4M3, 16, O>(f, sms, stream);
-    case 32: return launch_few<E4M3, 32, O>(f, sms, stream);
-    case 64: return launch_few<E4M3, 64, O>(f, sms, stream);
-    default: return launch_few<E4M3, 128, O>(f, sms, stream);
+    case 16: return launch_few<E4M3, 16, O, GATED>(f, sms, stream);
+    case 32: return launch_few<E4M3, 32, O, GATED>(f, sms, stream);
+    case 64: return launch_few<E4M3, 64, O, GATED>(f, sms, stream);
+    default: return launch_few<E4M3, 128, O, GATED>(f, sms, stream);
   }
+}
+template <bool GATED>
+static cudaError_t by_types(const Few& f, const Forward& a, int tn, int sms, cudaStream_t stream) {
+  if (a.e4m3) return a.out_f32 ? by_tokens<true, float, GATED>(f, tn, sms, stream) : by_tokens<true, __nv_bfloat16, GATED>(f, tn, sms, stream);
+  return a.out_f32 ? by_tokens<false, float, GATED>(f, tn, sms, stream) : by_tokens<false, __nv_bfloat16, GATED>(f, tn, sms, stream);
 }
 
 bool use_few(long long T, int kblocks) { return T <= 64 || (T <= 128 && kblocks >= 8) || (T <= 256 && kblocks >= 32); }
 
-cudaError_t forward_few(const Forward& a, const void* x, long long xs, const void* w, long long ws, unsigned int* err, int sms,
+cudaError_t forward_few(const Forward& a, const void* x, long long xs, const void* w, long long ws, bool gated, unsigned int* err, int sms,
                         cudaStream_t stream) {
   const int es = a.e4m3 ? 1 : 2, os = a.out_f32 ? 4 : 2, tn = a.T <= 16 ? 16 : a.T <= 32 ? 32 : a.T <= 64 ? 64 : 128;
   Few f{};
@@ -291,17 +309,17 @@ cudaError_t forward_few(const Forward& a, const void* x, long long xs, const voi
   auto fours = [&](const void* p, long long stride, int size) {
     return !p || (reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && (a.T == 1 || stride % 4 == 0));
   };
-  f.vec = fours(a.y, a.ys, os) && fours(a.r, a.rs, os) && fours(a.p, a.ps, 2);
+  f.vec = fours(a.y, a.ys, os) && fours(a.r, a.rs, os) && fours(a.p, a.ps, 2) && !(gated && a.p && a.N % 4);
   f.kblocks = static_cast<int>((static_cast<long long>(a.K) * es + 127) / 128);
-  f.tiles_n = (a.N + FEW_ROWS - 1) / FEW_ROWS;
+  const int out = gated ? FEW_ROWS / 2 : FEW_ROWS;
+  f.tiles_n = (a.N + out - 1) / out;
   // the K axis over 1, 2, 4 or 8 CTAs while two CTAs an SM are not reached and each keeps two blocks
   const long long tiles = static_cast<long long>(f.tiles_n) * ((a.T + tn - 1) / tn);
   f.splits = 1;
   while (f.splits < 8 && tiles * f.splits * 2 <= 2ll * sms && f.kblocks >= 4 * f.splits) f.splits *= 2;
-  if (!tma::encode_rows(&f.tw, w, es, a.N, a.K, ws, FEW_ROWS) || !tma::encode_rows(&f.tx, x, es, a.T, a.K, xs, tn))
+  if (!tma::encode_rows(&f.tw, w, es, gated ? 2ll * a.N : a.N, a.K, ws, out) || !tma::encode_rows(&f.tx, x, es, a.T, a.K, xs, tn))
     return cudaErrorInvalidValue;
-  if (a.e4m3) return a.out_f32 ? by_tokens<true, float>(f, tn, sms, stream) : by_tokens<true, __nv_bfloat16>(f, tn, sms, stream);
-  return a.out_f32 ? by_tokens<false, float>(f, tn, sms, stream) : by_tokens<false, __nv_bfloat16>(f, tn, sms, stream);
+  return gated ? by_types<true>(f, a, tn, sms, stream) : by_types<false>(f, a, tn, sms, stream);
 }
 
 }  // namespace linear

@@ -11,7 +11,8 @@ namespace linear {
 // 7.1 and 5.1, K = 1024 6.2 and 8.4; 250 tokens, K = 1024, N = 4096 12.6 and 8.7, K = N = 4096 19.0 and 22.7; 500 tokens,
 // K = N = 4096 24.7 and 25.0, K = N = 1024 10.3 and 8.6.
 bool use_few(long long T, int kblocks);
-cudaError_t forward_few(const Forward& a, const void* x, long long xs, const void* w, long long ws, unsigned int* err, int sms,
+// gated: W [2 N, K] and so on, as whtmix_gated.cuh has it
+cudaError_t forward_few(const Forward& a, const void* x, long long xs, const void* w, long long ws, bool gated, unsigned int* err, int sms,
                         cudaStream_t stream);
 
 }  // namespace linear

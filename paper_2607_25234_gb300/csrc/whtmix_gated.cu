@@ -1,0 +1,268 @@
+// whtmix_gated.cu -- host side of the gated feed-forward half (whtmix_gated.cuh) and the pass that makes dp = [dy u act'(g), dy act(g)] with
+// the bias's gradient.  The backward's products are the linear layer's, without an activation: dp and W have 2 N columns and rows.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "whtmix_few.cuh"
+#include "whtmix_gated.cuh"
+#include "whtmix_gemm_gated.cuh"
+#include "whtmix_linear_host.cuh"
+#include "whtmix_norm.cuh"
+#include "whtmix_unaligned.cuh"
+
+namespace whtmix {
+namespace linear {
+
+constexpr int THREADS_256 = 256;
+
+// d0 = d0 u0 act'(z0), v0 = d0 act(z0), and the same for the other value (one logistic function for value and slope; limits as in
+// activate and times_slope).
+__device__ __forceinline__ void gate_gradients(float& d0, float& d1, float& v0, float& v1, float z0, float z1, float u0, float u1, int act) {
+  v0 = d0, v1 = d1;
+  d0 *= u0, d1 *= u1;
+  if (act == ACT_NONE) {
+    v0 *= z0, v1 *= z1;
+  } else if (act == ACT_RELU) {
+    v0 *= z0 < 0.f ? 0.f : z0, v1 *= z1 < 0.f ? 0.f : z1;
+    d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
+  } else {
+    const Pair zv = pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), z = pair(between(z0, GATE_LOW, GATE_HIGH), between(z1, GATE_LOW, GATE_HIGH));
+    const Logistic l = logistic2(gate_exponent(z, act));
+    Pair g = z * (l.e * l.s);
+    if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
+    unpair(pair(d0, d1) * (l.s * (g + pair(1.f, 1.f))), d0, d1);
+    unpair(pair(v0, v1) * (zv * l.s), v0, v1);
+  }
+}
+
+// dp[t, n], dp[t, N + n] = bf16 of both gradients; part[chunk][n], [N + n] = the chunk's rows' float32 sums of them, before the rounding.
+// A CTA takes 8 TX channels (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.  AL: dy, p and dp
+// have 16-byte aligned rows and halves.
+template <bool AL, int TX>
+__global__ void __launch_bounds__(THREADS_256, 2) k_gated_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
+  constexpr int G = THREADS_256 / TX;  // rows at a time
+  __shared__ float s[G][TX][9];
+  const int lane = threadIdx.x % TX, g = threadIdx.x / TX, c0 = (blockIdx.x * TX + lane) * 8;
+  const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
+  float acc_g[8] = {}, acc_u[8] = {};
+  pdl_wait();
+  const uint16_t *dy = static_cast<const uint16_t*>(a.dy), *p = static_cast<const uint16_t*>(a.p);
+  const Span sd = span_of(a.dy, a.T, a.dys, a.N, 2), sp = span_of(a.p, a.T, a.ps, 2 * a.N, 2);
+  using Raw = typename std::conditional<AL, uint4, Granules>::type;
+  auto fetch = [&](const uint16_t* row, const Span& s) {
+    Raw u = Raw{};
+    if (c0 < a.N) {
+      if constexpr (AL)
+        u = *reinterpret_cast<const uint4*>(row + c0);
+      else
+        u = fetch16(reinterpret_cast<const uint8_t*>(row + c0), s);
+    }
+    return u;
+  };
+  auto values = [&](const Raw& raw, const uint16_t* row, const Span& s, float (&f)[8]) {
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (AL)
+      u = raw;
+    else if (c0 < a.N)
+      u = keep(finish16(raw, reinterpret_cast<const uint8_t*>(row + c0), s), min(16, 2 * (a.N - c0)));
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  };
+  auto store = [&](__nv_bfloat16* o, const float (&f)[8]) {
+    if constexpr (AL) {
+      uint32_t h[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+        h[j] = *reinterpret_cast<uint32_t*>(&b);
+      }
+      if (c0 < a.N) *reinterpret_cast<uint4*>(o + c0) = make_uint4(h[0], h[1], h[2], h[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c0 + j < a.N) o[c0 + j] = __float2bfloat16_rn(f[j]);
+    }
+  };
+  constexpr int U = 2;  // rows in flight
+  for (long long first = t0 + g; first < t1; first += G * U) {
+    Raw ud[U], uz[U], uu[U];
+#pragma unroll
+    for (int r = 0; r < U; ++r) {
+      const long long t = first + G * r;
+      if (t < t1) {
+        ud[r] = fetch(dy + t * a.dys, sd);
+        uz[r] = fetch(p + t * a.ps, sp);
+        uu[r] = fetch(p + t * a.ps + a.N, sp);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < U; ++r) {
+      const long long t = first + G * r;
+      if (t >= t1) break;
+      float d[8], z[8], u[8], v[8];
+      values(ud[r], dy + t * a.dys, sd, d);
+      values(uz[r], p + t * a.ps, sp, z);
+      values(uu[r], p + t * a.ps + a.N, sp, u);
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) gate_gradients(d[j], d[j + 1], v[j], v[j + 1], z[j], z[j + 1], u[j], u[j + 1], a.act);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc_g[j] += d[j], acc_u[j] += v[j];
+      if (dp) {
+        store(dp + t * dps, d);
+        store(dp + t * dps + a.N, v);
+      }
+    }
+  }
+  if (part) {
+    auto add = [&](const float (&acc)[8], float* to) {
+      __syncthreads();  // the last sums have been read
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[g][lane][j] = acc[j];
+      __syncthreads();
+      if (threadIdx.x < 8 * TX) {
+        float sum = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < G; ++i) sum += s[i][threadIdx.x >> 3][threadIdx.x & 7];
+        const int c = blockIdx.x * 8 * TX + threadIdx.x;
+        if (c < a.N) to[c] = sum;
+      }
+    };
+    float* row = part + static_cast<long long>(blockIdx.y) * 2 * a.N;
+    add(acc_g, row);
+    add(acc_u, row + a.N);
+  }
+  pdl_trigger();
+}
+
+// ---- host ----
+
+struct GatedForwardPlan {
+  bool pad_x, pad_w;
+  int kp;
+  size_t x_off, w_off, total;
+};
+static GatedForwardPlan plan_forward(const Forward& a) {
+  GatedForwardPlan f{};
+  const int es = a.e4m3 ? 1 : 2;
+  f.kp = pitch_of(a.K, es);
+  f.pad_x = !tma::mappable(a.x, a.T, a.xs, es);
+  f.pad_w = !tma::mappable(a.w, 2ll * a.N, a.ws, es);
+  if (f.pad_x) f.x_off = f.total, f.total += align256(static_cast<size_t>(a.T) * f.kp * es);
+  if (f.pad_w) f.w_off = f.total, f.total += align256(static_cast<size_t>(2ll * a.N) * f.kp * es);
+  return f;
+}
+
+size_t gated_forward_workspace(const Forward& a, int) { return plan_forward(a).total; }
+
+cudaError_t gated_forward(const Forward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
+  const GatedForwardPlan f = plan_forward(a);
+  const int es = a.e4m3 ? 1 : 2, os = a.out_f32 ? 4 : 2;
+  const void *x = a.x, *w = a.w;
+  long long xs = a.xs, wst = a.ws;
+  Copy cx{}, cw{};
+  if (f.pad_x) {
+    x = static_cast<char*>(ws) + f.x_off, xs = f.kp;
+    cx = copy_of(static_cast<char*>(ws) + f.x_off, a.x, a.T, a.K, a.xs, f.kp, es);
+  }
+  if (f.pad_w) {
+    w = static_cast<char*>(ws) + f.w_off, wst = f.kp;
+    cw = copy_of(static_cast<char*>(ws) + f.w_off, a.w, 2ll * a.N, a.K, a.ws, f.kp, es);
+  }
+  const cudaError_t e = to_pitch(cx, cw, sms, stream);
+  if (e != cudaSuccess) return e;
+  if (use_few(a.T, ceil_div(a.K, 128 / es))) return forward_few(a, x, xs, w, wst, true, err, sms, stream);
+  Gated g{};
+  g.kblocks = ceil_div(a.K, 128 / es);
+  // a product of 2 N columns by its clocks, 128 of them a tile at least
+  Plan pl = plan_product(a.T, 2 * a.N, g.kblocks, sms, 1);
+  if (pl.bn < 128) pl.bn = 128;
+  const int out = tile_cols(pl.bn) / 2;
+  g.tiles_m = ceil_div(a.T, tile_rows(pl.bn)), g.tiles_n = ceil_div(a.N, out);
+  g.M = static_cast<int>(a.T), g.N = a.N, g.act = a.act;
+  g.bias = a.bias, g.sm = a.x_scale, g.sn = a.w_scale;
+  g.y = a.y, g.p = a.p, g.ys = a.ys, g.ps = a.ps;
+  g.has_p = a.p != nullptr;
+  g.y_plain = !tma::storable(a.y, a.T, a.N, a.ys, os);
+  // (its halves apart: a store of the gate's last columns must not reach the value's first ones)
+  __nv_bfloat16* value = static_cast<__nv_bfloat16*>(a.p) + (a.p ? a.N : 0);
+  g.p_plain = a.p && !(tma::storable(a.p, a.T, a.N, a.ps, 2) && tma::storable(value, a.T, a.N, a.ps, 2));
+  g.err = err;
+  if (!tma::encode_rows(&g.ta, x, es, a.T, a.K, xs, GEMM_BM) || !tma::encode_rows(&g.tb, w, es, 2ll * a.N, a.K, wst, out) ||
+      (!g.y_plain && !tma::encode_rows(&g.ty, a.y, os, a.T, a.N, a.ys, GEMM_BM)) ||
+      (g.has_p && !g.p_plain && (!tma::encode_rows(&g.tg, a.p, 2, a.T, a.N, a.ps, GEMM_BM) || !tma::encode_rows(&g.tu, value, 2, a.T, a.N, a.ps, GEMM_BM))))
+    return cudaErrorInvalidValue;
+  return a.e4m3 ? gemm_gated_e4m3(g, a.out_f32, pl.bn, sms, stream) : gemm_gated(g, a.out_f32, pl.bn, sms, stream);
+}
+
+// Threads a row of k_gated_dp, eight channels each.
+static int dp_lanes(int N) { return N <= 64 ? 8 : N <= 128 ? 16 : 32; }
+
+// dp and db's partial sums, then the linear layer's products of them with W and x.
+struct GatedBackwardPlan {
+  Backward products;  // (its dy and workspace are filled in when the call runs)
+  int np, chunks;     // pitch of dp; db's chunks of rows
+  size_t dp_off, db_off, products_off, total;
+};
+static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
+  GatedBackwardPlan b{};
+  b.np = pitch_of(2 * a.N, 2);
+  auto take = [&](size_t bytes) {
+    const size_t off = b.total;
+    b.total += align256(bytes);
+    return off;
+  };
+  b.products = a;
+  b.products.N = 2 * a.N, b.products.act = ACT_NONE, b.products.p = nullptr, b.products.db = nullptr;
+  b.products.dy = nullptr, b.products.dys = b.np;  // (on a 16-byte boundary)
+  if (a.dx || a.dw) {
+    b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);
+    b.products_off = take(backward_workspace(b.products, sms));
+  }
+  const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (4 * sms + strips - 1) / strips;  // one wave
+  b.chunks = rows < most ? rows : most;
+  if (b.chunks > 65535) b.chunks = 65535;
+  if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
+  if (a.db && b.chunks > 1) b.db_off = take(static_cast<size_t>(b.chunks) * 2 * a.N * 4);
+  return b;
+}
+
+size_t gated_backward_workspace(const Backward& a, int sms) { return plan_backward(a, sms).total; }
+
+cudaError_t gated_backward(const Backward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
+  const GatedBackwardPlan b = plan_backward(a, sms);
+  char* base = static_cast<char*>(ws);
+  Backward c = a;
+  __nv_bfloat16* dp = a.dx || a.dw ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
+  float* part = !a.db ? nullptr : b.chunks > 1 ? reinterpret_cast<float*>(base + b.db_off) : a.db;
+  long long np = b.np;
+  int chunks = b.chunks;
+  const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && tma::mappable(a.p, a.T, a.ps, 2);
+  cudaLaunchConfig_t cfg = {};
+  const int tx = dp_lanes(a.N);
+  cfg.gridDim = dim3(ceil_div(a.N, 8 * tx), chunks);
+  cfg.blockDim = dim3(THREADS_256);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg,
+                                     tx == 8    ? (al ? k_gated_dp<true, 8> : k_gated_dp<false, 8>)
+                                     : tx == 16 ? (al ? k_gated_dp<true, 16> : k_gated_dp<false, 16>)
+                                                : (al ? k_gated_dp<true, 32> : k_gated_dp<false, 32>),
+                                     c, dp, np, part, chunks);
+  if (e != cudaSuccess) return e;
+  if (a.db && chunks > 1 && (e = norm::add_rows(part, a.db, 2 * a.N, chunks, stream)) != cudaSuccess) return e;
+  if (!dp) return cudaSuccess;
+  Backward products = b.products;
+  products.dy = dp;
+  return backward(products, base + b.products_off, err, sms, stream);
+}
+
+}  // namespace linear
+}  // namespace whtmix

@@ -1,0 +1,12 @@
+// whtmix_gemm_gated.cu -- the instances of whtmix_gemm_gated.cuh with bf16 operands, bf16 and float output.
+#include "whtmix_gemm_gated.cuh"
+
+namespace whtmix {
+namespace linear {
+
+cudaError_t gemm_gated(const Gated& g, bool out_f32, int bn, int sms, cudaStream_t stream) {
+  return out_f32 ? gated_by_width<false, float>(g, bn, sms, stream) : gated_by_width<false, __nv_bfloat16>(g, bn, sms, stream);
+}
+
+}  // namespace linear
+}  // namespace whtmix

@@ -1,0 +1,558 @@
+// whtmix_layer_norm.cu -- layer norm with the residual's addition, its 8-bit output, and its backward.
+//
+//   h = x + r,  m = mean(h),  c = h - m,  rstd = 1 / sqrt(mean(c^2) + eps),  y = c rstd w + b                one row of D channels
+//   8 bits: s = max_d |y_d| / 448,  q_d = e4m3(y_d / s)
+//   backward, with n = c rstd and a = dy w:
+//     dx = rstd (a - mean(a) - n mean(a n)) + dh,      dw = sum over rows of dy n,      db = sum over rows of dy
+//
+// Bound by memory: a row is read once into registers (packed as stored) and written once.  The variance is taken from the
+// differences to the mean, in a second reduction over the registers: as a difference of two sums it would lose what a mean far from
+// zero takes.  Of the backward's sums only the mean stands alone, the other three share a reduction.  Layouts, unaligned rows and
+// the sums over rows as whtmix_norm.cu has them (whtmix_rows.cuh), with two sets of column sums; rows beyond the registers are
+// read several times, from L2 (k_ln_long, k_ln_bwd_long).
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "whtmix_kernels.cuh"
+#include "whtmix_layer_norm.cuh"
+#include "whtmix_rows.cuh"
+
+namespace whtmix {
+namespace norm {
+
+// The sums of a[0 .. N - 1] (MAXB: the largest by its bits) over a row's TPR threads, the same value in each.  STEP numbers a row's
+// reductions: each has its own shared memory, so that one barrier a reduction is enough (whoever writes a step's again has passed
+// the next step's barrier, behind every read of it; a row has two steps at least).
+template <int TPR, int STEP, bool MAXB, int N>
+__device__ __forceinline__ void row_join(float (&a)[N]) {
+  constexpr int W = TPR < 32 ? TPR : 32;
+  auto join = [](float u, float v) { return MAXB ? __uint_as_float(max(__float_as_uint(u), __float_as_uint(v))) : u + v; };
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] = join(a[i], __shfl_xor_sync(0xffffffffu, a[i], o));
+  if constexpr (TPR > 32) {
+    __shared__ float s[N][TPR / 32];
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i][threadIdx.x >> 5] = a[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      a[i] = s[i][0];
+#pragma unroll
+      for (int j = 1; j < TPR / 32; ++j) a[i] = join(a[i], s[i][j]);
+    }
+  }
+}
+
+// Whether element j of vector k is the row's.
+template <typename R, bool AL>
+__device__ __forceinline__ bool mine(int lane, int k, int j, int off, int D) {
+  const int e = R::at(lane, k) - off;
+  return AL ? e < D : e + j >= 0 && e + j < D;
+}
+
+template <typename T, bool Q8, bool AL, int TPR, int NV>
+__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, const Same same) {
+  constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
+  using R = Row<T, AL, TPR>;
+  extern __shared__ float s_w[];  // unaligned rows: the gains, then the shifts
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  pdl_wait();
+  const bool short_launch = gridDim.x < 128;  // (lets the next kernel come in at once, as k_rms)
+  if (short_launch) pdl_trigger();
+  const int set = V * slots_of<V>(a.D);
+  if constexpr (!AL) {
+    gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
+    if (a.b) gains_to_shared<V, BLOCK>(s_w + set, a.b, a.D);
+    __syncthreads();
+  }
+  const float *gains = AL ? a.w : s_w, *shifts = AL || !a.b ? a.b : s_w + set;
+  Kept<R, AL, NV> kept_w, kept_b = {};
+  kept_w.fill(gains, lane, a.D);
+  if (a.b) kept_b.fill(shifts, lane, a.D);
+  const long long step = static_cast<long long>(gridDim.x) * ROWS;
+  const Bounds bx = bounds_of<T>(a.x, a.T, a.xs, a.D), br = bounds_of<T>(a.r, a.T, a.rs, a.D);
+  uint4 ux[NV], ur[NV];
+  auto fetch = [&](long long t) {
+    const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
+    const int D = t < a.T ? a.D : 0;  // a row past the end holds no elements
+    R::fetch(x, bx, lane, R::offset(x), true, D, ux);
+    if (a.r) R::fetch(r, br, lane, R::offset(x), same.a, D, ur);
+  };
+  fetch(static_cast<long long>(blockIdx.x) * ROWS + group);
+  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += step) {
+    const long long t = base + group;
+    const int D = t < a.T ? a.D : 0;
+    const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
+    const int off = R::offset(x);
+    const Places<V> places(off, a.D);
+    float h[NV][V], sum[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      R::values(x, bx, lane, k, off, true, D, ux[k], h[k]);
+      if (a.r) {
+        float f[V];
+        R::values(r, br, lane, k, off, same.a, D, ur[k], f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[k][j] += f[j];
+        if (a.h) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, off, same.b, D, h[k]);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] += h[k][j];
+    }
+    fetch(t + step);
+    row_join<TPR, 0, false>(sum);
+    const float mean = sum[0] * inv_d;
+    float sq[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        h[k][j] = mine<R, AL>(lane, k, j, off, a.D) ? h[k][j] - mean : 0.f;
+        sq[0] += h[k][j] * h[k][j];
+      }
+    row_join<TPR, 1, false>(sq);
+    const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
+    float top[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float w[V], b[V] = {};
+      kept_w.get(gains, places, lane, k, off, a.D, w);
+      if (a.b) kept_b.get(shifts, places, lane, k, off, a.D, b);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        h[k][j] = h[k][j] * rstd * w[j] + b[j];
+        if (Q8) top[0] = __uint_as_float(max(__float_as_uint(top[0]), __float_as_uint(magnitude(h[k][j]))));
+      }
+      if constexpr (!Q8) R::store(static_cast<T*>(a.y) + t * a.ys, lane, k, off, same.c, D, h[k]);
+    }
+    if constexpr (Q8) {
+      row_join<TPR, 2, true>(top);
+      const float lift = top[0] < TINY ? LIFT : 1.f, f = to_e4m3_range(top[0], lift);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[k][j] = h[k][j] * lift * f;
+        R::store_e4m3(static_cast<uint8_t*>(a.y) + t * a.ys, lane, k, off, same.c, D, h[k]);
+      }
+      if (lane == 0 && t < a.T) a.scale[t] = top[0] * (1.f / E4M3_MAX);
+    }
+  }
+  if (!short_launch) pdl_trigger();
+}
+
+// A long row's sum of f(e) by LONG_THREADS threads, 32 terms at a time: a thread's own sum stays short.
+template <class F>
+__device__ __forceinline__ float sum_along(int D, F&& f) {
+  float total = 0.f;
+  for (int e0 = threadIdx.x; e0 < D; e0 += 32 * LONG_THREADS) {
+    float s = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < 32; ++i) {
+      const int e = e0 + i * LONG_THREADS;
+      if (e < D) s += f(e);
+    }
+    total += s;
+  }
+  return total;
+}
+
+// Rows too long for the registers: a CTA a row.  Element loads.
+template <typename T, bool Q8>
+__global__ void __launch_bounds__(LONG_THREADS) k_ln_long(const LayerForward a) {
+  pdl_wait();
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + t * a.xs;
+    const T* r = static_cast<const T*>(a.r) + t * a.rs;
+    auto h = [&](int e) { return Io<T>::get(x, e) + (a.r ? Io<T>::get(r, e) : 0.f); };
+    float sum[1] = {sum_along(a.D, h)};
+    row_join<LONG_THREADS, 0, false>(sum);
+    const float mean = sum[0] * inv_d;
+    float sq[1] = {sum_along(a.D, [&](int e) {
+      const float c = h(e) - mean;
+      return c * c;
+    })};
+    row_join<LONG_THREADS, 1, false>(sq);
+    const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
+    auto y = [&](float v, int e) { return (v - mean) * rstd * __ldg(a.w + e) + (a.b ? __ldg(a.b + e) : 0.f); };
+    float top[1] = {0.f}, lift = 1.f, f = 1.f;
+    if constexpr (Q8) {
+      for (int e = threadIdx.x; e < a.D; e += LONG_THREADS)
+        top[0] = __uint_as_float(max(__float_as_uint(top[0]), __float_as_uint(magnitude(y(h(e), e)))));
+      row_join<LONG_THREADS, 2, true>(top);
+      lift = top[0] < TINY ? LIFT : 1.f, f = to_e4m3_range(top[0], lift);
+      if (threadIdx.x == 0) a.scale[t] = top[0] * (1.f / E4M3_MAX);
+    }
+    for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+      const float v = h(e), o = y(v, e);  // (before h or y take x's place)
+      if (a.r && a.h) Io<T>::put(static_cast<T*>(a.h) + t * a.hs, e, v);
+      if constexpr (Q8)
+        (static_cast<uint8_t*>(a.y) + t * a.ys)[e] = __nv_cvt_float_to_fp8(o * lift * f, __NV_SATFINITE, __NV_E4M3);
+      else
+        Io<T>::put(static_cast<T*>(a.y) + t * a.ys, e, o);
+    }
+  }
+  pdl_trigger();
+}
+
+// dx, and this CTA's partial row of dw and of db: part[blockIdx.x][0 .. 2 D).  Aligned rows: a thread's columns are the same in every
+// row, their sums stay in its registers.  Unaligned ones, and rows of more vectors than that leaves registers for: in shared memory,
+// two sets for each of the CTA's row groups (dynamic).
+template <typename T, bool AL, int TPR, int NV>
+__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln_bwd(const LayerBackward a, const Same same) {
+  constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
+  using R = Row<T, AL, TPR>;
+  extern __shared__ float s_acc[];  // a group's sums for dw, then for db; behind all groups' the gains
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  float acc_w[AL ? NV : 1][V] = {}, acc_b[AL ? NV : 1][V] = {};
+  const int set = V * slots_of<V>(a.D);
+  float *own_w = s_acc + (AL ? 0 : 2 * group * set), *own_b = own_w + (AL ? 0 : set);
+  if constexpr (!AL) {
+    for (int i = lane; i < 2 * set; i += TPR) own_w[i] = 0.f;
+  }
+  float* s_w = s_acc + 2 * ROWS * set;
+  pdl_wait();
+  if constexpr (!AL) {
+    gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
+    __syncthreads();
+  }
+  const float* gains = AL ? a.w : s_w;
+  Kept<R, AL, NV> kept;
+  kept.fill(gains, lane, a.D);
+  const long long step = static_cast<long long>(gridDim.x) * ROWS;
+  const Bounds bh = bounds_of<T>(a.h, a.T, a.hs, a.D), bd = bounds_of<T>(a.dy, a.T, a.ys, a.D), bg = bounds_of<T>(a.dh, a.T, a.ds, a.D);
+  uint4 uh[NV], ud[NV];
+  auto fetch = [&](long long t) {
+    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
+    const int D = t < a.T ? a.D : 0;
+    R::fetch(hp, bh, lane, R::offset(hp), true, D, uh);
+    R::fetch(dp, bd, lane, R::offset(hp), same.a, D, ud);
+  };
+  fetch(static_cast<long long>(blockIdx.x) * ROWS + group);
+  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += step) {
+    const long long t = base + group;
+    const int D = t < a.T ? a.D : 0;
+    float h[NV][V], d[NV][V], sum[1] = {0.f};
+    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
+    const int off = R::offset(hp);
+    const Places<V> places(off, a.D);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      R::values(hp, bh, lane, k, off, true, D, uh[k], h[k]);
+      R::values(dp, bd, lane, k, off, same.a, D, ud[k], d[k]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] += h[k][j];
+    }
+    uint4 ug[NV];
+    const T* gp = static_cast<const T*>(a.dh) + t * a.ds;
+    if (a.dh) R::fetch(gp, bg, lane, off, same.b, D, ug);
+    fetch(t + step);
+    row_join<TPR, 0, false>(sum);
+    const float mean = sum[0] * inv_d;
+    float s[3] = {};  // of c^2, a, a c
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float w[V];
+      kept.get(gains, places, lane, k, off, a.D, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        h[k][j] = mine<R, AL>(lane, k, j, off, a.D) ? h[k][j] - mean : 0.f;
+        const float g = d[k][j] * w[j];
+        s[0] += h[k][j] * h[k][j];
+        s[1] += g;
+        s[2] += g * h[k][j];
+      }
+    }
+    row_join<TPR, 1, false>(s);  // (more than a warp a row: a barrier, behind which the last row's columns are added)
+    if constexpr (!AL && TPR <= 32) __syncwarp();
+    const float rstd = t < a.T ? rsqrtf(s[0] * inv_d + a.eps) : 0.f;  // (a row past the end adds nothing to dw, with eps = 0 either)
+    const float ma = s[1] * inv_d, q = rstd * rstd * (s[2] * inv_d);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float w[V], o[V] = {};
+      kept.get(gains, places, lane, k, off, a.D, w);
+      if (a.dh) R::values(gp, bg, lane, k, off, same.b, D, ug[k], o);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float g = d[k][j] * (h[k][j] * rstd);
+        if constexpr (AL) {
+          acc_w[k][j] += g;
+          acc_b[k][j] += d[k][j];
+        } else if (R::at(lane, k) - off < D) {
+          own_w[places.at[j] + lane + TPR * k] += g;
+          own_b[places.at[j] + lane + TPR * k] += d[k][j];
+        }
+        o[j] += rstd * (d[k][j] * w[j] - ma - q * h[k][j]);
+      }
+      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o);
+    }
+  }
+  // the CTA's row groups hold the same columns: added in ascending group order
+  float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.x) * 2 * a.D;
+  if constexpr (!AL) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.D; i += BLOCK) {
+      const int e = i < a.D ? i : i - a.D;
+      const float* from = s_acc + (i < a.D ? 0 : set) + column_at<V>(e, a.D);
+      float sum = from[0];
+#pragma unroll 4
+      for (int g = 1; g < ROWS; ++g) sum += from[2 * g * set];
+      part[i] = sum;
+    }
+  } else if constexpr (ROWS == 1) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int e = R::at(lane, k) + j;
+        if (e < a.D) part[e] = acc_w[k][j], part[a.D + e] = acc_b[k][j];
+      }
+  } else {
+    __shared__ float s[ROWS][TPR][V + 1];
+    auto put = [&](const float (&acc)[AL ? NV : 1][V], float* to) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[group][lane][j] = acc[k][j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < TPR * V; i += BLOCK) {
+          const int l = i / V, j = i % V;
+          float sum = 0.f;
+#pragma unroll
+          for (int g = 0; g < ROWS; ++g) sum += s[g][l][j];
+          if (R::at(l, k) + j < a.D) to[R::at(l, k) + j] = sum;
+        }
+      }
+    };
+    put(acc_w, part);
+    put(acc_b, part + a.D);
+  }
+  pdl_trigger();
+}
+
+// Rows too long for the registers: dx (DX) by a CTA a row; coef[t] = mean and rstd for k_dwdb_long.
+template <typename T, bool DX>
+__global__ void __launch_bounds__(LONG_THREADS) k_ln_bwd_long(const LayerBackward a, float2* __restrict__ coef) {
+  pdl_wait();
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const T* h = static_cast<const T*>(a.h) + t * a.hs;
+    const T* dy = static_cast<const T*>(a.dy) + t * a.ys;
+    float sum[1] = {sum_along(a.D, [&](int e) { return Io<T>::get(h, e); })};
+    row_join<LONG_THREADS, 0, false>(sum);
+    const float mean = sum[0] * inv_d;
+    float s[3];
+    s[0] = sum_along(a.D, [&](int e) {
+      const float c = Io<T>::get(h, e) - mean;
+      return c * c;
+    });
+    s[1] = s[2] = 0.f;
+    if constexpr (DX) {
+      s[1] = sum_along(a.D, [&](int e) { return Io<T>::get(dy, e) * __ldg(a.w + e); });
+      s[2] = sum_along(a.D, [&](int e) { return Io<T>::get(dy, e) * __ldg(a.w + e) * (Io<T>::get(h, e) - mean); });
+    }
+    row_join<LONG_THREADS, 1, false>(s);
+    const float rstd = rsqrtf(s[0] * inv_d + a.eps), ma = s[1] * inv_d, q = rstd * rstd * (s[2] * inv_d);
+    if constexpr (DX) {
+      for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
+        float o = a.dh ? Io<T>::get(static_cast<const T*>(a.dh) + t * a.ds, e) : 0.f;
+        o += rstd * (Io<T>::get(dy, e) * __ldg(a.w + e) - ma - q * (Io<T>::get(h, e) - mean));
+        Io<T>::put(static_cast<T*>(a.dx) + t * a.xs, e, o);
+      }
+    }
+    if (threadIdx.x == 0) coef[t] = make_float2(mean, rstd);
+  }
+  pdl_trigger();
+}
+// part[blockIdx.y][e], [D + e] = sums over the rows of chunk blockIdx.y of dy n and dy
+template <typename T>
+__global__ void __launch_bounds__(256) k_dwdb_long(const LayerBackward a, const float2* coef, int chunks) {
+  pdl_wait();
+  const int e = blockIdx.x * 256 + threadIdx.x;
+  const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
+  if (e < a.D) {
+    float dw = 0.f, db = 0.f;
+    for (long long t = t0; t < t1; ++t) {
+      const float g = Io<T>::get(static_cast<const T*>(a.dy) + t * a.ys, e);
+      const float2 c = coef[t];
+      dw += g * ((Io<T>::get(static_cast<const T*>(a.h) + t * a.hs, e) - c.x) * c.y);
+      db += g;
+    }
+    float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.y) * 2 * a.D;
+    part[e] = dw, part[a.D + e] = db;
+  }
+  pdl_trigger();
+}
+
+// dw[e] and db[e] (or null) = the sums of `parts` partial rows of 2 D: 32 runs of consecutive rows, each in ascending order, then the
+// run sums in ascending order.  A CTA takes 32 columns.
+constexpr int DWDB_RUNS = 32;
+__global__ void __launch_bounds__(32 * DWDB_RUNS) k_dwdb(const float* part, float* dw, float* db, int D, int parts) {
+  __shared__ float s[DWDB_RUNS][33];
+  pdl_wait();
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, e = blockIdx.x * 32 + lane, n = db ? 2 * D : D;
+  const int p0 = parts * g / DWDB_RUNS, p1 = parts * (g + 1) / DWDB_RUNS;
+  float sum = 0.f;
+  if (e < n) {
+    const float* q = part + e;
+    int p = p0;
+    for (; p + 8 <= p1; p += 8) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = __ldcg(q + static_cast<long long>(p + u) * 2 * D);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum += v[u];
+    }
+    for (; p < p1; ++p) sum += __ldcg(q + static_cast<long long>(p) * 2 * D);
+  }
+  s[g][lane] = sum;
+  __syncthreads();
+  if (g == 0 && e < n) {
+    float total = s[0][lane];
+#pragma unroll
+    for (int i = 1; i < DWDB_RUNS; ++i) total += s[i][lane];
+    if (e < D) dw[e] = total; else db[e - D] = total;
+  }
+  pdl_trigger();
+}
+
+// ---- host ----
+
+template <typename T, bool Q8>
+static cudaError_t forward_t(const LayerForward& a, int sms, cudaStream_t stream) {
+  constexpr int V = Io<T>::V;
+  const size_t es = sizeof(T);
+  const bool al = a.D % V == 0 && aligned(a.w, 16) && (!a.b || aligned(a.b, 16)) && rows_aligned(a.x, a.xs, es) && rows_aligned(a.r, a.rs, es) &&
+                  rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, V) : rows_aligned(a.y, a.ys, es));
+  const int n = vectors(a.D, es == 2, al);
+  LayerForward c = a;
+  if (n > MAX_VECTORS) {
+    void* args[] = {&c};
+    return launch_pdl(reinterpret_cast<const void*>(k_ln_long<T, Q8>), grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args);
+  }
+  // (8 bits: a vector's V bytes start on a multiple of V)
+  const bool same_y = Q8 ? (reinterpret_cast<uintptr_t>(a.y) - reinterpret_cast<uintptr_t>(a.x) / es) % V == 0 && (a.ys - a.xs) % V == 0
+                         : rows_same(a.x, a.xs, a.y, a.ys, es);
+  Same same{rows_same(a.x, a.xs, a.r, a.rs, es), rows_same(a.x, a.xs, a.r ? a.h : nullptr, a.hs, es), same_y};
+  return by_length(n, a.T < sms, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
+    const void* k = al ? reinterpret_cast<const void*>(k_ln<T, Q8, true, TPR, NV>) : reinterpret_cast<const void*>(k_ln<T, Q8, false, TPR, NV>);
+    void* args[] = {&c, &same};
+    const size_t smem = al ? 0 : static_cast<size_t>(a.b ? 2 : 1) * V * slots_of<V>(a.D) * 4;  // at most 128 KB
+    int resident = 0;
+    const cudaError_t e = resident_ctas(k, BLOCK, smem, sms, &resident);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(k, grid_rows(a.T, BLOCK / TPR, resident), BLOCK, smem, stream, args);
+  });
+}
+
+cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, int sms, cudaStream_t stream) {
+  if (a.T <= 0) return cudaSuccess;
+  if (bf16) return to_e4m3 ? forward_t<__nv_bfloat16, true>(a, sms, stream) : forward_t<__nv_bfloat16, false>(a, sms, stream);
+  return to_e4m3 ? forward_t<float, true>(a, sms, stream) : forward_t<float, false>(a, sms, stream);
+}
+
+static int long_parts(long long T) { return static_cast<int>(T < 64 ? T : 64); }
+
+// How a backward call's rows are taken: aligned in registers up to MAX_SUMMED vectors (two sets of sums beside two inputs: with four
+// vectors a thread they would not fit 128 registers), else as unaligned ones.
+constexpr int MAX_SUMMED = 1024;
+struct LayerRows {
+  bool al;
+  int n;  // vectors
+};
+template <typename T>
+static LayerRows layer_rows(const LayerBackward& a) {
+  const size_t es = sizeof(T);
+  const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.h, a.hs, es) && rows_aligned(a.dy, a.ys, es) &&
+                  rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es) && vectors(a.D, es == 2, true) <= MAX_SUMMED;
+  return {al, vectors(a.D, es == 2, al)};
+}
+
+// A call's kernel, its shared memory and its CTAs, each of which leaves a partial row of dw and db.
+struct LayerPlan {
+  const void* kernel;
+  size_t smem;
+  int block, parts;
+};
+template <typename T>
+static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int sms, LayerPlan* p) {
+  return by_length_backward(rows.n, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
+    p->kernel = rows.al ? reinterpret_cast<const void*>(k_ln_bwd<T, (NV <= 2), TPR, NV>) : reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV>);
+    p->smem = rows.al ? 0 : static_cast<size_t>(2 * (BLOCK / TPR) + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 193 KB
+    p->block = BLOCK;
+    int resident = 0;
+    const cudaError_t e = resident_ctas(p->kernel, BLOCK, p->smem, sms, &resident);
+    if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, BLOCK / TPR, resident));
+    return e;
+  });
+}
+
+template <typename T>
+static cudaError_t workspace_t(const LayerBackward& a, int sms, size_t* bytes) {
+  const LayerRows rows = layer_rows<T>(a);
+  if (rows.n > MAX_VECTORS) {
+    *bytes = static_cast<size_t>(long_parts(a.T)) * 2 * a.D * 4 + static_cast<size_t>(a.T) * 8;
+    return cudaSuccess;
+  }
+  LayerPlan p;
+  const cudaError_t e = layer_plan<T>(a, rows, sms, &p);
+  if (e == cudaSuccess) *bytes = static_cast<size_t>(p.parts) * 2 * a.D * 4;
+  return e;
+}
+cudaError_t layer_backward_workspace(const LayerBackward& a, bool bf16, int sms, size_t* bytes) {
+  return bf16 ? workspace_t<__nv_bfloat16>(a, sms, bytes) : workspace_t<float>(a, sms, bytes);
+}
+
+template <typename T>
+static cudaError_t backward_t(const LayerBackward& a, int sms, cudaStream_t stream) {
+  const size_t es = sizeof(T);
+  const LayerRows rows = layer_rows<T>(a);
+  int parts = long_parts(a.T);
+  LayerBackward c = a;
+  cudaError_t e;
+  if (rows.n > MAX_VECTORS) {
+    float2* coef = reinterpret_cast<float2*>(static_cast<float*>(a.ws) + static_cast<size_t>(parts) * 2 * a.D);
+    // dw reads dy: where dx takes dy's place, the coefficients alone come first and dx last
+    const bool over_dy = a.dx == a.dy;
+    const void *with_dx = reinterpret_cast<const void*>(k_ln_bwd_long<T, true>), *without = reinterpret_cast<const void*>(k_ln_bwd_long<T, false>);
+    void* args[] = {&c, &coef};
+    auto take = [&](const void* k) { return launch_pdl(k, grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args); };
+    if ((e = take(over_dy ? without : with_dx)) != cudaSuccess) return e;
+    k_dwdb_long<T><<<dim3((a.D + 255) / 256, parts), 256, 0, stream>>>(c, coef, parts);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (over_dy) e = take(with_dx);
+  } else {
+    Same same{rows_same(a.h, a.hs, a.dy, a.ys, es), rows_same(a.h, a.hs, a.dh, a.ds, es), rows_same(a.h, a.hs, a.dx, a.xs, es)};
+    LayerPlan p;
+    if ((e = layer_plan<T>(a, rows, sms, &p)) != cudaSuccess) return e;
+    parts = p.parts;
+    void* args[] = {&c, &same};
+    e = launch_pdl(p.kernel, static_cast<unsigned>(parts), p.block, p.smem, stream, args);
+  }
+  if (e != cudaSuccess) return e;
+  const float* part = static_cast<const float*>(a.ws);
+  float *dw = a.dw, *db = a.db;
+  int D = a.D;
+  void* args[] = {&part, &dw, &db, &D, &parts};
+  return launch_pdl(reinterpret_cast<const void*>(k_dwdb), static_cast<unsigned>(((db ? 2 * D : D) + 31) / 32), 32 * DWDB_RUNS, 0, stream, args);
+}
+
+cudaError_t layer_backward(const LayerBackward& a, bool bf16, int sms, cudaStream_t stream) {
+  return bf16 ? backward_t<__nv_bfloat16>(a, sms, stream) : backward_t<float>(a, sms, stream);
+}
+
+}  // namespace norm
+}  // namespace whtmix

@@ -10,6 +10,7 @@
 #include "whtmix_few.cuh"
 #include "whtmix_gemm.cuh"
 #include "whtmix_linear.cuh"
+#include "whtmix_linear_host.cuh"
 #include "whtmix_norm.cuh"
 #include "whtmix_unaligned.cuh"
 
@@ -21,12 +22,6 @@ constexpr int THREADS_256 = 256;
 // ---- rows to a 16-byte pitch ----
 // dst [rows, pitch] = src [rows, cols] (stride elements a row), zeros beyond cols; a thread writes 16 bytes.  pitch is a multiple of
 // 16 bytes.  Up to two matrices a launch.
-struct Copy {
-  uint8_t* dst;
-  const uint8_t* src;
-  long long rows, stride, cols, pitch;  // stride, cols, pitch in bytes
-  long long chunks() const { return rows * (pitch / 16); }
-};
 template <typename I>  // 32-bit places where they suffice
 __global__ void __launch_bounds__(THREADS_256) k_pitch(const Copy a, const Copy b, long long na, long long n) {
   constexpr int U = 4;
@@ -61,11 +56,7 @@ __global__ void __launch_bounds__(THREADS_256) k_pitch(const Copy a, const Copy 
   pdl_trigger();
 }
 
-static Copy copy_of(void* dst, const void* src, long long rows, int cols, long long stride, int pitch, int es) {
-  return {static_cast<uint8_t*>(dst), static_cast<const uint8_t*>(src), rows, stride * es, static_cast<long long>(cols) * es,
-          static_cast<long long>(pitch) * es};
-}
-static cudaError_t to_pitch(const Copy& a, const Copy& b, int sms, cudaStream_t stream) {
+cudaError_t to_pitch(const Copy& a, const Copy& b, int sms, cudaStream_t stream) {
   long long na = a.dst ? a.chunks() : 0, n = na + (b.dst ? b.chunks() : 0);
   if (n == 0) return cudaSuccess;
   const long long need = (n + 4 * THREADS_256 - 1) / (4 * THREADS_256), most = 4ll * sms;
@@ -216,20 +207,13 @@ __global__ void __launch_bounds__(THREADS_256) k_sum_splits(O* __restrict__ out,
 
 // ---- host ----
 
-static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
-static int pitch_of(int cols, int es) { return (cols + 16 / es - 1) / (16 / es) * (16 / es); }
-static int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
-
 // Tile width and splits of a product of M rows, N columns and kblocks K blocks.  A block of a tile costs BLOCK clocks of an SM (of a
 // pair of them), not in proportion to its width: the operands' way from L2 and out of shared memory bounds the narrow tiles
 // (measured at [8192, 4096] x [4096, 4096]: 545 clocks at 256 columns, 450 at 128; a pair's 256 x 256 takes 470).  A tile costs about
 // TILE_CLOCKS besides, more where two CTAs wait for each other, a split product's partial tiles their way through memory.  Pairs
 // against single tiles, us: that product 157.7 and 168.5; [8192, 1024] x [1024, 1024] 18.7 and 17.2; 64800 tokens of 128 channels to
 // 512 32.2 and 28.6: long K axes take pairs, short ones do not.
-struct Plan {
-  int bn, splits;
-};
-static Plan plan_product(long long M, int N, int kblocks, int sms, int max_splits) {
+Plan plan_product(long long M, int N, int kblocks, int sms, int max_splits) {
   constexpr double TILE_CLOCKS = 1500.0, PAIR_TILE_CLOCKS = 3700.0;
   Plan best{256, 1};
   double best_cost = 1e300;
@@ -294,7 +278,7 @@ cudaError_t forward(const Forward& a, void* ws, unsigned int* err, int sms, cuda
     cw = copy_of(static_cast<char*>(ws) + f.w_off, a.w, a.N, a.K, a.ws, f.kp, es);
   }
   if ((e = to_pitch(cx, cw, sms, stream)) != cudaSuccess) return e;
-  if (use_few(a.T, ceil_div(a.K, 128 / es))) return forward_few(a, x, xs, w, wst, err, sms, stream);
+  if (use_few(a.T, ceil_div(a.K, 128 / es))) return forward_few(a, x, xs, w, wst, false, err, sms, stream);
   Gemm g{};
   g.kblocks = ceil_div(a.K, 128 / es);
   const Plan pl = plan_product(a.T, a.N, g.kblocks, sms, 1);

@@ -11,6 +11,8 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <vector>
+
 #include "whtmix.h"
 
 namespace {
@@ -223,6 +225,218 @@ PyObject* linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// x, w, b or None, residual or None, eps, out_dtype or None
+PyObject* layer_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor* x = n == 6 ? tensor(args[0]) : nullptr;
+  if (!x || !PyFloat_CheckExact(args[4]) || !x->is_cuda()) Py_RETURN_NONE;
+  const int device = x->get_device();
+  const at::ScalarType type = x->scalar_type();
+  if (!current(device) || (type != at::kBFloat16 && type != at::kFloat)) Py_RETURN_NONE;
+  at::ScalarType to = type;
+  if (args[5] != Py_None && (!type_of(args[5], &to) || (to != type && to != at::kFloat8_e4m3fn))) Py_RETURN_NONE;
+  Rows rx, rr;
+  const float *w, *b = nullptr;
+  if (!rows_of(*x, device, type, &rx) || !floats(args[1], {rx.cols}, device, &w) || (args[2] != Py_None && !floats(args[2], {rx.cols}, device, &b)))
+    Py_RETURN_NONE;
+  const bool sum = args[3] != Py_None, eight = to == at::kFloat8_e4m3fn;
+  const at::IntArrayRef shape = x->sizes();
+  if (sum && !rows_like(args[3], shape, device, type, &rr)) Py_RETURN_NONE;
+  if (eight && rx.cols % 16) Py_RETURN_NONE;  // its rows lie at a wider pitch
+  const at::Tensor y = empty(shape, to, *x), h = sum ? empty(shape, type, *x) : at::Tensor();
+  const at::Tensor s = eight ? empty(shape.slice(0, shape.size() - 1), at::kFloat, *x) : at::Tensor();
+  void *yp = y.data_ptr(), *hp = sum ? h.data_ptr() : nullptr;
+  float* sp = eight ? static_cast<float*>(s.data_ptr()) : nullptr;
+  const float eps = static_cast<float>(PyFloat_AS_DOUBLE(args[4]));
+  if (!run("whtmix_layer_norm", device, [&](void* stream) {
+        return whtmix_layer_norm(rx.p, rr.p, w, b, hp, yp, sp, rx.rows, rx.cols, rx.stride, rr.stride, sum ? rx.cols : 0, rx.cols, eps,
+                                 code(type), code(to), stream);
+      }))
+    return nullptr;
+  if (eight) return sum ? tuple(y, s, h) : tuple(y, s);
+  return sum ? tuple(y, h) : THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// h, w, dy, dh or None, eps, need_db
+PyObject* layer_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor* h = n == 6 ? tensor(args[0]) : nullptr;
+  if (!h || !PyFloat_CheckExact(args[4]) || !h->is_cuda()) Py_RETURN_NONE;
+  const int device = h->get_device();
+  const at::ScalarType type = h->scalar_type();
+  if (!current(device) || (type != at::kBFloat16 && type != at::kFloat)) Py_RETURN_NONE;
+  Rows rh, ry, rd;
+  const float* w;
+  if (!rows_of(*h, device, type, &rh) || !floats(args[1], {rh.cols}, device, &w) || !rows_like(args[2], h->sizes(), device, type, &ry) ||
+      (args[3] != Py_None && !rows_like(args[3], h->sizes(), device, type, &rd)))
+    Py_RETURN_NONE;
+  const int need = PyObject_IsTrue(args[5]);
+  if (need < 0) return nullptr;
+  const at::Tensor dx = empty(h->sizes(), type, *h), dw = empty({rh.cols}, at::kFloat, *h), db = need ? empty({rh.cols}, at::kFloat, *h) : at::Tensor();
+  void* dxp = dx.data_ptr();
+  float *dwp = static_cast<float*>(dw.data_ptr()), *dbp = need ? static_cast<float*>(db.data_ptr()) : nullptr;
+  const float eps = static_cast<float>(PyFloat_AS_DOUBLE(args[4]));
+  if (!run("whtmix_layer_norm_backward", device, [&](void* stream) {
+        return whtmix_layer_norm_backward(rh.p, w, ry.p, rd.p, dxp, dwp, dbp, rh.rows, rh.cols, rh.stride, ry.stride, rd.stride, rh.cols, eps,
+                                          code(type), stream);
+      }))
+    return nullptr;
+  return tuple(dx, dw, db);
+  END_HANDLE_TH_ERRORS
+}
+
+// x, w, bias or None, activation code, x_scale or None, w_scale or None, preact (None, False or True), out_dtype
+PyObject* gated_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *x = n == 8 ? tensor(args[0]) : nullptr, *w = x ? tensor(args[1]) : nullptr;
+  if (!w || !x->is_cuda() || w->dim() != 2 || w->size(0) < 2 || w->size(0) % 2) Py_RETURN_NONE;
+  const int device = x->get_device();
+  const at::ScalarType type = x->scalar_type();
+  const bool eight = type == at::kFloat8_e4m3fn, save = args[6] == Py_True;
+  at::ScalarType to;
+  if (!current(device) || (type != at::kBFloat16 && !eight) || !type_of(args[7], &to) || (to != at::kBFloat16 && to != at::kFloat) ||
+      (save && to != at::kBFloat16))
+    Py_RETURN_NONE;
+  Rows rx, rw;
+  if (!rows_of(*x, device, type, &rx) || !rows_of(*w, device, type, &rw) || rw.cols != rx.cols) Py_RETURN_NONE;
+  const int64_t N = w->size(0) / 2;
+  const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
+  at::DimVector shape(lead), both(lead);
+  shape.push_back(N), both.push_back(2 * N);
+  const float *bias = nullptr, *sx = nullptr, *sw = nullptr;
+  if (eight ? !floats(args[4], lead, device, &sx) || !floats(args[5], {2 * N}, device, &sw) : args[4] != Py_None || args[5] != Py_None)
+    Py_RETURN_NONE;
+  if (args[2] != Py_None && !floats(args[2], {2 * N}, device, &bias)) Py_RETURN_NONE;
+  const int act = static_cast<int>(PyLong_AsLong(args[3]));
+  const at::Tensor y = empty(shape, to, *x), p = save ? empty(both, at::kBFloat16, *x) : at::Tensor();
+  void *yp = y.data_ptr(), *pp = save ? p.data_ptr() : nullptr;
+  if (!run("whtmix_gated_linear", device, [&](void* stream) {
+        return whtmix_gated_linear(rx.p, rw.p, sx, sw, bias, pp, yp, rx.rows, N, rx.cols, rx.stride, rw.stride, save ? 2 * N : 0, N, act,
+                                   code(type), code(to), stream);
+      }))
+    return nullptr;
+  return save ? tuple(y, p) : THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// x, w, dy, p, activation code, need_dx, need_dw, need_db, dw_dtype
+PyObject* gated_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *x = n == 9 ? tensor(args[0]) : nullptr, *w = x ? tensor(args[1]) : nullptr;
+  if (!w || !x->is_cuda() || w->dim() != 2 || w->size(0) < 2 || w->size(0) % 2) Py_RETURN_NONE;
+  const int device = x->get_device();
+  at::ScalarType to;
+  if (!current(device) || !type_of(args[8], &to) || (to != at::kBFloat16 && to != at::kFloat)) Py_RETURN_NONE;
+  Rows rx, rw, ry, rp;
+  const at::ScalarType bf16 = at::kBFloat16;
+  if (!rows_of(*x, device, bf16, &rx) || !rows_of(*w, device, bf16, &rw) || rw.cols != rx.cols) Py_RETURN_NONE;
+  const int64_t N = w->size(0) / 2, K = rx.cols;
+  const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
+  at::DimVector shape(lead), both(lead);
+  shape.push_back(N), both.push_back(2 * N);
+  const int act = static_cast<int>(PyLong_AsLong(args[4]));
+  if (!rows_like(args[2], shape, device, bf16, &ry) || !rows_like(args[3], both, device, bf16, &rp)) Py_RETURN_NONE;
+  int need[3];
+  for (int i = 0; i < 3; ++i)
+    if ((need[i] = PyObject_IsTrue(args[5 + i])) < 0) return nullptr;
+  const at::Tensor dx = need[0] ? empty(x->sizes(), bf16, *x) : at::Tensor();
+  const at::Tensor dw = need[1] ? empty({2 * N, K}, to, *x) : at::Tensor();
+  const at::Tensor db = need[2] ? empty({2 * N}, at::kFloat, *x) : at::Tensor();
+  void *dxp = dx.defined() ? dx.data_ptr() : nullptr, *dwp = dw.defined() ? dw.data_ptr() : nullptr;
+  float* dbp = db.defined() ? static_cast<float*>(db.data_ptr()) : nullptr;
+  if (!run("whtmix_gated_linear_backward", device, [&](void* stream) {
+        return whtmix_gated_linear_backward(rx.p, rw.p, ry.p, rp.p, dxp, dwp, dbp, rx.rows, N, K, rx.stride, rw.stride, ry.stride, rp.stride,
+                                            dxp ? K : 0, act, code(to), stream);
+      }))
+    return nullptr;
+  return tuple(dx, dw, db);
+  END_HANDLE_TH_ERRORS
+}
+
+// A list of plain contiguous tensors on the current device, as the C ABI takes it; `outs`: another list (of their shapes) or null.
+bool entries_of(PyObject* list, PyObject* outs, std::vector<whtmix_tensor_t>* entries, const at::Tensor** first) {
+  if (!PyList_CheckExact(list) || (outs && (!PyList_CheckExact(outs) || PyList_GET_SIZE(outs) != PyList_GET_SIZE(list)))) return false;
+  const Py_ssize_t count = PyList_GET_SIZE(list);
+  if (count == 0) return false;
+  entries->reserve(static_cast<size_t>(count));
+  int device = -1;
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    const at::Tensor* t = tensor(PyList_GET_ITEM(list, i));
+    if (!t || !t->is_cuda()) return false;
+    if (i == 0) {
+      device = t->get_device(), *first = t;
+      if (!current(device)) return false;
+    }
+    const at::ScalarType type = t->scalar_type();
+    if ((type != at::kFloat && type != at::kBFloat16) || !placed(*t, device, type) || !t->is_contiguous()) return false;
+    void* o = nullptr;
+    if (outs) {
+      const at::Tensor* u = tensor(PyList_GET_ITEM(outs, i));
+      if (!u || !placed(*u, device, type) || u->sizes() != t->sizes() || !u->is_contiguous()) return false;
+      o = u->data_ptr();
+    }
+    entries->push_back({t->data_ptr(), o, t->numel(), code(type)});
+  }
+  return true;
+}
+
+// tensors
+PyObject* global_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  std::vector<whtmix_tensor_t> entries;
+  const at::Tensor* first;
+  if (n != 1 || !entries_of(args[0], nullptr, &entries, &first)) Py_RETURN_NONE;
+  const at::Tensor norm = empty({}, at::kFloat, *first);
+  float* p = static_cast<float*>(norm.data_ptr());
+  if (!run("whtmix_global_norm", first->get_device(),
+           [&](void* stream) { return whtmix_global_norm(entries.data(), static_cast<int64_t>(entries.size()), p, stream); }))
+    return nullptr;
+  return THPVariable_Wrap(norm);
+  END_HANDLE_TH_ERRORS
+}
+
+// tensors, max_norm, out or None
+PyObject* clip_by_global_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  std::vector<whtmix_tensor_t> entries;
+  const at::Tensor* first;
+  if (n != 3 || !PyFloat_CheckExact(args[1]) || !entries_of(args[0], args[2] == Py_None ? nullptr : args[2], &entries, &first)) Py_RETURN_NONE;
+  PyObject* out = args[2];
+  if (out == Py_None) {
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    out = PyList_New(count);
+    if (!out) return nullptr;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const at::Tensor& t = *tensor(PyList_GET_ITEM(args[0], i));
+      const at::Tensor o = empty(t.sizes(), t.scalar_type(), t);
+      entries[static_cast<size_t>(i)].out = o.data_ptr();
+      PyObject* w = THPVariable_Wrap(o);
+      if (!w) {
+        Py_DECREF(out);
+        return nullptr;
+      }
+      PyList_SET_ITEM(out, i, w);
+    }
+  } else {
+    Py_INCREF(out);
+  }
+  const at::Tensor norm = empty({}, at::kFloat, *first);
+  float* p = static_cast<float*>(norm.data_ptr());
+  const float max_norm = static_cast<float>(PyFloat_AS_DOUBLE(args[1]));
+  PyObject* both = nullptr;
+  if (run("whtmix_clip_by_global_norm", first->get_device(), [&](void* stream) {
+        return whtmix_clip_by_global_norm(entries.data(), static_cast<int64_t>(entries.size()), max_norm, p, stream);
+      })) {
+    PyObject* w = THPVariable_Wrap(norm);
+    if (w) both = PyTuple_Pack(2, out, w);
+    Py_XDECREF(w);
+  }
+  Py_DECREF(out);
+  return both;
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* bind(PyObject*, PyObject* check) {
   Py_INCREF(check);
   Py_XSETREF(g_check, check);
@@ -231,6 +445,8 @@ PyObject* bind(PyObject*, PyObject* check) {
 
 #define WHTMIX_QUICK(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {WHTMIX_QUICK(rms_norm), WHTMIX_QUICK(rms_norm_backward), WHTMIX_QUICK(linear), WHTMIX_QUICK(linear_backward),
+                         WHTMIX_QUICK(layer_norm), WHTMIX_QUICK(layer_norm_backward), WHTMIX_QUICK(gated_linear), WHTMIX_QUICK(gated_linear_backward),
+                         WHTMIX_QUICK(global_norm), WHTMIX_QUICK(clip_by_global_norm),
                          {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "whtmix_torch", nullptr, -1, methods};
 

@@ -26,7 +26,9 @@ __all__ = ["forward", "backward", "forward_ex", "backward_ex", "forward_noalloc"
            "forward_padded", "backward_padded", "project", "block_forward",
            "block_backward", "workspace_bytes", "sync", "plan", "release_workspaces", "WhtmixError", "WHTMixFunction",
            "WHTMixSeparableFunction", "WHTMixBlockFunction", "pad_tokens", "EXPORTS", "library",
-           "rms_norm", "rms_norm_backward", "linear", "linear_backward", "quantize_rows", "RMSNormFunction", "LinearFunction"]
+           "rms_norm", "rms_norm_backward", "linear", "linear_backward", "quantize_rows", "RMSNormFunction", "LinearFunction",
+           "layer_norm", "layer_norm_backward", "gated_linear", "gated_linear_backward", "global_norm", "clip_by_global_norm",
+           "LayerNormFunction", "GatedLinearFunction"]
 
 # status codes and dtype codes of include/whtmix.h
 OK = 0
@@ -41,7 +43,9 @@ EXPORTS = ("whtmix_forward", "whtmix_backward", "whtmix_workspace_bytes", "whtmi
            "whtmix_last_cuda_error", "whtmix_plan", "whtmix_forward_noalloc", "whtmix_forward_separable",
            "whtmix_backward_separable", "whtmix_forward_padded", "whtmix_backward_padded", "whtmix_project",
            "whtmix_block_forward", "whtmix_block_backward", "whtmix_forward_x16", "whtmix_rms_norm",
-           "whtmix_rms_norm_backward", "whtmix_linear", "whtmix_linear_backward")
+           "whtmix_rms_norm_backward", "whtmix_linear", "whtmix_linear_backward", "whtmix_layer_norm",
+           "whtmix_layer_norm_backward", "whtmix_gated_linear", "whtmix_gated_linear_backward", "whtmix_global_norm",
+           "whtmix_clip_by_global_norm")
 
 E4M3 = torch.float8_e4m3fn
 E4M3_MAX = 448.0
@@ -54,6 +58,11 @@ class WhtmixError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
         super().__init__(f"{what}: WHTMIX_{'ERR_' if status else ''}{STATUS.get(status, status)} ({status})")
+
+
+class _Tensor(ctypes.Structure):
+    """whtmix_tensor_t"""
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int)]
 
 
 _lock = threading.Lock()
@@ -95,6 +104,12 @@ def library(path: str | None = None) -> ctypes.CDLL:
             lib.whtmix_rms_norm_backward.argtypes = [p] * 6 + [i64] * 6 + [f, i, p]
             lib.whtmix_linear.argtypes = [p] * 8 + [i64] * 8 + [i, i, i, p]
             lib.whtmix_linear_backward.argtypes = [p] * 7 + [i64] * 8 + [i, i, p]
+            lib.whtmix_layer_norm.argtypes = [p] * 7 + [i64] * 6 + [f, i, i, p]
+            lib.whtmix_layer_norm_backward.argtypes = [p] * 7 + [i64] * 6 + [f, i, p]
+            lib.whtmix_gated_linear.argtypes = [p] * 7 + [i64] * 7 + [i, i, i, p]
+            lib.whtmix_gated_linear_backward.argtypes = [p] * 7 + [i64] * 8 + [i, i, p]
+            lib.whtmix_global_norm.argtypes = [p, i64, p, p]
+            lib.whtmix_clip_by_global_norm.argtypes = [p, i64, f, p, p]
             for name in EXPORTS:
                 if name != "whtmix_status_string":
                     getattr(lib, name).restype = ctypes.c_int
@@ -645,6 +660,294 @@ def quantize_rows(w: torch.Tensor):
     return (w / scale[:, None]).clamp(-E4M3_MAX, E4M3_MAX).to(E4M3), scale
 
 
+# ---- layer norm, the gated feed-forward half, clipping of a step's gradients ----
+
+def layer_norm(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+               eps: float = 1e-5, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+               h: torch.Tensor | None = None, scale: torch.Tensor | None = None, stream=None):
+    """h = x + residual; y = (h - mean(h)) w / sqrt(var(h) + eps) + b over the last axis (x float32 or bfloat16, w and b
+    float32; var without correction).
+
+    Returns, writes and allocates what rms_norm does: y, or with out_dtype float8_e4m3fn (values, scales); with a residual
+    h is appended."""
+    if x.is_cuda and out is None and h is None and scale is None and stream is None:
+        done = (_quick or _quick_path()).layer_norm(x, w, b, residual, eps, out_dtype)
+        if done is not None:
+            return done
+    if stream is not None and x.is_cuda and (out is None or (h is None and residual is not None) or
+                                             (scale is None and out_dtype == E4M3)):
+        with _on(stream, x.device):
+            return layer_norm(x, w, b, residual, eps, out_dtype, out, h, scale)
+    dtype = x.dtype
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError(f"layer_norm takes float32 or bfloat16, got {dtype}")
+    eight = out_dtype == E4M3
+    if not eight and out_dtype is not None and out_dtype != dtype:
+        raise TypeError(f"layer_norm of {dtype} writes {dtype} or {E4M3}, not {out_dtype}")
+    shape, index = x.shape, x.get_device()
+    T, D, xs = _rows(x, "x", index)
+    wp = _vector(w, (D,), "w", index)
+    bp = 0 if b is None else _vector(b, (D,), "b", index)
+    device = x.device
+    rp = rs = hp = hs = sp = 0
+    if residual is not None:
+        rs = _stride(residual, shape, dtype, "residual", index)
+        rp = residual.data_ptr()
+        if h is None:
+            h, hs = torch.empty(shape, dtype=dtype, device=device), D
+        else:
+            hs = _stride(h, shape, dtype, "h", index)
+        hp = h.data_ptr()
+    elif h is not None:
+        raise ValueError("h is the sum of x and the residual: it needs a residual")
+    if out is not None:
+        ys = _stride(out, shape, E4M3 if eight else dtype, "out", index)
+    elif eight and D % 16:
+        # rows at a 16-byte pitch, as the tensor cores' loads want them: linear and gated_linear take them as they lie
+        ys = (D + 15) // 16 * 16
+        out = torch.empty((*shape[:-1], ys), dtype=E4M3, device=device)[..., :D]
+    else:
+        out, ys = torch.empty(shape, dtype=E4M3 if eight else dtype, device=device), D
+    if eight:
+        if scale is None:
+            scale = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+            sp = scale.data_ptr()
+        else:
+            sp = _vector(scale, shape[:-1], "scale", index)
+    elif scale is not None:
+        raise ValueError(f"scale belongs to an output of {E4M3}")
+    code = LAYER_CODE[dtype]
+    _call("whtmix_layer_norm", device, stream, (_lib or library()).whtmix_layer_norm, x.data_ptr(), rp, wp, bp, hp, out.data_ptr(),
+          sp, T, D, xs, rs, hs, ys, eps, code, 3 if eight else code)
+    if eight:
+        return (out, scale) if residual is None else (out, scale, h)
+    return out if residual is None else (out, h)
+
+
+def layer_norm_backward(h: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, dh: torch.Tensor | None = None,
+                        eps: float = 1e-5, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None,
+                        db: torch.Tensor | None = None, need_db: bool = True, stream=None):
+    """(dx, dw, db) of layer_norm from its sum h (x where it had no residual); dh is the gradient that reaches h
+    directly.  dx is the gradient of x and of the residual; dw and db are float32, db None where it is not needed."""
+    if h.is_cuda and dx is None and dw is None and db is None and stream is None:
+        done = (_quick or _quick_path()).layer_norm_backward(h, w, dy, dh, eps, need_db)
+        if done is not None:
+            return done
+    if stream is not None and h.is_cuda and (dx is None or dw is None or (db is None and need_db)):
+        with _on(stream, h.device):
+            return layer_norm_backward(h, w, dy, dh, eps, dx, dw, db, need_db)
+    dtype = h.dtype
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError(f"layer_norm_backward takes float32 or bfloat16, got {dtype}")
+    shape, index = h.shape, h.get_device()
+    T, D, hs = _rows(h, "h", index)
+    wp = _vector(w, (D,), "w", index)
+    device = h.device
+    dys = _stride(dy, shape, dtype, "dy", index)
+    dhs = 0 if dh is None else _stride(dh, shape, dtype, "dh", index)
+    if dx is None:
+        dx, dxs = torch.empty(shape, dtype=dtype, device=device), D
+    else:
+        dxs = _stride(dx, shape, dtype, "dx", index)
+    dw = torch.empty(D, dtype=torch.float32, device=device) if dw is None else dw
+    dbp = 0
+    if db is not None or need_db:
+        db = torch.empty(D, dtype=torch.float32, device=device) if db is None else db
+        dbp = _vector(db, (D,), "db", index)
+    _call("whtmix_layer_norm_backward", device, stream, (_lib or library()).whtmix_layer_norm_backward, h.data_ptr(), wp,
+          dy.data_ptr(), 0 if dh is None else dh.data_ptr(), dx.data_ptr(), _vector(dw, (D,), "dw", index), dbp, T, D, hs, dys,
+          dhs, dxs, eps, LAYER_CODE[dtype])
+    return dx, dw, db
+
+
+def _halves(w: torch.Tensor, dtype: torch.dtype, K: int):
+    """(N, K) of a gated weight [2 N, K]."""
+    rows, cols = w.shape if w.dim() == 2 else (0, 0)
+    if w.dtype != dtype or cols != K or rows < 2 or rows % 2:
+        raise ValueError(f"w must be {dtype} [2 N, {K}], got {w.dtype} {list(w.shape)}")
+    return rows // 2, cols
+
+
+def gated_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, activation: str = "silu",
+                 x_scale: torch.Tensor | None = None, w_scale: torch.Tensor | None = None,
+                 preact: torch.Tensor | bool | None = None, out_dtype: torch.dtype = torch.bfloat16,
+                 out: torch.Tensor | None = None, stream=None):
+    """y = act(x wg^T + bg) (x wu^T + bu) over the last axis, the first half of a gated feed-forward block: x [..., K] and
+    w [2 N, K] (N rows wg, then N rows wu) bfloat16, or both float8_e4m3fn with float32 scales x_scale [...] and w_scale
+    [2 N]; bias [2 N] float32; y [..., N] of out_dtype (bfloat16 or float32).  preact=True, or a bfloat16 tensor
+    [..., 2 N], also returns both pre-activations: (y, preact)."""
+    act = _activation(activation)
+    if x.is_cuda and out is None and stream is None and (preact is None or preact.__class__ is bool):
+        done = (_quick or _quick_path()).gated_linear(x, w, bias, act, x_scale, w_scale, preact, out_dtype)
+        if done is not None:
+            return done
+    if stream is not None and x.is_cuda and (out is None or preact is True):
+        with _on(stream, x.device):
+            return gated_linear(x, w, bias, activation, x_scale, w_scale, preact, out_dtype, out)
+    dtype, device, index = x.dtype, x.device, x.get_device()
+    if dtype != torch.bfloat16 and dtype != E4M3:
+        raise TypeError(f"gated_linear takes bfloat16 or {E4M3}, got {dtype}")
+    if out_dtype != torch.bfloat16 and out_dtype != torch.float32:
+        raise TypeError(f"gated_linear writes bfloat16 or float32, not {out_dtype}")
+    T, K, xs = _rows(x, "x", index)
+    N, _ = _halves(w, dtype, K)
+    ws = _rows(w, "w", index)[2]
+    lead = x.shape[:-1]
+    xsp = wsp = bp = pp = ps = 0
+    if dtype == E4M3:
+        if x_scale is None or w_scale is None:
+            raise ValueError(f"{E4M3} needs x_scale and w_scale")
+        xsp, wsp = _vector(x_scale, lead, "x_scale", index), _vector(w_scale, (2 * N,), "w_scale", index)
+    elif x_scale is not None or w_scale is not None:
+        raise ValueError(f"scales belong to {E4M3} operands")
+    if bias is not None:
+        bp = _vector(bias, (2 * N,), "bias", index)
+    save = preact is not None and preact is not False
+    if save:
+        if out_dtype != torch.bfloat16:
+            raise ValueError("preact is bfloat16 and goes with a bfloat16 output")
+        if preact is True:
+            preact, ps = torch.empty(lead + (2 * N,), dtype=torch.bfloat16, device=device), 2 * N
+        else:
+            ps = _stride(preact, lead + (2 * N,), torch.bfloat16, "preact", index)
+        pp = preact.data_ptr()
+    if out is None:
+        out, ys = torch.empty(lead + (N,), dtype=out_dtype, device=device), N
+    else:
+        ys = _stride(out, lead + (N,), out_dtype, "out", index)
+    _call("whtmix_gated_linear", device, stream, (_lib or library()).whtmix_gated_linear, x.data_ptr(), w.data_ptr(), xsp, wsp, bp, pp,
+          out.data_ptr(), T, N, K, xs, ws, ps, ys, act, LAYER_CODE[dtype], LAYER_CODE[out_dtype])
+    return (out, preact) if save else out
+
+
+def gated_linear_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, p: torch.Tensor, activation: str = "silu",
+                          need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
+                          dw_dtype: torch.dtype = torch.bfloat16, dx: torch.Tensor | None = None,
+                          dw: torch.Tensor | None = None, db: torch.Tensor | None = None, stream=None):
+    """(dx, dw, db) of gated_linear for the upstream gradient dy of y (bfloat16), from the stored pre-activations p; None in
+    the place of a gradient that is not needed.  dw [2 N, K] is bfloat16 or float32, db [2 N] float32."""
+    act = _activation(activation)
+    if x.is_cuda and dx is None and dw is None and db is None and stream is None:
+        done = (_quick or _quick_path()).gated_linear_backward(x, w, dy, p, act, need_dx, need_dw, need_db, dw_dtype)
+        if done is not None:
+            return done
+    if stream is not None and x.is_cuda and ((dx is None and need_dx) or (dw is None and need_dw) or (db is None and need_db)):
+        with _on(stream, x.device):
+            return gated_linear_backward(x, w, dy, p, activation, need_dx, need_dw, need_db, dw_dtype, dx, dw, db)
+    device, index = x.device, x.get_device()
+    if x.dtype != torch.bfloat16:
+        raise TypeError(f"gated_linear_backward takes bfloat16, got {x.dtype}")
+    if dw_dtype != torch.bfloat16 and dw_dtype != torch.float32:
+        raise TypeError(f"dw is bfloat16 or float32, not {dw_dtype}")
+    T, K, xs = _rows(x, "x", index)
+    N, _ = _halves(w, torch.bfloat16, K)
+    ws = _rows(w, "w", index)[2]
+    lead = x.shape[:-1]
+    dys = _stride(dy, lead + (N,), torch.bfloat16, "dy", index)
+    ps = _stride(p, lead + (2 * N,), torch.bfloat16, "p", index)
+    dxp = dxs = dwp = dbp = 0
+    if dx is not None:
+        dxs = _stride(dx, x.shape, torch.bfloat16, "dx", index)
+        dxp = dx.data_ptr()
+    elif need_dx:
+        dx, dxs = torch.empty(x.shape, dtype=torch.bfloat16, device=device), K
+        dxp = dx.data_ptr()
+    if dw is not None or need_dw:
+        dw = _out(dw, (2 * N, K), dw_dtype, device, "dw")
+        dwp = dw.data_ptr()
+    if db is not None or need_db:
+        db = torch.empty(2 * N, dtype=torch.float32, device=device) if db is None else db
+        dbp = _vector(db, (2 * N,), "db", index)
+    _call("whtmix_gated_linear_backward", device, stream, (_lib or library()).whtmix_gated_linear_backward, x.data_ptr(), w.data_ptr(),
+          dy.data_ptr(), p.data_ptr(), dxp, dwp, dbp, T, N, K, xs, ws, dys, ps, dxs, act, LAYER_CODE[dw_dtype])
+    return dx, dw, db
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether t's elements are all of one piece of memory, in whatever order of its axes."""
+    expect = 1
+    for st, n in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if st != expect:
+            return False
+        expect *= n
+    return True
+
+
+def _list(tensors, out, device: torch.device):
+    """whtmix_tensor_t for each tensor (and the one in its place in out)."""
+    entries = (_Tensor * len(tensors))()
+    for i, t in enumerate(tensors):
+        if t.dtype != torch.float32 and t.dtype != torch.bfloat16:
+            raise TypeError(f"the tensors must be float32 or bfloat16, tensors[{i}] is {t.dtype}")
+        if not t.is_cuda or t.device != device:
+            raise ValueError(f"tensors[{i}] must be a CUDA tensor on the first tensor's device, it is on {t.device}")
+        if t.numel() and not _dense(t):
+            raise ValueError(f"tensors[{i}] must be dense, got shape {list(t.shape)}, strides {list(t.stride())}")
+        e = entries[i]
+        e.in_, e.n, e.dtype = t.data_ptr(), t.numel(), LAYER_CODE[t.dtype]
+        if out is not None:
+            o = out[i]
+            if o.dtype != t.dtype or o.shape != t.shape or o.device != device or (t.numel() and o.stride() != t.stride()):
+                raise ValueError(f"out[{i}] must be like tensors[{i}]: {t.dtype} {list(t.shape)}, strides {list(t.stride())}, on {device}")
+            e.out = o.data_ptr()
+    return entries
+
+
+def _norm_device(tensors) -> torch.device:
+    for t in tensors:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"a list of tensors is needed, got {type(t).__name__} in it")
+    if not tensors:
+        raise ValueError("the list of tensors is empty: it has no device")
+    if not tensors[0].is_cuda:
+        raise ValueError(f"tensors[0] must be a CUDA tensor (WHTMix runs on CUDA tensors only), it is on {tensors[0].device}")
+    return tensors[0].device
+
+
+def global_norm(tensors, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """sqrt(sum of all squares) of a list of float32 and bfloat16 tensors on one device, a float32 tensor without axes."""
+    tensors = list(tensors)
+    device = _norm_device(tensors)
+    if out is None and stream is None:
+        done = (_quick or _quick_path()).global_norm(tensors)
+        if done is not None:
+            return done
+    if stream is not None and out is None:
+        with _on(stream, device):
+            return global_norm(tensors)
+    entries = _list(tensors, None, device)
+    out = _out(out, (), torch.float32, device, "out")
+    _call("whtmix_global_norm", device, stream, (_lib or library()).whtmix_global_norm, entries, len(tensors), out.data_ptr())
+    return out
+
+
+def clip_by_global_norm(tensors, max_norm: float, out=None, norm: torch.Tensor | None = None, stream=None):
+    """(out, norm): each tensor of the list times min(1, max_norm / (norm + 1e-6)), norm = global_norm(tensors).
+
+    out is a list of tensors like the given ones; with out=tensors they are scaled in place."""
+    tensors = list(tensors)
+    device = _norm_device(tensors)
+    if out is not None:
+        out = list(out)
+        if len(out) != len(tensors):
+            raise ValueError(f"out must have a tensor for each of the {len(tensors)}, got {len(out)}")
+    if not max_norm >= 0:
+        raise ValueError(f"max_norm must not be negative, got {max_norm}")
+    if norm is None and stream is None:
+        done = (_quick or _quick_path()).clip_by_global_norm(tensors, float(max_norm), out)
+        if done is not None:
+            return done
+    if stream is not None and (norm is None or out is None):
+        with _on(stream, device):
+            return clip_by_global_norm(tensors, max_norm, out, norm)
+    out = [torch.empty_like(t) for t in tensors] if out is None else out
+    entries = _list(tensors, out, device)
+    norm = _out(norm, (), torch.float32, device, "norm")
+    _call("whtmix_clip_by_global_norm", device, stream, (_lib or library()).whtmix_clip_by_global_norm, entries, len(tensors), max_norm,
+          norm.data_ptr())
+    return out, norm
+
+
 def workspace_bytes(B: int, N: int, C: int, dtype: torch.dtype, backward: bool = False) -> int:
     out = ctypes.c_size_t(0)
     _check(library().whtmix_workspace_bytes(B, N, C, DTYPE_CODE[dtype], int(backward), ctypes.byref(out)),
@@ -801,3 +1104,52 @@ class LinearFunction(torch.autograd.Function):
             dx, dw, db = linear_backward(x, w, dy, p, ctx.activation, need_dx=need[0], need_dw=need[1],
                                          need_db=ctx.with_bias and need[2])
         return dx, dw, db, dy if ctx.with_residual else None, None
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """autograd wrapper of layer_norm: (x, w, b, residual, eps) -> (y, h), h = x where there is no residual."""
+
+    @staticmethod
+    def forward(ctx, x, w, b=None, residual=None, eps=1e-5):
+        if residual is None:
+            y, h = layer_norm(x, w, b, eps=eps), x
+        else:
+            y, h = layer_norm(x, w, b, residual=residual, eps=eps)
+        ctx.save_for_backward(h, w)
+        ctx.eps, ctx.with_b, ctx.with_residual = eps, b is not None, residual is not None
+        ctx.set_materialize_grads(False)  # where h (or y) is not used, no zeros are filled in and read as its gradient
+        return y, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        h, w = ctx.saved_tensors
+        if dy is None:
+            dx, dw = dh, None if dh is None else torch.zeros_like(w)
+            db = torch.zeros_like(dw) if ctx.with_b and dw is not None else None
+        else:
+            dx, dw, db = layer_norm_backward(h, w, dy.contiguous(), dh=None if dh is None else dh.contiguous(), eps=ctx.eps,
+                                             need_db=ctx.with_b)
+        return dx, dw, db, dx if ctx.with_residual else None, None
+
+
+class GatedLinearFunction(torch.autograd.Function):
+    """autograd wrapper of gated_linear in bfloat16: (x, w, bias, activation) -> y; dw comes in bfloat16."""
+
+    @staticmethod
+    def forward(ctx, x, w, bias=None, activation="silu"):
+        y, p = gated_linear(x, w, bias, activation, preact=True)
+        ctx.save_for_backward(x, w, p)
+        ctx.activation, ctx.with_bias = activation, bias is not None
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, w, p = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if need[0] or need[1] or (ctx.with_bias and need[2]):
+            dx, dw, db = gated_linear_backward(x, w, dy.contiguous(), p, ctx.activation, need_dx=need[0], need_dw=need[1],
+                                               need_db=ctx.with_bias and need[2])
+        return dx, dw, db, None
