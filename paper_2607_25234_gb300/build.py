@@ -25,7 +25,7 @@ SOURCES = ["whtmix_capi.cu", "whtmix_fast_f32.cu", "whtmix_fast_bf16.cu", "whtmi
            "whtmix_layer.cu", "whtmix_norm.cu", "whtmix_linear.cu", "whtmix_gemm_fwd.cu", "whtmix_gemm_e4m3.cu",
            "whtmix_gemm_four.cu", "whtmix_gemm_e4m3_four.cu", "whtmix_gemm_dx.cu", "whtmix_gemm_dw.cu",
            "whtmix_few.cu", "whtmix_gemm_dp.cu", "whtmix_layer_norm.cu", "whtmix_gated.cu", "whtmix_gemm_gated.cu",
-           "whtmix_gemm_gated_e4m3.cu", "whtmix_clip.cu"]
+           "whtmix_gemm_gated_e4m3.cu", "whtmix_gemm_gated_dp.cu", "whtmix_clip.cu"]
 OBJDIR = os.path.join(LIBDIR, "obj")
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 

@@ -4,10 +4,12 @@
 //
 // Bound by memory: the gradients are read for the norm and again for the scaling.  A tensor is cut into chunks of CHUNK 16-byte
 // vectors, counted from the 16-byte boundary at or before its first element, so that every load is aligned whatever its address; a
-// CTA takes chunks at the grid's stride.  A table of the tensors goes along as a kernel parameter (a captured graph keeps it), a
-// launch for every MAX of them.  The scaling takes the chunks in descending order: the last ones read are still in L2.
-// A thread's squares of one chunk are added in float32, those sums in float64; values whose squares leave float32's range are
-// scaled by a power of two first, so that every finite gradient has its finite norm.  Every CTA of the scaling adds up the partial
+// CTA takes a run of chunks, the next one's loads on their way while it works on one.  A table of the tensors goes along as a kernel
+// parameter (a captured graph keeps it), a launch for every MAX of them.  The scaling takes a run in descending order: the last chunks
+// read are still in L2.
+// A thread's squares of one chunk are added in float32, those sums in float32 with a compensation (float64 additions are slow
+// here: two a clock and SM), the threads' sums in float64; values whose squares leave float32's range are scaled by a power of two
+// first, so that every finite gradient has its finite norm.  Every CTA of the scaling adds up the partial
 // sums itself, in the same order: no atomics, results repeat bit for bit.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -19,7 +21,8 @@
 namespace whtmix {
 namespace clip {
 
-constexpr int CLIP_THREADS = 256, VECTORS = 8, CHUNK = CLIP_THREADS * VECTORS;
+constexpr int CLIP_THREADS = 256, VECTORS = 4, CHUNK = CLIP_THREADS * VECTORS;
+constexpr int CLIP_CTAS = 4;  // an SM
 constexpr double CLIP_EPS = 1e-6;
 
 struct Entry {
@@ -33,34 +36,52 @@ template <int MAX>
 struct Table {
   Entry e[MAX];
   int count, chunks;
+  bool in_place;  // every tensor of it
 };
 
-// A chunk: vectors v0 .. of the tensor, vector v at base + 16 v.
+// A thread's vectors of a chunk.
 struct Piece {
-  const uint8_t *base, *lo, *hi;  // base: the 16-byte boundary at or before lo
+  const uint8_t *base, *lo, *hi;  // base: this thread's first vector; the tensor's bytes
   long long shift;                // out - in
-  int v0;                         // (a tensor of 2^40 elements has 2^38 vectors: v0 counts chunks)
   bool bf16;
 };
-template <int MAX>
-__device__ __forceinline__ Piece piece(const Table<MAX>& t, int chunk) {
-  int lo = 0, hi = t.count - 1;  // the last tensor whose first chunk is not beyond this one
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if ((t.e[mid].first & ~BF16_BIT) <= chunk) lo = mid; else hi = mid - 1;
+// The chunks of a run, one after another (UP) or from its last to its first.
+template <int MAX, bool UP>
+struct Run {
+  const Table<MAX>& t;
+  int chunk, end, i;  // end: one beyond the last to come
+  __device__ __forceinline__ Run(const Table<MAX>& table) : t(table) {
+    const int first = static_cast<int>(static_cast<long long>(t.chunks) * blockIdx.x / gridDim.x);
+    const int last = static_cast<int>(static_cast<long long>(t.chunks) * (blockIdx.x + 1) / gridDim.x);  // (never empty)
+    chunk = UP ? first : last - 1, end = UP ? last : first - 1;
+    int lo = 0, hi = t.count - 1;  // the last tensor whose first chunk is not beyond this one
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((t.e[mid].first & ~BF16_BIT) <= chunk) lo = mid; else hi = mid - 1;
+    }
+    i = lo;
   }
-  const Entry e = t.e[lo];
-  Piece p;
-  p.lo = e.in, p.hi = e.in + e.bytes;
-  p.base = e.in - (reinterpret_cast<uintptr_t>(e.in) & 15u);
-  p.shift = e.out - e.in;
-  p.v0 = chunk - (e.first & ~BF16_BIT);
-  p.bf16 = e.first < 0;
-  return p;
-}
-__device__ __forceinline__ const uint8_t* vector_at(const Piece& p, int u) {
-  return p.base + (static_cast<long long>(p.v0) * CHUNK + threadIdx.x + u * CLIP_THREADS) * 16;
-}
+  __device__ __forceinline__ bool more() const { return chunk != end; }
+  // this chunk, and on to the next one
+  __device__ __forceinline__ Piece take() {
+    const Entry e = t.e[i];
+    const int first = e.first & ~BF16_BIT;
+    Piece p;
+    p.lo = e.in, p.hi = e.in + e.bytes;
+    p.base = e.in - (reinterpret_cast<uintptr_t>(e.in) & 15u) + (static_cast<long long>(chunk - first) * CHUNK + threadIdx.x) * 16;
+    p.shift = e.out - e.in;
+    p.bf16 = e.first < 0;
+    if (UP) {
+      ++chunk;
+      if (i + 1 < t.count && (t.e[i + 1].first & ~BF16_BIT) <= chunk) ++i;  // (a tensor has a chunk at least)
+    } else {
+      --chunk;
+      if (chunk < first) --i;
+    }
+    return p;
+  }
+};
+__device__ __forceinline__ const uint8_t* vector_at(const Piece& p, int u) { return p.base + u * (CLIP_THREADS * 16); }
 // the vector at q, zeros outside the tensor
 __device__ __forceinline__ uint4 load(const Piece& p, const uint8_t* q) {
   uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -74,6 +95,10 @@ __device__ __forceinline__ uint4 load(const Piece& p, const uint8_t* q) {
     v = make_uint4(w[0], w[1], w[2], w[3]);
   }
   return v;
+}
+__device__ __forceinline__ void load_all(const Piece& p, uint4 (&u)[VECTORS]) {
+#pragma unroll
+  for (int k = 0; k < VECTORS; ++k) u[k] = load(p, vector_at(p, k));
 }
 
 // sum of the squares of s times the values of u, two accumulators
@@ -95,17 +120,28 @@ __device__ __forceinline__ float squares(const uint4 (&u)[VECTORS], bool bf16, f
   }
   return a + b;
 }
-// Beyond [2^-100, 2^120] the sum is taken again with the values scaled by 2^110 (all of them are below 2^-50 then) or 2^-72.
-__device__ __forceinline__ double sum_of_squares(const uint4 (&u)[VECTORS], bool bf16) {
-  const float s = squares(u, bf16, 1.f);
-  if (s >= 0x1p-100f && s <= 0x1p120f) return s;
-  uint32_t any = 0;
+// A thread's sum: float32 with the rounding errors beside it, and in float64 what lies beyond [2^-100, 2^90] (2^37 chunks in range
+// stay finite).  Beyond, the squares are taken again with the values scaled by 2^110 (all of them are below 2^-50 then) or 2^-72.
+struct Sum {
+  float s = 0.f, err = 0.f;
+  double far = 0.0;
+  __device__ __forceinline__ void add(const uint4 (&u)[VECTORS], bool bf16) {
+    const float v = squares(u, bf16, 1.f);
+    if (v >= 0x1p-100f && v <= 0x1p90f) {
+      const float y = v - err, t = s + y;
+      err = (t - s) - y;
+      s = t;
+      return;
+    }
+    uint32_t any = 0;
 #pragma unroll
-  for (int k = 0; k < VECTORS; ++k) any |= u[k].x | u[k].y | u[k].z | u[k].w;
-  if ((any & 0x7fff7fffu) == 0 && (bf16 || (any & 0x7fffffffu) == 0)) return 0.0;
-  const bool tiny = s < 1.f;
-  return static_cast<double>(squares(u, bf16, tiny ? 0x1p110f : 0x1p-72f)) * (tiny ? 0x1p-220 : 0x1p144);
-}
+    for (int k = 0; k < VECTORS; ++k) any |= u[k].x | u[k].y | u[k].z | u[k].w;
+    if ((any & 0x7fff7fffu) == 0 && (bf16 || (any & 0x7fffffffu) == 0)) return;
+    const bool tiny = v < 1.f;
+    far += static_cast<double>(squares(u, bf16, tiny ? 0x1p110f : 0x1p-72f)) * (tiny ? 0x1p-220 : 0x1p144);
+  }
+  __device__ __forceinline__ double get() const { return far + (static_cast<double>(s) - static_cast<double>(err)); }
+};
 
 // The sum of a over the CTA's threads, in each of them; the same order everywhere.
 __device__ __forceinline__ double add_up(double a) {
@@ -127,18 +163,25 @@ __device__ __forceinline__ double add_parts(const double* part, int parts) {
 
 // part[blockIdx.x] = the sum of squares of this CTA's chunks
 template <int MAX>
-__global__ void __launch_bounds__(CLIP_THREADS) k_squares(const __grid_constant__ Table<MAX> t, double* part) {
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_CTAS) k_squares(const __grid_constant__ Table<MAX> t, double* part) {
   pdl_wait();
-  double sum = 0.0;
-  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const Piece p = piece(t, c);
-    uint4 u[VECTORS];
+  Run<MAX, true> run(t);
+  Sum sum;
+  Piece p = run.take();
+  uint4 u[VECTORS];
+  load_all(p, u);
+  while (run.more()) {
+    const bool bf16 = p.bf16;
+    uint4 next[VECTORS];
+    p = run.take();
+    load_all(p, next);
+    sum.add(u, bf16);
 #pragma unroll
-    for (int k = 0; k < VECTORS; ++k) u[k] = load(p, vector_at(p, k));
-    sum += sum_of_squares(u, p.bf16);
+    for (int k = 0; k < VECTORS; ++k) u[k] = next[k];
   }
-  sum = add_up(sum);
-  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+  sum.add(u, p.bf16);
+  const double all = add_up(sum.get());
+  if (threadIdx.x == 0) part[blockIdx.x] = all;
   pdl_trigger();
 }
 
@@ -153,42 +196,65 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_total(const double* part, int 
   pdl_trigger();
 }
 
+// f(x) of each value of u, to the piece's place
+template <class F>
+__device__ __forceinline__ void store_mapped(const Piece& p, const uint4 (&u)[VECTORS], F&& f) {
+#pragma unroll
+  for (int k = 0; k < VECTORS; ++k) {
+    uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (p.bf16) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(f(__uint_as_float(w[j] << 16)), f(__uint_as_float(w[j] & 0xffff0000u)));
+        w[j] = *reinterpret_cast<uint32_t*>(&b);
+      } else {
+        w[j] = __float_as_uint(f(__uint_as_float(w[j])));
+      }
+    }
+    const uint8_t* q = vector_at(p, k);
+    uint8_t* o = const_cast<uint8_t*>(q) + p.shift;
+    if (q >= p.lo && q + 16 <= p.hi && (p.shift & 15) == 0) {
+      *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (q + 16 > p.lo && q < p.hi) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (q + 2 * j >= p.lo && q + 2 * j < p.hi) *reinterpret_cast<uint16_t*>(o + 2 * j) = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+    }
+  }
+}
+// A factor below 2^-120 (norms that float32 does not hold) would lose its digits as a float32: the products in float64, kept out of
+// the usual path (on both sides of a choice an element they took 1.25 ms of 0.6 GB).
+static __device__ __noinline__ float times_far(float x, double ratio) { return static_cast<float>(x * ratio); }
+__device__ __forceinline__ void store_scaled(const Piece& p, const uint4 (&u)[VECTORS], float f, double ratio) {
+  if (ratio < 0x1p-120)
+    store_mapped(p, u, [&](float x) { return times_far(x, ratio); });
+  else
+    store_mapped(p, u, [&](float x) { return x * f; });
+}
+
+// The first chunk is on its way while the parts are added up.
 template <int MAX>
-__global__ void __launch_bounds__(CLIP_THREADS) k_scale(const __grid_constant__ Table<MAX> t, const double* part, int parts, float max_norm,
-                                                        float* norm) {
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_CTAS) k_scale(const __grid_constant__ Table<MAX> t, const double* part, int parts,
+                                                                   float max_norm, float* norm) {
   pdl_wait();
+  Run<MAX, false> run(t);
+  Piece p = run.take();
+  uint4 u[VECTORS];
+  load_all(p, u);
   const double root = sqrt(add_parts(part, parts)), ratio = max_norm / (root + CLIP_EPS);
   const float f = ratio >= 1.0 ? 1.f : static_cast<float>(ratio);  // (NaN stays)
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(root);
-  for (int i = blockIdx.x; i < t.chunks; i += gridDim.x) {
-    const Piece p = piece(t, t.chunks - 1 - i);
-    if (f == 1.f && p.shift == 0) continue;
-    uint4 u[VECTORS];
+  if (f == 1.f && t.in_place) return;
+  while (run.more()) {
+    const Piece at = p;
+    uint4 next[VECTORS];
+    p = run.take();
+    load_all(p, next);
+    store_scaled(at, u, f, ratio);
 #pragma unroll
-    for (int k = 0; k < VECTORS; ++k) u[k] = load(p, vector_at(p, k));
-#pragma unroll
-    for (int k = 0; k < VECTORS; ++k) {
-      uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (p.bf16) {
-          __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
-          w[j] = *reinterpret_cast<uint32_t*>(&b);
-        } else {
-          w[j] = __float_as_uint(__uint_as_float(w[j]) * f);
-        }
-      }
-      const uint8_t* q = vector_at(p, k);
-      uint8_t* o = const_cast<uint8_t*>(q) + p.shift;
-      if (q >= p.lo && q + 16 <= p.hi && (p.shift & 15) == 0) {
-        *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (q + 2 * j >= p.lo && q + 2 * j < p.hi) *reinterpret_cast<uint16_t*>(o + 2 * j) = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
-      }
-    }
+    for (int k = 0; k < VECTORS; ++k) u[k] = next[k];
   }
+  store_scaled(p, u, f, ratio);
   pdl_trigger();
 }
 
@@ -203,7 +269,7 @@ static long long chunks_of(const Item& i) {
   return (bytes + 16ll * CHUNK - 1) / (16ll * CHUNK);
 }
 static int ctas(long long chunks, int sms) {
-  const long long most = 4ll * sms;
+  const long long most = static_cast<long long>(CLIP_CTAS) * sms;
   return static_cast<int>(chunks < most ? chunks : most);
 }
 
@@ -211,16 +277,17 @@ static int ctas(long long chunks, int sms) {
 template <int MAX, class F>
 static cudaError_t each(const Call& a, int sms, F&& f) {
   Table<MAX> t;
-  t.count = 0, t.chunks = 0;
+  t.count = 0, t.chunks = 0, t.in_place = true;
   for (long long i = 0; i < a.count; ++i) {
     const Item& m = a.items[i];
     t.e[t.count++] = {static_cast<const uint8_t*>(m.in), static_cast<uint8_t*>(m.out ? m.out : const_cast<void*>(m.in)), m.n * (m.bf16 ? 2 : 4),
                       t.chunks | (m.bf16 ? BF16_BIT : 0)};
     t.chunks += static_cast<int>(chunks_of(m));
+    t.in_place = t.in_place && m.out == m.in;
     if (t.count == MAX || i + 1 == a.count || t.chunks + chunks_of(a.items[i + 1]) >= (1ll << 31)) {
       const cudaError_t e = f(t, ctas(t.chunks, sms));
       if (e != cudaSuccess) return e;
-      t.count = 0, t.chunks = 0;
+      t.count = 0, t.chunks = 0, t.in_place = true;
     }
   }
   return cudaSuccess;

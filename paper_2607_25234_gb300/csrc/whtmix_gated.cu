@@ -18,26 +18,6 @@ namespace linear {
 
 constexpr int THREADS_256 = 256;
 
-// d0 = d0 u0 act'(z0), v0 = d0 act(z0), and the same for the other value (one logistic function for value and slope; limits as in
-// activate and times_slope).
-__device__ __forceinline__ void gate_gradients(float& d0, float& d1, float& v0, float& v1, float z0, float z1, float u0, float u1, int act) {
-  v0 = d0, v1 = d1;
-  d0 *= u0, d1 *= u1;
-  if (act == ACT_NONE) {
-    v0 *= z0, v1 *= z1;
-  } else if (act == ACT_RELU) {
-    v0 *= z0 < 0.f ? 0.f : z0, v1 *= z1 < 0.f ? 0.f : z1;
-    d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
-  } else {
-    const Pair zv = pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), z = pair(between(z0, GATE_LOW, GATE_HIGH), between(z1, GATE_LOW, GATE_HIGH));
-    const Logistic l = logistic2(gate_exponent(z, act));
-    Pair g = z * (l.e * l.s);
-    if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
-    unpair(pair(d0, d1) * (l.s * (g + pair(1.f, 1.f))), d0, d1);
-    unpair(pair(v0, v1) * (zv * l.s), v0, v1);
-  }
-}
-
 // dp[t, n], dp[t, N + n] = bf16 of both gradients; part[chunk][n], [N + n] = the chunk's rows' float32 sums of them, before the rounding.
 // A CTA takes 8 TX channels (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.  AL: dy, p and dp
 // have 16-byte aligned rows and halves.
@@ -156,6 +136,14 @@ static GatedForwardPlan plan_forward(const Forward& a) {
   return f;
 }
 
+// Four epilogue groups instead of two, at the price of a shorter ring, where the epilogue is longer than a tile's products.  Two and
+// four, us: [64800, 128] to 344, gelu 26.0 and 22.6, with p 40.5 and 33.9; [64800, 256] to 688 with p 74.7 and 66.2; [64800, 384] to
+// 1024 77.8 and 81.8, with p 117 and 108; [32768, 512] to 1408 64.3 and 72.3, with p 95.8 and 89.3; [32768, 768] to 2048 with p 155
+// and 162.
+static bool four_groups(const Gated& g, int sms) {
+  return g.kblocks <= (g.has_p ? 8 : 4) && static_cast<long long>(g.tiles_m) * g.tiles_n > sms;
+}
+
 size_t gated_forward_workspace(const Forward& a, int) { return plan_forward(a).total; }
 
 cudaError_t gated_forward(const Forward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
@@ -182,6 +170,7 @@ cudaError_t gated_forward(const Forward& a, void* ws, unsigned int* err, int sms
   if (pl.bn < 128) pl.bn = 128;
   const int out = tile_cols(pl.bn) / 2;
   g.tiles_m = ceil_div(a.T, tile_rows(pl.bn)), g.tiles_n = ceil_div(a.N, out);
+  g.band = 16;
   g.M = static_cast<int>(a.T), g.N = a.N, g.act = a.act;
   g.bias = a.bias, g.sm = a.x_scale, g.sn = a.w_scale;
   g.y = a.y, g.p = a.p, g.ys = a.ys, g.ps = a.ps;
@@ -195,17 +184,20 @@ cudaError_t gated_forward(const Forward& a, void* ws, unsigned int* err, int sms
       (!g.y_plain && !tma::encode_rows(&g.ty, a.y, os, a.T, a.N, a.ys, GEMM_BM)) ||
       (g.has_p && !g.p_plain && (!tma::encode_rows(&g.tg, a.p, 2, a.T, a.N, a.ps, GEMM_BM) || !tma::encode_rows(&g.tu, value, 2, a.T, a.N, a.ps, GEMM_BM))))
     return cudaErrorInvalidValue;
-  return a.e4m3 ? gemm_gated_e4m3(g, a.out_f32, pl.bn, sms, stream) : gemm_gated(g, a.out_f32, pl.bn, sms, stream);
+  const bool four = four_groups(g, sms);
+  return a.e4m3 ? gemm_gated_e4m3(g, a.out_f32, pl.bn, four, sms, stream) : gemm_gated(g, a.out_f32, pl.bn, four, sms, stream);
 }
 
 // Threads a row of k_gated_dp, eight channels each.
 static int dp_lanes(int N) { return N <= 64 ? 8 : N <= 128 ? 16 : 32; }
 
-// dp and db's partial sums, then the linear layer's products of them with W and x.
+// dp and db's partial sums (fused: and dx), then the linear layer's products of them with W and x.
 struct GatedBackwardPlan {
+  bool fused;         // whtmix_gemm_gated_dp.cu
   Backward products;  // (its dy and workspace are filled in when the call runs)
   int np, chunks;     // pitch of dp; db's chunks of rows
-  size_t dp_off, db_off, products_off, total;
+  bool pad_w;         // fused: W to a 16-byte pitch
+  size_t dp_off, db_off, w_off, products_off, total;
 };
 static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
   GatedBackwardPlan b{};
@@ -215,47 +207,90 @@ static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
     b.total += align256(bytes);
     return off;
   };
+  // one pass over dy and p instead of a kernel for dp and a product that reads it again; tiles of 128 tokens on half the SMs at least,
+  // dy's rows and both halves' on 16-byte boundaries
+  b.fused = a.dx && a.K <= 256 && a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && tma::mappable(a.p, a.T, a.ps, 2) &&
+            2ll * ceil_div(a.T, GEMM_BM) >= sms;
   b.products = a;
   b.products.N = 2 * a.N, b.products.act = ACT_NONE, b.products.p = nullptr, b.products.db = nullptr;
   b.products.dy = nullptr, b.products.dys = b.np;  // (on a 16-byte boundary)
-  if (a.dx || a.dw) {
+  if (b.fused) b.products.dx = nullptr;
+  if (b.products.dx || a.dw) {
     b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);
     b.products_off = take(backward_workspace(b.products, sms));
   }
-  const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (4 * sms + strips - 1) / strips;  // one wave
-  b.chunks = rows < most ? rows : most;
-  if (b.chunks > 65535) b.chunks = 65535;
-  if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
+  if (b.fused) {
+    b.chunks = ceil_div(a.T, GEMM_BM);
+    b.pad_w = !tma::mappable(a.w, 2ll * a.N, a.ws, 2);
+    if (b.pad_w) b.w_off = take(static_cast<size_t>(2ll * a.N) * pitch_of(a.K, 2) * 2);
+  } else {
+    const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (4 * sms + strips - 1) / strips;  // one wave
+    b.chunks = rows < most ? rows : most;
+    if (b.chunks > 65535) b.chunks = 65535;
+    if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
+  }
   if (a.db && b.chunks > 1) b.db_off = take(static_cast<size_t>(b.chunks) * 2 * a.N * 4);
   return b;
 }
 
 size_t gated_backward_workspace(const Backward& a, int sms) { return plan_backward(a, sms).total; }
 
+// dp, dx and db's partial sums
+static cudaError_t fused_backward(const Backward& a, const GatedBackwardPlan& b, char* base, float* part, unsigned int* err, int sms,
+                                  cudaStream_t stream) {
+  const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(a.w);
+  long long wst = a.ws;
+  if (b.pad_w) {
+    w = reinterpret_cast<const __nv_bfloat16*>(base + b.w_off), wst = pitch_of(a.K, 2);
+    const cudaError_t e = to_pitch(copy_of(base + b.w_off, a.w, 2ll * a.N, a.K, a.ws, static_cast<int>(wst), 2), Copy{}, sms, stream);
+    if (e != cudaSuccess) return e;
+  }
+  const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(a.p);
+  __nv_bfloat16* dp = a.dw ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
+  GatedDp g{};
+  g.M = static_cast<int>(a.T), g.N = a.N, g.K = a.K, g.tiles_m = ceil_div(a.T, GEMM_BM), g.kblocks = ceil_div(a.N, 64), g.act = a.act;
+  g.part = part;
+  g.store_dp = dp != nullptr;
+  g.dx = a.dx, g.dxs = a.dxs, g.dx_plain = !tma::storable(a.dx, a.T, a.K, a.dxs, 2);
+  g.err = err;
+  if (!tma::encode_rows(&g.tdy, a.dy, 2, a.T, a.N, a.dys, GEMM_BM) || !tma::encode_rows(&g.tg, p, 2, a.T, a.N, a.ps, GEMM_BM) ||
+      !tma::encode_rows(&g.tu, p + a.N, 2, a.T, a.N, a.ps, GEMM_BM) || !tma::encode_rows(&g.twg, w, 2, a.N, a.K, wst, 64) ||
+      !tma::encode_rows(&g.twu, w + static_cast<size_t>(a.N) * wst, 2, a.N, a.K, wst, 64) ||
+      (dp && (!tma::encode_rows(&g.tdg, dp, 2, a.T, a.N, b.np, GEMM_BM) || !tma::encode_rows(&g.tdu, dp + a.N, 2, a.T, a.N, b.np, GEMM_BM))) ||
+      (!g.dx_plain && !tma::encode_rows(&g.tdx, a.dx, 2, a.T, a.K, a.dxs, GEMM_BM)))
+    return cudaErrorInvalidValue;
+  return gemm_gated_dp(g, sms, stream);
+}
+
 cudaError_t gated_backward(const Backward& a, void* ws, unsigned int* err, int sms, cudaStream_t stream) {
   const GatedBackwardPlan b = plan_backward(a, sms);
   char* base = static_cast<char*>(ws);
   Backward c = a;
-  __nv_bfloat16* dp = a.dx || a.dw ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
+  __nv_bfloat16* dp = b.products.dx || a.dw ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
   float* part = !a.db ? nullptr : b.chunks > 1 ? reinterpret_cast<float*>(base + b.db_off) : a.db;
-  long long np = b.np;
   int chunks = b.chunks;
-  const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && tma::mappable(a.p, a.T, a.ps, 2);
-  cudaLaunchConfig_t cfg = {};
-  const int tx = dp_lanes(a.N);
-  cfg.gridDim = dim3(ceil_div(a.N, 8 * tx), chunks);
-  cfg.blockDim = dim3(THREADS_256);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg,
-                                     tx == 8    ? (al ? k_gated_dp<true, 8> : k_gated_dp<false, 8>)
-                                     : tx == 16 ? (al ? k_gated_dp<true, 16> : k_gated_dp<false, 16>)
-                                                : (al ? k_gated_dp<true, 32> : k_gated_dp<false, 32>),
-                                     c, dp, np, part, chunks);
+  cudaError_t e;
+  if (b.fused) {
+    e = fused_backward(a, b, base, part, err, sms, stream);
+  } else {
+    long long np = b.np;
+    const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && tma::mappable(a.p, a.T, a.ps, 2);
+    cudaLaunchConfig_t cfg = {};
+    const int tx = dp_lanes(a.N);
+    cfg.gridDim = dim3(ceil_div(a.N, 8 * tx), chunks);
+    cfg.blockDim = dim3(THREADS_256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg,
+                           tx == 8    ? (al ? k_gated_dp<true, 8> : k_gated_dp<false, 8>)
+                           : tx == 16 ? (al ? k_gated_dp<true, 16> : k_gated_dp<false, 16>)
+                                      : (al ? k_gated_dp<true, 32> : k_gated_dp<false, 32>),
+                           c, dp, np, part, chunks);
+  }
   if (e != cudaSuccess) return e;
   if (a.db && chunks > 1 && (e = norm::add_rows(part, a.db, 2 * a.N, chunks, stream)) != cudaSuccess) return e;
   if (!dp) return cudaSuccess;

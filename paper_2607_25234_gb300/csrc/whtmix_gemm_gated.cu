@@ -4,8 +4,8 @@
 namespace whtmix {
 namespace linear {
 
-cudaError_t gemm_gated(const Gated& g, bool out_f32, int bn, int sms, cudaStream_t stream) {
-  return out_f32 ? gated_by_width<false, float>(g, bn, sms, stream) : gated_by_width<false, __nv_bfloat16>(g, bn, sms, stream);
+cudaError_t gemm_gated(const Gated& g, bool out_f32, int bn, bool four, int sms, cudaStream_t stream) {
+  return out_f32 ? gated_by_width<false, float>(g, bn, four, sms, stream) : gated_by_width<false, __nv_bfloat16>(g, bn, four, sms, stream);
 }
 
 }  // namespace linear

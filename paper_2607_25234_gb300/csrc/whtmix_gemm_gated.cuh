@@ -22,22 +22,43 @@ struct Gated {
   void* p;
   long long ys, ps;
   const float *bias, *sm, *sn;  // sm, sn: scales of the rows of A and B, or null
-  int M, N, kblocks, tiles_m, tiles_n, act;
+  int M, N, kblocks, tiles_m, tiles_n, band, act;
   bool has_p, y_plain, p_plain;
   unsigned int* err;
 };
 
+// d0 = d0 u0 act'(z0), v0 = d0 act(z0), and the same for the other value (one logistic function for value and slope; limits as in
+// activate and times_slope).
+__device__ __forceinline__ void gate_gradients(float& d0, float& d1, float& v0, float& v1, float z0, float z1, float u0, float u1, int act) {
+  v0 = d0, v1 = d1;
+  d0 *= u0, d1 *= u1;
+  if (act == ACT_NONE) {
+    v0 *= z0, v1 *= z1;
+  } else if (act == ACT_RELU) {
+    v0 *= z0 < 0.f ? 0.f : z0, v1 *= z1 < 0.f ? 0.f : z1;
+    d0 = z0 > 0.f ? d0 : d0 * 0.f, d1 = z1 > 0.f ? d1 : d1 * 0.f;
+  } else {
+    const Pair zv = pair(above(z0, GATE_LOW), above(z1, GATE_LOW)), z = pair(between(z0, GATE_LOW, GATE_HIGH), between(z1, GATE_LOW, GATE_HIGH));
+    const Logistic l = logistic2(gate_exponent(z, act));
+    Pair g = z * (l.e * l.s);
+    if (act == ACT_GELU) g = g * fma(z * z, pair(3.f * GELU_2A * GELU_B, 3.f * GELU_2A * GELU_B), pair(GELU_2A, GELU_2A));
+    unpair(pair(d0, d1) * (l.s * (g + pair(1.f, 1.f))), d0, d1);
+    unpair(pair(v0, v1) * (zv * l.s), v0, v1);
+  }
+}
+
 // (the ring, two panels and what is declared here are an SM's 227 KB to the last: one set of biases and scales a group)
-template <bool E4M3, int BN, bool PAIR, typename O>
-__global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_constant__ Gated a) {
+template <bool E4M3, int BN, bool PAIR, int GROUPS, typename O>
+__global__ void __launch_bounds__(GEMM_THREADS<GROUPS>, 1) k_gated(const __grid_constant__ Gated a) {
   static_assert(!PAIR || BN == 256, "a pair's tile is 256 x 256");
-  constexpr int GROUPS = 2, OUT = BN / 2;
+  static_assert(GROUPS == 2 || (GROUPS == 4 && !PAIR), "two or four epilogue groups");
+  constexpr int OUT = BN / 2, TEAM = GROUPS / 2;  // groups on a tile
   using R = Ring<BN, PAIR, GROUPS>;
   constexpr int CTAS = PAIR ? 2 : 1, TILE_M = CTAS * GEMM_BM;
   constexpr int S = R::STAGES, BK = E4M3 ? 128 : 64, PW = Panel<O>::W, PANELS = OUT / PW;
   constexpr uint32_t IDESC = (1u << 4) | (E4M3 ? 0u : (1u << 7) | (1u << 10)) | (static_cast<uint32_t>(BN >> 3) << 17) |
                              (static_cast<uint32_t>(TILE_M >> 4) << 24);
-  constexpr int CH = 32, Q = CH * static_cast<int>(sizeof(O)) / 16;  // columns of each half in registers, their pieces
+  constexpr int CH = GROUPS == 2 ? 32 : 16, Q = CH * static_cast<int>(sizeof(O)) / 16;  // columns of each half in registers, their pieces
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ GemmBars<BN, PAIR, GROUPS> bars;
   __shared__ uint32_t tmem_slot;
@@ -57,7 +78,7 @@ __global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_const
   }
   if (tid == 32) {
     for (int s = 0; s < S; ++s) tc::mbar_init(&bars.full[s], 1), tc::mbar_init(&bars.empty[s], 1);
-    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], CTAS * (alternate ? 4 : 8));
+    for (int s = 0; s < 2; ++s) tc::mbar_init(&bars.dfull[s], 1), tc::mbar_init(&bars.dempty[s], CTAS * (alternate ? 4 * TEAM : 4 * GROUPS));
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma::prefetch(&a.ta);
     tma::prefetch(&a.tb);
@@ -68,10 +89,12 @@ __global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_const
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   pdl_wait();
   const uint32_t tmem = tmem_slot;
-  // item -> tile, n fastest
+  // item -> tile: bands of `band` tiles down, m fastest in a band, so that the tiles at work together are a near square of the output
+  // ([8192, 4096] to 8192, whose W does not fit L2: 660 us a row of tiles at a time, 570 in bands of 16)
   auto place = [&](int item, int& m0, int& n0) {
-    m0 = item / a.tiles_n * TILE_M + rank * GEMM_BM;  // this CTA's rows
-    n0 = item % a.tiles_n * OUT;
+    const int per = a.band * a.tiles_n, b = item / per, i = item - b * per, rows = min(a.band, a.tiles_m - b * a.band), n = i / rows;
+    m0 = (b * a.band + i - n * rows) * TILE_M + rank * GEMM_BM;  // this CTA's rows
+    n0 = n * OUT;
   };
   unsigned bad = 0;
   if (warp == 0) {
@@ -150,7 +173,7 @@ __global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_const
     };
     // the group's tiles (a CTA with one tile: its every other panel), and of the next one's columns gt, gt + 128 the bias and scale, of
     // its row the scale: on their way while a tile is stored
-    const int step = alternate ? 1 : GROUPS, p0 = alternate ? 0 : g, stride = alternate ? 2 * units : units;
+    const int step = alternate ? TEAM : GROUPS, p0 = alternate ? g % TEAM : g, stride = alternate ? 2 * units : units;
     auto accumulator_read = [&](int d) {
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -175,8 +198,8 @@ __global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_const
       }
       if (a.sm) next_sm = m0 + row < a.M ? __ldg(a.sm + m0 + row) : 1.f;
     };
-    const int first = unit + (alternate ? g * units : 0);
-    uint32_t i = alternate ? g : 0;
+    const int first = unit + (alternate ? g / TEAM * units : 0);
+    uint32_t i = alternate ? g / TEAM : 0;
     fetch(first);
     for (int item = first; item < items; item += stride, i += alternate ? 2 : 1) {
       int m0, n0;
@@ -207,7 +230,13 @@ __global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_const
           waited = true;
         }
         // columns c0 .. of the panel in one half, scaled, with their bias
-        auto load = [&](int half, int c0, float (&v)[CH]) { tmem_ld32(tmem + lanes + d * BN + half * OUT + p * PW + c0, v); };
+        auto load = [&](int half, int c0, float (&v)[CH]) {
+          const uint32_t from = tmem + lanes + d * BN + half * OUT + p * PW + c0;
+          if constexpr (CH == 32)
+            tmem_ld32(from, v);
+          else
+            tc::tmem_ld16(from, v);
+        };
         auto finish = [&](int half, int c0, float (&v)[CH]) {
           if (a.sm) {
             const float* ss = s_scale[g][half] + c0;
@@ -310,18 +339,18 @@ __global__ void __launch_bounds__(GEMM_THREADS<2>, 1) k_gated(const __grid_const
 }
 
 // One instance's launch: a persistent grid of at most one CTA per SM.
-template <bool E4M3, int BN, bool PAIR, typename O>
+template <bool E4M3, int BN, bool PAIR, typename O, int GROUPS = 2>
 cudaError_t launch_gated(const Gated& g, int sms, cudaStream_t stream) {
-  auto k = k_gated<E4M3, BN, PAIR, O>;
+  auto k = k_gated<E4M3, BN, PAIR, GROUPS, O>;
   static std::atomic<uint64_t> raised{0};
-  const cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), GEMM_SMEM<2>, raised);
+  const cudaError_t e = raise_smem(reinterpret_cast<const void*>(k), GEMM_SMEM<GROUPS>, raised);
   if (e != cudaSuccess) return e;
   constexpr int CTAS = PAIR ? 2 : 1;
   const long long items = static_cast<long long>(g.tiles_m) * g.tiles_n, most = sms / CTAS;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(CTAS * (items < most ? items : most)));
-  cfg.blockDim = dim3(GEMM_THREADS<2>);
-  cfg.dynamicSmemBytes = GEMM_SMEM<2>;
+  cfg.blockDim = dim3(GEMM_THREADS<GROUPS>);
+  cfg.dynamicSmemBytes = GEMM_SMEM<GROUPS>;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -334,19 +363,32 @@ cudaError_t launch_gated(const Gated& g, int sms, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, k, g);
 }
 
-// By accumulator width: 128, 256, or TILE_PAIR.
+// By accumulator width: 128, 256, or TILE_PAIR; `four` epilogue groups only with 256.
 template <bool E4M3, typename O>
-cudaError_t gated_by_width(const Gated& g, int bn, int sms, cudaStream_t stream) {
+cudaError_t gated_by_width(const Gated& g, int bn, bool four, int sms, cudaStream_t stream) {
   switch (bn) {
     case 128: return launch_gated<E4M3, 128, false, O>(g, sms, stream);
-    case 256: return launch_gated<E4M3, 256, false, O>(g, sms, stream);
+    case 256: return four ? launch_gated<E4M3, 256, false, O, 4>(g, sms, stream) : launch_gated<E4M3, 256, false, O>(g, sms, stream);
     default: return launch_gated<E4M3, 256, true, O>(g, sms, stream);
   }
 }
 
+// whtmix_gemm_gated_dp.cu: dp = [dg, du], its column sums and dx = dp W in one pass, for K <= 256 (one tile of columns).
+// part [tiles_m, 2 N]: the 128-token tiles' sums of unrounded dp, or null; tdg, tdu, dp's halves, are written where store_dp.
+struct GatedDp {
+  CUtensorMap tdy, tg, tu, twg, twu, tdg, tdu, tdx;
+  float* part;
+  void* dx;
+  long long dxs;
+  int M, N, K, tiles_m, kblocks, act;
+  bool store_dp, dx_plain;
+  unsigned int* err;
+};
+cudaError_t gemm_gated_dp(const GatedDp& g, int sms, cudaStream_t stream);
+
 // whtmix_gemm_gated.cu, whtmix_gemm_gated_e4m3.cu
-cudaError_t gemm_gated(const Gated& g, bool out_f32, int bn, int sms, cudaStream_t stream);
-cudaError_t gemm_gated_e4m3(const Gated& g, bool out_f32, int bn, int sms, cudaStream_t stream);
+cudaError_t gemm_gated(const Gated& g, bool out_f32, int bn, bool four, int sms, cudaStream_t stream);
+cudaError_t gemm_gated_e4m3(const Gated& g, bool out_f32, int bn, bool four, int sms, cudaStream_t stream);
 
 }  // namespace linear
 }  // namespace whtmix

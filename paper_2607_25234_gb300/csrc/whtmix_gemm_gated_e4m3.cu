@@ -4,8 +4,8 @@
 namespace whtmix {
 namespace linear {
 
-cudaError_t gemm_gated_e4m3(const Gated& g, bool out_f32, int bn, int sms, cudaStream_t stream) {
-  return out_f32 ? gated_by_width<true, float>(g, bn, sms, stream) : gated_by_width<true, __nv_bfloat16>(g, bn, sms, stream);
+cudaError_t gemm_gated_e4m3(const Gated& g, bool out_f32, int bn, bool four, int sms, cudaStream_t stream) {
+  return out_f32 ? gated_by_width<true, float>(g, bn, four, sms, stream) : gated_by_width<true, __nv_bfloat16>(g, bn, four, sms, stream);
 }
 
 }  // namespace linear

@@ -261,7 +261,10 @@ int whtmix_layer_norm(const void* x, const void* residual, const float* w, const
     rc = host::device(&dev, &sms);
     if (rc != WHTMIX_OK) return rc;
     norm::LayerForward a{x, residual, w, b, h, y, y_scale, T, x_stride, residual_stride, h_stride, y_stride, static_cast<int>(D), eps};
-    return done(norm::layer_forward(a, dtype == WHTMIX_BF16, q8, sms, static_cast<cudaStream_t>(stream_v)));
+    unsigned int* err = nullptr;
+    rc = host::error_word(dev, &err);
+    if (rc != WHTMIX_OK) return rc;
+    return done(norm::layer_forward(a, dtype == WHTMIX_BF16, q8, err, sms, static_cast<cudaStream_t>(stream_v)));
   });
 }
 
@@ -300,7 +303,10 @@ int whtmix_layer_norm_backward(const void* h, const float* w, const void* dy, co
     rc = scratch.take(dev, stream, need);
     if (rc != WHTMIX_OK) return rc;
     a.ws = scratch.get();
-    rc = done(norm::layer_backward(a, bf16, sms, stream));
+    unsigned int* err = nullptr;
+    rc = host::error_word(dev, &err);
+    if (rc != WHTMIX_OK) return rc;
+    rc = done(norm::layer_backward(a, bf16, err, sms, stream));
     return rc != WHTMIX_OK ? rc : scratch.give_back();
   });
 }

@@ -20,9 +20,20 @@
 #include "whtmix_kernels.cuh"
 #include "whtmix_layer_norm.cuh"
 #include "whtmix_rows.cuh"
+#include "whtmix_tc.cuh"
+#include "whtmix_tma.cuh"
 
 namespace whtmix {
 namespace norm {
+
+// `bytes` (a multiple of 16) between shared and global memory, both on 16-byte boundaries.
+__device__ __forceinline__ void bulk_load(void* s, const void* g, int bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(tc::smem_u32(s)), "l"(g), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* g, const void* s, int bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(g), "r"(tc::smem_u32(s)), "r"(bytes) : "memory");
+}
 
 // The sums of a[0 .. N - 1] (MAXB: the largest by its bits) over a row's TPR threads, the same value in each.  STEP numbers a row's
 // reductions: each has its own shared memory, so that one barrier a reduction is enough (whoever writes a step's again has passed
@@ -427,16 +438,327 @@ __global__ void __launch_bounds__(32 * DWDB_RUNS) k_dwdb(const float* part, floa
   pdl_trigger();
 }
 
+// ---- contiguous rows of an odd length ----
+// Rows that are no whole 16-byte pieces, one behind another: tiles of 8, 16 or 32 rows (whole pieces together) come and go as they
+// lie, in bulk copies (three stages, each with a place for every matrix read; what is computed takes a read one's place), and between
+// the two LANES lanes take a row's elements, lane l those at l, l + LANES, ..: neither the rows' offsets nor their cut vectors cost anything, and
+// a lane's columns are the same in every row.  NE: elements a lane.
+constexpr int TILE_THREADS = 256, TILE_STAGES = 3;
+
+// Rows of a tile, about 10 KB of a matrix.
+template <typename T>
+__host__ __device__ constexpr int tile_rows(int D) {
+  const int bytes = D * static_cast<int>(sizeof(T));
+  return bytes <= 320 ? 32 : bytes <= 640 ? 16 : 8;
+}
+template <typename T>
+__host__ __device__ constexpr int tile_bytes(int D) { return tile_rows<T>(D) * D * static_cast<int>(sizeof(T)); }
+
+// A contiguous matrix [T, D] that is copied tile by tile.  The last tile's bytes beyond whole 16-byte pieces go element by element.
+template <typename T>
+struct Tiles {
+  const void* p;
+  long long rows;
+  int D;
+  __device__ __forceinline__ int bytes(long long tile) const {
+    const long long left = rows - tile * tile_rows<T>(D);
+    return left < tile_rows<T>(D) ? static_cast<int>(left) * D * static_cast<int>(sizeof(T)) : tile_bytes<T>(D);
+  }
+  __device__ __forceinline__ uint8_t* at(long long tile) const {
+    return const_cast<uint8_t*>(static_cast<const uint8_t*>(p)) + tile * tile_bytes<T>(D);
+  }
+  // by one thread; the bytes that will arrive at the barrier
+  __device__ __forceinline__ uint32_t load(long long tile, unsigned char* s, uint64_t* bar) const {
+    const int n = bytes(tile) & ~15;
+    if (n) bulk_load(s, at(tile), n, bar);
+    return static_cast<uint32_t>(n);
+  }
+  // what a bulk copy leaves out, by the first threads; before (STORE: behind) a barrier
+  template <bool STORE>
+  __device__ __forceinline__ void ends(long long tile, unsigned char* s) const {
+    const int n = bytes(tile), e = (n & ~15) / static_cast<int>(sizeof(T)) + static_cast<int>(threadIdx.x);
+    if (threadIdx.x < 16 / sizeof(T) && e * static_cast<int>(sizeof(T)) < n) {
+      T *g = reinterpret_cast<T*>(at(tile)) + e, *m = reinterpret_cast<T*>(s) + e;
+      if (STORE) *g = *m; else *m = *g;
+    }
+  }
+  __device__ __forceinline__ void store(long long tile, const unsigned char* s) const {  // by one thread
+    const int n = bytes(tile) & ~15;
+    if (n) bulk_store(at(tile), s, n);
+  }
+};
+
+// The sums of a[0 .. N - 1] over a row's LANES lanes, the same value in each.
+template <int LANES, int N>
+__device__ __forceinline__ void lanes_join(float (&a)[N]) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] += __shfl_xor_sync(0xffffffffu, a[i], o);
+}
+
+// Stages of a kernel whose tiles have M matrices read: who loads, waits and stores.
+template <typename T, int M>
+struct Stages {
+  unsigned char* smem;
+  uint64_t* full;  // TILE_STAGES barriers
+  Tiles<T> in[M];
+  int live;  // matrices of a call
+  int D;
+  __device__ __forceinline__ unsigned char* place(int stage, int m) const { return smem + (stage * live + m) * tile_bytes<T>(D); }
+  __device__ __forceinline__ void load(long long tile, int stage) const {  // thread 0
+    uint32_t n = 0;
+    for (int m = 0; m < live; ++m) n += static_cast<uint32_t>(in[m].bytes(tile) & ~15);
+    tma::expect_tx(&full[stage], n);
+    for (int m = 0; m < live; ++m) in[m].load(tile, place(stage, m), &full[stage]);
+  }
+  __device__ __forceinline__ void ends(long long tile, int stage) const {
+    for (int m = 0; m < live; ++m) in[m].template ends<false>(tile, place(stage, m));
+  }
+};
+
+template <typename T, int LANES, int NE>
+__global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, unsigned int* err) {
+  constexpr int ROWS = TILE_THREADS / LANES;  // at a time
+  extern __shared__ __align__(128) unsigned char s_tiles[];
+  __shared__ uint64_t full[TILE_STAGES];
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, D = a.D, R = tile_rows<T>(D);
+  const float inv_d = 1.f / static_cast<float>(D);
+  const long long tiles = (a.T + R - 1) / R;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < TILE_STAGES; ++s) tc::mbar_init(&full[s], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  pdl_wait();
+  const Stages<T, 2> st{s_tiles, full, {{a.x, a.T, D}, {a.r, a.T, D}}, a.r ? 2 : 1, D};
+  const Tiles<T> y{a.y, a.T, D}, h_out{a.h, a.T, D};
+  float w[NE], b[NE];
+#pragma unroll
+  for (int k = 0; k < NE; ++k) {
+    const int e = lane + LANES * k;
+    w[k] = e < D ? __ldg(a.w + e) : 0.f;
+    b[k] = a.b && e < D ? __ldg(a.b + e) : 0.f;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < TILE_STAGES - 1; ++i)
+      if (blockIdx.x + static_cast<long long>(i) * gridDim.x < tiles) st.load(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
+  }
+  unsigned bad = 0;
+  uint32_t it = 0;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++it) {
+    const int s = it % TILE_STAGES;
+    st.ends(tile, s);
+    if (!bad && !tma::wait(&full[s], (it / TILE_STAGES) & 1)) bad |= 1;
+    __syncthreads();  // the ends too
+    T *xs = reinterpret_cast<T*>(st.place(s, 0)), *rs = reinterpret_cast<T*>(st.place(s, st.live - 1));
+#pragma unroll 1
+    for (int r0 = 0; r0 < R; r0 += ROWS) {
+      const int at = (r0 + group) * D + lane;
+      float v[NE], sum[1] = {0.f};
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        const bool in = lane + LANES * k < D;
+        v[k] = in ? Io<T>::get(xs, at + LANES * k) : 0.f;
+        if (a.r && in) {
+          v[k] += Io<T>::get(rs, at + LANES * k);
+          Io<T>::put(rs, at + LANES * k, v[k]);
+        }
+        sum[0] += v[k];
+      }
+      lanes_join<LANES>(sum);
+      const float mean = sum[0] * inv_d;
+      float sq[1] = {0.f};
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        v[k] = lane + LANES * k < D ? v[k] - mean : 0.f;
+        sq[0] += v[k] * v[k];
+      }
+      lanes_join<LANES>(sq);
+      const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
+#pragma unroll
+      for (int k = 0; k < NE; ++k)
+        if (lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, v[k] * rstd * w[k] + b[k]);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      y.store(tile, reinterpret_cast<unsigned char*>(xs));
+      if (a.r && a.h) h_out.store(tile, reinterpret_cast<unsigned char*>(rs));
+      tma::commit();
+      const long long next = tile + static_cast<long long>(TILE_STAGES - 1) * gridDim.x;
+      if (next < tiles) {
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the last tile has left the stage
+        st.load(next, (it + TILE_STAGES - 1) % TILE_STAGES);
+      }
+    }
+    y.template ends<true>(tile, reinterpret_cast<unsigned char*>(xs));
+    if (a.r && a.h) h_out.template ends<true>(tile, reinterpret_cast<unsigned char*>(rs));
+  }
+  if (threadIdx.x == 0) {
+    tma::wait_done();
+    // a wait that gave up: the copies in flight have landed before the CTA can end
+    for (uint32_t j = it > TILE_STAGES ? it - TILE_STAGES : 0; bad && j < it; ++j) (void)tma::wait(&full[j % TILE_STAGES], (j / TILE_STAGES) & 1);
+    if (bad) atomicOr(err, bad);
+  }
+  pdl_trigger();
+}
+
+template <typename T, int LANES, int NE>
+__global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackward a, unsigned int* err) {
+  constexpr int ROWS = TILE_THREADS / LANES;  // at a time
+  extern __shared__ __align__(128) unsigned char s_tiles[];
+  __shared__ uint64_t full[TILE_STAGES];
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, D = a.D, R = tile_rows<T>(D);
+  const float inv_d = 1.f / static_cast<float>(D);
+  const long long tiles = (a.T + R - 1) / R;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < TILE_STAGES; ++s) tc::mbar_init(&full[s], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  pdl_wait();
+  const Stages<T, 3> st{s_tiles, full, {{a.h, a.T, D}, {a.dy, a.T, D}, {a.dh, a.T, D}}, a.dh ? 3 : 2, D};
+  const Tiles<T> dx{a.dx, a.T, D};
+  float w[NE], acc_w[NE], acc_b[NE];
+#pragma unroll
+  for (int k = 0; k < NE; ++k) {
+    const int e = lane + LANES * k;
+    w[k] = e < D ? __ldg(a.w + e) : 0.f;
+    acc_w[k] = acc_b[k] = 0.f;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < TILE_STAGES - 1; ++i)
+      if (blockIdx.x + static_cast<long long>(i) * gridDim.x < tiles) st.load(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
+  }
+  unsigned bad = 0;
+  uint32_t it = 0;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++it) {
+    const int s = it % TILE_STAGES, rows = static_cast<int>(min(static_cast<long long>(R), a.T - tile * R));
+    st.ends(tile, s);
+    if (!bad && !tma::wait(&full[s], (it / TILE_STAGES) & 1)) bad |= 1;
+    __syncthreads();  // the ends too
+    const T *hs = reinterpret_cast<const T*>(st.place(s, 0)), *gs = reinterpret_cast<const T*>(st.place(s, 2));
+    T* ds = reinterpret_cast<T*>(st.place(s, 1));
+#pragma unroll 1
+    for (int r0 = 0; r0 < R; r0 += ROWS) {
+      const bool live = r0 + group < rows;  // (a row past the end adds nothing to dw and db)
+      const int at = (r0 + group) * D + lane;
+      float c[NE], d[NE], sum[1] = {0.f};
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        const bool in = live && lane + LANES * k < D;
+        c[k] = in ? Io<T>::get(hs, at + LANES * k) : 0.f;
+        d[k] = in ? Io<T>::get(ds, at + LANES * k) : 0.f;
+        sum[0] += c[k];
+      }
+      lanes_join<LANES>(sum);
+      const float mean = sum[0] * inv_d;
+      float q[3] = {};  // sums of c^2, a, a c
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        c[k] = lane + LANES * k < D ? c[k] - mean : 0.f;
+        const float g = d[k] * w[k];
+        q[0] += c[k] * c[k];
+        q[1] += g;
+        q[2] += g * c[k];
+      }
+      lanes_join<LANES>(q);
+      const float rstd = live ? rsqrtf(q[0] * inv_d + a.eps) : 0.f;
+      const float ma = q[1] * inv_d, m = rstd * rstd * (q[2] * inv_d);
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        acc_w[k] += d[k] * (c[k] * rstd);
+        acc_b[k] += d[k];
+        if (live && lane + LANES * k < D)
+          Io<T>::put(ds, at + LANES * k, rstd * (d[k] * w[k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, at + LANES * k) : 0.f));
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      dx.store(tile, reinterpret_cast<unsigned char*>(ds));
+      tma::commit();
+      const long long next = tile + static_cast<long long>(TILE_STAGES - 1) * gridDim.x;
+      if (next < tiles) {
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the last tile has left the stage
+        st.load(next, (it + TILE_STAGES - 1) % TILE_STAGES);
+      }
+    }
+    dx.template ends<true>(tile, reinterpret_cast<unsigned char*>(ds));
+  }
+  if (threadIdx.x == 0) {
+    tma::wait_done();
+    // a wait that gave up: the copies in flight have landed before the CTA can end
+    for (uint32_t j = it > TILE_STAGES ? it - TILE_STAGES : 0; bad && j < it; ++j) (void)tma::wait(&full[j % TILE_STAGES], (j / TILE_STAGES) & 1);
+    if (bad) atomicOr(err, bad);
+  }
+  __syncthreads();  // the stages are free: every load has been waited for, every store has left
+  // the row groups hold the same columns: added in ascending group order
+  float* s_acc = reinterpret_cast<float*>(s_tiles);  // [group][2][D]
+  float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.x) * 2 * D;
+#pragma unroll
+  for (int k = 0; k < NE; ++k) {
+    const int e = lane + LANES * k;
+    if (e < D) s_acc[(2 * group) * D + e] = acc_w[k], s_acc[(2 * group + 1) * D + e] = acc_b[k];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * D; i += TILE_THREADS) {
+    float sum = s_acc[i];
+#pragma unroll 4
+    for (int g = 1; g < ROWS; ++g) sum += s_acc[2 * g * D + i];
+    part[i] = sum;
+  }
+  pdl_trigger();
+}
+
 // ---- host ----
 
+// The longest rows that go as tiles, and the least of them (two tiles an SM).
+constexpr int TILE_FORWARD = 1024, TILE_BACKWARD = 512;
+template <typename T>
+static bool tiled(long long rows, int D, int most, int sms) {
+  return D % Io<T>::V != 0 && D >= 8 && D <= most && rows >= 2ll * tile_rows<T>(D) * sms;
+}
+static bool contiguous(const void* p, long long stride, int D) { return !p || (stride == D && aligned(p, 16)); }
+// Lanes a row and elements a lane for rows of D.
+template <class F>
+static void by_columns(int D, F&& f) {
+#define WHTMIX_LANES(L, N) f(std::integral_constant<int, L>(), std::integral_constant<int, N>())
+  if (D <= 32) WHTMIX_LANES(8, 4);
+  else if (D <= 48) WHTMIX_LANES(8, 6);
+  else if (D <= 64) WHTMIX_LANES(8, 8);
+  else if (D <= 96) WHTMIX_LANES(16, 6);
+  else if (D <= 128) WHTMIX_LANES(16, 8);
+  else if (D <= 192) WHTMIX_LANES(32, 6);
+  else if (D <= 256) WHTMIX_LANES(32, 8);
+  else if (D <= 384) WHTMIX_LANES(32, 12);
+  else if (D <= 512) WHTMIX_LANES(32, 16);
+  else WHTMIX_LANES(32, 32);
+#undef WHTMIX_LANES
+}
+
 template <typename T, bool Q8>
-static cudaError_t forward_t(const LayerForward& a, int sms, cudaStream_t stream) {
+static cudaError_t forward_t(const LayerForward& a, unsigned int* err, int sms, cudaStream_t stream) {
   constexpr int V = Io<T>::V;
   const size_t es = sizeof(T);
   const bool al = a.D % V == 0 && aligned(a.w, 16) && (!a.b || aligned(a.b, 16)) && rows_aligned(a.x, a.xs, es) && rows_aligned(a.r, a.rs, es) &&
                   rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, V) : rows_aligned(a.y, a.ys, es));
   const int n = vectors(a.D, es == 2, al);
   LayerForward c = a;
+  if constexpr (!Q8) {
+    if (tiled<T>(a.T, a.D, TILE_FORWARD, sms) && contiguous(a.x, a.xs, a.D) && contiguous(a.r, a.rs, a.D) &&
+        contiguous(a.r ? a.h : nullptr, a.hs, a.D) && contiguous(a.y, a.ys, a.D)) {
+      const void* k = nullptr;
+      by_columns(a.D, [&](auto lanes, auto ne) { k = reinterpret_cast<const void*>(k_ln_tile<T, decltype(lanes)::value, decltype(ne)::value>); });
+      const size_t smem = static_cast<size_t>(TILE_STAGES) * (a.r ? 2 : 1) * tile_bytes<T>(a.D);  // at most 192 KB
+      int resident = 0;
+      const cudaError_t e = resident_ctas(k, TILE_THREADS, smem, sms, &resident);
+      if (e != cudaSuccess) return e;
+      void* args[] = {&c, &err};
+      return launch_pdl(k, grid_rows(a.T, tile_rows<T>(a.D), resident), TILE_THREADS, smem, stream, args);
+    }
+  }
   if (n > MAX_VECTORS) {
     void* args[] = {&c};
     return launch_pdl(reinterpret_cast<const void*>(k_ln_long<T, Q8>), grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args);
@@ -457,10 +779,10 @@ static cudaError_t forward_t(const LayerForward& a, int sms, cudaStream_t stream
   });
 }
 
-cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, int sms, cudaStream_t stream) {
+cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, unsigned int* err, int sms, cudaStream_t stream) {
   if (a.T <= 0) return cudaSuccess;
-  if (bf16) return to_e4m3 ? forward_t<__nv_bfloat16, true>(a, sms, stream) : forward_t<__nv_bfloat16, false>(a, sms, stream);
-  return to_e4m3 ? forward_t<float, true>(a, sms, stream) : forward_t<float, false>(a, sms, stream);
+  if (bf16) return to_e4m3 ? forward_t<__nv_bfloat16, true>(a, err, sms, stream) : forward_t<__nv_bfloat16, false>(a, err, sms, stream);
+  return to_e4m3 ? forward_t<float, true>(a, err, sms, stream) : forward_t<float, false>(a, err, sms, stream);
 }
 
 static int long_parts(long long T) { return static_cast<int>(T < 64 ? T : 64); }
@@ -485,9 +807,26 @@ struct LayerPlan {
   const void* kernel;
   size_t smem;
   int block, parts;
+  bool tiles;
 };
 template <typename T>
 static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int sms, LayerPlan* p) {
+  const size_t stages = static_cast<size_t>(TILE_STAGES) * (a.dh ? 3 : 2) * tile_bytes<T>(a.D);  // at most 144 KB
+  p->tiles = tiled<T>(a.T, a.D, TILE_BACKWARD, sms) && contiguous(a.h, a.hs, a.D) && contiguous(a.dy, a.ys, a.D) &&
+             contiguous(a.dh, a.ds, a.D) && contiguous(a.dx, a.xs, a.D);
+  if (p->tiles) {
+    by_columns(a.D, [&](auto lanes, auto ne) {
+      constexpr int LANES = decltype(lanes)::value, NE = decltype(ne)::value;
+      if constexpr (LANES * NE <= TILE_BACKWARD) p->kernel = reinterpret_cast<const void*>(k_ln_bwd_tile<T, LANES, NE>);
+      const size_t sums = static_cast<size_t>(TILE_THREADS / LANES) * 2 * a.D * 4;  // in the stages' place at the end
+      p->smem = stages > sums ? stages : sums;
+    });
+    p->block = TILE_THREADS;
+    int resident = 0;
+    const cudaError_t e = resident_ctas(p->kernel, TILE_THREADS, p->smem, sms, &resident);
+    if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, tile_rows<T>(a.D), resident));
+    return e;
+  }
   return by_length_backward(rows.n, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
     p->kernel = rows.al ? reinterpret_cast<const void*>(k_ln_bwd<T, (NV <= 2), TPR, NV>) : reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV>);
@@ -517,7 +856,7 @@ cudaError_t layer_backward_workspace(const LayerBackward& a, bool bf16, int sms,
 }
 
 template <typename T>
-static cudaError_t backward_t(const LayerBackward& a, int sms, cudaStream_t stream) {
+static cudaError_t backward_t(const LayerBackward& a, unsigned int* err, int sms, cudaStream_t stream) {
   const size_t es = sizeof(T);
   const LayerRows rows = layer_rows<T>(a);
   int parts = long_parts(a.T);
@@ -539,8 +878,8 @@ static cudaError_t backward_t(const LayerBackward& a, int sms, cudaStream_t stre
     LayerPlan p;
     if ((e = layer_plan<T>(a, rows, sms, &p)) != cudaSuccess) return e;
     parts = p.parts;
-    void* args[] = {&c, &same};
-    e = launch_pdl(p.kernel, static_cast<unsigned>(parts), p.block, p.smem, stream, args);
+    void *args[] = {&c, &same}, *tile_args[] = {&c, &err};
+    e = launch_pdl(p.kernel, static_cast<unsigned>(parts), p.block, p.smem, stream, p.tiles ? tile_args : args);
   }
   if (e != cudaSuccess) return e;
   const float* part = static_cast<const float*>(a.ws);
@@ -550,8 +889,8 @@ static cudaError_t backward_t(const LayerBackward& a, int sms, cudaStream_t stre
   return launch_pdl(reinterpret_cast<const void*>(k_dwdb), static_cast<unsigned>(((db ? 2 * D : D) + 31) / 32), 32 * DWDB_RUNS, 0, stream, args);
 }
 
-cudaError_t layer_backward(const LayerBackward& a, bool bf16, int sms, cudaStream_t stream) {
-  return bf16 ? backward_t<__nv_bfloat16>(a, sms, stream) : backward_t<float>(a, sms, stream);
+cudaError_t layer_backward(const LayerBackward& a, bool bf16, unsigned int* err, int sms, cudaStream_t stream) {
+  return bf16 ? backward_t<__nv_bfloat16>(a, err, sms, stream) : backward_t<float>(a, err, sms, stream);
 }
 
 }  // namespace norm

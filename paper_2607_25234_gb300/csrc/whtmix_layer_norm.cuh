@@ -35,9 +35,10 @@ struct LayerBackward {
   float eps;
 };
 
-cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, int sms, cudaStream_t stream);
+// err: the word that a wait that gave up leaves its mark in
+cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, unsigned int* err, int sms, cudaStream_t stream);
 cudaError_t layer_backward_workspace(const LayerBackward& a, bool bf16, int sms, size_t* bytes);  // (of a its ws is not read)
-cudaError_t layer_backward(const LayerBackward& a, bool bf16, int sms, cudaStream_t stream);
+cudaError_t layer_backward(const LayerBackward& a, bool bf16, unsigned int* err, int sms, cudaStream_t stream);
 
 }  // namespace norm
 }  // namespace whtmix

@@ -489,11 +489,12 @@ def test_values_that_are_not_finite_stay_where_they_are():
         close(db, torch.cat([2 * slope, value]), torch.cat([2.0 ** -15 * torch.ones_like(z).double(), 2.0 ** -16 * zb.clamp_min(0) + 1e-15]))
 
 
-def check_gated_backward(T, N, K, act, dw_dtype=BF):
+def check_gated_backward(T, N, K, act, dw_dtype=BF, **need):
     x, w = rand(1, T, K).to(BF), (rand(2, 2 * N, K) / math.sqrt(K)).to(BF)
     dy, p = rand(3, T, N).to(BF), rand(4, T, 2 * N).to(BF)
     outs = [guarded((T, K), BF), guarded((2 * N, K), dw_dtype), guarded((2 * N,), F32)]
-    dx, dw, db = whtmix.gated_linear_backward(x, w, dy, p, act, dw_dtype=dw_dtype, dx=outs[0][0], dw=outs[1][0], db=outs[2][0])
+    given = {name: o for name, (o, _) in zip(("dx", "dw", "db"), outs) if need.get("need_" + name, True)}
+    dx, dw, db = whtmix.gated_linear_backward(x, w, dy, p, act, dw_dtype=dw_dtype, **given, **need)
     for _, ok in outs:
         ok()
     D, (g, u) = dy.double(), p.double().split(N, 1)
@@ -501,16 +502,20 @@ def check_gated_backward(T, N, K, act, dw_dtype=BF):
     dp = torch.cat([D * u * slope, D * value], 1)
     exact = act in ("none", "relu")
     dp_err = 2 * U32 * dp.abs() if exact else torch.cat([2.0 ** -16 * (D * u).abs(), 2.0 ** -16 * (D * g).abs()], 1)
-    close(db, dp.sum(0), (T / 16 + 100) * U32 * dp.abs().sum(0) + dp_err.sum(0) + 1e-30)
+    if db is not None:
+        close(db, dp.sum(0), (T / 16 + 100) * U32 * dp.abs().sum(0) + dp_err.sum(0) + 1e-30)
     term = U16 * dp.abs() + dp_err  # dp rounded once
     for got, a, b_, e in ((dx, dp, w.double(), term), (dw, dp.T, x.double(), term.T)):
+        if got is None:
+            continue
         ref = a @ b_
         err = e @ b_.abs() + a.shape[1] * 2.0 ** -23 * (a.abs() @ b_.abs())
         close(got, ref, rounded(ref, err, got.dtype) + 1e-30)
         # and as a whole: roundings of random sign
         assert float((got.double() - ref).norm()) <= 2 * U16 * float(ref.norm()) + 1e-30
-    again = whtmix.gated_linear_backward(x, w, dy, p, act, dw_dtype=dw_dtype)  # the compiled way; a fixed order of additions
-    assert all(torch.equal(s, t) for s, t in zip(again, (dx, dw, db)))
+    again = whtmix.gated_linear_backward(x, w, dy, p, act, dw_dtype=dw_dtype, **need)  # the compiled way; a fixed order of additions
+    for s, t, name in zip(again, (dx, dw, db), ("dx", "dw", "db")):
+        assert torch.equal(s, t) if need.get("need_" + name, True) else s is None and t is None
     return x, w, dy, p, (dx, dw, db)
 
 
@@ -528,12 +533,10 @@ def test_gated_backward_of_many_tokens(T, N, K, act):
     x, w, dy, p, (dx, dw, db) = check_gated_backward(T, N, K, act)
     one = whtmix.gated_linear_backward(x, w, dy, p, act, need_dw=False, need_db=False)
     assert torch.equal(one[0], dx) and one[1] is None and one[2] is None
-    two = whtmix.gated_linear_backward(x, w, dy, p, act, need_dx=False)
-    assert two[0] is None and torch.equal(two[1], dw)
-    close(two[2], db.double(), (T / 16 + 100) * 2 * U32 * (dy.double().abs().sum(0).max() * 30))
-    three = whtmix.gated_linear_backward(x, w, dy, p, act, need_dx=False, need_dw=False)
-    assert three[0] is None and three[1] is None
-    close(three[2], db.double(), (T / 16 + 100) * 2 * U32 * (dy.double().abs().sum(0).max() * 30))
+    # without dx another kernel makes dp: its float32 values may differ in their last bit, the bounds are the same
+    check_gated_backward(T, N, K, act, need_dx=False)
+    check_gated_backward(T, N, K, act, need_dx=False, need_dw=False)
+    check_gated_backward(T, N, K, act, need_dx=False, need_db=False)
 
 
 def test_gated_gradients_by_differences():
