@@ -23,7 +23,7 @@ struct Call {
   bool scale;
 };
 
-size_t workspace(const Call& a, int sms);
+size_t workspace(const Call& a, int sms);  // may be 0
 cudaError_t run(const Call& a, void* ws, int sms, cudaStream_t stream);
 
 }  // namespace clip

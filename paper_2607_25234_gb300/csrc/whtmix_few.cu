@@ -317,6 +317,10 @@ cudaError_t forward_few(const Forward& a, const void* x, long long xs, const voi
   const long long tiles = static_cast<long long>(f.tiles_n) * ((a.T + tn - 1) / tn);
   f.splits = 1;
   while (f.splits < 8 && tiles * f.splits * 2 <= 2ll * sms && f.kblocks >= 4 * f.splits) f.splits *= 2;
+  // (gated: a pair of CTAs a tile costs more than it gives for more than a few tokens on a short K axis, or where the tiles alone nearly
+  // fill the SMs.  One CTA and two, us, bf16, K and N: 1 token 1024, 5464 7.1 and 6.4; 32 tokens 1024, 8192 9.9 and 11.0; 64 tokens 1024,
+  // 5464 11.1 and 13.1, 4096, 5464 26.5 and 25.9, 4096, 8192 30.2 and 31.7)
+  if (gated && f.splits == 2 && ((a.T > 8 && f.kblocks < 32) || (a.T > 16 && 4 * tiles > 3ll * sms))) f.splits = 1;
   if (!tma::encode_rows(&f.tw, w, es, gated ? 2ll * a.N : a.N, a.K, ws, out) || !tma::encode_rows(&f.tx, x, es, a.T, a.K, xs, tn))
     return cudaErrorInvalidValue;
   return gated ? by_types<true>(f, a, tn, sms, stream) : by_types<false>(f, a, tn, sms, stream);

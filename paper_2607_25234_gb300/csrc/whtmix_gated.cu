@@ -18,11 +18,15 @@ namespace linear {
 
 constexpr int THREADS_256 = 256;
 
+// CTAs of k_gated_dp an SM.  One row in flight and three CTAs against two rows and two CTAs, whole backward, us: [65536, 512] to 1408
+// 398 and 508, [8192, 1024] to 2736 211 and 215, to 2733 263 and 391; four CTAs 455, 205, 260 (registers spill).
+constexpr int DP_CTAS = 3;
+
 // dp[t, n], dp[t, N + n] = bf16 of both gradients; part[chunk][n], [N + n] = the chunk's rows' float32 sums of them, before the rounding.
 // A CTA takes 8 TX channels (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.  AL: dy, p and dp
 // have 16-byte aligned rows and halves.
 template <bool AL, int TX>
-__global__ void __launch_bounds__(THREADS_256, 2) k_gated_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
+__global__ void __launch_bounds__(THREADS_256, DP_CTAS) k_gated_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
   constexpr int G = THREADS_256 / TX;  // rows at a time
   __shared__ float s[G][TX][9];
   const int lane = threadIdx.x % TX, g = threadIdx.x / TX, c0 = (blockIdx.x * TX + lane) * 8;
@@ -52,49 +56,51 @@ __global__ void __launch_bounds__(THREADS_256, 2) k_gated_dp(const Backward a, _
 #pragma unroll
     for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
   };
-  auto store = [&](__nv_bfloat16* o, const float (&f)[8]) {
-    if constexpr (AL) {
-      uint32_t h[4];
+  // Eight values at column c0 of a half that starts s elements behind a 16-byte boundary (dp's rows start on one): whole vectors lie s
+  // elements lower, their first s values are the lane before's.  What no vector holds, at the ends of a strip and of the half, goes
+  // element by element.  ([3001, 777] with every element on its own: 31 us)
+  const uint32_t segment = TX == 32 ? 0xffffffffu : ((1u << TX) - 1u) << (threadIdx.x & 31u & ~static_cast<uint32_t>(TX - 1));
+  auto store = [&](__nv_bfloat16* o, int s, const float (&f)[8]) {
+    const int left = a.N - c0;
+    uint32_t h[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-        h[j] = *reinterpret_cast<uint32_t*>(&b);
+    for (int j = 0; j < 4; ++j) {
+      __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+      h[4 + j] = *reinterpret_cast<uint32_t*>(&b);
+    }
+    bool whole = left >= 8, next = true;  // this lane's vector, and the next one's
+    if constexpr (!AL) {
+      if (s > 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = __shfl_up_sync(segment, h[4 + j], 1, TX);
+        shift_bytes<4>(h, static_cast<uint32_t>(16 - 2 * s));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[4 + j] = h[j];
+        whole = lane > 0 && left >= 8 - s, next = lane < TX - 1 && left - 8 >= 8 - s;
       }
-      if (c0 < a.N) *reinterpret_cast<uint4*>(o + c0) = make_uint4(h[0], h[1], h[2], h[3]);
-    } else {
+    }
+    if (whole) *reinterpret_cast<uint4*>(o + c0 - s) = make_uint4(h[4], h[5], h[6], h[7]);
+    if constexpr (!AL) {
+      if (!whole || !next) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c0 + j < a.N) o[c0 + j] = __float2bfloat16_rn(f[j]);
+        for (int j = 0; j < 8; ++j)
+          if (j < left && (j < 8 - s ? !whole : !next)) o[c0 + j] = __float2bfloat16_rn(f[j]);
+      }
     }
   };
-  constexpr int U = 2;  // rows in flight
-  for (long long first = t0 + g; first < t1; first += G * U) {
-    Raw ud[U], uz[U], uu[U];
+  for (long long t = t0 + g; t < t1; t += G) {
+    const Raw ud = fetch(dy + t * a.dys, sd), uz = fetch(p + t * a.ps, sp), uu = fetch(p + t * a.ps + a.N, sp);
+    float d[8], z[8], u[8], v[8];
+    values(ud, dy + t * a.dys, sd, d);
+    values(uz, p + t * a.ps, sp, z);
+    values(uu, p + t * a.ps + a.N, sp, u);
 #pragma unroll
-    for (int r = 0; r < U; ++r) {
-      const long long t = first + G * r;
-      if (t < t1) {
-        ud[r] = fetch(dy + t * a.dys, sd);
-        uz[r] = fetch(p + t * a.ps, sp);
-        uu[r] = fetch(p + t * a.ps + a.N, sp);
-      }
-    }
+    for (int j = 0; j < 8; j += 2) gate_gradients(d[j], d[j + 1], v[j], v[j + 1], z[j], z[j + 1], u[j], u[j + 1], a.act);
 #pragma unroll
-    for (int r = 0; r < U; ++r) {
-      const long long t = first + G * r;
-      if (t >= t1) break;
-      float d[8], z[8], u[8], v[8];
-      values(ud[r], dy + t * a.dys, sd, d);
-      values(uz[r], p + t * a.ps, sp, z);
-      values(uu[r], p + t * a.ps + a.N, sp, u);
-#pragma unroll
-      for (int j = 0; j < 8; j += 2) gate_gradients(d[j], d[j + 1], v[j], v[j + 1], z[j], z[j + 1], u[j], u[j + 1], a.act);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc_g[j] += d[j], acc_u[j] += v[j];
-      if (dp) {
-        store(dp + t * dps, d);
-        store(dp + t * dps + a.N, v);
-      }
+    for (int j = 0; j < 8; ++j) acc_g[j] += d[j], acc_u[j] += v[j];
+    if (dp) {
+      store(dp + t * dps, 0, d);
+      store(dp + t * dps + a.N, a.N % 8, v);
     }
   }
   if (part) {
@@ -224,7 +230,7 @@ static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
     b.pad_w = !tma::mappable(a.w, 2ll * a.N, a.ws, 2);
     if (b.pad_w) b.w_off = take(static_cast<size_t>(2ll * a.N) * pitch_of(a.K, 2) * 2);
   } else {
-    const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (4 * sms + strips - 1) / strips;  // one wave
+    const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (DP_CTAS * sms + strips - 1) / strips;  // one wave
     b.chunks = rows < most ? rows : most;
     if (b.chunks > 65535) b.chunks = 65535;
     if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less

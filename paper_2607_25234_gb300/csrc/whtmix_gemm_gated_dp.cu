@@ -2,7 +2,7 @@
 // sums and dx = dg Wg + du Wu, for K <= 256, where one tile of columns holds all of dx's.
 //
 // One persistent CTA per SM, 512 threads, tiles of 128 tokens, the hidden channels in blocks of 64:
-//   warp 0      TMA loads of a block of dy, g and u (128 x 64 each), two stages;
+//   warp 0      TMA loads of a block of dy, g and u (128 x 64 each), two or three stages;
 //   warp 2      TMA loads of its rows of Wg and of Wu (64 rows of BN columns each), a ring of three;
 //   warps 8-15  read the block in shared memory, write bf16 dg over g and du over u, where they lie as the products' operand wants
 //               them, and add up the block's columns unrounded;
@@ -15,24 +15,29 @@
 namespace whtmix {
 namespace linear {
 
-constexpr int GDP_THREADS = 512, GDP_STAGES = 2, GDP_UNITS = 3;
+constexpr int GDP_THREADS = 512;
 template <int BN>
 struct GdpRing {
+  // ([65536, 128] to 344, two and three stages: 85.4 and 76.9 us.  At 256 columns W's way from L2 takes the room: two stages and three
+  // units of 32 KB 258 us where three stages and three units of 128 columns took 297, six of those 280)
+  static constexpr int STAGES = BN == 256 ? 2 : 3, UNITS = 3;
   static constexpr uint32_t TILE = 128 * 128, STAGE = 3 * TILE, UNIT = BN * 128;
-  static constexpr uint32_t W = GDP_STAGES * STAGE, PANEL = W + GDP_UNITS * UNIT;
+  static constexpr uint32_t W = STAGES * STAGE, PANEL = W + UNITS * UNIT;
   static constexpr size_t SMEM = PANEL + PANEL_BYTES;
 };
+template <int BN>
 struct GdpBars {
-  uint64_t full[GDP_STAGES], ready[GDP_STAGES], empty[GDP_STAGES], wfull[GDP_UNITS], wempty[GDP_UNITS], dfull[2], dempty[2];
+  uint64_t full[GdpRing<BN>::STAGES], ready[GdpRing<BN>::STAGES], empty[GdpRing<BN>::STAGES];
+  uint64_t wfull[GdpRing<BN>::UNITS], wempty[GdpRing<BN>::UNITS], dfull[2], dempty[2];
 };
 
 template <int BN, int ACT>
 __global__ void __launch_bounds__(GDP_THREADS, 1) k_dx_gated(const __grid_constant__ GatedDp a) {
   using R = GdpRing<BN>;
-  constexpr int S = GDP_STAGES, U = GDP_UNITS;
+  constexpr int S = R::STAGES, U = R::UNITS;
   constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (static_cast<uint32_t>(BN >> 3) << 17) | ((128u >> 4) << 24);
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ GdpBars bars;
+  __shared__ GdpBars<BN> bars;
   __shared__ uint32_t tmem_slot;
   __shared__ __align__(16) float s_sum[2][8][128];  // the warps' column sums of a block, dg's and du's, and of the next
   const uint32_t ring = tc::smem_u32(smem);

@@ -443,8 +443,10 @@ static int global_norm(const whtmix_tensor_t* tensors, int64_t count, float max_
     if (items.empty()) return zero(norm, 4, stream);
     const clip::Call a{items.data(), static_cast<long long>(items.size()), norm, max_norm, scale};
     host::Scratch scratch;
-    rc = scratch.take(dev, stream, clip::workspace(a, sms));
-    if (rc != WHTMIX_OK) return rc;
+    if (const size_t need = clip::workspace(a, sms)) {
+      rc = scratch.take(dev, stream, need);
+      if (rc != WHTMIX_OK) return rc;
+    }
     rc = done(clip::run(a, scratch.get(), sms, stream));
     return rc != WHTMIX_OK ? rc : scratch.give_back();
   });

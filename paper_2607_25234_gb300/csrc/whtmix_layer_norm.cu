@@ -76,9 +76,11 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, cons
   extern __shared__ float s_w[];  // unaligned rows: the gains, then the shifts
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
-  pdl_wait();
-  const bool short_launch = gridDim.x < 128;  // (lets the next kernel come in at once, as k_rms)
+  // A short launch lets the next kernel come in at once, which may ask for its weights before this one's rows are there (24 rows to 8 bits
+  // and their gated product 19.7 -> 19.4 us); a long one would have it wait in the SMs' way.
+  const bool short_launch = gridDim.x < 128;
   if (short_launch) pdl_trigger();
+  pdl_wait();
   const int set = V * slots_of<V>(a.D);
   if constexpr (!AL) {
     gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
@@ -215,14 +217,19 @@ __global__ void __launch_bounds__(LONG_THREADS) k_ln_long(const LayerForward a) 
   pdl_trigger();
 }
 
+// Rows on their way to a thread of k_ln_bwd, 48 KB a CTA of 256 threads: registers for one row ahead (113 of them, two CTAs an SM) keep too
+// little in flight: [131072, 256] bf16 with dh 59.5 us, this way 49.2.
+template <int BLOCK, int NV>
+constexpr int LN_DEPTH = NV == 1 ? 4 : 2;
+
 // dx, and this CTA's partial row of dw and of db: part[blockIdx.x][0 .. 2 D).  Aligned rows: a thread's columns are the same in every
 // row, their sums stay in its registers.  Unaligned ones, and rows of more vectors than that leaves registers for: in shared memory,
 // two sets for each of the CTA's row groups (dynamic).
 template <typename T, bool AL, int TPR, int NV>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln_bwd(const LayerBackward a, const Same same) {
+__global__ void __launch_bounds__(BLOCK_OF<TPR>, AL && TPR == 512 && NV == 1 ? 2 : 1) k_ln_bwd(const LayerBackward a, const Same same) {
   constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
-  extern __shared__ float s_acc[];  // a group's sums for dw, then for db; behind all groups' the gains
+  extern __shared__ __align__(16) float s_acc[];  // unaligned: a group's sums for dw, then for db; behind all groups' the gains.  Aligned: the rows
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
   float acc_w[AL ? NV : 1][V] = {}, acc_b[AL ? NV : 1][V] = {};
@@ -242,32 +249,66 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln_bwd(const LayerBackward a,
   kept.fill(gains, lane, a.D);
   const long long step = static_cast<long long>(gridDim.x) * ROWS;
   const Bounds bh = bounds_of<T>(a.h, a.T, a.hs, a.D), bd = bounds_of<T>(a.dy, a.T, a.ys, a.D), bg = bounds_of<T>(a.dh, a.T, a.ds, a.D);
-  uint4 uh[NV], ud[NV];
-  auto fetch = [&](long long t) {
-    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
+  // the row's vectors: aligned rows come through shared memory, DEPTH of them on their way (a thread's own places: nobody else waits),
+  // unaligned ones through registers, one row ahead
+  constexpr int DEPTH = LN_DEPTH<BLOCK, NV>;
+  uint4* ring = reinterpret_cast<uint4*>(s_acc) + threadIdx.x;
+  auto place = [&](int i, int m, int k) { return ring + ((i * 3 + m) * NV + k) * BLOCK; };
+  uint4 uh[AL ? 1 : NV], ud[AL ? 1 : NV], un[AL ? 1 : NV];
+  auto fetch = [&](long long t, int i) {
+    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys, *gp = static_cast<const T*>(a.dh) + t * a.ds;
     const int D = t < a.T ? a.D : 0;
-    R::fetch(hp, bh, lane, R::offset(hp), true, D, uh);
-    R::fetch(dp, bd, lane, R::offset(hp), same.a, D, ud);
+    if constexpr (AL) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int e = R::at(lane, k), n = e < D ? 16 : 0;  // (0: zeros)
+        const T* from[3] = {n ? hp + e : static_cast<const T*>(a.h), n ? dp + e : static_cast<const T*>(a.dy), n ? gp + e : static_cast<const T*>(a.dh)};
+#pragma unroll
+        for (int m = 0; m < 3; ++m)
+          if (m < 2 || a.dh)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(place(i, m, k))), "l"(from[m]), "r"(n) : "memory");
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    } else {
+      R::fetch(hp, bh, lane, R::offset(hp), true, D, uh);
+      R::fetch(dp, bd, lane, R::offset(hp), same.a, D, ud);
+      if (a.dh) R::fetch(gp, bg, lane, R::offset(hp), same.b, D, un);
+    }
   };
-  fetch(static_cast<long long>(blockIdx.x) * ROWS + group);
-  for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += step) {
+  const long long first = static_cast<long long>(blockIdx.x) * ROWS;
+#pragma unroll
+  for (int i = 0; i < (AL ? DEPTH - 1 : 1); ++i) fetch(first + i * step + group, i);
+  int turn = 0;
+  for (long long base = first; base < a.T; base += step, turn = (turn + 1) % DEPTH) {
     const long long t = base + group;
     const int D = t < a.T ? a.D : 0;
     float h[NV][V], d[NV][V], sum[1] = {0.f};
-    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys;
+    const T *hp = static_cast<const T*>(a.h) + t * a.hs, *dp = static_cast<const T*>(a.dy) + t * a.ys, *gp = static_cast<const T*>(a.dh) + t * a.ds;
     const int off = R::offset(hp);
     const Places<V> places(off, a.D);
+    uint4 ug[NV];
+    if constexpr (AL) {
+      fetch(t + (DEPTH - 1) * step, (turn + DEPTH - 1) % DEPTH);
+      asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      R::values(hp, bh, lane, k, off, true, D, uh[k], h[k]);
-      R::values(dp, bd, lane, k, off, same.a, D, ud[k], d[k]);
+      for (int k = 0; k < NV; ++k) {
+        Io<T>::unpack(*place(turn, 0, k), h[k]);
+        Io<T>::unpack(*place(turn, 1, k), d[k]);
+        if (a.dh) ug[k] = *place(turn, 2, k);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        R::values(hp, bh, lane, k, off, true, D, uh[k], h[k]);
+        R::values(dp, bd, lane, k, off, same.a, D, ud[k], d[k]);
+        ug[k] = un[k];
+      }
+      fetch(t + step, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] += h[k][j];
-    }
-    uint4 ug[NV];
-    const T* gp = static_cast<const T*>(a.dh) + t * a.ds;
-    if (a.dh) R::fetch(gp, bg, lane, off, same.b, D, ug);
-    fetch(t + step);
     row_join<TPR, 0, false>(sum);
     const float mean = sum[0] * inv_d;
     float s[3] = {};  // of c^2, a, a c
@@ -308,6 +349,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln_bwd(const LayerBackward a,
       R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o);
     }
   }
+  if constexpr (AL) asm volatile("cp.async.wait_all;" ::: "memory");
   // the CTA's row groups hold the same columns: added in ascending group order
   float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.x) * 2 * a.D;
   if constexpr (!AL) {
@@ -324,9 +366,11 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln_bwd(const LayerBackward a,
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
+      for (int j = 0; j < V; j += 4) {
         const int e = R::at(lane, k) + j;
-        if (e < a.D) part[e] = acc_w[k][j], part[a.D + e] = acc_b[k][j];
+        if (e >= a.D) continue;
+        *reinterpret_cast<float4*>(part + e) = make_float4(acc_w[k][j], acc_w[k][j + 1], acc_w[k][j + 2], acc_w[k][j + 3]);
+        *reinterpret_cast<float4*>(part + a.D + e) = make_float4(acc_b[k][j], acc_b[k][j + 1], acc_b[k][j + 2], acc_b[k][j + 3]);
       }
   } else {
     __shared__ float s[ROWS][TPR][V + 1];
@@ -714,7 +758,8 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackwar
 
 // ---- host ----
 
-// The longest rows that go as tiles, and the least of them (two tiles an SM).
+// The longest rows that go as tiles, and the least of them (two tiles an SM).  Rows of whole vectors stay with their own kernels
+// (backward, us, tiles read by vectors and row kernels: [131072, 256] bf16 69.1 and 59.6, [128000, 64] float32 21.4 and 20.8).
 constexpr int TILE_FORWARD = 1024, TILE_BACKWARD = 512;
 template <typename T>
 static bool tiled(long long rows, int D, int most, int sms) {
@@ -830,7 +875,8 @@ static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int
   return by_length_backward(rows.n, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
     p->kernel = rows.al ? reinterpret_cast<const void*>(k_ln_bwd<T, (NV <= 2), TPR, NV>) : reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV>);
-    p->smem = rows.al ? 0 : static_cast<size_t>(2 * (BLOCK / TPR) + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 193 KB
+    p->smem = rows.al ? static_cast<size_t>(LN_DEPTH<BLOCK, NV>) * 3 * NV * BLOCK * 16  // at most 96 KB
+                      : static_cast<size_t>(2 * (BLOCK / TPR) + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 193 KB
     p->block = BLOCK;
     int resident = 0;
     const cudaError_t e = resident_ctas(p->kernel, BLOCK, p->smem, sms, &resident);
