@@ -142,6 +142,16 @@ static GatedForwardPlan plan_forward(const Forward& a) {
   return f;
 }
 
+// Calls for whtmix_few.cu: few tokens; a long K axis and tiles of 64 channels that four CTAs each can share; or few tiles for a long K
+// axis, which the tiled products would walk along on their own.  The tiled products and those, us, bf16, K and N: 32 tokens 1024, 8192
+// 9.5 and 9.9; 64 tokens 1024, 2736 8.4 and 9.3, 4096, 4096 23.7 and 18.6, 4096, 8192 26.5 and 30.2; 100 tokens 2048, 5464 14.6 and 22.6;
+// 171 tokens 7448, 1176 44.7 and 27.5; 500 tokens 2048, 144 13.3 and 9.2, 7448, 1176 45.0 and 55.4; 3200 tokens 4096, 64 23.2 and 15.2,
+// 2048, 144 13.8 and 28.9.
+static bool few_tokens(long long T, int N, int kblocks, int sms) {
+  const long long tiles = static_cast<long long>(ceil_div(N, 64)) * ceil_div(T, 128);
+  return T <= 32 || (T <= 64 && kblocks >= 32 && 4 * tiles <= 2ll * sms) || 5 * tiles <= 3ll * kblocks;
+}
+
 // Four epilogue groups instead of two, at the price of a shorter ring, where the epilogue is longer than a tile's products.  Two and
 // four, us: [64800, 128] to 344, gelu 26.0 and 22.6, with p 40.5 and 33.9; [64800, 256] to 688 with p 74.7 and 66.2; [64800, 384] to
 // 1024 77.8 and 81.8, with p 117 and 108; [32768, 512] to 1408 64.3 and 72.3, with p 95.8 and 89.3; [32768, 768] to 2048 with p 155
@@ -168,12 +178,16 @@ cudaError_t gated_forward(const Forward& a, void* ws, unsigned int* err, int sms
   }
   const cudaError_t e = to_pitch(cx, cw, sms, stream);
   if (e != cudaSuccess) return e;
-  if (use_few(a.T, ceil_div(a.K, 128 / es))) return forward_few(a, x, xs, w, wst, true, err, sms, stream);
+  if (few_tokens(a.T, a.N, ceil_div(a.K, 128 / es), sms)) return forward_few(a, x, xs, w, wst, true, err, sms, stream);
   Gated g{};
   g.kblocks = ceil_div(a.K, 128 / es);
   // a product of 2 N columns by its clocks, 128 of them a tile at least
   Plan pl = plan_product(a.T, 2 * a.N, g.kblocks, sms, 1);
   if (pl.bn < 128) pl.bn = 128;
+  // Rows that are no whole 128-byte lines cost twice the way out of L2, of which a pair needs less: [15944, 408] to 5456 171 and 138 us
+  // (with p 207 and 195), where [64800, 384] to 1024 takes 78 and 84; [6192, 216] to 6272 with p, 4 K blocks, 73 and 81.
+  const bool lines = static_cast<unsigned long long>(xs) * es % 128 == 0 && static_cast<unsigned long long>(wst) * es % 128 == 0;
+  if (pl.bn == 256 && !lines && g.kblocks > 4 && static_cast<long long>(ceil_div(a.T, 256)) * ceil_div(a.N, 128) >= sms) pl.bn = TILE_PAIR;
   const int out = tile_cols(pl.bn) / 2;
   g.tiles_m = ceil_div(a.T, tile_rows(pl.bn)), g.tiles_n = ceil_div(a.N, out);
   g.band = 16;
@@ -220,6 +234,7 @@ static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
   b.products = a;
   b.products.N = 2 * a.N, b.products.act = ACT_NONE, b.products.p = nullptr, b.products.db = nullptr;
   b.products.dy = nullptr, b.products.dys = b.np;  // (on a 16-byte boundary)
+  b.products.split_dx = true;
   if (b.fused) b.products.dx = nullptr;
   if (b.products.dx || a.dw) {
     b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);

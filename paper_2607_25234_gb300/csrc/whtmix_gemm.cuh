@@ -673,7 +673,7 @@ cudaError_t gemm_e4m3(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t
 // whtmix_gemm_four.cu, whtmix_gemm_e4m3_four.cu: the same with four epilogue groups
 cudaError_t gemm_forward_four(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_e4m3_four(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
-cudaError_t gemm_dx(const Gemm& g, int bn, int sms, cudaStream_t stream);
+cudaError_t gemm_dx(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 cudaError_t gemm_dw(const Gemm& g, bool out_f32, int bn, int sms, cudaStream_t stream);
 
 // whtmix_gemm_dp.cu: dp = dy act'(p), its column sums and dx = dp W in one pass, for K <= 256 (one tile of columns) and an

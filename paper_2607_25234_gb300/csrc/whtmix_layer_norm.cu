@@ -832,9 +832,10 @@ cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, unsign
 
 static int long_parts(long long T) { return static_cast<int>(T < 64 ? T : 64); }
 
-// How a backward call's rows are taken: aligned in registers up to MAX_SUMMED vectors (two sets of sums beside two inputs: with four
-// vectors a thread they would not fit 128 registers), else as unaligned ones.
-constexpr int MAX_SUMMED = 1024;
+// How a backward call's rows are taken: aligned with the sums in registers up to MAX_SUMMED vectors (512 threads have 128 registers each),
+// else as unaligned ones.  (1024 threads with one vector each: [11870, 4696] bf16 148 -> 230 us.)
+template <typename T>
+constexpr int MAX_SUMMED = sizeof(T) == 4 ? 2048 : 1024;
 struct LayerRows {
   bool al;
   int n;  // vectors
@@ -843,7 +844,7 @@ template <typename T>
 static LayerRows layer_rows(const LayerBackward& a) {
   const size_t es = sizeof(T);
   const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.h, a.hs, es) && rows_aligned(a.dy, a.ys, es) &&
-                  rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es) && vectors(a.D, es == 2, true) <= MAX_SUMMED;
+                  rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es) && vectors(a.D, es == 2, true) <= MAX_SUMMED<T>;
   return {al, vectors(a.D, es == 2, al)};
 }
 
@@ -872,17 +873,27 @@ static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int
     if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, tile_rows<T>(a.D), resident));
     return e;
   }
-  return by_length_backward(rows.n, [&](auto tpr, auto nv) {
+  auto take = [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
-    p->kernel = rows.al ? reinterpret_cast<const void*>(k_ln_bwd<T, (NV <= 2), TPR, NV>) : reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV>);
-    p->smem = rows.al ? static_cast<size_t>(LN_DEPTH<BLOCK, NV>) * 3 * NV * BLOCK * 16  // at most 96 KB
+    constexpr bool ALIGNED = NV * TPR <= MAX_SUMMED<T>, ODD = TPR != 192 && TPR != 384;
+    if (rows.al) {
+      if constexpr (ALIGNED) p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, true, TPR, NV>);
+    } else {
+      if constexpr (ODD) p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV>);
+    }
+    p->smem = rows.al ? static_cast<size_t>(LN_DEPTH<BLOCK, NV>) * 3 * NV * BLOCK * 16  // at most 192 KB
                       : static_cast<size_t>(2 * (BLOCK / TPR) + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 193 KB
     p->block = BLOCK;
     int resident = 0;
     const cudaError_t e = resident_ctas(p->kernel, BLOCK, p->smem, sms, &resident);
     if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, BLOCK / TPR, resident));
     return e;
-  });
+  };
+  // (aligned rows in registers: threads in steps of two thirds too, [5288, 2232] bf16 41.5 us with 512 of them and 34.7 with 384)
+  if (rows.al && rows.n > 128 && rows.n <= 192) return take(Int<192>(), Int<1>());
+  if (rows.al && rows.n > 256 && rows.n <= 384) return take(Int<384>(), Int<1>());
+  if (rows.al && rows.n > 512 && rows.n <= 768) return take(Int<384>(), Int<2>());
+  return by_length_backward(rows.n, take);
 }
 
 template <typename T>

@@ -151,12 +151,12 @@ __global__ void __launch_bounds__(THREADS_256, AL ? 4 : 3) k_dp(const Backward a
 }
 
 // ---- the sum of a split product ----
-// out [rows, cols] contiguous = sum over s of part[s * split_rows + row][pitch].  A CTA takes 256 / G fours of columns; its G groups
+// out [rows, cols] (out_stride elements a row) = sum over s of part[s * split_rows + row][pitch].  A CTA takes 256 / G fours of columns; its G groups
 // of threads sum runs of consecutive splits, each in ascending order, then the run sums are added in ascending order.  Many splits
 // take G = 8: with a thread for all the splits of its four, 152 splits of [77, 488] took 12.5 us.
 template <typename O, int G>
 __global__ void __launch_bounds__(THREADS_256) k_sum_splits(O* __restrict__ out, const float* part, int rows, int cols, int pitch,
-                                                            int split_rows, int splits) {
+                                                            int split_rows, int splits, long long out_stride) {
   constexpr int L = THREADS_256 / G;
   __shared__ float4 s[G][L];
   pdl_wait();
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(THREADS_256) k_sum_splits(O* __restrict__ out,
         sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
       }
       const float f[4] = {sum.x, sum.y, sum.z, sum.w};
-      O* o = out + static_cast<long long>(r) * cols + c;
+      O* o = out + static_cast<long long>(r) * out_stride + c;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (c + j < cols) o[j] = static_cast<O>(f[j]);
@@ -206,6 +206,17 @@ __global__ void __launch_bounds__(THREADS_256) k_sum_splits(O* __restrict__ out,
 }
 
 // ---- host ----
+
+static cudaError_t sum_splits(void* out, bool f32, long long out_stride, const float* part, int rows, int cols, int pitch, int split_rows,
+                              int splits, int sms, cudaStream_t stream) {
+  void* args[] = {&out, &part, &rows, &cols, &pitch, &split_rows, &splits, &out_stride};
+  const bool many = splits >= 16;
+  const long long n = static_cast<long long>(rows) * ceil_div(cols, 4), need = (n + (many ? 31 : 255)) / (many ? 32 : 256);
+  return launch_pdl(f32 ? (many ? reinterpret_cast<const void*>(k_sum_splits<float, 8>) : reinterpret_cast<const void*>(k_sum_splits<float, 1>))
+                        : (many ? reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16, 8>)
+                                : reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16, 1>)),
+                    static_cast<unsigned>(need < 8ll * sms ? need : 8ll * sms), THREADS_256, 0, stream, args);
+}
 
 // Tile width and splits of a product of M rows, N columns and kblocks K blocks.  A block of a tile costs BLOCK clocks of an SM (of a
 // pair of them), not in proportion to its width: the operands' way from L2 and out of shared memory bounds the narrow tiles
@@ -309,9 +320,9 @@ struct BackwardPlan {
   bool fused;  // dp, db's partial sums and dx in one kernel (whtmix_gemm_dp.cu)
   bool own_dp, pad_x, pad_w;
   int np, kp, chunks;  // pitches of dp, and of x and W; db's chunks of rows
-  Plan dw;
-  int split_rows;
-  size_t dp_off, x_off, w_off, db_off, dw_off, total;
+  Plan dx, dw;
+  int dx_split_rows, split_rows;
+  size_t dp_off, x_off, w_off, db_off, dx_off, dw_off, total;
 };
 static BackwardPlan plan_backward(const Backward& a, int sms) {
   BackwardPlan b{};
@@ -339,6 +350,11 @@ static BackwardPlan plan_backward(const Backward& a, int sms) {
     if (b.chunks > 65535) b.chunks = 65535;
     if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
     if (a.db && b.chunks > 1) b.db_off = take(static_cast<size_t>(b.chunks) * a.N * 4);
+  }
+  if (a.dx && !b.fused) {
+    b.dx = plan_product(a.T, a.K, ceil_div(a.N, 64), sms, a.split_dx ? 2 * sms : 1);
+    b.dx_split_rows = ceil_div(a.T, tile_rows(b.dx.bn)) * tile_rows(b.dx.bn);
+    if (b.dx.splits > 1) b.dx_off = take(static_cast<size_t>(b.dx.splits) * b.dx_split_rows * pitch_of(a.K, 4) * 4);
   }
   if (a.dw) {
     b.dw = plan_product(a.N, a.K, ceil_div(a.T, 64), sms, 2 * sms);
@@ -404,17 +420,24 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
   if (a.dx && !b.fused) {
     Gemm g{};
     g.kblocks = ceil_div(a.N, 64);
-    const Plan pl = plan_product(a.T, a.K, g.kblocks, sms, 1);
-    g.tiles_m = ceil_div(a.T, tile_rows(pl.bn)), g.tiles_n = ceil_div(a.K, tile_cols(pl.bn));
-    g.splits = 1;
+    g.tiles_m = ceil_div(a.T, tile_rows(b.dx.bn)), g.tiles_n = ceil_div(a.K, tile_cols(b.dx.bn));
+    g.splits = b.dx.splits;
+    g.split_rows = g.splits > 1 ? b.dx_split_rows : 0;
     g.M = static_cast<int>(a.T), g.N = a.K;
-    g.y = a.dx, g.ys = a.dxs, g.y_plain = !tma::storable(a.dx, a.T, a.K, a.dxs, 2);
     g.err = err;
+    const bool split = g.splits > 1;
+    const int os = split ? 4 : 2;
+    void* out = split ? static_cast<void*>(base + b.dx_off) : a.dx;
+    const long long rows = split ? static_cast<long long>(g.splits) * b.dx_split_rows : a.T, stride = split ? pitch_of(a.K, 4) : a.dxs;
+    g.y = out, g.ys = stride, g.y_plain = !split && !tma::storable(a.dx, a.T, a.K, a.dxs, 2);
     if (!tma::encode_rows(&g.ta, dp, 2, a.T, a.N, dps, GEMM_BM) ||
         !tma::encode_rows(&g.tb, b.pad_w ? base + b.w_off : a.w, 2, a.N, a.K, b.pad_w ? b.kp : a.ws, 64) ||
-        (!g.y_plain && !tma::encode_rows(&g.ty, a.dx, 2, a.T, a.K, a.dxs, GEMM_BM)))
+        (!g.y_plain && !tma::encode_rows(&g.ty, out, os, rows, a.K, stride, GEMM_BM)))
       return cudaErrorInvalidValue;
-    if ((e = gemm_dx(g, pl.bn, sms, stream)) != cudaSuccess) return e;
+    if ((e = gemm_dx(g, split, b.dx.bn, sms, stream)) != cudaSuccess) return e;
+    if (split && (e = sum_splits(a.dx, false, a.dxs, static_cast<const float*>(out), static_cast<int>(a.T), a.K, pitch_of(a.K, 4), b.dx_split_rows,
+                                 g.splits, sms, stream)) != cudaSuccess)
+      return e;
   }
   if (a.dw) {
     Gemm g{};
@@ -435,18 +458,8 @@ cudaError_t backward(const Backward& a, void* ws, unsigned int* err, int sms, cu
         (!g.y_plain && !tma::encode_rows(&g.ty, out, os, rows, a.K, pitch, GEMM_BM)))
       return cudaErrorInvalidValue;
     if ((e = gemm_dw(g, os == 4, b.dw.bn, sms, stream)) != cudaSuccess) return e;
-    if (split) {
-      const float* part = static_cast<const float*>(out);
-      int rows_ = a.N, cols = a.K, sr = b.split_rows, splits = g.splits;
-      void* dw = a.dw;
-      void* args[] = {&dw, &part, &rows_, &cols, &pitch, &sr, &splits};
-      const long long n = static_cast<long long>(a.N) * ceil_div(a.K, 4), need = (n + (splits >= 16 ? 31 : 255)) / (splits >= 16 ? 32 : 256);
-      const bool many = splits >= 16;
-      e = launch_pdl(a.dw_f32 ? (many ? reinterpret_cast<const void*>(k_sum_splits<float, 8>) : reinterpret_cast<const void*>(k_sum_splits<float, 1>))
-                              : (many ? reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16, 8>)
-                                      : reinterpret_cast<const void*>(k_sum_splits<__nv_bfloat16, 1>)),
-                     static_cast<unsigned>(need < 8ll * sms ? need : 8ll * sms), THREADS_256, 0, stream, args);
-    }
+    if (split)
+      e = sum_splits(a.dw, a.dw_f32, a.K, static_cast<const float*>(out), a.N, a.K, pitch, b.split_rows, g.splits, sms, stream);
   }
   return e;
 }

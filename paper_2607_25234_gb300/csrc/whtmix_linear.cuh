@@ -33,6 +33,7 @@ struct Backward {
   long long T, xs, ws, dys, ps, dxs;
   int K, N, act;
   bool dw_f32;
+  bool split_dx = false;  // dx's contraction over N may be split over CTAs, as dw's over T is
 };
 
 size_t forward_workspace(const Forward& a, int sms);
