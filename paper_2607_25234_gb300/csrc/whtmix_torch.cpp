@@ -354,43 +354,47 @@ PyObject* gated_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) 
   END_HANDLE_TH_ERRORS
 }
 
-// A list of plain contiguous tensors on the current device, as the C ABI takes it; `outs`: another list (of their shapes) or null.
-bool entries_of(PyObject* list, PyObject* outs, std::vector<whtmix_tensor_t>* entries, const at::Tensor** first) {
-  if (!PyList_CheckExact(list) || (outs && (!PyList_CheckExact(outs) || PyList_GET_SIZE(outs) != PyList_GET_SIZE(list)))) return false;
-  const Py_ssize_t count = PyList_GET_SIZE(list);
-  if (count == 0) return false;
-  entries->reserve(static_cast<size_t>(count));
+// A list or tuple of plain contiguous tensors on the current device, as the C ABI takes it, held for the call (another thread may change
+// the list meanwhile); `outs`: another one (of their shapes) or None.
+struct Listed {
+  std::vector<at::Tensor> in, out;
+  std::vector<whtmix_tensor_t> entries;
   int device = -1;
-  for (Py_ssize_t i = 0; i < count; ++i) {
-    const at::Tensor* t = tensor(PyList_GET_ITEM(list, i));
-    if (!t || !t->is_cuda()) return false;
-    if (i == 0) {
-      device = t->get_device(), *first = t;
-      if (!current(device)) return false;
+  static bool plain(PyObject* o) { return PyList_CheckExact(o) || PyTuple_CheckExact(o); }
+  bool take(PyObject* list, PyObject* outs, bool scale) {
+    if (!plain(list) || (outs != Py_None && (!plain(outs) || PySequence_Fast_GET_SIZE(outs) != PySequence_Fast_GET_SIZE(list)))) return false;
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(list);
+    if (count == 0) return false;
+    in.reserve(static_cast<size_t>(count)), entries.reserve(static_cast<size_t>(count));
+    if (scale) out.reserve(static_cast<size_t>(count));
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const at::Tensor* t = tensor(PySequence_Fast_GET_ITEM(list, i));
+      if (!t || !t->is_cuda()) return false;
+      if (i == 0 && !current(device = t->get_device())) return false;
+      const at::ScalarType type = t->scalar_type();
+      if ((type != at::kFloat && type != at::kBFloat16) || !placed(*t, device, type) || !t->is_contiguous()) return false;
+      const at::Tensor* u = outs == Py_None ? nullptr : tensor(PySequence_Fast_GET_ITEM(outs, i));
+      if (outs != Py_None && (!u || !placed(*u, device, type) || u->sizes() != t->sizes() || !u->is_contiguous())) return false;
+      in.push_back(*t);
+      if (scale && u) out.push_back(*u);
     }
-    const at::ScalarType type = t->scalar_type();
-    if ((type != at::kFloat && type != at::kBFloat16) || !placed(*t, device, type) || !t->is_contiguous()) return false;
-    void* o = nullptr;
-    if (outs) {
-      const at::Tensor* u = tensor(PyList_GET_ITEM(outs, i));
-      if (!u || !placed(*u, device, type) || u->sizes() != t->sizes() || !u->is_contiguous()) return false;
-      o = u->data_ptr();
+    for (size_t i = 0; i < in.size(); ++i) {  // (nothing is allocated for a call that is not taken)
+      if (scale && outs == Py_None) out.push_back(empty(in[i].sizes(), in[i].scalar_type(), in[i]));
+      entries.push_back({in[i].data_ptr(), scale ? out[i].data_ptr() : nullptr, in[i].numel(), code(in[i].scalar_type())});
     }
-    entries->push_back({t->data_ptr(), o, t->numel(), code(type)});
+    return true;
   }
-  return true;
-}
+};
 
 // tensors
 PyObject* global_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  std::vector<whtmix_tensor_t> entries;
-  const at::Tensor* first;
-  if (n != 1 || !entries_of(args[0], nullptr, &entries, &first)) Py_RETURN_NONE;
-  const at::Tensor norm = empty({}, at::kFloat, *first);
+  Listed l;
+  if (n != 1 || !l.take(args[0], Py_None, false)) Py_RETURN_NONE;
+  const at::Tensor norm = empty({}, at::kFloat, l.in[0]);
   float* p = static_cast<float*>(norm.data_ptr());
-  if (!run("whtmix_global_norm", first->get_device(),
-           [&](void* stream) { return whtmix_global_norm(entries.data(), static_cast<int64_t>(entries.size()), p, stream); }))
+  if (!run("whtmix_global_norm", l.device,
+           [&](void* stream) { return whtmix_global_norm(l.entries.data(), static_cast<int64_t>(l.entries.size()), p, stream); }))
     return nullptr;
   return THPVariable_Wrap(norm);
   END_HANDLE_TH_ERRORS
@@ -399,40 +403,26 @@ PyObject* global_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // tensors, max_norm, out or None
 PyObject* clip_by_global_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  std::vector<whtmix_tensor_t> entries;
-  const at::Tensor* first;
-  if (n != 3 || !PyFloat_CheckExact(args[1]) || !entries_of(args[0], args[2] == Py_None ? nullptr : args[2], &entries, &first)) Py_RETURN_NONE;
-  PyObject* out = args[2];
-  if (out == Py_None) {
-    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
-    out = PyList_New(count);
-    if (!out) return nullptr;
-    for (Py_ssize_t i = 0; i < count; ++i) {
-      const at::Tensor& t = *tensor(PyList_GET_ITEM(args[0], i));
-      const at::Tensor o = empty(t.sizes(), t.scalar_type(), t);
-      entries[static_cast<size_t>(i)].out = o.data_ptr();
-      PyObject* w = THPVariable_Wrap(o);
-      if (!w) {
-        Py_DECREF(out);
-        return nullptr;
-      }
-      PyList_SET_ITEM(out, i, w);
-    }
-  } else {
-    Py_INCREF(out);
-  }
-  const at::Tensor norm = empty({}, at::kFloat, *first);
+  Listed l;
+  if (n != 3 || !PyFloat_CheckExact(args[1]) || !(PyFloat_AS_DOUBLE(args[1]) >= 0.0) || !l.take(args[0], args[2], true)) Py_RETURN_NONE;
+  const at::Tensor norm = empty({}, at::kFloat, l.in[0]);
   float* p = static_cast<float*>(norm.data_ptr());
   const float max_norm = static_cast<float>(PyFloat_AS_DOUBLE(args[1]));
-  PyObject* both = nullptr;
-  if (run("whtmix_clip_by_global_norm", first->get_device(), [&](void* stream) {
-        return whtmix_clip_by_global_norm(entries.data(), static_cast<int64_t>(entries.size()), max_norm, p, stream);
-      })) {
-    PyObject* w = THPVariable_Wrap(norm);
-    if (w) both = PyTuple_Pack(2, out, w);
-    Py_XDECREF(w);
+  if (!run("whtmix_clip_by_global_norm", l.device, [&](void* stream) {
+        return whtmix_clip_by_global_norm(l.entries.data(), static_cast<int64_t>(l.entries.size()), max_norm, p, stream);
+      }))
+    return nullptr;
+  const Py_ssize_t count = static_cast<Py_ssize_t>(l.out.size());
+  PyObject *list = PyList_New(count), *both = nullptr, *w = THPVariable_Wrap(norm);
+  bool ok = list && w;
+  for (Py_ssize_t i = 0; ok && i < count; ++i) {
+    PyObject* o = THPVariable_Wrap(l.out[static_cast<size_t>(i)]);
+    ok = o != nullptr;
+    if (ok) PyList_SET_ITEM(list, i, o);
   }
-  Py_DECREF(out);
+  if (ok) both = PyTuple_Pack(2, list, w);
+  Py_XDECREF(list);
+  Py_XDECREF(w);
   return both;
   END_HANDLE_TH_ERRORS
 }

@@ -906,12 +906,14 @@ def _norm_device(tensors) -> torch.device:
 
 def global_norm(tensors, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """sqrt(sum of all squares) of a list of float32 and bfloat16 tensors on one device, a float32 tensor without axes."""
-    tensors = list(tensors)
-    device = _norm_device(tensors)
+    if not isinstance(tensors, (list, tuple)):
+        tensors = list(tensors)
     if out is None and stream is None:
         done = (_quick or _quick_path()).global_norm(tensors)
         if done is not None:
             return done
+    tensors = list(tensors)
+    device = _norm_device(tensors)
     if stream is not None and out is None:
         with _on(stream, device):
             return global_norm(tensors)
@@ -925,6 +927,12 @@ def clip_by_global_norm(tensors, max_norm: float, out=None, norm: torch.Tensor |
     """(out, norm): each tensor of the list times min(1, max_norm / (norm + 1e-6)), norm = global_norm(tensors).
 
     out is a list of tensors like the given ones; with out=tensors they are scaled in place."""
+    if not isinstance(tensors, (list, tuple)):
+        tensors = list(tensors)
+    if norm is None and stream is None:
+        done = (_quick or _quick_path()).clip_by_global_norm(tensors, float(max_norm), out)
+        if done is not None:
+            return done
     tensors = list(tensors)
     device = _norm_device(tensors)
     if out is not None:
@@ -933,10 +941,6 @@ def clip_by_global_norm(tensors, max_norm: float, out=None, norm: torch.Tensor |
             raise ValueError(f"out must have a tensor for each of the {len(tensors)}, got {len(out)}")
     if not max_norm >= 0:
         raise ValueError(f"max_norm must not be negative, got {max_norm}")
-    if norm is None and stream is None:
-        done = (_quick or _quick_path()).clip_by_global_norm(tensors, float(max_norm), out)
-        if done is not None:
-            return done
     if stream is not None and (norm is None or out is None):
         with _on(stream, device):
             return clip_by_global_norm(tensors, max_norm, out, norm)

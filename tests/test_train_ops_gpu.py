@@ -909,3 +909,73 @@ def example():
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
     return m
+
+
+def hadamard(n):
+    h = torch.ones(1, 1, dtype=torch.float64, device="cuda")
+    while h.shape[0] < n:
+        h = torch.cat([torch.cat([h, h], 1), torch.cat([h, -h], 1)], 0)
+    return h
+
+
+def plain_layer(layer, x, params):
+    """The layer in float64, without any of the library."""
+    norm1, norm2, w_in, w_out, gains, w1, b1, w2, b2 = params[:9]
+    shift1, shift2 = params[9:] if layer.norm == "layer" else (0.0, 0.0)
+    N, C = gains.shape
+
+    def norm(v, g, b):
+        if layer.norm == "rms":
+            return v * torch.rsqrt(v.square().mean(-1, keepdim=True) + 1e-6) * g
+        return (v - v.mean(-1, keepdim=True)) * torch.rsqrt(v.var(-1, keepdim=True, unbiased=False) + EPS) * g + b
+
+    HN, HC = hadamard(N), hadamard(C)
+    z = norm(x, norm1, shift1) @ w_in.T
+    h = x + (HN @ (gains * (HN @ z @ HC)) @ HC / (N * C)) @ w_out.T
+    p = norm(h, norm2, shift2) @ w1.T + b1
+    if layer.gated:
+        hidden = w2.shape[1]
+        u = p[..., :hidden] * torch.sigmoid(p[..., :hidden]) * p[..., hidden:]
+    else:
+        u = phi(p, "gelu")[0]
+    return h + u @ w2.T + b2
+
+
+@pytest.mark.parametrize("norm,gated", [("layer", True), ("layer", False), ("rms", True)])
+@pytest.mark.parametrize("B,N,C", [(2, 256, 64), (1, 1024, 128)])
+def test_the_example_with_layer_norm_and_gated_half(example, norm, gated, B, N, C):
+    layer = example.MixerLayer(N, C, norm=norm, gated=gated)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    params = layer.parameters()
+    for p in params:
+        if p.dtype == F32:
+            p += 0.1 * torch.randn(p.shape, generator=g, device="cuda")
+    x, dy = torch.randn(B, N, C, generator=g, device="cuda").to(BF), torch.randn(B, N, C, generator=g, device="cuda").to(BF)
+    exact = [p.double().requires_grad_(True) for p in params]
+    xe = x.double().requires_grad_(True)
+    ye = plain_layer(layer, xe, exact)
+    (ye * dy.double()).sum().backward()
+    for p in params:
+        p.requires_grad_(True)
+    xr = x.clone().requires_grad_(True)
+    y = layer.train_forward(xr)
+    # about ten bf16 roundings of activations on the way, each 2^-8 of a value at most: the bf16 tolerance 1e-2 in the 2-norm
+    assert float((y.detach().double() - ye.detach()).norm() / ye.detach().norm()) <= 1e-2
+    (y.float() * dy.float()).sum().backward()
+    for got, want in zip([xr] + params, [xe] + exact):
+        assert float((got.grad.double() - want.grad).norm() / want.grad.norm()) <= 2e-2  # both ways' roundings together
+    grads = [p.grad.clone() for p in params]
+    n = norm_of(grads)
+    clipped, _ = whtmix.clip_by_global_norm([p.grad for p in params], 0.5 * n, out=[p.grad for p in params])
+    for p, before in zip(params, grads):
+        close(p.grad, before.double() * 0.5, rounded(before.double() * 0.5, 40 * U32 * before.double().abs(), p.dtype))
+        p.requires_grad_(False)
+    out = layer.forward(x)
+    assert torch.equal(out, y.detach())
+    layer.quantize()
+    # e4m3 rounds each activation and weight by 2^-5 of it on average at most: the first product's error is that, one half of y
+    assert float((layer.forward(x).double() - ye.detach()).norm() / ye.detach().norm()) <= 6e-2
+    losses = example.train(layer, x, dy.float(), 3, max_norm=1.0)
+    assert len(losses) == 3 and all(math.isfinite(v) for v in losses)
+    whtmix.sync()
