@@ -18,8 +18,9 @@ namespace linear {
 constexpr int GDP_THREADS = 512;
 template <int BN>
 struct GdpRing {
-  // ([65536, 128] to 344, two and three stages: 85.4 and 76.9 us.  At 256 columns W's way from L2 takes the room: two stages and three
-  // units of 32 KB 258 us where three stages and three units of 128 columns took 297, six of those 280)
+  // ([65536, 128] to 344, two and three stages: 85.4 and 76.9 us.  256 columns, [131072, 256] to 688: W's units of 32 KB leave room for
+  // two stages, 258 us; three stages and units of 16 KB 297; three stages, two units and dx stored from the registers 260; pairs of CTAs
+  // that share W, three stages 279)
   static constexpr int STAGES = BN == 256 ? 2 : 3, UNITS = 3;
   static constexpr uint32_t TILE = 128 * 128, STAGE = 3 * TILE, UNIT = BN * 128;
   static constexpr uint32_t W = STAGES * STAGE, PANEL = W + UNITS * UNIT;

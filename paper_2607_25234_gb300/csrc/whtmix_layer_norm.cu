@@ -461,15 +461,15 @@ __global__ void __launch_bounds__(32 * DWDB_RUNS) k_dwdb(const float* part, floa
   float sum = 0.f;
   if (e < n) {
     const float* q = part + e;
-    int p = p0;
-    for (; p + 8 <= p1; p += 8) {
-      float v[8];
+    for (int p = p0; p < p1; p += 16) {  // (the last ones too: a load at a time is the latency of each)
+      float v[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = __ldcg(q + static_cast<long long>(p + u) * 2 * D);
+      for (int u = 0; u < 16; ++u)
+        if (p + u < p1) v[u] = __ldcg(q + static_cast<long long>(p + u) * 2 * D);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum += v[u];
+      for (int u = 0; u < 16; ++u)
+        if (p + u < p1) sum += v[u];
     }
-    for (; p < p1; ++p) sum += __ldcg(q + static_cast<long long>(p) * 2 * D);
   }
   s[g][lane] = sum;
   __syncthreads();
@@ -493,10 +493,14 @@ constexpr int TILE_THREADS = 256, TILE_STAGES = 3;
 template <typename T>
 __host__ __device__ constexpr int tile_rows(int D) {
   const int bytes = D * static_cast<int>(sizeof(T));
-  return bytes <= 320 ? 32 : bytes <= 640 ? 16 : 8;
+  return bytes <= 320 ? 32 : bytes <= 640 ? 16 : 8;  // (64 rows up to 320 bytes: [64000, 77] float32 17.4 -> 25.5 us; 16: 18.9)
 }
 template <typename T>
 __host__ __device__ constexpr int tile_bytes(int D) { return tile_rows<T>(D) * D * static_cast<int>(sizeof(T)); }
+
+// Of a lane's NE elements the first SURE are inside every row that by_columns sends here (more than LANES SURE channels).
+template <int NE>
+constexpr int SURE = NE == 4 ? 0 : NE == 6 ? 4 : NE == 8 ? 6 : NE == 12 ? 8 : NE == 16 ? 12 : 16;
 
 // A contiguous matrix [T, D] that is copied tile by tile.  The last tile's bytes beyond whole 16-byte pieces go element by element.
 template <typename T>
@@ -602,7 +606,7 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
       float v[NE], sum[1] = {0.f};
 #pragma unroll
       for (int k = 0; k < NE; ++k) {
-        const bool in = lane + LANES * k < D;
+        const bool in = k < SURE<NE> || lane + LANES * k < D;
         v[k] = in ? Io<T>::get(xs, at + LANES * k) : 0.f;
         if (a.r && in) {
           v[k] += Io<T>::get(rs, at + LANES * k);
@@ -615,14 +619,14 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
       float sq[1] = {0.f};
 #pragma unroll
       for (int k = 0; k < NE; ++k) {
-        v[k] = lane + LANES * k < D ? v[k] - mean : 0.f;
+        v[k] = k < SURE<NE> || lane + LANES * k < D ? v[k] - mean : 0.f;
         sq[0] += v[k] * v[k];
       }
       lanes_join<LANES>(sq);
       const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
 #pragma unroll
       for (int k = 0; k < NE; ++k)
-        if (lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, v[k] * rstd * w[k] + b[k]);
+        if (k < SURE<NE> || lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, v[k] * rstd * w[k] + b[k]);
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
@@ -691,7 +695,7 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackwar
       float c[NE], d[NE], sum[1] = {0.f};
 #pragma unroll
       for (int k = 0; k < NE; ++k) {
-        const bool in = live && lane + LANES * k < D;
+        const bool in = live && (k < SURE<NE> || lane + LANES * k < D);
         c[k] = in ? Io<T>::get(hs, at + LANES * k) : 0.f;
         d[k] = in ? Io<T>::get(ds, at + LANES * k) : 0.f;
         sum[0] += c[k];
@@ -701,7 +705,7 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackwar
       float q[3] = {};  // sums of c^2, a, a c
 #pragma unroll
       for (int k = 0; k < NE; ++k) {
-        c[k] = lane + LANES * k < D ? c[k] - mean : 0.f;
+        c[k] = k < SURE<NE> || lane + LANES * k < D ? c[k] - mean : 0.f;
         const float g = d[k] * w[k];
         q[0] += c[k] * c[k];
         q[1] += g;
@@ -714,7 +718,7 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackwar
       for (int k = 0; k < NE; ++k) {
         acc_w[k] += d[k] * (c[k] * rstd);
         acc_b[k] += d[k];
-        if (live && lane + LANES * k < D)
+        if (live && (k < SURE<NE> || lane + LANES * k < D))
           Io<T>::put(ds, at + LANES * k, rstd * (d[k] * w[k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, at + LANES * k) : 0.f));
       }
     }

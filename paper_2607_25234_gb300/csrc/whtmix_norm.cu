@@ -308,15 +308,15 @@ __global__ void __launch_bounds__(32 * DW_RUNS) k_dw(const float* part, float* _
   const int p0 = parts * g / DW_RUNS, p1 = parts * (g + 1) / DW_RUNS;
   float sum = 0.f;
   if (e < D) {
-    int p = p0;
-    for (; p + 8 <= p1; p += 8) {
-      float v[8];
+    for (int p = p0; p < p1; p += 16) {  // (the last ones too: a load at a time is the latency of each)
+      float v[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = __ldcg(part + static_cast<long long>(p + u) * D + e);
+      for (int u = 0; u < 16; ++u)
+        if (p + u < p1) v[u] = __ldcg(part + static_cast<long long>(p + u) * D + e);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum += v[u];
+      for (int u = 0; u < 16; ++u)
+        if (p + u < p1) sum += v[u];
     }
-    for (; p < p1; ++p) sum += __ldcg(part + static_cast<long long>(p) * D + e);
   }
   s[g][lane] = sum;
   __syncthreads();
