@@ -22,6 +22,7 @@
 #include "whtmix_rows.cuh"
 #include "whtmix_tc.cuh"
 #include "whtmix_tma.cuh"
+#include "whtmix_unaligned.cuh"
 
 namespace whtmix {
 namespace norm {
@@ -62,11 +63,17 @@ __device__ __forceinline__ void row_join(float (&a)[N]) {
   }
 }
 
-// Whether element j of vector k is the row's.
+// c = h - mean for the elements of vector k, zero for those that are not the row's.
 template <typename R, bool AL>
-__device__ __forceinline__ bool mine(int lane, int k, int j, int off, int D) {
+__device__ __forceinline__ void center(float (&h)[R::V], float mean, int lane, int k, int off, int D) {
   const int e = R::at(lane, k) - off;
-  return AL ? e < D : e + j >= 0 && e + j < D;
+  if (AL ? e < D : e >= 0 && e + R::V <= D) {  // (a whole vector, nearly always)
+#pragma unroll
+    for (int j = 0; j < R::V; ++j) h[j] -= mean;
+  } else {
+#pragma unroll
+    for (int j = 0; j < R::V; ++j) h[j] = !AL && e + j >= 0 && e + j < D ? h[j] - mean : 0.f;
+  }
 }
 
 template <typename T, bool Q8, bool AL, int TPR, int NV>
@@ -126,12 +133,11 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, cons
     const float mean = sum[0] * inv_d;
     float sq[1] = {0.f};
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      center<R, AL>(h[k], mean, lane, k, off, a.D);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        h[k][j] = mine<R, AL>(lane, k, j, off, a.D) ? h[k][j] - mean : 0.f;
-        sq[0] += h[k][j] * h[k][j];
-      }
+      for (int j = 0; j < V; ++j) sq[0] += h[k][j] * h[k][j];
+    }
     row_join<TPR, 1, false>(sq);
     const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
     float top[1] = {0.f};
@@ -224,9 +230,13 @@ constexpr int LN_DEPTH = NV == 1 ? 4 : 2;
 
 // dx, and this CTA's partial row of dw and of db: part[blockIdx.x][0 .. 2 D).  Aligned rows: a thread's columns are the same in every
 // row, their sums stay in its registers.  Unaligned ones, and rows of more vectors than that leaves registers for: in shared memory,
-// two sets for each of the CTA's row groups (dynamic).
-template <typename T, bool AL, int TPR, int NV>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>, AL && TPR == 512 && NV == 1 ? 2 : 1) k_ln_bwd(const LayerBackward a, const Same same) {
+// two sets for each of the CTA's row groups (dynamic), or, where those would cost more than reading h and dy again, not here (SUMS): coef[t]
+// = mean and rstd for k_ln_columns.
+// (Odd rows on 256 threads are kept to 80 registers, three CTAs an SM: left alone they take 152, and one CTA an SM cannot hide what a row
+// waits for: [20000, 601] float32 167 -> 127 us.)
+template <typename T, bool AL, int TPR, int NV, bool SUMS>
+__global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 3 : AL && TPR == 512 && NV == 1 ? 2 : 1) k_ln_bwd(const LayerBackward a, const Same same, float2* coef) {
+  static_assert(SUMS || !AL, "the sums of aligned rows stay in registers");
   constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
   extern __shared__ __align__(16) float s_acc[];  // unaligned: a group's sums for dw, then for db; behind all groups' the gains.  Aligned: the rows
@@ -235,10 +245,10 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, AL && TPR == 512 && NV == 1 ? 2
   float acc_w[AL ? NV : 1][V] = {}, acc_b[AL ? NV : 1][V] = {};
   const int set = V * slots_of<V>(a.D);
   float *own_w = s_acc + (AL ? 0 : 2 * group * set), *own_b = own_w + (AL ? 0 : set);
-  if constexpr (!AL) {
+  if constexpr (!AL && SUMS) {
     for (int i = lane; i < 2 * set; i += TPR) own_w[i] = 0.f;
   }
-  float* s_w = s_acc + 2 * ROWS * set;
+  float* s_w = s_acc + (SUMS ? 2 * ROWS * set : 0);
   pdl_wait();
   if constexpr (!AL) {
     gains_to_shared<V, BLOCK>(s_w, a.w, a.D);
@@ -316,9 +326,9 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, AL && TPR == 512 && NV == 1 ? 2
     for (int k = 0; k < NV; ++k) {
       float w[V];
       kept.get(gains, places, lane, k, off, a.D, w);
+      center<R, AL>(h[k], mean, lane, k, off, a.D);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        h[k][j] = mine<R, AL>(lane, k, j, off, a.D) ? h[k][j] - mean : 0.f;
         const float g = d[k][j] * w[j];
         s[0] += h[k][j] * h[k][j];
         s[1] += g;
@@ -340,14 +350,19 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, AL && TPR == 512 && NV == 1 ? 2
         if constexpr (AL) {
           acc_w[k][j] += g;
           acc_b[k][j] += d[k][j];
-        } else if (R::at(lane, k) - off < D) {
+        } else if (SUMS && R::at(lane, k) - off < D) {
           own_w[places.at[j] + lane + TPR * k] += g;
           own_b[places.at[j] + lane + TPR * k] += d[k][j];
         }
         o[j] += rstd * (d[k][j] * w[j] - ma - q * h[k][j]);
       }
-      R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o);
+      if (SUMS || a.dx) R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o);
     }
+    if (!SUMS && lane == 0 && t < a.T) coef[t] = make_float2(mean, rstd);
+  }
+  if constexpr (!SUMS) {
+    pdl_trigger();
+    return;
   }
   if constexpr (AL) asm volatile("cp.async.wait_all;" ::: "memory");
   // the CTA's row groups hold the same columns: added in ascending group order
@@ -396,7 +411,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, AL && TPR == 512 && NV == 1 ? 2
   pdl_trigger();
 }
 
-// Rows too long for the registers: dx (DX) by a CTA a row; coef[t] = mean and rstd for k_dwdb_long.
+// Rows too long for the registers: dx (DX) by a CTA a row; coef[t] = mean and rstd for k_ln_columns.
 template <typename T, bool DX>
 __global__ void __launch_bounds__(LONG_THREADS) k_ln_bwd_long(const LayerBackward a, float2* __restrict__ coef) {
   pdl_wait();
@@ -430,22 +445,43 @@ __global__ void __launch_bounds__(LONG_THREADS) k_ln_bwd_long(const LayerBackwar
   }
   pdl_trigger();
 }
-// part[blockIdx.y][e], [D + e] = sums over the rows of chunk blockIdx.y of dy n and dy
+// part[blockIdx.y][e], [D + e] = sums over the rows of chunk blockIdx.y of dy n and dy.  A CTA takes a strip of 32 vectors, a thread the V
+// columns of one in every eighth row of the chunk, wherever the rows start.
+constexpr int COLUMN_THREADS = 256, COLUMN_CTAS = 3;
 template <typename T>
-__global__ void __launch_bounds__(256) k_dwdb_long(const LayerBackward a, const float2* coef, int chunks) {
-  pdl_wait();
-  const int e = blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(COLUMN_THREADS, COLUMN_CTAS) k_ln_columns(const LayerBackward a, const float2* coef, int chunks) {
+  constexpr int V = Io<T>::V, G = COLUMN_THREADS / 32;  // rows at a time
+  __shared__ float s[2][G][32][V + 1];
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c0 = (blockIdx.x * 32 + lane) * V;
   const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
-  if (e < a.D) {
-    float dw = 0.f, db = 0.f;
-    for (long long t = t0; t < t1; ++t) {
-      const float g = Io<T>::get(static_cast<const T*>(a.dy) + t * a.ys, e);
-      const float2 c = coef[t];
-      dw += g * ((Io<T>::get(static_cast<const T*>(a.h) + t * a.hs, e) - c.x) * c.y);
-      db += g;
+  const int left = min(16, (a.D - c0) * static_cast<int>(sizeof(T)));  // bytes of the vector that are the row's
+  pdl_wait();
+  const Span sh = span_of(a.h, a.T, a.hs, a.D, sizeof(T)), sd = span_of(a.dy, a.T, a.ys, a.D, sizeof(T));
+  float dw[V] = {}, db[V] = {};
+  for (long long t = t0 + g; t < t1 && left > 0; t += G) {
+    const uint8_t *hp = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.h) + t * a.hs + c0),
+                  *dp = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.dy) + t * a.ys + c0);
+    const Granules uh = fetch16(hp, sh), ud = fetch16(dp, sd);
+    const float2 c = coef[t];
+    float h[V], d[V];
+    Io<T>::unpack(finish16(uh, hp, sh), h);
+    Io<T>::unpack(keep(finish16(ud, dp, sd), left), d);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (c0 + j < a.D) dw[j] += d[j] * ((h[j] - c.x) * c.y);
+      db[j] += d[j];
     }
-    float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.y) * 2 * a.D;
-    part[e] = dw, part[a.D + e] = db;
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) s[0][g][lane][j] = dw[j], s[1][g][lane][j] = db[j];
+  __syncthreads();
+  float* part = static_cast<float*>(a.ws) + static_cast<long long>(blockIdx.y) * 2 * a.D;
+  for (int i = threadIdx.x; i < 2 * 32 * V; i += COLUMN_THREADS) {
+    const int which = i / (32 * V), l = i % (32 * V) / V, j = i % V, e = blockIdx.x * 32 * V + l * V + j;
+    float sum = s[which][0][l][j];
+#pragma unroll
+    for (int k = 1; k < G; ++k) sum += s[which][k][l][j];
+    if (e < a.D) part[which * a.D + e] = sum;
   }
   pdl_trigger();
 }
@@ -834,7 +870,27 @@ cudaError_t layer_forward(const LayerForward& a, bool bf16, bool to_e4m3, unsign
   return to_e4m3 ? forward_t<float, true>(a, err, sms, stream) : forward_t<float, false>(a, err, sms, stream);
 }
 
-static int long_parts(long long T) { return static_cast<int>(T < 64 ? T : 64); }
+// Chunks of rows of k_ln_columns: one wave, eight rows each at least.
+template <typename T>
+static int column_chunks(const LayerBackward& a, int sms) {
+  const long long strips = (a.D + 32 * Io<T>::V - 1) / (32 * Io<T>::V), rows = (a.T + 7) / 8;
+  long long most = (static_cast<long long>(COLUMN_CTAS) * sms + strips - 1) / strips;
+  if (most > 256) most = 256;
+  return static_cast<int>(rows < most ? rows : most);
+}
+template <typename T>
+static cudaError_t columns(const LayerBackward& a, float2* coef, int chunks, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((a.D + 32 * Io<T>::V - 1) / (32 * Io<T>::V)), static_cast<unsigned>(chunks));
+  cfg.blockDim = dim3(COLUMN_THREADS);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_ln_columns<T>, a, static_cast<const float2*>(coef), chunks);
+}
 
 // How a backward call's rows are taken: aligned with the sums in registers up to MAX_SUMMED vectors (512 threads have 128 registers each),
 // else as unaligned ones.  (1024 threads with one vector each: [11870, 4696] bf16 148 -> 230 us.)
@@ -843,13 +899,17 @@ constexpr int MAX_SUMMED = sizeof(T) == 4 ? 2048 : 1024;
 struct LayerRows {
   bool al;
   int n;  // vectors
+  bool apart;  // the sums by k_ln_columns
 };
 template <typename T>
 static LayerRows layer_rows(const LayerBackward& a) {
   const size_t es = sizeof(T);
   const bool al = a.D % Io<T>::V == 0 && aligned(a.w, 16) && rows_aligned(a.h, a.hs, es) && rows_aligned(a.dy, a.ys, es) &&
                   rows_aligned(a.dh, a.ds, es) && rows_aligned(a.dx, a.xs, es) && vectors(a.D, es == 2, true) <= MAX_SUMMED<T>;
-  return {al, vectors(a.D, es == 2, al)};
+  const int n = vectors(a.D, es == 2, al);
+  // Odd rows of more than 64 vectors and enough of them: [5000, 1001] bf16 31.1 -> 25.2 us; of more than 512 it does not pay
+  // ([12856, 5565] 362 -> 399).
+  return {al, n, n > MAX_VECTORS || (!al && n > 64 && n <= 512 && a.T * a.D >= 1ll << 20)};
 }
 
 // A call's kernel, its shared memory and its CTAs, each of which leaves a partial row of dw and db.
@@ -881,12 +941,15 @@ static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, BLOCK = BLOCK_OF<TPR>;
     constexpr bool ALIGNED = NV * TPR <= MAX_SUMMED<T>, ODD = TPR != 192 && TPR != 384;
     if (rows.al) {
-      if constexpr (ALIGNED) p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, true, TPR, NV>);
-    } else {
-      if constexpr (ODD) p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV>);
+      if constexpr (ALIGNED) p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, true, TPR, NV, true>);
+    } else if constexpr (ODD) {
+      p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV, true>);
+      if constexpr (TPR * NV > 64 && TPR * NV <= 512) {
+        if (rows.apart) p->kernel = reinterpret_cast<const void*>(k_ln_bwd<T, false, TPR, NV, false>);
+      }
     }
     p->smem = rows.al ? static_cast<size_t>(LN_DEPTH<BLOCK, NV>) * 3 * NV * BLOCK * 16  // at most 192 KB
-                      : static_cast<size_t>(2 * (BLOCK / TPR) + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 193 KB
+                      : static_cast<size_t>(rows.apart ? 1 : 2 * (BLOCK / TPR) + 1) * Io<T>::V * slots_of<Io<T>::V>(a.D) * 4;  // at most 193 KB
     p->block = BLOCK;
     int resident = 0;
     const cudaError_t e = resident_ctas(p->kernel, BLOCK, p->smem, sms, &resident);
@@ -903,14 +966,14 @@ static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int
 template <typename T>
 static cudaError_t workspace_t(const LayerBackward& a, int sms, size_t* bytes) {
   const LayerRows rows = layer_rows<T>(a);
-  if (rows.n > MAX_VECTORS) {
-    *bytes = static_cast<size_t>(long_parts(a.T)) * 2 * a.D * 4 + static_cast<size_t>(a.T) * 8;
-    return cudaSuccess;
+  LayerPlan p{};
+  if (rows.n <= MAX_VECTORS) {
+    const cudaError_t e = layer_plan<T>(a, rows, sms, &p);
+    if (e != cudaSuccess) return e;
   }
-  LayerPlan p;
-  const cudaError_t e = layer_plan<T>(a, rows, sms, &p);
-  if (e == cudaSuccess) *bytes = static_cast<size_t>(p.parts) * 2 * a.D * 4;
-  return e;
+  const bool apart = rows.apart && !p.tiles;
+  *bytes = static_cast<size_t>(apart ? column_chunks<T>(a, sms) : p.parts) * 2 * a.D * 4 + (apart ? static_cast<size_t>(a.T) * 8 : 0);
+  return cudaSuccess;
 }
 cudaError_t layer_backward_workspace(const LayerBackward& a, bool bf16, int sms, size_t* bytes) {
   return bf16 ? workspace_t<__nv_bfloat16>(a, sms, bytes) : workspace_t<float>(a, sms, bytes);
@@ -920,27 +983,32 @@ template <typename T>
 static cudaError_t backward_t(const LayerBackward& a, unsigned int* err, int sms, cudaStream_t stream) {
   const size_t es = sizeof(T);
   const LayerRows rows = layer_rows<T>(a);
-  int parts = long_parts(a.T);
   LayerBackward c = a;
-  cudaError_t e;
+  LayerPlan p{};
+  cudaError_t e = cudaSuccess;
+  if (rows.n <= MAX_VECTORS && (e = layer_plan<T>(a, rows, sms, &p)) != cudaSuccess) return e;
+  const bool apart = rows.apart && !p.tiles;
+  int parts = apart ? column_chunks<T>(a, sms) : p.parts;
+  float2* coef = apart ? reinterpret_cast<float2*>(static_cast<float*>(a.ws) + static_cast<size_t>(parts) * 2 * a.D) : nullptr;
   if (rows.n > MAX_VECTORS) {
-    float2* coef = reinterpret_cast<float2*>(static_cast<float*>(a.ws) + static_cast<size_t>(parts) * 2 * a.D);
     // dw reads dy: where dx takes dy's place, the coefficients alone come first and dx last
     const bool over_dy = a.dx == a.dy;
     const void *with_dx = reinterpret_cast<const void*>(k_ln_bwd_long<T, true>), *without = reinterpret_cast<const void*>(k_ln_bwd_long<T, false>);
     void* args[] = {&c, &coef};
     auto take = [&](const void* k) { return launch_pdl(k, grid_rows(a.T, 1, 4 * sms), LONG_THREADS, 0, stream, args); };
     if ((e = take(over_dy ? without : with_dx)) != cudaSuccess) return e;
-    k_dwdb_long<T><<<dim3((a.D + 255) / 256, parts), 256, 0, stream>>>(c, coef, parts);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = columns<T>(a, coef, parts, stream)) != cudaSuccess) return e;
     if (over_dy) e = take(with_dx);
   } else {
     Same same{rows_same(a.h, a.hs, a.dy, a.ys, es), rows_same(a.h, a.hs, a.dh, a.ds, es), rows_same(a.h, a.hs, a.dx, a.xs, es)};
-    LayerPlan p;
-    if ((e = layer_plan<T>(a, rows, sms, &p)) != cudaSuccess) return e;
-    parts = p.parts;
-    void *args[] = {&c, &same}, *tile_args[] = {&c, &err};
-    e = launch_pdl(p.kernel, static_cast<unsigned>(parts), p.block, p.smem, stream, p.tiles ? tile_args : args);
+    void *args[] = {&c, &same, &coef}, *tile_args[] = {&c, &err};
+    auto take = [&] { return launch_pdl(p.kernel, static_cast<unsigned>(p.parts), p.block, p.smem, stream, p.tiles ? tile_args : args); };
+    // (dw reads dy, as above)
+    const bool over_dy = apart && a.dx == a.dy;
+    if (over_dy) c.dx = nullptr;
+    e = take();
+    if (e == cudaSuccess && apart) e = columns<T>(a, coef, parts, stream);
+    if (e == cudaSuccess && over_dy) c.dx = a.dx, e = take();
   }
   if (e != cudaSuccess) return e;
   const float* part = static_cast<const float*>(a.ws);
