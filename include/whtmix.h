@@ -232,8 +232,7 @@ WHTMIX_API int whtmix_block_backward(const void *x, const void *w_in, const void
 /* ---- The layer around the mixer ----
  * A transformer layer is h = x + block(norm(x)), y = h + W2 act(W1 norm(h) + b1) + b2 (Section III-B: the block is linear and
  * the feed-forward half supplies the nonlinearity).  The calls below are its norms, its products and, last, the clipping of its
- * gradients.  They take rows: T
- * tokens of D, K or N channels, channels contiguous, `*_stride` elements from one row to the next (at least a row's length;
+ * gradients.  They take rows: T tokens of D, K or N channels, channels contiguous, `*_stride` elements from one row to the next (at least a row's length;
  * of no meaning where T <= 1).  T >= 0; channels from 1 to 2^24; T < 2^31 - 256 and every matrix at most 2^40 elements
  * (WHTMIX_ERR_BAD_SHAPE).  Any size and any alignment of the element type runs (WHTMIX_ERR_MISALIGNED below that); 16-byte
  * aligned rows are the fast ones.  An output may share no address range with an input or another output, except where stated.
@@ -295,7 +294,8 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w, const void *
  *     h = x + residual,    y = (h - mean(h)) w / sqrt(mean((h - mean(h))^2) + eps) + b
  * Arguments, types and overlaps as whtmix_rms_norm's, and
  *   b            [D] float32 shifts, or NULL
- * y is computed from the unrounded sum.  A row with an infinity or a NaN yields NaN (and a NaN scale); a row of equal values yields b.
+ * y is computed from the unrounded sum.  A row with an infinity or a NaN yields NaN (and a NaN scale); a row of equal values yields
+ * b (eps > 0), up to the rounding of its mean.
  * WHTMIX_E4M3: a row whose y is all zero has scale 0 and values 0. */
 WHTMIX_API int whtmix_layer_norm(const void *x, const void *residual, const float *w, const float *b, void *h, void *y,
                                  float *y_scale, int64_t T, int64_t D, int64_t x_stride, int64_t residual_stride,
@@ -305,8 +305,8 @@ WHTMIX_API int whtmix_layer_norm(const void *x, const void *residual, const floa
  *     dx = r (a - mean(a) - n mean(a n)) + dh,     dw = sum over the rows of dy n,     db = sum over the rows of dy
  * Arguments as whtmix_rms_norm_backward's, and
  *   db         [D] float32, overwritten; or NULL
- * Two launches (for rows beyond the registers three, four if dx is dy).  What a stream that is being captured needs in between
- * belongs to the graph; so it is with the four calls below. */
+ * Two launches (three for rows beyond the registers and for many rows of which some are not 16-byte aligned, four there if dx is
+ * dy).  What a stream that is being captured needs in between belongs to the graph; so it is with the four calls below. */
 WHTMIX_API int whtmix_layer_norm_backward(const void *h, const float *w, const void *dy, const void *dh, void *dx, float *dw,
                                           float *db, int64_t T, int64_t D, int64_t h_stride, int64_t dy_stride,
                                           int64_t dh_stride, int64_t dx_stride, float eps, int dtype, void *stream);
@@ -332,7 +332,8 @@ WHTMIX_API int whtmix_gated_linear(const void *x, const void *w, const float *x_
  *   dx         [T, K] bf16, or NULL
  *   dw         [2 N, K] contiguous, of dw_dtype WHTMIX_BF16 or WHTMIX_F32, overwritten; or NULL
  *   db         [2 N] float32, overwritten; or NULL
- * dp is rounded to bf16 for the two products; db sums it unrounded.  Two to six launches. */
+ * dp is rounded to bf16 for the two products; db sums it unrounded.  One
+ * to seven launches. */
 WHTMIX_API int whtmix_gated_linear_backward(const void *x, const void *w, const void *dy, const void *preact, void *dx, void *dw,
                                             float *db, int64_t T, int64_t N, int64_t K, int64_t x_stride, int64_t w_stride,
                                             int64_t dy_stride, int64_t preact_stride, int64_t dx_stride, int act, int dw_dtype,
@@ -351,9 +352,11 @@ typedef struct {
  *   tensors    `count` entries in HOST memory, read during the call; count from 0 (norm = 0) to 2^20
  *   norm       one float32 on the device; whtmix_clip_by_global_norm: or NULL
  *   max_norm   >= 0
- * The sum is float64; every finite list has its norm, whatever its values' size (`norm` is its float32: infinite beyond 3.4e38, where
- * the factor is still right).  The factor is rounded to float32, its products to the tensor's type.  An infinity makes the norm infinite and the factor 0 (max_norm finite), a NaN makes both
- * NaN: what comes out then is not to be used.  Two launches for up to 64 tensors, two for every 480 beyond. */
+ * Squares are float32 and added 16 at a time, those sums as if in float64; every finite list has its norm, whatever its values' size (`norm` is its
+ * float32: infinite beyond 3.4e38, where the factor is still right).  The factor is rounded to float32, its products to the tensor's
+ * type.  An infinity makes the norm infinite and the factor 0 (max_norm finite), a NaN makes both NaN: what comes out then is not to
+ * be used.  One launch for lists of up to 24 pieces of 16 KB, two for up to 64 tensors, two for every 480 of longer lists, one more
+ * for very long ones. */
 WHTMIX_API int whtmix_global_norm(const whtmix_tensor_t *tensors, int64_t count, float *norm, void *stream);
 WHTMIX_API int whtmix_clip_by_global_norm(const whtmix_tensor_t *tensors, int64_t count, float max_norm, float *norm, void *stream);
 
@@ -362,8 +365,8 @@ WHTMIX_API int whtmix_clip_by_global_norm(const whtmix_tensor_t *tensors, int64_
  * then resets that workspace's barrier), WHTMIX_ERR_CUDA if the synchronisation itself failed,
  * WHTMIX_OK otherwise.  Checked: the library-managed workspace of `stream` and, on the current
  * device, the fixed scratch of whtmix_forward_noalloc (pass the stream those calls used, so that
- * they have finished) and the error word of the gated products.  Caller-owned _ex workspaces are the caller's to read (error word at byte
- * offset 8). */
+ * they have finished) and the error word of the gated products and the layer norms.  Caller-owned _ex workspaces are the caller's
+ * to read (error word at byte offset 8). */
 WHTMIX_API int whtmix_sync(void *stream);
 
 /* Frees every library-managed workspace on the current device (synchronises the device). */

@@ -912,8 +912,8 @@ int Scratch::take(int dev, cudaStream_t stream, size_t bytes) {
   cudaError_t e = cudaStreamIsCapturing(stream, &status);
   if (e != cudaSuccess) return cuda_fail(e);
   stream_ = stream;
-  captured_ = status != cudaStreamCaptureStatusNone;
-  if (captured_) {
+  own_ = status != cudaStreamCaptureStatusNone || stream == cudaStreamPerThread;
+  if (own_) {
     e = cudaMallocAsync(&p_, bytes, stream);
     return e == cudaSuccess ? WHTMIX_OK : cuda_fail(e);
   }
@@ -924,7 +924,7 @@ int Scratch::give_back() {
   void* p = p_;
   p_ = nullptr;
   if (turn_.owns_lock()) turn_.unlock();
-  if (!p || !captured_) return WHTMIX_OK;
+  if (!p || !own_) return WHTMIX_OK;
   const cudaError_t e = cudaFreeAsync(p, stream_);
   return e == cudaSuccess ? WHTMIX_OK : cuda_fail(e);
 }
@@ -1160,7 +1160,7 @@ int whtmix_sync(void* stream_v) {
     if (it != g_ws.end()) ptrs[0] = it->second.ptr;
   }
   // the stream's library-managed workspace, then this device's no-allocation scratch and the headers of the
-  // one-plane-per-CTA kernels and of the gated products (all keep a set error word until it is reported here)
+  // one-plane-per-CTA kernels and of the gated products and layer norms (all keep a set error word until it is reported here)
   int rc = WHTMIX_OK;
   for (void* ptr : ptrs) {
     if (!ptr) continue;

@@ -16,8 +16,9 @@ int workspace(int dev, cudaStream_t stream, size_t bytes, int slot, void** out);
 int error_word(int dev, unsigned int** err);
 
 // The scratch of one call.  On a stream that is being captured it is allocated and freed by nodes of the graph, so that no other
-// graph, no later call and no growing workspace shares or ends it.  Elsewhere it is the stream's workspace of slot 2, and calls of
-// several host threads on one stream are let through one after another, whole.
+// graph, no later call and no growing workspace shares or ends it; on the per-thread default stream, one handle for a stream of each host
+// thread, it is allocated and freed on that stream.  Elsewhere it is the stream's workspace of slot 2, and calls of several host threads on
+// one stream are let through one after another, whole.
 class Scratch {
  public:
   Scratch() = default;
@@ -31,7 +32,7 @@ class Scratch {
  private:
   void* p_ = nullptr;
   cudaStream_t stream_ = nullptr;
-  bool captured_ = false;
+  bool own_ = false;  // allocated for this call
   std::unique_lock<std::mutex> turn_;
 };
 

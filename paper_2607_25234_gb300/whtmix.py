@@ -929,8 +929,9 @@ def clip_by_global_norm(tensors, max_norm: float, out=None, norm: torch.Tensor |
     out is a list of tensors like the given ones; with out=tensors they are scaled in place."""
     if not isinstance(tensors, (list, tuple)):
         tensors = list(tensors)
+    max_norm = float(max_norm)
     if norm is None and stream is None:
-        done = (_quick or _quick_path()).clip_by_global_norm(tensors, float(max_norm), out)
+        done = (_quick or _quick_path()).clip_by_global_norm(tensors, max_norm, out)
         if done is not None:
             return done
     tensors = list(tensors)

@@ -813,6 +813,65 @@ def test_two_threads_on_one_stream():
     assert not wrong
 
 
+def test_two_threads_on_their_default_streams():
+    """cudaStreamPerThread is one handle (2) for a stream of each host thread: their calls run at the same time."""
+    import ctypes
+    import threading
+    lib = whtmix.library()
+    cases = []
+    for i, T in enumerate((4000, 5000)):
+        h, w, dy = rand(i, T, 130).to(BF), 1 + 0.1 * rand(9, 130), rand(10 + i, T, 130).to(BF)
+        cases.append((h, w, dy, whtmix.layer_norm_backward(h, w, dy), [torch.empty_like(h), torch.empty_like(w), torch.empty_like(w)]))
+    torch.cuda.synchronize()
+    codes = []
+
+    def work(case):
+        h, w, dy, _, (dx, dw, db) = case
+        torch.cuda.set_device(0)
+        for _ in range(100):
+            codes.append(lib.whtmix_layer_norm_backward(h.data_ptr(), w.data_ptr(), dy.data_ptr(), None, dx.data_ptr(), dw.data_ptr(), db.data_ptr(),
+                                                        *h.shape, 130, 130, 0, 130, 1e-5, 1, ctypes.c_void_p(2)))
+
+    threads = [threading.Thread(target=work, args=(c,)) for c in cases]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert codes == [0] * 200
+    for case in cases:
+        assert all(torch.equal(a, b) for a, b in zip(case[4], case[3]))
+
+
+FIRST_CALLS_IN_A_GRAPH = """
+import torch
+from paper_2607_25234_gb300 import whtmix
+x, w = torch.randn(5000, 77, device="cuda"), torch.ones(77, device="cuda")
+xb, wb = torch.randn(3000, 100, device="cuda").bfloat16(), torch.randn(120, 100, device="cuda").bfloat16()
+def calls():
+    dx = whtmix.layer_norm_backward(x, w, x)
+    y, p = whtmix.gated_linear(xb, wb, preact=True)
+    return [whtmix.layer_norm(x, w), *dx, y, p, *whtmix.gated_linear_backward(xb, wb, y, p), whtmix.global_norm([x, w])]
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = calls()
+g.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, calls()))
+whtmix.sync()
+print("the same")
+"""
+
+
+def test_a_processs_first_calls_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS_IN_A_GRAPH], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                          capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "the same" in done.stdout, done.stderr[-2000:]
+
+
 def test_a_backward_pass_in_a_graph():
     """Forward and backward captured after eager passes of the same leaves on another stream (whose autograd graphs are gone: torch joins
     the leaves' streams of a live one, which no capture allows, whatever the operators)."""

@@ -217,6 +217,20 @@ def test_copies_and_products_in_flight_are_waited_for_whichever_wait_gave_up():
     assert waits_before_it_ends(text)
 
 
+def test_the_fused_backwards_copies_and_products_are_waited_for():
+    """Its three rings: the inputs' and W's copies by their own barriers, the products by their accumulators', dp's way out by its group."""
+    text = dict(functions(read("whtmix_gemm_gated_dp.cu")))["k_dx_gated"]
+    for name, first, last in (("full", "if (warp == 0) {\n    if (lane", "else if (warp == 2)"), ("wfull", "else if (warp == 2)", "else if (warp == 1)"),
+                              ("dfull", "else if (warp == 1)", "else if (warp == 3)")):
+        part = text[text.index(first):text.index(last)]
+        tail = part[part.rindex("for (uint32_t j ="):]
+        assert re.search(r"j < (it|i); \+\+j\)\s*if \(!tma::wait\(&bars\.%s\[" % name, tail), name
+        assert tail.count("bad") == 1  # (waited for whichever wait gave up)
+    part = text[text.index("else if (warp == 3)"):text.index("else if (warp >= 8)")]
+    assert part.rindex("tma::wait_done();") > part.rindex("tma::store_2d(")
+    assert text.index("bars.dempty[d]", text.index("else if (warp >= 4)")) > 0 and text.rindex("tmem_dealloc") > text.rindex("__syncthreads")
+
+
 def test_tables_of_tensors_fit_a_kernels_parameters():
     """An entry is 32 bytes (two pointers, a size, a chunk); 32,764 bytes is the most a launch can pass."""
     text = read("whtmix_clip.cu")
