@@ -146,10 +146,11 @@ static GatedForwardPlan plan_forward(const Forward& a) {
 // axis, which the tiled products would walk along on their own.  The tiled products and those, us, bf16, K and N: 32 tokens 1024, 8192
 // 9.5 and 9.9; 64 tokens 1024, 2736 8.4 and 9.3, 4096, 4096 23.7 and 18.6, 4096, 8192 26.5 and 30.2; 100 tokens 2048, 5464 14.6 and 22.6;
 // 171 tokens 7448, 1176 44.7 and 27.5; 500 tokens 2048, 144 13.3 and 9.2, 7448, 1176 45.0 and 55.4; 3200 tokens 4096, 64 23.2 and 15.2,
-// 2048, 144 13.8 and 28.9.
+// 2048, 144 13.8 and 28.9.  Beyond three tiles for four SMs the tiled products fill the SMs on their own: 512 tokens 32768, 1600 157.0 and 117.1;
+// 1024 tokens 16384, 1024 81.7 and 100.6; 128 tokens 16384, 8192 98.8 and 113.7.
 static bool few_tokens(long long T, int N, int kblocks, int sms) {
   const long long tiles = static_cast<long long>(ceil_div(N, 64)) * ceil_div(T, 128);
-  return T <= 32 || (T <= 64 && kblocks >= 32 && 4 * tiles <= 2ll * sms) || 5 * tiles <= 3ll * kblocks;
+  return T <= 32 || (T <= 64 && kblocks >= 32 && 4 * tiles <= 2ll * sms) || (5 * tiles <= 3ll * kblocks && 4 * tiles <= 3ll * sms);
 }
 
 // Four epilogue groups instead of two, at the price of a shorter ring, where the epilogue is longer than a tile's products.  Two and
