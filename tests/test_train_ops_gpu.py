@@ -539,6 +539,13 @@ def test_gated_backward_of_many_tokens(T, N, K, act):
     check_gated_backward(T, N, K, act, need_dx=False, need_db=False)
 
 
+@pytest.mark.parametrize("T,N,K", [(9601, 64, 40), (9700, 8, 256), (9729, 6400, 64), (10001, 136, 129), (20000, 1000, 100), (9601, 9728, 8)])
+def test_gated_backward_of_many_tokens_and_its_weight_gradient(T, N, K):
+    check_gated_backward(T, N, K, "silu")
+    check_gated_backward(T, N, K, "gelu", dw_dtype=F32, need_db=False)
+    check_gated_backward(T, N, K, "relu", need_dw=False)
+
+
 def test_gated_gradients_by_differences():
     """Against central differences of the float64 definition, through autograd; values that bf16 holds, small sizes."""
     T, N, K = 4, 12, 24
