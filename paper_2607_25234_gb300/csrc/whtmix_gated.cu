@@ -209,8 +209,14 @@ cudaError_t gated_forward(const Forward& a, void* ws, unsigned int* err, int sms
   return a.e4m3 ? gemm_gated_e4m3(g, a.out_f32, pl.bn, four, sms, stream) : gemm_gated(g, a.out_f32, pl.bn, four, sms, stream);
 }
 
-// Threads a row of k_gated_dp, eight channels each.
-static int dp_lanes(int N) { return N <= 64 ? 8 : N <= 128 ? 16 : 32; }
+// Threads a row of k_gated_dp, eight channels each: 32 unless they would be idle in a third of the last strip's places, and eight where one
+// CTA a strip takes all rows.  32 and 8, dp alone, us: [128224, 150] 104.2 and 81.4, [60000, 176] 25.3 and 22.3, [3001, 301] 9.3 and
+// 8.1, but [20000, 601] 58.1 and 75.9, [3001, 777] 15.1 and 18.2; [128, 1408] in one chunk 12.0 and 4.7, [64, 149] 14.6 and 6.2.
+static int dp_lanes(long long T, int N) {
+  if (N <= 64 || T <= 128) return 8;
+  if (N <= 128) return 16;
+  return 3 * ceil_div(N, 256) * 256 >= 4 * ceil_div(N, 64) * 64 ? 8 : 32;
+}
 
 // dp and db's partial sums (fused: and dx), then the linear layer's products of them with W and x.
 struct GatedBackwardPlan {
@@ -246,7 +252,7 @@ static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
     b.pad_w = !tma::mappable(a.w, 2ll * a.N, a.ws, 2);
     if (b.pad_w) b.w_off = take(static_cast<size_t>(2ll * a.N) * pitch_of(a.K, 2) * 2);
   } else {
-    const int strips = ceil_div(a.N, 8 * dp_lanes(a.N)), rows = ceil_div(a.T, 512 / dp_lanes(a.N)), most = (DP_CTAS * sms + strips - 1) / strips;  // one wave
+    const int tx = dp_lanes(a.T, a.N), strips = ceil_div(a.N, 8 * tx), rows = ceil_div(a.T, 512 / tx), most = (DP_CTAS * sms + strips - 1) / strips;  // one wave
     b.chunks = rows < most ? rows : most;
     if (b.chunks > 65535) b.chunks = 65535;
     if (a.T <= 128) b.chunks = 1;  // db comes whole from one CTA a strip: a launch less
@@ -298,7 +304,7 @@ cudaError_t gated_backward(const Backward& a, void* ws, unsigned int* err, int s
     long long np = b.np;
     const bool al = a.N % 8 == 0 && tma::mappable(a.dy, a.T, a.dys, 2) && tma::mappable(a.p, a.T, a.ps, 2);
     cudaLaunchConfig_t cfg = {};
-    const int tx = dp_lanes(a.N);
+    const int tx = dp_lanes(a.T, a.N);
     cfg.gridDim = dim3(ceil_div(a.N, 8 * tx), chunks);
     cfg.blockDim = dim3(THREADS_256);
     cfg.stream = stream;
