@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "whtmix_few.cuh"
@@ -18,27 +19,82 @@ namespace linear {
 
 constexpr int THREADS_256 = 256;
 
-// CTAs of k_gated_dp an SM.  One row in flight and three CTAs against two rows and two CTAs, whole backward, us: [65536, 512] to 1408
-// 398 and 508, [8192, 1024] to 2736 211 and 215, to 2733 263 and 391; four CTAs 455, 205, 260 (registers spill).
+// CTAs of k_gated_dp an SM.  Three and two or four, rows through registers, whole backward, us: [65536, 512] to 1408 398 and 508 (two with a
+// row more in flight), [8192, 1024] to 2736 211 and 215, 205, to 2733 263 and 391, 260.
 constexpr int DP_CTAS = 3;
+
+// Rows on their way to a thread of k_gated_dp with many of them, in shared memory: a place for each of dy, g and u a lane, for unaligned
+// rows one more a row.  With fewer than DP_RING rows a thread they come through registers, one at a time.  Registers and ring, dp alone, us:
+// [8192, 2736] (24 rows a thread) 61.9 and 46.4, [5456, 2240] (13) 31.6 and 23.1, [20000, 200] (6) 10.6 and 11.9, [20000, 104] (3) 6.6 and 8.0;
+// unaligned [27104, 5238] (154) 706 and 582, [8192, 2733] (24) 119.3 and 103.8, [20000, 601] (16) 57.6 and 56.6, [3001, 777] (3) 15.0
+// and 17.6.
+constexpr int DP_DEPTH = 4, DP_RING = 10;
+template <bool AL, int TX>
+constexpr int DP_PLACES = THREADS_256 / TX * (AL ? TX : TX + 1);
+template <bool AL, int TX>
+constexpr size_t DP_SMEM = size_t{DP_DEPTH} * 3 * DP_PLACES<AL, TX> * 16;
 
 // dp[t, n], dp[t, N + n] = bf16 of both gradients; part[chunk][n], [N + n] = the chunk's rows' float32 sums of them, before the rounding.
 // A CTA takes 8 TX channels (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.  AL: dy, p and dp
-// have 16-byte aligned rows and halves.
-template <bool AL, int TX>
+// have 16-byte aligned rows and halves.  Unaligned rows come as the whole 16-byte granules around them: a lane takes its own, and the
+// next lane's for the bytes it misses.
+template <bool AL, int TX, bool RING>
 __global__ void __launch_bounds__(THREADS_256, DP_CTAS) k_gated_dp(const Backward a, __nv_bfloat16* dp, long long dps, float* part, int chunks) {
-  constexpr int G = THREADS_256 / TX;  // rows at a time
+  constexpr int G = THREADS_256 / TX, PITCH = AL ? TX : TX + 1;  // rows at a time, places a row
+  extern __shared__ __align__(16) uint4 s_ring[];
   __shared__ float s[G][TX][9];
   const int lane = threadIdx.x % TX, g = threadIdx.x / TX, c0 = (blockIdx.x * TX + lane) * 8;
   const long long t0 = a.T * blockIdx.y / chunks, t1 = a.T * (blockIdx.y + 1) / chunks;
   float acc_g[8] = {}, acc_u[8] = {};
   pdl_wait();
   const uint16_t *dy = static_cast<const uint16_t*>(a.dy), *p = static_cast<const uint16_t*>(a.p);
+  auto place = [&](int i, int m) { return s_ring + (i * 3 + m) * DP_PLACES<AL, TX> + g * PITCH + lane; };
+  // a row's granules: of each the bytes from the matrix's first to the row's last, zeros beyond
+  auto fetch = [&](long long t, int i) {
+    const uint16_t *matrix[3] = {dy, p, p}, *row[3] = {dy + t * a.dys, p + t * a.ps, p + t * a.ps + a.N};
+#pragma unroll
+    for (int m = 0; m < 3; ++m) {
+      const uint8_t *lo = reinterpret_cast<const uint8_t*>(matrix[m]), *end = reinterpret_cast<const uint8_t*>(row[m] + a.N);
+      const uint8_t* q = reinterpret_cast<const uint8_t*>(row[m] + c0);
+      q -= reinterpret_cast<uintptr_t>(q) & 15u;
+#pragma unroll
+      for (int extra = 0; extra < (AL ? 1 : 2); ++extra, q += 16) {
+        if (extra && lane < TX - 1) continue;
+        uint4* to = place(i, m) + extra;
+        const int n = t >= t1 || q >= end ? 0 : end - q < 16 ? static_cast<int>(end - q) : 16;
+        if (AL || n == 0 || q >= lo) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(to)), "l"(n ? q : lo - (reinterpret_cast<uintptr_t>(lo) & 15u)), "r"(n) : "memory");
+        } else {  // the matrix starts inside it
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) reinterpret_cast<uint16_t*>(to)[j] = q + 2 * j >= lo && q + 2 * j < end ? *reinterpret_cast<const uint16_t*>(q + 2 * j) : 0;
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto unpack = [&](const uint32_t* w, float (&f)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  };
+  auto values = [&](const uint4* from, const uint16_t* row, float (&f)[8]) {
+    const uint4 u = *from;
+    uint32_t w[8] = {u.x, u.y, u.z, u.w};
+    if constexpr (!AL) {
+      const uint32_t r = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + c0)) & 15u;
+      if (r) {
+        const uint4 v = from[1];
+        w[4] = v.x, w[5] = v.y, w[6] = v.z, w[7] = v.w;
+        shift_bytes<4>(w, r);
+      }
+    }
+    unpack(w, f);
+  };
+  // the same through registers
   const Span sd = span_of(a.dy, a.T, a.dys, a.N, 2), sp = span_of(a.p, a.T, a.ps, 2 * a.N, 2);
   using Raw = typename std::conditional<AL, uint4, Granules>::type;
-  auto fetch = [&](const uint16_t* row, const Span& s) {
+  auto load = [&](const uint16_t* row, const Span& s, bool in) {
     Raw u = Raw{};
-    if (c0 < a.N) {
+    if (in && c0 < a.N) {
       if constexpr (AL)
         u = *reinterpret_cast<const uint4*>(row + c0);
       else
@@ -46,15 +102,14 @@ __global__ void __launch_bounds__(THREADS_256, DP_CTAS) k_gated_dp(const Backwar
     }
     return u;
   };
-  auto values = [&](const Raw& raw, const uint16_t* row, const Span& s, float (&f)[8]) {
+  auto loaded = [&](const Raw& raw, const uint16_t* row, const Span& s, bool in, float (&f)[8]) {
     uint4 u = make_uint4(0u, 0u, 0u, 0u);
     if constexpr (AL)
       u = raw;
-    else if (c0 < a.N)
+    else if (in && c0 < a.N)
       u = keep(finish16(raw, reinterpret_cast<const uint8_t*>(row + c0), s), min(16, 2 * (a.N - c0)));
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    unpack(w, f);
   };
   // Eight values at column c0 of a half that starts s elements behind a 16-byte boundary (dp's rows start on one): whole vectors lie s
   // elements lower, their first s values are the lane before's.  What no vector holds, at the ends of a strip and of the half, goes
@@ -88,21 +143,39 @@ __global__ void __launch_bounds__(THREADS_256, DP_CTAS) k_gated_dp(const Backwar
       }
     }
   };
-  for (long long t = t0 + g; t < t1; t += G) {
-    const Raw ud = fetch(dy + t * a.dys, sd), uz = fetch(p + t * a.ps, sp), uu = fetch(p + t * a.ps + a.N, sp);
+  if constexpr (RING) {
+#pragma unroll
+    for (int i = 0; i < DP_DEPTH - 1; ++i) fetch(t0 + i * G + g, i);
+  }
+  int turn = 0;
+  for (long long base = t0; base < t1; base += G, turn = (turn + 1) % DP_DEPTH) {
+    const long long t = base + g;
+    const uint16_t *rd = dy + t * a.dys, *rz = p + t * a.ps, *ru = rz + a.N;
     float d[8], z[8], u[8], v[8];
-    values(ud, dy + t * a.dys, sd, d);
-    values(uz, p + t * a.ps, sp, z);
-    values(uu, p + t * a.ps + a.N, sp, u);
+    if constexpr (RING) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(DP_DEPTH - 2) : "memory");
+      if constexpr (!AL) __syncwarp();  // the other lanes' granules are there, and those of the last row have been read
+      fetch(t + (DP_DEPTH - 1) * G, (turn + DP_DEPTH - 1) % DP_DEPTH);
+      values(place(turn, 0), rd, d);
+      values(place(turn, 1), rz, z);
+      values(place(turn, 2), ru, u);
+    } else {
+      const bool in = t < t1;
+      const Raw xd = load(rd, sd, in), xz = load(rz, sp, in), xu = load(ru, sp, in);
+      loaded(xd, rd, sd, in, d);
+      loaded(xz, rz, sp, in, z);
+      loaded(xu, ru, sp, in, u);
+    }
 #pragma unroll
     for (int j = 0; j < 8; j += 2) gate_gradients(d[j], d[j + 1], v[j], v[j + 1], z[j], z[j + 1], u[j], u[j + 1], a.act);
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc_g[j] += d[j], acc_u[j] += v[j];
-    if (dp) {
+    if (dp && t < t1) {
       store(dp + t * dps, 0, d);
       store(dp + t * dps + a.N, a.N % 8, v);
     }
   }
+  if constexpr (RING) asm volatile("cp.async.wait_all;" ::: "memory");
   if (part) {
     auto add = [&](const float (&acc)[8], float* to) {
       __syncthreads();  // the last sums have been read
@@ -313,11 +386,22 @@ cudaError_t gated_backward(const Backward& a, void* ws, unsigned int* err, int s
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg,
-                           tx == 8    ? (al ? k_gated_dp<true, 8> : k_gated_dp<false, 8>)
-                           : tx == 16 ? (al ? k_gated_dp<true, 16> : k_gated_dp<false, 16>)
-                                      : (al ? k_gated_dp<true, 32> : k_gated_dp<false, 32>),
-                           c, dp, np, part, chunks);
+    const bool ring = a.T * tx >= static_cast<long long>(DP_RING) * THREADS_256 * chunks;
+    auto launch = [&](auto aligned, auto lanes) {
+      constexpr bool AL = decltype(aligned)::value;
+      constexpr int TX = decltype(lanes)::value;
+      if (!ring) return cudaLaunchKernelEx(&cfg, k_gated_dp<AL, TX, false>, c, dp, np, part, chunks);
+      static std::atomic<uint64_t> raised{0};
+      const cudaError_t r = raise_smem(reinterpret_cast<const void*>(k_gated_dp<AL, TX, true>), DP_SMEM<AL, TX>, raised);
+      cfg.dynamicSmemBytes = DP_SMEM<AL, TX>;
+      return r != cudaSuccess ? r : cudaLaunchKernelEx(&cfg, k_gated_dp<AL, TX, true>, c, dp, np, part, chunks);
+    };
+    auto by_lanes = [&](auto aligned) {
+      return tx == 8    ? launch(aligned, std::integral_constant<int, 8>())
+             : tx == 16 ? launch(aligned, std::integral_constant<int, 16>())
+                        : launch(aligned, std::integral_constant<int, 32>());
+    };
+    e = al ? by_lanes(std::true_type()) : by_lanes(std::false_type());
   }
   if (e != cudaSuccess) return e;
   if (a.db && chunks > 1 && (e = norm::add_rows(part, a.db, 2 * a.N, chunks, stream)) != cudaSuccess) return e;

@@ -546,6 +546,22 @@ def test_gated_backward_of_many_tokens_and_its_weight_gradient(T, N, K):
     check_gated_backward(T, N, K, "relu", need_dw=False)
 
 
+@pytest.mark.parametrize("T,N,K", [(8200, 1001, 40), (62000, 130, 24), (76000, 101, 16), (120000, 57, 33), (6000, 1600, 300), (64, 1408, 96), (127, 149, 33)])
+def test_gated_backward_of_rows_in_a_ring(T, N, K):
+    """Enough rows a thread for them to come through shared memory, each number of threads a row; rows that start anywhere between others'
+    values, the first one inside its granule."""
+    x, w, dy, p, want = check_gated_backward(T, N, K, "silu")
+    if N % 8 == 0:
+        return
+    for offset, gap in ((1, 3), (5, 0), (7, 8)):
+        buffers = [torch.full((T * (n + gap) + 16,), math.nan, device="cuda").to(BF) for n in (N, 2 * N)]
+        dy2, p2 = (b[offset:offset + T * (n + gap)].view(T, n + gap)[:, :n] for b, n in zip(buffers, (N, 2 * N)))
+        dy2.copy_(dy)
+        p2.copy_(p)
+        got = whtmix.gated_linear_backward(x, w, dy2, p2, "silu")
+        assert all(torch.equal(s, t) for s, t in zip(got, want))
+
+
 def test_gated_gradients_by_differences():
     """Against central differences of the float64 definition, through autograd; values that bf16 holds, small sizes."""
     T, N, K = 4, 12, 24
