@@ -296,8 +296,8 @@ struct GatedBackwardPlan {
   bool fused;         // whtmix_gemm_gated_dp.cu
   Backward products;  // (its dy and workspace are filled in when the call runs)
   int np, chunks;     // pitch of dp; db's chunks of rows
-  bool pad_w;         // fused: W to a 16-byte pitch
-  size_t dp_off, db_off, w_off, products_off, total;
+  bool pad_w, pad_x;  // fused: W, x to a 16-byte pitch, in one launch
+  size_t dp_off, db_off, w_off, x_off, products_off, total;
 };
 static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
   GatedBackwardPlan b{};
@@ -315,7 +315,11 @@ static GatedBackwardPlan plan_backward(const Backward& a, int sms) {
   b.products.N = 2 * a.N, b.products.act = ACT_NONE, b.products.p = nullptr, b.products.db = nullptr;
   b.products.dy = nullptr, b.products.dys = b.np;  // (on a 16-byte boundary)
   b.products.split_dx = true;
-  if (b.fused) b.products.dx = nullptr;
+  if (b.fused) {
+    b.products.dx = nullptr;
+    b.pad_x = a.dw && !tma::mappable(a.x, a.T, a.xs, 2);
+    if (b.pad_x) b.x_off = take(static_cast<size_t>(a.T) * pitch_of(a.K, 2) * 2), b.products.x = nullptr, b.products.xs = pitch_of(a.K, 2);
+  }
   if (b.products.dx || a.dw) {
     b.dp_off = take(static_cast<size_t>(a.T) * b.np * 2);
     b.products_off = take(backward_workspace(b.products, sms));
@@ -341,11 +345,12 @@ static cudaError_t fused_backward(const Backward& a, const GatedBackwardPlan& b,
                                   cudaStream_t stream) {
   const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(a.w);
   long long wst = a.ws;
-  if (b.pad_w) {
-    w = reinterpret_cast<const __nv_bfloat16*>(base + b.w_off), wst = pitch_of(a.K, 2);
-    const cudaError_t e = to_pitch(copy_of(base + b.w_off, a.w, 2ll * a.N, a.K, a.ws, static_cast<int>(wst), 2), Copy{}, sms, stream);
-    if (e != cudaSuccess) return e;
-  }
+  const int kp = pitch_of(a.K, 2);
+  const Copy cx = b.pad_x ? copy_of(base + b.x_off, a.x, a.T, a.K, a.xs, kp, 2) : Copy{};
+  const Copy cw = b.pad_w ? copy_of(base + b.w_off, a.w, 2ll * a.N, a.K, a.ws, kp, 2) : Copy{};
+  const cudaError_t e = to_pitch(cx, cw, sms, stream);
+  if (e != cudaSuccess) return e;
+  if (b.pad_w) w = reinterpret_cast<const __nv_bfloat16*>(base + b.w_off), wst = kp;
   const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(a.p);
   __nv_bfloat16* dp = a.dw ? reinterpret_cast<__nv_bfloat16*>(base + b.dp_off) : nullptr;
   GatedDp g{};
@@ -408,6 +413,7 @@ cudaError_t gated_backward(const Backward& a, void* ws, unsigned int* err, int s
   if (!dp) return cudaSuccess;
   Backward products = b.products;
   products.dy = dp;
+  if (b.pad_x) products.x = base + b.x_off;
   return backward(products, base + b.products_off, err, sms, stream);
 }
 
