@@ -25,10 +25,10 @@ constexpr int DP_CTAS = 3;
 
 // Rows on their way to a thread of k_gated_dp with many of them, in shared memory: a place for each of dy, g and u a lane, for unaligned
 // rows one more a row.  With fewer than DP_RING rows a thread they come through registers, one at a time.  Registers and ring, dp alone, us:
-// [8192, 2736] (24 rows a thread) 61.9 and 46.4, [5456, 2240] (13) 31.6 and 23.1, [20000, 200] (6) 10.6 and 11.9, [20000, 104] (3) 6.6 and 8.0;
-// unaligned [27104, 5238] (154) 706 and 582, [8192, 2733] (24) 119.3 and 103.8, [20000, 601] (16) 57.6 and 56.6, [3001, 777] (3) 15.0
+// [8192, 2736] (24 rows a thread) 61.9 and 46.4, [5456, 2240] (13) 31.6 and 23.1, [2003, 3776] (8) 22.7 and 19.4, [20000, 200] (6) 10.6 and 11.9, [20000, 104] (3) 6.6 and 8.0;
+// unaligned [27104, 5238] (154) 706 and 592, [8192, 2733] (24) 119.3 and 103.8, [20000, 601] (16) 57.6 and 57 to 62, [3001, 777] (3) 15.0
 // and 17.6.
-constexpr int DP_DEPTH = 4, DP_RING = 10;
+constexpr int DP_DEPTH = 4, DP_RING = 8;
 template <bool AL, int TX>
 constexpr int DP_PLACES = THREADS_256 / TX * (AL ? TX : TX + 1);
 template <bool AL, int TX>
