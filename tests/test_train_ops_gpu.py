@@ -154,6 +154,31 @@ def test_layer_norm_to_eight_bits(T, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(20011, 77), (9800, 33), (10000, 9), (9737, 50), (9729, 67), (4900, 177), (9801, 130), (5000, 301), (2440, 499), (2500, 1001)])
+def test_many_odd_rows_to_eight_bits(T, D, dtype):
+    """Rows that come as tiles; what lies between the output's rows stays."""
+    test_layer_norm_to_eight_bits(T, D, dtype)
+    x, res, w, b = norm_inputs(T, D, dtype)
+    q, scale, h = whtmix.layer_norm(x, w, b, residual=res, out_dtype=E4M3)
+    for gap in (0, 3, 16):
+        whole = torch.full((T, D + gap), 0x5a, dtype=torch.uint8, device="cuda")
+        out = whole.view(E4M3)[:, :D]
+        q2, scale2, h2 = whtmix.layer_norm(x, w, b, residual=res, out_dtype=E4M3, out=out)
+        assert torch.equal(q2.view(torch.uint8), q.view(torch.uint8)) and torch.equal(scale2, scale) and torch.equal(h2, h)
+        assert bool((whole[:, D:] == 0x5a).all())
+    alone, s = whtmix.layer_norm(x, w, out_dtype=E4M3)  # neither residual nor shifts, as each row on its own
+    few, s_few = whtmix.layer_norm(x[5:9], w, out_dtype=E4M3)
+    assert float((alone[5:9].float() - few.float()).abs().max()) <= 32 and float((s[5:9] - s_few).abs().max()) <= 1e-5 * float(s_few.max())
+    x[7, D // 2] = math.inf
+    x[8] = 2.5
+    odd, s_odd = whtmix.layer_norm(x, w, out_dtype=E4M3)
+    assert bool(torch.isnan(s_odd[7])) and bool(torch.isnan(odd[7].float()).all())
+    rows = [i for i in range(T) if i not in (7, 8)]
+    assert torch.equal(odd.view(torch.uint8)[rows], alone.view(torch.uint8)[rows]) and torch.equal(s_odd[rows], s[rows])
+    assert bool((odd[8].float() == 0).all() or float(s_odd[8]) <= 1e-3)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T,D", [(2, 20001), (1, 100000), (3, 33000), (3, 1 << 20)])
 def test_layer_norm_of_rows_beyond_the_registers(T, D, dtype):
     x, res, w, b = norm_inputs(T, D, dtype)
