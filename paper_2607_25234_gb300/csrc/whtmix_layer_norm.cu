@@ -233,7 +233,7 @@ constexpr int LN_DEPTH = NV == 1 ? 4 : 2;
 // two sets for each of the CTA's row groups (dynamic), or, where those would cost more than reading h and dy again, not here (SUMS): coef[t]
 // = mean and rstd for k_ln_columns.
 // (Odd rows on 256 threads are kept to 80 registers, three CTAs an SM: left alone they take 152, and one CTA an SM cannot hide what a row
-// waits for: [20000, 601] float32 167 -> 127 us.)
+// waits for: [20000, 601] float32 167 -> 127 us before such rows went as tiles.)
 template <typename T, bool AL, int TPR, int NV, bool SUMS>
 __global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 3 : AL && TPR == 512 && NV == 1 ? 2 : 1) k_ln_bwd(const LayerBackward a, const Same same, float2* coef) {
   static_assert(SUMS || !AL, "the sums of aligned rows stay in registers");
@@ -818,11 +818,109 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackwar
   pdl_trigger();
 }
 
+// The same for wider rows, a warp a row: dx (null: not) and coef[t] = mean and rstd for k_ln_columns, the column sums of which would not fit
+// the registers.  Gains in shared memory, two or three stages.  (Whole backward, row kernels and this, us: [20000, 601] float32 128 and 65,
+// [28453, 1356] bf16 with dh 242 and 132, [5000, 1001] bf16 25.3 and 19.6, [8000, 1601] float32 115 and 78, bf16 78 and 56.)
+constexpr int WIDE_ROWS = TILE_THREADS / 32;
+template <int NE>
+constexpr int WIDE_SURE = NE == 20 ? 16 : NE == 24 ? 20 : NE == 32 ? 24 : NE == 40 ? 32 : NE == 48 ? 40 : 48;
+template <typename T, int NE>
+__global__ void __launch_bounds__(TILE_THREADS, NE <= 40 ? 2 : 1) k_ln_dx_tile(const LayerBackward a, float2* coef, int stages, unsigned int* err) {
+  extern __shared__ __align__(128) unsigned char s_tiles[];
+  __shared__ uint64_t full[TILE_STAGES];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.D;
+  const float inv_d = 1.f / static_cast<float>(D);
+  const long long tiles = (a.T + WIDE_ROWS - 1) / WIDE_ROWS;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) tc::mbar_init(&full[s], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  pdl_wait();
+  const Stages<T, 3> st{s_tiles, full, {{a.h, a.T, D}, {a.dy, a.T, D}, {a.dh, a.T, D}}, a.dh ? 3 : 2, D};
+  const Tiles<T> dx{a.dx, a.T, D};
+  float* s_w = reinterpret_cast<float*>(s_tiles + stages * st.live * tile_bytes<T>(D));
+  for (int e = threadIdx.x; e < D; e += TILE_THREADS) s_w[e] = __ldg(a.w + e);  // (behind the first tile's barrier)
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < stages - 1; ++i)
+      if (blockIdx.x + static_cast<long long>(i) * gridDim.x < tiles) st.load(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
+  }
+  unsigned bad = 0;
+  uint32_t it = 0;
+  int s = 0;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++it, s = s + 1 == stages ? 0 : s + 1) {
+    if (threadIdx.x == 0) {
+      const long long next = tile + static_cast<long long>(stages - 1) * gridDim.x;
+      if (next < tiles) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last tile has left the stage
+        st.load(next, s == 0 ? stages - 1 : s - 1);
+      }
+    }
+    st.ends(tile, s);
+    if (!bad && !tma::wait(&full[s], (it / stages) & 1)) bad |= 1;
+    __syncthreads();  // the ends and the gains too
+    const long long t = tile * WIDE_ROWS + warp;
+    if (t < a.T) {
+      const T* hs = reinterpret_cast<const T*>(st.place(s, 0)) + warp * D + lane;
+      const T* gs = reinterpret_cast<const T*>(st.place(s, 2)) + warp * D + lane;
+      T* ds = reinterpret_cast<T*>(st.place(s, 1)) + warp * D + lane;
+      const float* ws = s_w + lane;
+      float c[NE], d[NE], sum[1] = {0.f};
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        const bool in = k < WIDE_SURE<NE> || lane + 32 * k < D;
+        c[k] = in ? Io<T>::get(hs, 32 * k) : 0.f;
+        d[k] = in ? Io<T>::get(ds, 32 * k) : 0.f;
+        sum[0] += c[k];
+      }
+      lanes_join<32>(sum);
+      const float mean = sum[0] * inv_d;
+      float q[3] = {};  // sums of c^2, a, a c
+#pragma unroll
+      for (int k = 0; k < NE; ++k) {
+        const bool in = k < WIDE_SURE<NE> || lane + 32 * k < D;
+        c[k] = in ? c[k] - mean : 0.f;
+        const float g = in ? d[k] * ws[32 * k] : 0.f;
+        q[0] += c[k] * c[k];
+        q[1] += g;
+        q[2] += g * c[k];
+      }
+      lanes_join<32>(q);
+      const float rstd = rsqrtf(q[0] * inv_d + a.eps), ma = q[1] * inv_d, m = rstd * rstd * (q[2] * inv_d);
+      if (a.dx) {
+#pragma unroll
+        for (int k = 0; k < NE; ++k)
+          if (k < WIDE_SURE<NE> || lane + 32 * k < D)
+            Io<T>::put(ds, 32 * k, rstd * (d[k] * ws[32 * k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, 32 * k) : 0.f));
+      }
+      if (lane == 0) coef[t] = make_float2(mean, rstd);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    if (a.dx) {
+      if (threadIdx.x == 0) {
+        dx.store(tile, reinterpret_cast<unsigned char*>(st.place(s, 1)));
+        tma::commit();
+      }
+      dx.template ends<true>(tile, reinterpret_cast<unsigned char*>(st.place(s, 1)));
+    }
+  }
+  if (threadIdx.x == 0) {
+    tma::wait_done();
+    // a wait that gave up: the copies in flight have landed before the CTA can end
+    const uint32_t n = stages;
+    for (uint32_t j = it > n ? it - n : 0; bad && j < it; ++j) (void)tma::wait(&full[j % n], (j / n) & 1);
+    if (bad) atomicOr(err, bad);
+  }
+  pdl_trigger();
+}
+
 // ---- host ----
 
 // The longest rows that go as tiles, and the least of them (two tiles an SM).  Rows of whole vectors stay with their own kernels
 // (backward, us, tiles read by vectors and row kernels: [131072, 256] bf16 69.1 and 59.6, [128000, 64] float32 21.4 and 20.8).
-constexpr int TILE_FORWARD = 1024, TILE_BACKWARD = 512;
+constexpr int TILE_FORWARD = 1024, TILE_BACKWARD = 512, TILE_WIDE = 2048;
+constexpr size_t WIDE_SMEM = 220 * 1024;  // an SM's, less what its CTAs declare themselves
 template <typename T>
 static bool tiled(long long rows, int D, int most, int sms) {
   return D % Io<T>::V != 0 && D >= 8 && D <= most && rows >= 2ll * tile_rows<T>(D) * sms;
@@ -938,7 +1036,26 @@ struct LayerPlan {
   size_t smem;
   int block, parts;
   bool tiles;
+  int wide;  // stages of k_ln_dx_tile, or 0
 };
+
+// Stages of k_ln_dx_tile for a call, its kernel and shared memory; 0 where two do not fit or the rows are not for it.
+template <typename T>
+static int wide_tiles(const LayerBackward& a, int sms, const void** kernel, size_t* smem) {
+  if (!tiled<T>(a.T, a.D, TILE_WIDE, sms) || a.D <= TILE_BACKWARD || !contiguous(a.h, a.hs, a.D) || !contiguous(a.dy, a.ys, a.D) ||
+      !contiguous(a.dh, a.ds, a.D) || !contiguous(a.dx, a.xs, a.D))
+    return 0;
+  const size_t stage = static_cast<size_t>(a.dh ? 3 : 2) * tile_bytes<T>(a.D), gains = static_cast<size_t>(a.D) * 4;
+  const int most = static_cast<int>((WIDE_SMEM - gains) / stage), pair = static_cast<int>((WIDE_SMEM / 2 - gains) / stage);
+  const int stages = pair >= 2 ? pair : most;  // two CTAs an SM before a third stage
+  if (stages < 2) return 0;
+  const int used = stages < TILE_STAGES ? stages : TILE_STAGES;
+  *smem = used * stage + gains;
+  auto k = [](auto ne) { return reinterpret_cast<const void*>(k_ln_dx_tile<T, decltype(ne)::value>); };
+  const int ne = (a.D + 31) / 32;
+  *kernel = ne <= 20 ? k(Int<20>()) : ne <= 24 ? k(Int<24>()) : ne <= 32 ? k(Int<32>()) : ne <= 40 ? k(Int<40>()) : ne <= 48 ? k(Int<48>()) : k(Int<64>());
+  return used;
+}
 template <typename T>
 static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int sms, LayerPlan* p) {
   const size_t stages = static_cast<size_t>(TILE_STAGES) * (a.dh ? 3 : 2) * tile_bytes<T>(a.D);  // at most 144 KB
@@ -955,6 +1072,13 @@ static cudaError_t layer_plan(const LayerBackward& a, const LayerRows& rows, int
     int resident = 0;
     const cudaError_t e = resident_ctas(p->kernel, TILE_THREADS, p->smem, sms, &resident);
     if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, tile_rows<T>(a.D), resident));
+    return e;
+  }
+  if (rows.apart && (p->wide = wide_tiles<T>(a, sms, &p->kernel, &p->smem)) > 0) {
+    p->block = TILE_THREADS;
+    int resident = 0;
+    const cudaError_t e = resident_ctas(p->kernel, TILE_THREADS, p->smem, sms, &resident);
+    if (e == cudaSuccess) p->parts = static_cast<int>(grid_rows(a.T, WIDE_ROWS, resident));
     return e;
   }
   auto take = [&](auto tpr, auto nv) {
@@ -1021,8 +1145,8 @@ static cudaError_t backward_t(const LayerBackward& a, unsigned int* err, int sms
     if (over_dy) e = take(with_dx);
   } else {
     Same same{rows_same(a.h, a.hs, a.dy, a.ys, es), rows_same(a.h, a.hs, a.dh, a.ds, es), rows_same(a.h, a.hs, a.dx, a.xs, es)};
-    void *args[] = {&c, &same, &coef}, *tile_args[] = {&c, &err};
-    auto take = [&] { return launch_pdl(p.kernel, static_cast<unsigned>(p.parts), p.block, p.smem, stream, p.tiles ? tile_args : args); };
+    void *args[] = {&c, &same, &coef}, *tile_args[] = {&c, &err}, *wide_args[] = {&c, &coef, &p.wide, &err};
+    auto take = [&] { return launch_pdl(p.kernel, static_cast<unsigned>(p.parts), p.block, p.smem, stream, p.tiles ? tile_args : p.wide ? wide_args : args); };
     // (dw reads dy, as above)
     const bool over_dy = apart && a.dx == a.dy;
     if (over_dy) c.dx = nullptr;

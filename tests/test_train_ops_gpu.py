@@ -308,6 +308,22 @@ def test_layer_norm_backward_against_float64(T, D, dtype):
         assert all(torch.equal(p, q) for p, q in zip(got, (dx, dw, db)))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(2433, 529), (2500, 601), (2441, 765), (4999, 1021), (2440, 1277), (2600, 1502), (2433, 2047), (2435, 1135)])
+def test_layer_norm_backward_of_many_wide_odd_rows(T, D, dtype):
+    test_layer_norm_backward_against_float64(T, D, dtype)
+    h, w, dy, dh = rand(1, T, D).to(dtype), 1 + 0.1 * rand(2, D), rand(3, T, D).to(dtype), rand(4, T, D).to(dtype)
+    for extra in (None, dh):
+        want = whtmix.layer_norm_backward(h, w, dy, dh=extra)
+        over = dy.clone()
+        got = whtmix.layer_norm_backward(h, w, over, dh=extra, dx=over)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        if extra is not None:
+            over = dh.clone()
+            got = whtmix.layer_norm_backward(h, w, dy, dh=over, dx=over)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_layer_norm_gradients_by_differences():
     T, D = 3, 24
     x, r, w, b = rand(1, T, D) + 1.0, rand(2, T, D), 1.0 + 0.1 * rand(3, D), 0.1 * rand(4, D)
