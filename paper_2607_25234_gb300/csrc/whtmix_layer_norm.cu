@@ -536,7 +536,7 @@ __host__ __device__ constexpr int tile_bytes(int D) { return tile_rows<T>(D) * D
 
 // Of a lane's NE elements the first SURE are inside every row that by_columns sends here (more than LANES SURE channels).
 template <int NE>
-constexpr int SURE = NE == 4 ? 0 : NE == 6 ? 4 : NE == 8 ? 6 : NE == 12 ? 8 : NE == 16 ? 12 : 16;
+constexpr int SURE = NE == 4 ? 0 : NE == 6 ? 4 : NE == 8 ? 6 : NE == 12 ? 8 : NE == 16 ? 12 : NE == 32 ? 16 : 32;
 
 // A contiguous matrix [T, D] that is copied tile by tile.  The last tile's bytes beyond whole 16-byte pieces go element by element.
 template <typename T>
@@ -619,13 +619,21 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
   pdl_wait();
   const Stages<T, 2> st{s_tiles, full, {{a.x, a.T, D}, {a.r, a.T, D}}, a.r ? 2 : 1, D};
   const Tiles<T> y{a.y, a.T, D}, h_out{a.h, a.T, D};
-  float w[NE], b[NE];
+  constexpr bool KEEP = NE <= 32;  // gains and shifts in registers, or from L1 with each row
+  float kept_w[KEEP ? NE : 1], kept_b[KEEP ? NE : 1];
+  if constexpr (KEEP) {
 #pragma unroll
-  for (int k = 0; k < NE; ++k) {
-    const int e = lane + LANES * k;
-    w[k] = e < D ? __ldg(a.w + e) : 0.f;
-    b[k] = a.b && e < D ? __ldg(a.b + e) : 0.f;
+    for (int k = 0; k < NE; ++k) {
+      const int e = lane + LANES * k;
+      kept_w[k] = e < D ? __ldg(a.w + e) : 0.f;
+      kept_b[k] = a.b && e < D ? __ldg(a.b + e) : 0.f;
+    }
   }
+  // y's element k of a lane (inside the row), from c rstd
+  auto affine = [&](float n, int k) {
+    if constexpr (KEEP) return n * kept_w[k] + kept_b[k];
+    return n * __ldg(a.w + lane + LANES * k) + (a.b ? __ldg(a.b + lane + LANES * k) : 0.f);
+  };
   if (threadIdx.x == 0) {
     for (int i = 0; i < TILE_STAGES - 1; ++i)
       if (blockIdx.x + static_cast<long long>(i) * gridDim.x < tiles) st.load(blockIdx.x + static_cast<long long>(i) * gridDim.x, i);
@@ -666,8 +674,10 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
         uint32_t top = 0;
 #pragma unroll
         for (int k = 0; k < NE; ++k) {
-          v[k] = v[k] * rstd * w[k] + b[k];
-          if (k < SURE<NE> || lane + LANES * k < D) top = max(top, __float_as_uint(magnitude(v[k])));
+          if (k < SURE<NE> || lane + LANES * k < D) {
+            v[k] = affine(v[k] * rstd, k);
+            top = max(top, __float_as_uint(magnitude(v[k])));
+          }
         }
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -683,7 +693,7 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
       } else {
 #pragma unroll
         for (int k = 0; k < NE; ++k)
-          if (k < SURE<NE> || lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, v[k] * rstd * w[k] + b[k]);
+          if (k < SURE<NE> || lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, affine(v[k] * rstd, k));
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -919,7 +929,9 @@ __global__ void __launch_bounds__(TILE_THREADS, NE <= 40 ? 2 : 1) k_ln_dx_tile(c
 
 // The longest rows that go as tiles, and the least of them (two tiles an SM).  Rows of whole vectors stay with their own kernels
 // (backward, us, tiles read by vectors and row kernels: [131072, 256] bf16 69.1 and 59.6, [128000, 64] float32 21.4 and 20.8).
-constexpr int TILE_FORWARD = 1024, TILE_BACKWARD = 512, TILE_WIDE = 2048;
+// Forward with a residual, row kernels and tiles: [20000, 1500] bf16 72.1 and 64.7, [2500, 1101] 12.7 and 9.8, [8000, 1101] float32 34.6 and
+// 29.7, but [10000, 2001] bf16 37.6 and 47.7; to 8 bits with its gated product [8000, 1501] 57.3 and 59.3.
+constexpr int TILE_FORWARD = 1536, TILE_FORWARD_Q8 = 1024, TILE_BACKWARD = 512, TILE_WIDE = 2048;
 constexpr size_t WIDE_SMEM = 220 * 1024;  // an SM's, less what its CTAs declare themselves
 template <typename T>
 static bool tiled(long long rows, int D, int most, int sms) {
@@ -939,7 +951,8 @@ static void by_columns(int D, F&& f) {
   else if (D <= 256) WHTMIX_LANES(32, 8);
   else if (D <= 384) WHTMIX_LANES(32, 12);
   else if (D <= 512) WHTMIX_LANES(32, 16);
-  else WHTMIX_LANES(32, 32);
+  else if (D <= 1024) WHTMIX_LANES(32, 32);
+  else WHTMIX_LANES(32, 48);
 #undef WHTMIX_LANES
 }
 
@@ -951,16 +964,19 @@ static cudaError_t forward_t(const LayerForward& a, unsigned int* err, int sms, 
                   rows_aligned(a.r ? a.h : nullptr, a.hs, es) && (Q8 ? rows_aligned(a.y, a.ys, 1, V) : rows_aligned(a.y, a.ys, es));
   const int n = vectors(a.D, es == 2, al);
   LayerForward c = a;
-  if (tiled<T>(a.T, a.D, TILE_FORWARD, sms) && contiguous(a.x, a.xs, a.D) && contiguous(a.r, a.rs, a.D) &&
+  const size_t stages = static_cast<size_t>(TILE_STAGES) * (a.r ? 2 : 1) * tile_bytes<T>(a.D);
+  if (tiled<T>(a.T, a.D, Q8 ? TILE_FORWARD_Q8 : TILE_FORWARD, sms) && stages <= WIDE_SMEM && contiguous(a.x, a.xs, a.D) && contiguous(a.r, a.rs, a.D) &&
       contiguous(a.r ? a.h : nullptr, a.hs, a.D) && (Q8 || contiguous(a.y, a.ys, a.D))) {
     const void* k = nullptr;
-    by_columns(a.D, [&](auto lanes, auto ne) { k = reinterpret_cast<const void*>(k_ln_tile<T, Q8, decltype(lanes)::value, decltype(ne)::value>); });
-    const size_t smem = static_cast<size_t>(TILE_STAGES) * (a.r ? 2 : 1) * tile_bytes<T>(a.D);  // at most 192 KB
+    by_columns(a.D, [&](auto lanes, auto ne) {
+      constexpr int LANES = decltype(lanes)::value, NE = decltype(ne)::value;
+      if constexpr (LANES * NE <= (Q8 ? TILE_FORWARD_Q8 : TILE_FORWARD)) k = reinterpret_cast<const void*>(k_ln_tile<T, Q8, LANES, NE>);
+    });
     int resident = 0;
-    const cudaError_t e = resident_ctas(k, TILE_THREADS, smem, sms, &resident);
+    const cudaError_t e = resident_ctas(k, TILE_THREADS, stages, sms, &resident);
     if (e != cudaSuccess) return e;
     void* args[] = {&c, &err};
-    return launch_pdl(k, grid_rows(a.T, tile_rows<T>(a.D), resident), TILE_THREADS, smem, stream, args);
+    return launch_pdl(k, grid_rows(a.T, tile_rows<T>(a.D), resident), TILE_THREADS, stages, stream, args);
   }
   if (n > MAX_VECTORS) {
     void* args[] = {&c};

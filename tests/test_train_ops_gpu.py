@@ -154,7 +154,7 @@ def test_layer_norm_to_eight_bits(T, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("T,D", [(20011, 77), (9800, 33), (10000, 9), (9737, 50), (9729, 67), (4900, 177), (9801, 130), (5000, 301), (2440, 499), (2500, 1001)])
+@pytest.mark.parametrize("T,D", [(20011, 77), (9800, 33), (10000, 9), (9737, 50), (9729, 67), (4900, 177), (9801, 130), (5000, 301), (2440, 499), (2500, 1001), (2433, 1027), (2500, 1537), (2440, 2047)])
 def test_many_odd_rows_to_eight_bits(T, D, dtype):
     """Rows that come as tiles; what lies between the output's rows stays."""
     test_layer_norm_to_eight_bits(T, D, dtype)
@@ -306,6 +306,12 @@ def test_layer_norm_backward_against_float64(T, D, dtype):
         a, b = dy.clone(), dh.clone()
         got = whtmix.layer_norm_backward(h, w, a, dh=b, dx=a if inplace == "dy" else b)
         assert all(torch.equal(p, q) for p, q in zip(got, (dx, dw, db)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(2433, 1027), (2500, 1373), (2441, 1537), (2440, 2047)])
+def test_layer_norm_of_many_wide_odd_rows(T, D, dtype):
+    test_layer_norm_against_float64(T, D, dtype)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
