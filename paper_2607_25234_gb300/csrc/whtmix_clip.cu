@@ -314,14 +314,16 @@ __global__ void __launch_bounds__(CLIP_THREADS, CLIP_CTAS) k_scale(const __grid_
 }
 
 // ---- few chunks ----
-// Lists of up to SMALL chunks: one cluster holds them all in registers between the sum and the scaling; its CTAs read one another's
-// sums from shared memory.  One launch, no scratch.
+// Lists of up to SMALL chunks: one cluster holds them all in registers between the sum and the scaling; its CTAs put their sums into
+// one another's shared memory, behind a barrier of the cluster that the loads hide (a CTA's shared memory is there once it has
+// started) and before another.  One launch, no scratch.
 constexpr int CLUSTER = 8, HELD = 3, SMALL = CLUSTER * HELD;
 __global__ void __launch_bounds__(CLIP_THREADS) k_clip_few(const __grid_constant__ Table<FEW> t, float max_norm, float* norm, int scale) {
   __shared__ double s_all[CLUSTER];
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = static_cast<int>(cluster.block_rank());
+  cluster.barrier_arrive();  // waited for before the first store to another CTA: by then all have started
   pdl_wait();
   Piece p[HELD];
   uint4 u[HELD][VECTORS];
@@ -338,6 +340,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_clip_few(const __grid_constant
   for (int i = 0; i < HELD; ++i)
     if (rank + CLUSTER * i < t.chunks) sum.add(u[i], p[i].bf16);
   const double mine = __shfl_sync(0xffffffffu, add_up(sum), 0);
+  cluster.barrier_wait();
   if (threadIdx.x < CLUSTER) *cluster.map_shared_rank(&s_all[rank], threadIdx.x) = mine;
   cluster.sync();
   __shared__ Scale s_scale;
