@@ -294,8 +294,8 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w, const void *
  *     h = x + residual,    y = (h - mean(h)) w / sqrt(mean((h - mean(h))^2) + eps) + b
  * Arguments, types and overlaps as whtmix_rms_norm's, and
  *   b            [D] float32 shifts, or NULL
- * y is computed from the unrounded sum.  A row with an infinity or a NaN yields NaN (and a NaN scale); a row of equal values yields
- * b (eps > 0), up to the rounding of its mean.
+ * y is computed from the unrounded sum.  Every row whose h is finite has its norm, whatever the size of its values; a row with an
+ * infinity or a NaN in h yields NaN (and a NaN scale); a row of equal values yields b (eps > 0), up to the rounding of its mean.
  * WHTMIX_E4M3: a row whose y is all zero has scale 0 and values 0. */
 WHTMIX_API int whtmix_layer_norm(const void *x, const void *residual, const float *w, const float *b, void *h, void *y,
                                  float *y_scale, int64_t T, int64_t D, int64_t x_stride, int64_t residual_stride,
@@ -305,8 +305,8 @@ WHTMIX_API int whtmix_layer_norm(const void *x, const void *residual, const floa
  *     dx = r (a - mean(a) - n mean(a n)) + dh,     dw = sum over the rows of dy n,     db = sum over the rows of dy
  * Arguments as whtmix_rms_norm_backward's, and
  *   db         [D] float32, overwritten; or NULL
- * Two launches (three for rows beyond the registers and for many rows of which some are not 16-byte aligned, four there if dx is
- * dy).  What a stream that is being captured needs in between belongs to the graph; so it is with the four calls below. */
+ * Every finite row has its gradients, as it has its norm.  Two launches (three for rows beyond the registers and for many rows of which
+ * some are not 16-byte aligned, four there if dx is dy).  What a stream that is being captured needs in between belongs to the graph; so it is with the four calls below. */
 WHTMIX_API int whtmix_layer_norm_backward(const void *h, const float *w, const void *dy, const void *dh, void *dx, float *dw,
                                           float *db, int64_t T, int64_t D, int64_t h_stride, int64_t dy_stride,
                                           int64_t dh_stride, int64_t dx_stride, float eps, int dtype, void *stream);

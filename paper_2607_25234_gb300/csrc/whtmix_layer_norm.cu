@@ -36,6 +36,34 @@ __device__ __forceinline__ void bulk_store(void* g, const void* s, int bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(g), "r"(tc::smem_u32(s)), "r"(bytes) : "memory");
 }
 
+// Finite rows whose sums leave float32's range: where var + eps is not within [1 / FAR, FAR], or no number, the row is taken again with its
+// values times a power of two (exact, but for elements too small to count):
+//   s h - mean(s h) = s c,     c rstd = s c r,     rstd = s r,     r = 1 / sqrt(mean((s c)^2) + s^2 eps)
+// DOWN leaves the squares of 2^24 of float32's largest below 2^122, UP the smallest's above 2^-138.  For a row in range s = 1.  The check is a
+// vote and a branch in every row, 0 to 7 % of a kernel's time ([131072, 256] bf16 backward with dh 44.8 -> 45.7 us).
+constexpr float FAR = 0x1p100f, DOWN = 0x1p-80f, UP = 0x1p80f;
+__device__ __forceinline__ bool in_range(float v) { return v >= 1.f / FAR && v <= FAR; }
+// s, from var + eps and the mean.  (Equal values of 2^20 and more with an eps below 1 / FAR: c is 0 as it is.)
+__device__ __forceinline__ float range_of(float v, float mean) {
+  return in_range(v) ? 1.f : v < 1.f / FAR ? fabsf(mean) < 0x1p20f ? UP : 1.f : DOWN;
+}
+// s^2 eps; DOWN keeps an eps from vanishing, for equal values whose sum was infinite (c = 0; any other c is 1 and more there)
+__device__ __forceinline__ float eps_of(float eps, float by) {
+  const float e = eps * by * by;
+  return by < 1.f && eps > 0.f ? fmaxf(e, 0x1p-90f) : e;
+}
+// Whether b holds for one of the rows that this one shares a warp with (LANES threads a row; more than a warp: in all of a CTA's it is the
+// same): what follows takes all lanes.
+template <int LANES>
+__device__ __forceinline__ bool any_row(bool b) {
+  if constexpr (LANES > 32) return b;
+  return __any_sync(0xffffffffu, b);
+}
+// mean(s h) and r for k_ln_columns.  s rides along in r's sign and, below 1 or above, its size: 2^-50 <= r <= 2^45 with DOWN, 2^-30 <= r with UP.
+__device__ __forceinline__ float2 coefficients(float mean, float r, float by) {
+  return make_float2(mean, by == 1.f ? r : by < 1.f ? r * -0x1p-60f : r * -0x1p40f);
+}
+
 // The sums of a[0 .. N - 1] (MAXB: the largest by its bits) over a row's TPR threads, the same value in each.  STEP numbers a row's
 // reductions: each has its own shared memory, so that one barrier a reduction is enough (whoever writes a step's again has passed
 // the next step's barrier, behind every read of it; a row has two steps at least).
@@ -65,19 +93,27 @@ __device__ __forceinline__ void row_join(float (&a)[N]) {
 
 // c = h - mean for the elements of vector k, zero for those that are not the row's.
 template <typename R, bool AL>
-__device__ __forceinline__ void center(float (&h)[R::V], float mean, int lane, int k, int off, int D) {
+__device__ __forceinline__ void center(const float (&h)[R::V], float (&c)[R::V], float mean, int lane, int k, int off, int D) {
   const int e = R::at(lane, k) - off;
   if (AL ? e < D : e >= 0 && e + R::V <= D) {  // (a whole vector, nearly always)
 #pragma unroll
-    for (int j = 0; j < R::V; ++j) h[j] -= mean;
+    for (int j = 0; j < R::V; ++j) c[j] = h[j] - mean;
   } else {
 #pragma unroll
-    for (int j = 0; j < R::V; ++j) h[j] = !AL && e + j >= 0 && e + j < D ? h[j] - mean : 0.f;
+    for (int j = 0; j < R::V; ++j) c[j] = !AL && e + j >= 0 && e + j < D ? h[j] - mean : 0.f;
   }
 }
 
+// CTAs an SM that k_ln's registers are bounded for (0: as they come), so that the way of rows out of range costs none of them.  As they come
+// and bounded, us: [16384, 768] float32 37.2 and 35.4, [8192, 4096] 88.8 and 82.4.
 template <typename T, bool Q8, bool AL, int TPR, int NV>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, const Same same) {
+constexpr int LN_CTAS = !AL ? (TPR == 256 && NV == 2 ? 3 : 0) : sizeof(T) == 2 ? 0 : 65536 / BLOCK_OF<TPR> / (NV == 1 ? Q8 ? 56 : 48 : NV == 2 ? Q8 ? 72 : 64 : NV == 3 ? 72 : 80);
+// Rows of k_ln on their way to a thread.  One and two for rows of one float32 vector a lane, at 40 and 48 registers, us: [64800, 128] 11.2 and
+// 10.8 (9.7 without the check of each row's range, which keeps the loads from moving), with residual 23.4 and 20.2 (19.7).
+template <typename T, bool Q8, bool AL, int TPR, int NV>
+constexpr int LN_AHEAD = sizeof(T) == 4 && !Q8 && AL && TPR <= 32 && NV == 1 ? 2 : 1;
+template <typename T, bool Q8, bool AL, int TPR, int NV>
+__global__ void __launch_bounds__(BLOCK_OF<TPR>, LN_CTAS<T, Q8, AL, TPR, NV>) k_ln(const LayerForward a, const Same same) {
   constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
   extern __shared__ float s_w[];  // unaligned rows: the gains, then the shifts
@@ -100,14 +136,16 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, cons
   if (a.b) kept_b.fill(shifts, lane, a.D);
   const long long step = static_cast<long long>(gridDim.x) * ROWS;
   const Bounds bx = bounds_of<T>(a.x, a.T, a.xs, a.D), br = bounds_of<T>(a.r, a.T, a.rs, a.D);
-  uint4 ux[NV], ur[NV];
-  auto fetch = [&](long long t) {
+  constexpr int AHEAD = LN_AHEAD<T, Q8, AL, TPR, NV>;
+  uint4 ux[AHEAD][NV], ur[AHEAD][NV];  // the next rows
+  auto fetch = [&](long long t, int i) {
     const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
     const int D = t < a.T ? a.D : 0;  // a row past the end holds no elements
-    R::fetch(x, bx, lane, R::offset(x), true, D, ux);
-    if (a.r) R::fetch(r, br, lane, R::offset(x), same.a, D, ur);
+    R::fetch(x, bx, lane, R::offset(x), true, D, ux[i]);
+    if (a.r) R::fetch(r, br, lane, R::offset(x), same.a, D, ur[i]);
   };
-  fetch(static_cast<long long>(blockIdx.x) * ROWS + group);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(static_cast<long long>(blockIdx.x) * ROWS + group + i * step, i);
   for (long long base = static_cast<long long>(blockIdx.x) * ROWS; base < a.T; base += step) {
     const long long t = base + group;
     const int D = t < a.T ? a.D : 0;
@@ -117,10 +155,10 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, cons
     float h[NV][V], sum[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      R::values(x, bx, lane, k, off, true, D, ux[k], h[k]);
+      R::values(x, bx, lane, k, off, true, D, ux[0][k], h[k]);
       if (a.r) {
         float f[V];
-        R::values(r, br, lane, k, off, same.a, D, ur[k], f);
+        R::values(r, br, lane, k, off, same.a, D, ur[0][k], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) h[k][j] += f[j];
         if (a.h) R::store(static_cast<T*>(a.h) + t * a.hs, lane, k, off, same.b, D, h[k]);
@@ -128,18 +166,40 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, cons
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] += h[k][j];
     }
-    fetch(t + step);
+#pragma unroll
+    for (int i = 1; i < AHEAD; ++i)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) ux[i - 1][k] = ux[i][k], ur[i - 1][k] = ur[i][k];
+    fetch(t + AHEAD * step, AHEAD - 1);
     row_join<TPR, 0, false>(sum);
-    const float mean = sum[0] * inv_d;
-    float sq[1] = {0.f};
+    float mean = sum[0] * inv_d, sq[1];
+    auto squares = [&] {
+      sq[0] = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      center<R, AL>(h[k], mean, lane, k, off, a.D);
+      for (int k = 0; k < NV; ++k) {
+        float c[V];
+        center<R, AL>(h[k], c, mean, lane, k, off, a.D);
 #pragma unroll
-      for (int j = 0; j < V; ++j) sq[0] += h[k][j] * h[k][j];
-    }
+        for (int j = 0; j < V; ++j) sq[0] += c[j] * c[j];
+      }
+    };
+    squares();
     row_join<TPR, 1, false>(sq);
-    const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
+    float v = sq[0] * inv_d + a.eps;
+    if (any_row<TPR>(!in_range(v))) {
+      const float by = range_of(v, mean);
+      sum[0] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[0] += h[k][j] *= by;
+      row_join<TPR, 3, false>(sum);
+      mean = sum[0] * inv_d;
+      squares();
+      row_join<TPR, 4, false>(sq);
+      v = sq[0] * inv_d + eps_of(a.eps, by);
+    }
+    const float rstd = rsqrtf(v);
     float top[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -148,7 +208,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>) k_ln(const LayerForward a, cons
       if (a.b) kept_b.get(shifts, places, lane, k, off, a.D, b);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        h[k][j] = h[k][j] * rstd * w[j] + b[j];
+        h[k][j] = (h[k][j] - mean) * rstd * w[j] + b[j];  // (not the row's: w = b = 0)
         if (Q8) top[0] = __uint_as_float(max(__float_as_uint(top[0]), __float_as_uint(magnitude(h[k][j]))));
       }
       if constexpr (!Q8) R::store(static_cast<T*>(a.y) + t * a.ys, lane, k, off, same.c, D, h[k]);
@@ -184,9 +244,10 @@ __device__ __forceinline__ float sum_along(int D, F&& f) {
   return total;
 }
 
-// Rows too long for the registers: a CTA a row.  Element loads.
+// Rows too long for the registers: a CTA a row.  Element loads.  (Four CTAs an SM, where 40 registers leave three: [2000, 12001] float32 with residual
+// 109 -> 98 us; 8 bits would spill.)
 template <typename T, bool Q8>
-__global__ void __launch_bounds__(LONG_THREADS) k_ln_long(const LayerForward a) {
+__global__ void __launch_bounds__(LONG_THREADS, Q8 ? 3 : 4) k_ln_long(const LayerForward a) {
   pdl_wait();
   const float inv_d = 1.f / static_cast<float>(a.D);
   for (long long t = blockIdx.x; t < a.T; t += gridDim.x) {
@@ -195,14 +256,27 @@ __global__ void __launch_bounds__(LONG_THREADS) k_ln_long(const LayerForward a) 
     auto h = [&](int e) { return Io<T>::get(x, e) + (a.r ? Io<T>::get(r, e) : 0.f); };
     float sum[1] = {sum_along(a.D, h)};
     row_join<LONG_THREADS, 0, false>(sum);
-    const float mean = sum[0] * inv_d;
+    float mean = sum[0] * inv_d, by = 1.f;
     float sq[1] = {sum_along(a.D, [&](int e) {
       const float c = h(e) - mean;
       return c * c;
     })};
     row_join<LONG_THREADS, 1, false>(sq);
-    const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
-    auto y = [&](float v, int e) { return (v - mean) * rstd * __ldg(a.w + e) + (a.b ? __ldg(a.b + e) : 0.f); };
+    float v = sq[0] * inv_d + a.eps;
+    if (!in_range(v)) {
+      by = range_of(v, mean);
+      sum[0] = sum_along(a.D, [&](int e) { return h(e) * by; });
+      row_join<LONG_THREADS, 3, false>(sum);
+      mean = sum[0] * inv_d;
+      sq[0] = sum_along(a.D, [&](int e) {
+        const float c = h(e) * by - mean;
+        return c * c;
+      });
+      row_join<LONG_THREADS, 4, false>(sq);
+      v = sq[0] * inv_d + eps_of(a.eps, by);
+    }
+    const float rstd = rsqrtf(v);
+    auto y = [&](float u, int e) { return (u * by - mean) * rstd * __ldg(a.w + e) + (a.b ? __ldg(a.b + e) : 0.f); };
     float top[1] = {0.f}, lift = 1.f, f = 1.f;
     if constexpr (Q8) {
       for (int e = threadIdx.x; e < a.D; e += LONG_THREADS)
@@ -233,9 +307,9 @@ constexpr int LN_DEPTH = NV == 1 ? 4 : 2;
 // two sets for each of the CTA's row groups (dynamic), or, where those would cost more than reading h and dy again, not here (SUMS): coef[t]
 // = mean and rstd for k_ln_columns.
 // (Odd rows on 256 threads are kept to 80 registers, three CTAs an SM: left alone they take 152, and one CTA an SM cannot hide what a row
-// waits for: [20000, 601] float32 167 -> 127 us before such rows went as tiles.)
+// waits for: [20000, 601] float32 167 -> 127 us before such rows went as tiles.  Aligned float32 rows of one vector a lane are bounded as k_ln's are.)
 template <typename T, bool AL, int TPR, int NV, bool SUMS>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 3 : AL && TPR == 512 && NV == 1 ? 2 : 1) k_ln_bwd(const LayerBackward a, const Same same, float2* coef) {
+__global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 3 : AL && NV == 1 && TPR == 512 ? 2 : AL && NV == 1 && sizeof(T) == 4 ? (TPR == 128 ? 8 : 65536 / 80 / BLOCK_OF<TPR>) : 1) k_ln_bwd(const LayerBackward a, const Same same, float2* coef) {
   static_assert(SUMS || !AL, "the sums of aligned rows stay in registers");
   constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
@@ -320,13 +394,13 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] += h[k][j];
     row_join<TPR, 0, false>(sum);
-    const float mean = sum[0] * inv_d;
+    float mean = sum[0] * inv_d, by = 1.f;
     float s[3] = {};  // of c^2, a, a c
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V];
       kept.get(gains, places, lane, k, off, a.D, w);
-      center<R, AL>(h[k], mean, lane, k, off, a.D);
+      center<R, AL>(h[k], h[k], mean, lane, k, off, a.D);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float g = d[k][j] * w[j];
@@ -337,8 +411,47 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 
     }
     row_join<TPR, 1, false>(s);  // (more than a warp a row: a barrier, behind which the last row's columns are added)
     if constexpr (!AL && TPR <= 32) __syncwarp();
-    const float rstd = t < a.T ? rsqrtf(s[0] * inv_d + a.eps) : 0.f;  // (a row past the end adds nothing to dw, with eps = 0 either)
-    const float ma = s[1] * inv_d, q = rstd * rstd * (s[2] * inv_d);
+    float v = s[0] * inv_d + a.eps;
+    if (any_row<TPR>(!in_range(v))) {
+      by = range_of(v, mean);
+      sum[0] = 0.f;
+      if constexpr (AL) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          Io<T>::unpack(*place(turn, 0, k), h[k]);
+#pragma unroll
+          for (int j = 0; j < V; ++j) sum[0] += h[k][j] *= by;
+        }
+      } else {
+#pragma unroll 1
+        for (int e = lane; e < D; e += TPR) sum[0] += Io<T>::get(hp, e) * by;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int e = R::at(lane, k) - off;
+#pragma unroll
+          for (int j = 0; j < V; ++j) h[k][j] = e + j >= 0 && e + j < D ? Io<T>::get(hp, e + j) * by : 0.f;
+        }
+      }
+      row_join<TPR, 3, false>(sum);
+      mean = sum[0] * inv_d;
+      float again[2] = {};
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float w[V];
+        kept.get(gains, places, lane, k, off, a.D, w);
+        center<R, AL>(h[k], h[k], mean, lane, k, off, a.D);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          again[0] += h[k][j] * h[k][j];
+          again[1] += d[k][j] * w[j] * h[k][j];
+        }
+      }
+      row_join<TPR, 4, false>(again);
+      s[2] = again[1];
+      v = again[0] * inv_d + eps_of(a.eps, by);
+    }
+    const float rstd = t < a.T ? rsqrtf(v) : 0.f;  // (a row past the end adds nothing to dw, with eps = 0 either)
+    const float ma = s[1] * inv_d, q = rstd * rstd * (s[2] * inv_d), rdx = rstd * by;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float w[V], o[V] = {};
@@ -354,11 +467,11 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, !AL && TPR == 256 && NV == 1 ? 
           own_w[places.at[j] + lane + TPR * k] += g;
           own_b[places.at[j] + lane + TPR * k] += d[k][j];
         }
-        o[j] += rstd * (d[k][j] * w[j] - ma - q * h[k][j]);
+        o[j] += rdx * (d[k][j] * w[j] - ma - q * h[k][j]);
       }
       if (SUMS || a.dx) R::store(static_cast<T*>(a.dx) + t * a.xs, lane, k, off, same.c, D, o);
     }
-    if (!SUMS && lane == 0 && t < a.T) coef[t] = make_float2(mean, rstd);
+    if (!SUMS && lane == 0 && t < a.T) coef[t] = coefficients(mean, rstd, by);
   }
   if constexpr (!SUMS) {
     pdl_trigger();
@@ -421,27 +534,41 @@ __global__ void __launch_bounds__(LONG_THREADS) k_ln_bwd_long(const LayerBackwar
     const T* dy = static_cast<const T*>(a.dy) + t * a.ys;
     float sum[1] = {sum_along(a.D, [&](int e) { return Io<T>::get(h, e); })};
     row_join<LONG_THREADS, 0, false>(sum);
-    const float mean = sum[0] * inv_d;
-    float s[3];
-    s[0] = sum_along(a.D, [&](int e) {
-      const float c = Io<T>::get(h, e) - mean;
+    float mean = sum[0] * inv_d, by = 1.f;
+    auto centred = [&](int e) { return Io<T>::get(h, e) * by - mean; };
+    auto square = [&](int e) {
+      const float c = centred(e);
       return c * c;
-    });
+    };
+    auto product = [&](int e) { return Io<T>::get(dy, e) * __ldg(a.w + e) * centred(e); };
+    float s[3];
+    s[0] = sum_along(a.D, square);
     s[1] = s[2] = 0.f;
     if constexpr (DX) {
       s[1] = sum_along(a.D, [&](int e) { return Io<T>::get(dy, e) * __ldg(a.w + e); });
-      s[2] = sum_along(a.D, [&](int e) { return Io<T>::get(dy, e) * __ldg(a.w + e) * (Io<T>::get(h, e) - mean); });
+      s[2] = sum_along(a.D, product);
     }
     row_join<LONG_THREADS, 1, false>(s);
-    const float rstd = rsqrtf(s[0] * inv_d + a.eps), ma = s[1] * inv_d, q = rstd * rstd * (s[2] * inv_d);
+    float v = s[0] * inv_d + a.eps;
+    if (!in_range(v)) {
+      by = range_of(v, mean);
+      sum[0] = sum_along(a.D, [&](int e) { return Io<T>::get(h, e) * by; });
+      row_join<LONG_THREADS, 3, false>(sum);
+      mean = sum[0] * inv_d;
+      float again[2] = {sum_along(a.D, square), DX ? sum_along(a.D, product) : 0.f};
+      row_join<LONG_THREADS, 4, false>(again);
+      s[2] = again[1];
+      v = again[0] * inv_d + eps_of(a.eps, by);
+    }
+    const float rstd = rsqrtf(v), ma = s[1] * inv_d, q = rstd * rstd * (s[2] * inv_d), rdx = rstd * by;
     if constexpr (DX) {
       for (int e = threadIdx.x; e < a.D; e += LONG_THREADS) {
         float o = a.dh ? Io<T>::get(static_cast<const T*>(a.dh) + t * a.ds, e) : 0.f;
-        o += rstd * (Io<T>::get(dy, e) * __ldg(a.w + e) - ma - q * (Io<T>::get(h, e) - mean));
+        o += rdx * (Io<T>::get(dy, e) * __ldg(a.w + e) - ma - q * centred(e));
         Io<T>::put(static_cast<T*>(a.dx) + t * a.xs, e, o);
       }
     }
-    if (threadIdx.x == 0) coef[t] = make_float2(mean, rstd);
+    if (threadIdx.x == 0) coef[t] = coefficients(mean, rstd, by);
   }
   pdl_trigger();
 }
@@ -462,13 +589,17 @@ __global__ void __launch_bounds__(COLUMN_THREADS, COLUMN_CTAS) k_ln_columns(cons
     const uint8_t *hp = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.h) + t * a.hs + c0),
                   *dp = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.dy) + t * a.ys + c0);
     const Granules uh = fetch16(hp, sh), ud = fetch16(dp, sd);
-    const float2 c = coef[t];
-    float h[V], d[V];
+    float2 c = coef[t];
+    float h[V], d[V], by = 1.f;
+    if (c.y < 0.f) {  // a row that is taken times a power of two (coefficients)
+      by = c.y > -1.f ? DOWN : UP;
+      c.y *= c.y > -1.f ? -0x1p60f : -0x1p-40f;
+    }
     Io<T>::unpack(finish16(uh, hp, sh), h);
     Io<T>::unpack(keep(finish16(ud, dp, sd), left), d);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (c0 + j < a.D) dw[j] += d[j] * ((h[j] - c.x) * c.y);
+      if (c0 + j < a.D) dw[j] += d[j] * (fmaf(h[j], by, -c.x) * c.y);
       db[j] += d[j];
     }
   }
@@ -661,21 +792,44 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
         sum[0] += v[k];
       }
       lanes_join<LANES>(sum);
-      const float mean = sum[0] * inv_d;
-      float sq[1] = {0.f};
+      float mean = sum[0] * inv_d, sq[1];
+      auto squares = [&] {
+        sq[0] = 0.f;
 #pragma unroll
-      for (int k = 0; k < NE; ++k) {
-        v[k] = k < SURE<NE> || lane + LANES * k < D ? v[k] - mean : 0.f;
-        sq[0] += v[k] * v[k];
+        for (int k = 0; k < NE; ++k) {
+          const float c = k < SURE<NE> || lane + LANES * k < D ? v[k] - mean : 0.f;
+          sq[0] += c * c;
+        }
+        lanes_join<LANES>(sq);
+      };
+      squares();
+      const float var = sq[0] * inv_d + a.eps;
+      float rstd = rsqrtf(var);
+      auto finish = [&] {
+#pragma unroll
+        for (int k = 0; k < NE; ++k)
+          if (k < SURE<NE> || lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, affine((v[k] - mean) * rstd, k));
+      };
+      // (few elements a lane: y before the check, which then costs less, [10000, 501] bf16 9.05 and 8.6 us; many: [20000, 1500] 66.6 and 92)
+      constexpr bool LATE = !Q8 && NE <= 16;
+      if constexpr (LATE) finish();
+      if (any_row<LANES>(!in_range(var))) {
+        const float by = range_of(var, mean);
+        sum[0] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NE; ++k) sum[0] += v[k] *= by;
+        lanes_join<LANES>(sum);
+        mean = sum[0] * inv_d;
+        squares();
+        rstd = rsqrtf(sq[0] * inv_d + eps_of(a.eps, by));
+        if constexpr (LATE) finish();
       }
-      lanes_join<LANES>(sq);
-      const float rstd = rsqrtf(sq[0] * inv_d + a.eps);
       if constexpr (Q8) {
         uint32_t top = 0;
 #pragma unroll
         for (int k = 0; k < NE; ++k) {
           if (k < SURE<NE> || lane + LANES * k < D) {
-            v[k] = affine(v[k] * rstd, k);
+            v[k] = affine((v[k] - mean) * rstd, k);
             top = max(top, __float_as_uint(magnitude(v[k])));
           }
         }
@@ -690,10 +844,8 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_tile(const LayerForward a, 
             if (k < SURE<NE> || lane + LANES * k < D) y8[LANES * k] = __nv_cvt_float_to_fp8(v[k] * lift * f, __NV_SATFINITE, __NV_E4M3);
           if (lane == 0) a.scale[t] = most * (1.f / E4M3_MAX);
         }
-      } else {
-#pragma unroll
-        for (int k = 0; k < NE; ++k)
-          if (k < SURE<NE> || lane + LANES * k < D) Io<T>::put(xs, at + LANES * k, affine(v[k] * rstd, k));
+      } else if constexpr (!LATE) {
+        finish();
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -780,14 +932,34 @@ __global__ void __launch_bounds__(TILE_THREADS) k_ln_bwd_tile(const LayerBackwar
         q[2] += g * c[k];
       }
       lanes_join<LANES>(q);
-      const float rstd = live ? rsqrtf(q[0] * inv_d + a.eps) : 0.f;
-      const float ma = q[1] * inv_d, m = rstd * rstd * (q[2] * inv_d);
+      float v = q[0] * inv_d + a.eps, by = 1.f;
+      if (any_row<LANES>(!in_range(v))) {
+        by = range_of(v, mean);
+        const int end = live ? D - lane : 0;
+        sum[0] = 0.f;
+#pragma unroll 1
+        for (int e = 0; e < end; e += LANES) sum[0] += Io<T>::get(hs, at + e) * by;
+        lanes_join<LANES>(sum);
+        const float m = sum[0] * inv_d;
+        float again[2] = {};
+#pragma unroll
+        for (int k = 0; k < NE; ++k) {
+          c[k] = LANES * k < end ? Io<T>::get(hs, at + LANES * k) * by - m : 0.f;
+          again[0] += c[k] * c[k];
+          again[1] += d[k] * w[k] * c[k];
+        }
+        lanes_join<LANES>(again);
+        q[2] = again[1];
+        v = again[0] * inv_d + eps_of(a.eps, by);
+      }
+      const float rstd = live ? rsqrtf(v) : 0.f;
+      const float ma = q[1] * inv_d, m = rstd * rstd * (q[2] * inv_d), rdx = rstd * by;
 #pragma unroll
       for (int k = 0; k < NE; ++k) {
         acc_w[k] += d[k] * (c[k] * rstd);
         acc_b[k] += d[k];
         if (live && (k < SURE<NE> || lane + LANES * k < D))
-          Io<T>::put(ds, at + LANES * k, rstd * (d[k] * w[k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, at + LANES * k) : 0.f));
+          Io<T>::put(ds, at + LANES * k, rdx * (d[k] * w[k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, at + LANES * k) : 0.f));
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -835,7 +1007,7 @@ constexpr int WIDE_ROWS = TILE_THREADS / 32;
 template <int NE>
 constexpr int WIDE_SURE = NE == 20 ? 16 : NE == 24 ? 20 : NE == 32 ? 24 : NE == 40 ? 32 : NE == 48 ? 40 : 48;
 template <typename T, int NE>
-__global__ void __launch_bounds__(TILE_THREADS, NE <= 40 ? 2 : 1) k_ln_dx_tile(const LayerBackward a, float2* coef, int stages, unsigned int* err) {
+__global__ void __launch_bounds__(TILE_THREADS, NE <= 24 ? 3 : NE <= 40 ? 2 : 1) k_ln_dx_tile(const LayerBackward a, float2* coef, int stages, unsigned int* err) {
   extern __shared__ __align__(128) unsigned char s_tiles[];
   __shared__ uint64_t full[TILE_STAGES];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.D;
@@ -884,7 +1056,7 @@ __global__ void __launch_bounds__(TILE_THREADS, NE <= 40 ? 2 : 1) k_ln_dx_tile(c
         sum[0] += c[k];
       }
       lanes_join<32>(sum);
-      const float mean = sum[0] * inv_d;
+      float mean = sum[0] * inv_d, by = 1.f;
       float q[3] = {};  // sums of c^2, a, a c
 #pragma unroll
       for (int k = 0; k < NE; ++k) {
@@ -896,14 +1068,35 @@ __global__ void __launch_bounds__(TILE_THREADS, NE <= 40 ? 2 : 1) k_ln_dx_tile(c
         q[2] += g * c[k];
       }
       lanes_join<32>(q);
-      const float rstd = rsqrtf(q[0] * inv_d + a.eps), ma = q[1] * inv_d, m = rstd * rstd * (q[2] * inv_d);
+      float v = q[0] * inv_d + a.eps;
+      if (any_row<32>(!in_range(v))) {
+        by = range_of(v, mean);
+        sum[0] = 0.f;
+#pragma unroll 1
+        for (int e = 0; lane + e < D; e += 32) sum[0] += Io<T>::get(hs, e) * by;
+        lanes_join<32>(sum);
+        mean = sum[0] * inv_d;
+        float again[2] = {};
+#pragma unroll
+        for (int k = 0; k < NE; ++k) c[k] = k < WIDE_SURE<NE> || lane + 32 * k < D ? Io<T>::get(hs, 32 * k) * by - mean : 0.f;
+#pragma unroll 1
+        for (int e = 0; lane + e < D; e += 32) {
+          const float u = Io<T>::get(hs, e) * by - mean;
+          again[0] += u * u;
+          again[1] += Io<T>::get(ds, e) * ws[e] * u;
+        }
+        lanes_join<32>(again);
+        q[2] = again[1];
+        v = again[0] * inv_d + eps_of(a.eps, by);
+      }
+      const float rstd = rsqrtf(v), ma = q[1] * inv_d, m = rstd * rstd * (q[2] * inv_d), rdx = rstd * by;
       if (a.dx) {
 #pragma unroll
         for (int k = 0; k < NE; ++k)
           if (k < WIDE_SURE<NE> || lane + 32 * k < D)
-            Io<T>::put(ds, 32 * k, rstd * (d[k] * ws[32 * k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, 32 * k) : 0.f));
+            Io<T>::put(ds, 32 * k, rdx * (d[k] * ws[32 * k] - ma - m * c[k]) + (a.dh ? Io<T>::get(gs, 32 * k) : 0.f));
       }
-      if (lane == 0) coef[t] = make_float2(mean, rstd);
+      if (lane == 0) coef[t] = coefficients(mean, rstd, by);
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
