@@ -352,8 +352,9 @@ typedef struct {
  *   tensors    `count` entries in HOST memory, read during the call; count from 0 (norm = 0) to 2^20
  *   norm       one float32 on the device; whtmix_clip_by_global_norm: or NULL
  *   max_norm   >= 0
- * Squares are float32 and added 16 at a time, those sums as if in float64; every finite list has its norm, whatever its values' size (`norm` is its
- * float32: infinite beyond 3.4e38, where the factor is still right).  The factor is rounded to float32, its products to the tensor's
+ * Squares are float32; a thread adds those of 64 bytes (16 float32 values, 32 bf16) in float32, and what it has of each 64 bytes as if in
+ * float64.  Every finite list has its norm, whatever its values' size (`norm` is its float32: infinite beyond 3.4e38, where the factor is
+ * still right).  The factor is rounded to float32, its products to the tensor's
  * type.  An infinity makes the norm infinite and the factor 0 (max_norm finite), a NaN makes both NaN: what comes out then is not to
  * be used.  One launch for lists of up to 24 pieces of 16 KB, two for up to 64 tensors, two for every 480 of longer lists, one more
  * for very long ones. */

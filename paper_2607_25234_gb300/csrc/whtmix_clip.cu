@@ -5,8 +5,9 @@
 // Bound by memory: the gradients are read for the norm and again for the scaling.  A tensor is cut into chunks of CHUNK 16-byte
 // vectors, counted from the 16-byte boundary at or before its first element, so that every load is aligned whatever its address; a
 // CTA takes a run of chunks, the next one's loads on their way while it works on one.  A table of the tensors goes along as a kernel
-// parameter (a captured graph keeps it), a launch for every MAX of them.  The scaling takes a run in descending order: the last chunks
-// read are still in L2.  Short lists stay in one cluster's registers between the two.
+// parameter (a captured graph keeps it), a launch for every MAX of them.  The scaling takes a run in descending order, the last chunks
+// read first; ascending it takes as long (0.6 GB 280 and 279 us, 67 MB 33.9 and 33.5).  Short lists stay in one cluster's registers
+// between the two.
 // A thread's squares of one chunk are added in float32, those sums in float32 with a compensation (float64 additions are slow
 // here: two a clock and SM), the threads' sums in float64; values whose squares leave float32's range are scaled by a power of two
 // first, so that every finite gradient has its finite norm.  Every CTA of the scaling adds up the partial

@@ -19,21 +19,23 @@ namespace linear {
 
 constexpr int THREADS_256 = 256;
 
-// CTAs of k_gated_dp an SM.  Three and two or four, rows through registers, whole backward, us: [65536, 512] to 1408 398 and 508 (two with a
-// row more in flight), [8192, 1024] to 2736 211 and 215, 205, to 2733 263 and 391, 260.
+// CTAs of k_gated_dp an SM.  Two, three and four, whole backward, us: [65536, 512] to 1408 450, 391 and 422; [20000, 512] to 608 93, 81 and
+// 88, to 601 135, 113 and 127; [8192, 1024] to 2736 203, 199 and 198, to 2733 261, 253 and 246; [27104, 184] to 5238 904, 851 and 810.
 constexpr int DP_CTAS = 3;
 
 // Rows on their way to a thread of k_gated_dp with many of them, in shared memory: a place for each of dy, g and u a lane, for unaligned
 // rows one more a row.  With fewer than DP_RING rows a thread they come through registers, one at a time.  Registers and ring, dp alone, us:
 // [8192, 2736] (24 rows a thread) 61.9 and 46.4, [5456, 2240] (13) 31.6 and 23.1, [2003, 3776] (8) 22.7 and 19.4, [20000, 200] (6) 10.6 and 11.9, [20000, 104] (3) 6.6 and 8.0;
-// unaligned [27104, 5238] (154) 706 and 592, [8192, 2733] (24) 119.3 and 103.8, [20000, 601] (16) 57.6 and 57 to 62, [3001, 777] (3) 15.0
-// and 17.6.
+// unaligned [27104, 5238] (154) 706 and 592, [8192, 2733] (24) 119.3 and 103.8, [3001, 777] (3) 15.0 and 17.6.  With 16 rows, whole backward,
+// [20000, 512] to 608 83.5 and 81.2, unaligned to 601 111.8 and 113.4: the one rule for both costs the latter 1.5 %.
 constexpr int DP_DEPTH = 4, DP_RING = 8;
 template <bool AL, int TX>
 constexpr int DP_PLACES = THREADS_256 / TX * (AL ? TX : TX + 1);
 template <bool AL, int TX>
 constexpr size_t DP_SMEM = size_t{DP_DEPTH} * 3 * DP_PLACES<AL, TX> * 16;
 
+// dp goes to bf16: the products behind it take both operands in one type, and W and x are bf16 (dp in two bf16 parts would double them).
+// dx and dw are off by 2.3e-3 of their norm for it, by 1.7e-3, their own rounding, with dp in 32 bits; db sums the 32 bits.
 // dp[t, n], dp[t, N + n] = bf16 of both gradients; part[chunk][n], [N + n] = the chunk's rows' float32 sums of them, before the rounding.
 // A CTA takes 8 TX channels (a thread 8) and the rows of chunk blockIdx.y, 256 / TX at a time.  dp, part: or null.  AL: dy, p and dp
 // have 16-byte aligned rows and halves.  Unaligned rows come as the whole 16-byte granules around them: a lane takes its own, and the

@@ -5,7 +5,7 @@
 //   warp 0      TMA loads of a block of dy, g and u (128 x 64 each), two or three stages;
 //   warp 2      TMA loads of its rows of Wg and of Wu (64 rows of BN columns each), a ring of three;
 //   warps 8-15  read the block in shared memory, write bf16 dg over g and du over u, where they lie as the products' operand wants
-//               them, and add up the block's columns unrounded;
+//               them (why in bf16: k_gated_dp), and add up the block's columns unrounded;
 //   warp 3      both go out to memory by TMA as well, for dw (a warp of its own: the stage is free again as soon as they have left);
 //   warp 1      four tcgen05.mma for each of the two, dg and du with k along their rows, W with n along its rows, as they lie;
 //   warps 4-7   the accumulator (two tiles' worth) to dx, as whtmix_gemm.cuh.

@@ -119,8 +119,9 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, LN_CTAS<T, Q8, AL, TPR, NV>) k_
   extern __shared__ float s_w[];  // unaligned rows: the gains, then the shifts
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv_d = 1.f / static_cast<float>(a.D);
-  // A short launch lets the next kernel come in at once, which may ask for its weights before this one's rows are there (24 rows to 8 bits
-  // and their gated product 19.7 -> 19.4 us); a long one would have it wait in the SMs' way.
+  // A short launch lets the next kernel come in at once: its launch, its barriers and its tensor memory are set up beside this one's rows
+  // (24 rows to 8 bits and their gated product 19.7 -> 19.4 us); a long one would have it wait in the SMs' way.  This comes before the wait:
+  // the kernel before this one may still be writing, so that no kernel reads global data in front of its own pdl_wait.
   const bool short_launch = gridDim.x < 128;
   if (short_launch) pdl_trigger();
   pdl_wait();
