@@ -207,9 +207,15 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, LN_CTAS<T, Q8, AL, TPR, NV>) k_
       float w[V], b[V] = {};
       kept_w.get(gains, places, lane, k, off, a.D, w);
       if (a.b) kept_b.get(shifts, places, lane, k, off, a.D, b);
+      if constexpr (Q8) {
+        center<R, AL>(h[k], h[k], mean, lane, k, off, a.D);  // what is not the row's counts as 0 in `top`
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[k][j] -= mean;
+      }
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        h[k][j] = (h[k][j] - mean) * rstd * w[j] + b[j];  // (not the row's: w = b = 0)
+        h[k][j] = h[k][j] * rstd * w[j] + b[j];
         if (Q8) top[0] = __uint_as_float(max(__float_as_uint(top[0]), __float_as_uint(magnitude(h[k][j]))));
       }
       if constexpr (!Q8) R::store(static_cast<T*>(a.y) + t * a.ys, lane, k, off, same.c, D, h[k]);

@@ -139,3 +139,19 @@ def test_large_equal_values_and_rows_that_are_not_finite(T, D, dtype):
     q, scale = whtmix.layer_norm(x, w, b, out_dtype=E4M3)
     assert bool(torch.isfinite(scale[[0, 1, 4, 5]]).all()) and bool(torch.isnan(scale[2:4]).all())
     assert bool(torch.isnan(q[2:4].float()).all()) and bool(torch.isfinite(q[[0, 1, 4, 5]].float()).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,D", [(5, 16), (300, 16), (5, 48), (5, 200), (5, 1000), (300, 1000), (5, 77), (5, 1001), (5, 4100), (20011, 77)])
+def test_large_equal_values_with_a_small_eps_to_eight_bits(T, D, dtype):
+    """mean rstd leaves float32 here; places that are not the row's must not see it.  2^100 is its own mean where D is a power of two; else
+    the mean's rounding is the row's c, whose norm is at most sqrt(D)."""
+    w, b = 1.0 + 0.1 * rand(3, D), 0.1 * rand(4, D)
+    x = torch.full((T, D), 2.0 ** 100, device="cuda").to(dtype)
+    q, scale = whtmix.layer_norm(x, w, b, eps=1e-30, out_dtype=E4M3)
+    y = whtmix.layer_norm(x, w, b, eps=1e-30)
+    top = float((w.abs() * math.sqrt(D) + b.abs()).max()) * 1.001
+    assert bool(torch.isfinite(scale).all()) and float(scale.max()) <= top / 448.0 and bool(torch.isfinite(q.float()).all())
+    assert bool(torch.isfinite(y).all()) and float(y.float().abs().max()) <= top * (1 + U16)
+    if D & (D - 1) == 0:
+        assert torch.equal(scale, b.abs().max().expand(T) * (1.0 / 448.0)) and torch.equal(y, b.to(dtype).expand(T, D))
