@@ -105,15 +105,22 @@ __device__ __forceinline__ void center(const float (&h)[R::V], float (&c)[R::V],
 }
 
 // CTAs an SM that k_ln's registers are bounded for (0: as they come), so that the way of rows out of range costs none of them.  As they come
-// and bounded, us: [16384, 768] float32 37.2 and 35.4, [8192, 4096] 88.8 and 82.4.
+// and bounded, us: [16384, 768] float32 37.2 and 35.4, [8192, 4096] 88.8 and 82.4; to 8 bits [4096, 6144] 78.3 and 59.8, odd [2000, 2999]
+// 27.1 and 25.0.
 template <typename T, bool Q8, bool AL, int TPR, int NV>
-constexpr int LN_CTAS = !AL ? (TPR == 256 && NV == 2 ? 3 : 0) : sizeof(T) == 2 ? 0 : 65536 / BLOCK_OF<TPR> / (NV == 1 ? Q8 ? 56 : 48 : NV == 2 ? Q8 ? 72 : 64 : NV == 3 ? 72 : 80);
-// Rows of k_ln on their way to a thread.  One and two for rows of one float32 vector a lane, at 40 and 48 registers, us: [64800, 128] 11.2 and
-// 10.8 (9.7 without the check of each row's range, which keeps the loads from moving), with residual 23.4 and 20.2 (19.7).
+constexpr int ln_ctas() {
+  if constexpr (!AL) return TPR != 256 ? 0 : NV == 2 ? (sizeof(T) == 4 && Q8 ? 4 : 3) : NV == 3 && sizeof(T) == 4 && Q8 ? 3 : 0;
+  if constexpr (sizeof(T) == 2) return 0;
+  constexpr int registers = NV == 1 ? (Q8 ? 64 : 48) : NV == 2 ? (Q8 ? 72 : 64) : NV == 3 ? (Q8 && TPR == 512 ? 64 : 72) : 80;
+  return 65536 / BLOCK_OF<TPR> / registers;
+}
+// Rows of k_ln on their way to a thread.  One and two for rows of one float32 vector a lane, at 40 and 48 registers (8 bits: 56 and 64), us:
+// [64800, 128] 11.2 and 10.8 (9.7 without the check of each row's range, which keeps the loads from moving), with residual 23.4 and
+// 20.2 (19.7), to 8 bits 26.4 and 18.9 (19.1).
+template <typename T, bool AL, int TPR, int NV>
+constexpr int LN_AHEAD = sizeof(T) == 4 && AL && TPR <= 32 && NV == 1 ? 2 : 1;
 template <typename T, bool Q8, bool AL, int TPR, int NV>
-constexpr int LN_AHEAD = sizeof(T) == 4 && !Q8 && AL && TPR <= 32 && NV == 1 ? 2 : 1;
-template <typename T, bool Q8, bool AL, int TPR, int NV>
-__global__ void __launch_bounds__(BLOCK_OF<TPR>, LN_CTAS<T, Q8, AL, TPR, NV>) k_ln(const LayerForward a, const Same same) {
+__global__ void __launch_bounds__(BLOCK_OF<TPR>, ln_ctas<T, Q8, AL, TPR, NV>()) k_ln(const LayerForward a, const Same same) {
   constexpr int V = Io<T>::V, BLOCK = BLOCK_OF<TPR>, ROWS = BLOCK / TPR;
   using R = Row<T, AL, TPR>;
   extern __shared__ float s_w[];  // unaligned rows: the gains, then the shifts
@@ -137,7 +144,7 @@ __global__ void __launch_bounds__(BLOCK_OF<TPR>, LN_CTAS<T, Q8, AL, TPR, NV>) k_
   if (a.b) kept_b.fill(shifts, lane, a.D);
   const long long step = static_cast<long long>(gridDim.x) * ROWS;
   const Bounds bx = bounds_of<T>(a.x, a.T, a.xs, a.D), br = bounds_of<T>(a.r, a.T, a.rs, a.D);
-  constexpr int AHEAD = LN_AHEAD<T, Q8, AL, TPR, NV>;
+  constexpr int AHEAD = LN_AHEAD<T, AL, TPR, NV>;
   uint4 ux[AHEAD][NV], ur[AHEAD][NV];  // the next rows
   auto fetch = [&](long long t, int i) {
     const T *x = static_cast<const T*>(a.x) + t * a.xs, *r = static_cast<const T*>(a.r) + t * a.rs;
